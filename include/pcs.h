@@ -636,6 +636,134 @@ pcs_status pcs_snapshot_write_file(pcs_ctx *ctx, const pcs_snapshot *snap, const
 pcs_status pcs_snapshot_read_file(pcs_ctx *ctx, const char *path, uint32_t placement,
                                   pcs_snapshot **out);
 
+/* ---- Operators over a paged cache of keys and values ---------------------
+ *
+ * What a session's model does with its KV context between a restore and the
+ * next checkpoint: give new tokens their positions, write them into the pages
+ * of the window, attend over it.  (The paper's runtime leaves the model to its
+ * caller, Sec. 3 "Boundary"; the pages are those of Sec. 7.2's addressable KV
+ * and of the copy-on-write pool above.)
+ */
+
+/* Heads of tokens: element d of head h of token t is at
+ * data + t * token_stride + h * head_stride + d (strides in elements). */
+typedef struct pcs_heads {
+    void *data;              /* device                                      */
+    int64_t token_stride, head_stride;
+    int32_t heads, head_dim;
+    uint32_t dtype;          /* PCS_DT_F16, PCS_DT_BF16 (pcs_rotate: F32)   */
+    uint32_t reserved;       /* 0                                           */
+} pcs_heads;
+
+#define PCS_ROT_INTERLEAVED 1 /* pair i is elements 2i, 2i + 1; else i and  */
+                              /* i + (pairs of all axes)                    */
+#define PCS_ROT_INVERSE 2     /* turn back: the gradient of the rotation    */
+
+/*
+ * Rotary positions with several axes (time, height, width): the first pairs[0]
+ * pairs of a head turn with axis 0, the next pairs[1] with axis 1, and so on;
+ * elements behind the last pair stay.  Pair i of axis a turns by
+ * pos[t][a] * freq[i]: (x, y) -> (x cos - y sin, x sin + y cos).
+ */
+typedef struct pcs_rotary {
+    const int32_t *pos;      /* device [tokens][axes], any sign             */
+    const float *freq;       /* device [pairs of all axes]: angle per unit  */
+    int32_t axes;            /* 1..4                                        */
+    int32_t pairs[4];        /* 0 for axes that are not there               */
+    uint32_t flags;          /* PCS_ROT_*                                   */
+} pcs_rotary;
+
+/*
+ * The pages of many sessions' keys and values.  The token at position p of a
+ * session (its first one is 0) has slot
+ *   p                              if ring == 0 or p < sinks
+ *   sinks + (p - sinks) mod ring   else
+ * and lies in row slot mod page_rows of page table[slot / page_rows]: element
+ * d of head h at page * page_stride + row * row_stride + h * head_stride + d.
+ * With a ring only the last `ring` positions are there, and the first `sinks`
+ * (sinks = 0: a RING section's window, with ring start len mod ring).  Page -1
+ * is empty: its tokens are not written and not seen.
+ */
+typedef struct pcs_kv_cache {
+    void *k, *v;             /* device page pools                           */
+    const int32_t *table;    /* device [sessions][table_stride]             */
+    const int32_t *v_table;  /* the values' pages; NULL: the keys' page ids */
+    int64_t table_stride;    /* entries from one session's table to the     */
+                             /* next, at least table_pages                  */
+    int64_t page_stride, row_stride, head_stride; /* elements, both pools;  */
+                             /* multiples of 8                              */
+    int32_t n_pages;         /* pages in each pool                          */
+    int32_t table_pages;     /* entries of one table                        */
+    int32_t page_rows;
+    int32_t heads, head_dim; /* head_dim: a multiple of 8, 8..128           */
+    int32_t sinks;           /* first tokens that stay                      */
+    int32_t ring;            /* slots reused in turn; 0: every token stays  */
+    uint32_t dtype;          /* PCS_DT_F16 or PCS_DT_BF16                   */
+} pcs_kv_cache;
+
+/* The new tokens of a call: rows [q_off[s], q_off[s + 1]) of its tensors are
+ * the last tokens of session s, whose length with them is lens[s]. */
+typedef struct pcs_kv_batch {
+    const int32_t *lens;     /* device [sessions]                           */
+    const int32_t *q_off;    /* device [sessions + 1], ascending from 0 to  */
+                             /* tokens; NULL: tokens / sessions each        */
+    int64_t tokens;
+    int32_t sessions;
+    int32_t max_new;         /* with q_off: no session has more new tokens  */
+    int32_t max_len;         /* a hint: no session is longer; 0: not known  */
+    uint32_t reserved;       /* 0                                           */
+} pcs_kv_batch;
+
+typedef struct pcs_attend_params {
+    float scale;             /* of q.k; 0: 1 / sqrt(head_dim)               */
+    int32_t window;          /* position p sees (p - window, p] and the     */
+                             /* sinks; 0: everything up to p                */
+    uint32_t flags;          /* 0                                           */
+    uint32_t reserved;       /* 0                                           */
+} pcs_attend_params;
+
+/*
+ * Rotate n tensors (at most 8, same tokens, head_dim up to 256 and type):
+ * y[i] = R x[i], or with PCS_ROT_INVERSE its gradient, R^T x[i].  y[i] may be
+ * x[i]; any other overlap is undefined.  Any alignment of whole elements;
+ * tensors, strides and pairs of 16-byte multiples move as vectors.  Angles
+ * keep float accuracy at any position (no loss at far ones); the result is
+ * rounded once.
+ */
+pcs_status pcs_rotate(pcs_ctx *ctx, const pcs_rotary *rotary, const pcs_heads *x,
+                      const pcs_heads *y, int32_t n, int64_t tokens, void *stream);
+
+/*
+ * Append the new tokens to the cache: k (rotated; rotary NULL: as it is) and v
+ * go to the slots of their positions, and q, if given, is rotated into q_out
+ * (which may be q).  Of new tokens that share a slot of the ring the last one
+ * is written.  Pages shared with a fork have to be made the session's own first
+ * (pcs_pool_prepare_write).  A slot beyond the table, a page id outside the
+ * pool or more new tokens than lens says -> PCS_E_RANGE at the next pcs_sync
+ * (those tokens are not written).
+ */
+pcs_status pcs_kv_append(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_batch *batch,
+                         const pcs_rotary *rotary, const pcs_heads *k, const pcs_heads *v,
+                         const pcs_heads *q, const pcs_heads *q_out, void *stream);
+
+/*
+ * Attention of the new tokens (already appended) over the cache: out of a
+ * token at position p and query head h is sum_j w_j v_j over the positions j
+ * that it sees -- j <= p, j > p - window or j < sinks, and in a page -- with
+ * w = softmax(scale * q.k_j), key head h / (q heads / cache heads).  A token
+ * that sees nothing gives 0.  lse: device float[tokens][q heads] or NULL,
+ * log sum exp(scale * q.k_j) (-inf if it sees nothing), by which results over
+ * several caches can be joined.  Sums are in 32 bits, weights are rounded to
+ * the cache's type before they multiply values.  What is in slots that no new
+ * token sees (infinities, NaN) does not matter.  q and out: 16-byte multiples
+ * (else PCS_E_ALIGN).  Page ids outside the pool, slots beyond the table, more
+ * new tokens than max_new or than lens says -> PCS_E_RANGE at the next
+ * pcs_sync (unseen; sessions over max_new are skipped).
+ */
+pcs_status pcs_attend(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_batch *batch,
+                      const pcs_attend_params *params, const pcs_heads *q, const pcs_heads *out,
+                      float *lse, void *stream);
+
 /*
  * Fingerprints without any allocation.  The paper has no counterpart: this is
  * a service of this library for callers that cannot allocate device memory,

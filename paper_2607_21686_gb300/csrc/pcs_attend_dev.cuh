@@ -1,0 +1,148 @@
+// pcs_attend_dev.cuh -- device code that the attention kernels share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdint>
+
+#include "pcs_attend.h"
+#include "pcs_internal.h"
+
+namespace pcs {
+
+// Raises a kernel's limit of dynamic shared memory, once per device.
+struct SmemLimit {
+  std::atomic<uint64_t> done{0};
+  template <typename K>
+  cudaError_t set(K kernel, uint32_t bytes) {
+    int dev = 0;
+    if (cudaError_t e = cudaGetDevice(&dev)) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+  }
+};
+
+__device__ __forceinline__ void attend_dependency() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+
+// 2^x; 0 for -inf.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Two floats rounded to a pair of 16-bit elements, the first in the low half.
+// The weights of a softmax are rounded to the cache's type for the matrix
+// instruction, each by at most 2^-8 (bf16) or 2^-11 of itself, which is what
+// the rounding of the result itself costs; their sum stays in 32 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// 16 bytes from global to shared memory, zeros where there is no source.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(there ? 16 : 0)
+               : "memory");
+}
+
+// The new tokens of a session and what they see together.
+struct SessionView {
+  int64_t q0;       // the first new token's row
+  int32_t m;        // new tokens
+  int32_t first;    // position of the first one (negative: before the session)
+  int32_t sinks;    // first tokens seen besides the run
+  int32_t lo;       // the run: [lo, first + m)
+  int32_t seen;     // sinks + run
+};
+
+__device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) {
+  SessionView v;
+  const BatchDev& b = a.batch;
+  if (b.q_off) {
+    v.q0 = __ldg(b.q_off + s);
+    v.m = __ldg(b.q_off + s + 1) - static_cast<int32_t>(v.q0);
+  } else {
+    v.q0 = static_cast<int64_t>(s) * b.each;
+    v.m = b.each;
+  }
+  const int32_t len = __ldg(b.lens + s);
+  v.first = len - v.m;
+  int32_t lo = a.window ? v.first - a.window + 1 : 0;
+  if (a.cache.ring_rows) lo = max(lo, len - a.cache.ring_rows);
+  const bool apart = lo > a.cache.sinks;
+  v.sinks = apart ? a.cache.sinks : 0;
+  v.lo = apart ? lo : 0;
+  v.seen = max(len, 0) - v.lo + v.sinks;
+  return v;
+}
+
+// Narrows the view of a whole session to what rows of new tokens [t0, t1) see.
+__device__ __forceinline__ SessionView rows_view(const AttendArgs& a, const SessionView& s, int t0,
+                                                 int t1) {
+  SessionView v = s;
+  int32_t lo = a.window ? s.first + t0 - a.window + 1 : 0;
+  if (a.cache.ring_rows) lo = max(lo, s.first + s.m - a.cache.ring_rows);
+  const int32_t end = max(s.first + t1, 0);
+  const bool apart = lo > a.cache.sinks;
+  v.sinks = apart ? min(a.cache.sinks, end) : 0;
+  v.lo = apart ? lo : 0;
+  v.seen = max(end - v.lo, 0) + v.sinks;
+  return v;
+}
+
+// Position of the e-th token of a view.
+__device__ __forceinline__ int32_t seen_position(const SessionView& v, int32_t e) {
+  return e < v.sinks ? e : v.lo + (e - v.sinks);
+}
+
+// Where position p of session s is in the cache (of head 0): byte offsets of
+// its key and value, or k = -1 if it is in no page.
+struct RowPlace {
+  int64_t k, v;
+};
+__device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_t p) {
+  const CacheDev& c = a.cache;
+  RowPlace r = {-1, -1};
+  const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
+  if (slot >= static_cast<uint32_t>(c.slots)) {
+    atomicOr(a.err, kDevErrIndex);
+    return r;
+  }
+  const uint32_t page = c.page_rows.div(slot);
+  const int64_t row = static_cast<int64_t>(slot - page * c.page_rows.d) * c.row_bytes;
+  const int64_t e = s * c.table_stride + page;
+  const int32_t kp = __ldg(c.table + e);
+  const int32_t vp = c.v_table ? __ldg(c.v_table + e) : kp;
+  if (kp < 0 || kp >= c.n_pages || vp < 0 || vp >= c.n_pages) {
+    if (kp < -1 || kp >= c.n_pages || vp < -1 || vp >= c.n_pages) atomicOr(a.err, kDevErrIndex);
+    return r;
+  }
+  r.k = kp * c.page_bytes + row;
+  r.v = vp * c.page_bytes + row;
+  return r;
+}
+
+}  // namespace pcs

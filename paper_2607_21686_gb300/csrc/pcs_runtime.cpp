@@ -28,6 +28,7 @@
 #include <vector>
 
 #include "pcs.h"
+#include "pcs_attend.h"
 #include "pcs_internal.h"
 #include "pcs_ptrset.h"
 
@@ -451,7 +452,8 @@ enum KernelKind {
   kKStreamHash, kKStreamPack, kKStreamRestore, kKStreamRestoreV, kKFinalizeHash,
   kKFinalizePack, kKFinalizeRestoreV, kKScore, kKTopk, kKBulkHash, kKBulkPack,
   kKBulkRestore, kKBulkRestoreV, kKReduce, kKGSelect, kKGFinish, kKPoolAlloc, kKPoolShare,
-  kKPoolCow, kKPoolRelease, kKMismatch, kKClassifyReads, kKUpload, kKernelKinds
+  kKPoolCow, kKPoolRelease, kKMismatch, kKClassifyReads, kKUpload, kKRotate, kKAppend, kKAttendToken, kKAttendBlock,
+  kKAttendJoin, kKernelKinds
 };
 static_assert(kKernelKinds <= 32, "kernel timing table");
 const char* kKernelNames[kKernelKinds] = {
@@ -459,7 +461,8 @@ const char* kKernelNames[kKernelKinds] = {
     "k_finalize<hash>", "k_finalize<pack>", "k_finalize<restore_verify>", "k_score", "k_topk",
     "k_hash", "k_bulk<pack>", "k_bulk<restore>", "k_bulk<restore_verify>",
     "k_reduce_nodes", "k_gselect", "k_gfinish", "k_pool_alloc", "k_pool_share", "k_pool_cow",
-    "k_pool_release", "k_mismatch", "k_classify_reads", "k_upload"};
+    "k_pool_release", "k_mismatch", "k_classify_reads", "k_upload", "k_rotate", "k_rotate<append>",
+    "k_attend_token", "k_attend_block", "k_attend_join"};
 
 cudaEvent_t timing_event(pcs_ctx* c) {
   if (!c->timing_events.empty()) {
@@ -520,8 +523,9 @@ Arena* arena_of(pcs_ctx* c, uint32_t placement) {
 constexpr uint64_t kWsHeader = 8192;  // per-call device words before the descriptors
 constexpr int kWordBulkSched = 4;    // header words [4], [5]: the TMA kernel's work sharing
 constexpr int kWordDone = 64;        // [64 .. 127]: the small-call kernel's tasks done per item
-constexpr int kWordSums = 128;        // [128 ..]: sums or a bitmap of a call of few items
+constexpr int kWordSums = 128;        // [128 ..]: sums, a bitmap or tickets of a call of few items
 static_assert(kWordDone + kSmallMaxItems <= kWordSums, "header words");
+static_assert(4 * (kWordSums + kOpWords) <= kWsHeader, "header words");
 static_assert(4 * kWordSums + 8 * kMmBlob <= kWsHeader && kReadBlob / 32 <= 2 * kMmBlob, "header words");
 
 // The header words of a call: they sit just below its descriptors, in a
@@ -3276,3 +3280,58 @@ pcs_status pcs_fingerprint_static(const pcs_buf* bufs, int32_t n, uint64_t* fp_o
 }
 
 }  // extern "C"
+
+// ---- Calls whose host side is in a file of its own (pcs_attend.cpp) -----------
+
+namespace pcs {
+
+pcs_status op_fail(pcs_status s, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(s, "%s", buf);
+}
+
+OpCall::OpCall(pcs_ctx* c, const char* name, void* stream)
+    : c_(c), stream_(static_cast<cudaStream_t>(stream)) {
+  nvtxRangePushA(name);
+}
+
+OpCall::~OpCall() {
+  delete static_cast<LaunchScope*>(scope_);
+  if (locked_) c_->mu.unlock();
+  nvtxRangePop();
+}
+
+pcs_status OpCall::begin() {
+  if (!c_) return fail(PCS_E_INVAL, "ctx is null");
+  c_->mu.lock();
+  locked_ = true;
+  return set_device(c_);
+}
+
+pcs_status OpCall::scratch(uint64_t bytes, uint8_t** out, uint32_t** words) {
+  pcs_status st = ws_acquire(c_, bytes, stream_, out);
+  if (st) return st;
+  c_->plan_slot_used = -1;
+  *words = c_->call_words + kWordSums;
+  scratch_ = true;
+  return PCS_OK;
+}
+
+void OpCall::before(OpKernel k) { scope_ = new LaunchScope(c_, kKRotate + static_cast<int>(k), stream_); }
+
+pcs_status OpCall::after(cudaError_t e) {
+  delete static_cast<LaunchScope*>(scope_);
+  scope_ = nullptr;
+  return e == cudaSuccess ? PCS_OK : cuda_fail(e, "kernel launch");
+}
+
+pcs_status OpCall::end() { return scratch_ ? ws_release(c_, stream_) : PCS_OK; }
+
+uint32_t* OpCall::errors() const { return c_->words; }
+int OpCall::sm_count() const { return c_->sm_count; }
+
+}  // namespace pcs

@@ -37,6 +37,7 @@ PCS_KIND_MARKOV, PCS_KIND_BANK, PCS_KIND_KV = 1, 2, 3
 PCS_LAYOUT_CONTIG, PCS_LAYOUT_ROWS, PCS_LAYOUT_RING = 0, 1, 2
 PCS_PLACE_DEVICE, PCS_PLACE_PINNED_HOST = 0, 1
 PCS_RING_START_FROM_SNAPSHOT = 0xFFFFFFFF
+PCS_ROT_INTERLEAVED, PCS_ROT_INVERSE = 1, 2
 PCS_K_FIXED, PCS_K_BUDGET, PCS_K_FRACTION = 0, 1, 2
 
 _DT_OF_TORCH = {
@@ -107,6 +108,39 @@ class pcs_kernel_time(ctypes.Structure):
                 ("total_ms", ctypes.c_double)]
 
 
+class pcs_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
+
+
+class pcs_rotary(ctypes.Structure):
+    _fields_ = [("pos", ctypes.c_void_p), ("freq", ctypes.c_void_p), ("axes", ctypes.c_int32),
+                ("pairs", ctypes.c_int32 * 4), ("flags", ctypes.c_uint32)]
+
+
+class pcs_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("v_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("table_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("ring", ctypes.c_int32), ("dtype", ctypes.c_uint32)]
+
+
+class pcs_kv_batch(ctypes.Structure):
+    _fields_ = [("lens", ctypes.c_void_p), ("q_off", ctypes.c_void_p), ("tokens", ctypes.c_int64),
+                ("sessions", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("reserved", ctypes.c_uint32)]
+
+
+class pcs_attend_params(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("window", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _u32 = ctypes.c_uint32
@@ -170,6 +204,15 @@ SIGNATURES = {
     "pcs_set_arena_limit": (_st, [_vp, _u32, _u64]),
     "pcs_prune_global_part": (_st, [_vp, ctypes.POINTER(pcs_bank), _i32, _u64, _u64, _vp, _vp,
                                     _vp, _vp, _vp, _vp]),
+    "pcs_rotate": (_st, [_vp, ctypes.POINTER(pcs_rotary), ctypes.POINTER(pcs_heads),
+                         ctypes.POINTER(pcs_heads), _i32, ctypes.c_int64, _vp]),
+    "pcs_kv_append": (_st, [_vp, ctypes.POINTER(pcs_kv_cache), ctypes.POINTER(pcs_kv_batch),
+                            ctypes.POINTER(pcs_rotary), ctypes.POINTER(pcs_heads),
+                            ctypes.POINTER(pcs_heads), ctypes.POINTER(pcs_heads),
+                            ctypes.POINTER(pcs_heads), _vp]),
+    "pcs_attend": (_st, [_vp, ctypes.POINTER(pcs_kv_cache), ctypes.POINTER(pcs_kv_batch),
+                         ctypes.POINTER(pcs_attend_params), ctypes.POINTER(pcs_heads),
+                         ctypes.POINTER(pcs_heads), _vp, _vp]),
     "pcs_fingerprint_static": (_st, [ctypes.POINTER(pcs_buf), _i32, _vp, _vp]),
 }
 # int32 exchange(void* user, uint64_t* counts, uint64_t* bytes, int32 bins)
@@ -371,6 +414,107 @@ def kv_session(session_id: int, meta: torch.Tensor, k_pool: torch.Tensor, v_pool
         secs.append(ring_section(PCS_SEC_K, k_pool, page_table[l], ring_start, window, layer=l))
         secs.append(ring_section(PCS_SEC_V, v_pool, vt[l], ring_start, window, layer=l))
     return Session(session_id, PCS_KIND_KV, secs, keep=[meta, k_pool, v_pool, page_table, vt])
+
+
+# --------------------------------------------------------------------------
+# Paged cache of keys and values
+# --------------------------------------------------------------------------
+
+_HEAD_DTYPES = {torch.float16: PCS_DT_F16, torch.bfloat16: PCS_DT_BF16, torch.float32: PCS_DT_F32}
+
+
+def _heads(t: torch.Tensor, what: str) -> pcs_heads:
+    """pcs_heads of a [tokens, heads, head_dim] tensor."""
+    if t.dim() != 3 or not t.is_cuda or t.dtype not in _HEAD_DTYPES:
+        raise ValueError("%s: a CUDA tensor [tokens, heads, head_dim] of float16, bfloat16 or "
+                         "float32 is wanted" % what)
+    n, h, d = t.shape
+    ts, hs, es = t.stride()
+    if es != 1 and d > 1:
+        raise ValueError("%s: the elements of a head must be contiguous" % what)
+    # A stride over one item is never taken and may be anything.
+    return pcs_heads(t.data_ptr(), ts if n > 1 else h * d, hs if h > 1 else d, h, d,
+                     _HEAD_DTYPES[t.dtype], 0)
+
+
+def _int32(t: torch.Tensor, what: str, dim: int) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != dim:
+        raise ValueError("%s: a CUDA int32 tensor of %d dimensions is wanted" % (what, dim))
+    if t.numel() > 1 and t.stride(-1) != 1:
+        raise ValueError("%s must be contiguous" % what)
+    return t
+
+
+class Rotary:
+    """Rotary positions: pos int32 [tokens, axes], freq float32 [pairs of all
+    axes] (angle per unit position), pairs of each axis.  `interleaved`: a pair
+    is two neighbours; else an element of each half (keeps its tensors alive)."""
+
+    def __init__(self, pos: torch.Tensor, freq: torch.Tensor, pairs, interleaved: bool = False):
+        pairs = tuple(int(p) for p in pairs)
+        _int32(pos, "pos", 2)
+        if not 1 <= len(pairs) <= 4 or pos.shape[1] != len(pairs) or not pos.is_contiguous():
+            raise ValueError("pos must be a contiguous [tokens, axes] with 1 to 4 axes, as many as pairs")
+        if freq.dtype != torch.float32 or not freq.is_cuda or not freq.is_contiguous() \
+                or freq.numel() != sum(pairs):
+            raise ValueError("freq must be a contiguous CUDA float32 tensor of sum(pairs) elements")
+        self.tokens = pos.shape[0]
+        self.keep = (pos, freq)
+        p4 = (ctypes.c_int32 * 4)(*pairs)
+        flags = PCS_ROT_INTERLEAVED if interleaved else 0
+        self.forward = pcs_rotary(_ptr(pos), _ptr(freq), len(pairs), p4, flags)
+        self.inverse = pcs_rotary(_ptr(pos), _ptr(freq), len(pairs), p4, flags | PCS_ROT_INVERSE)
+
+
+class KvCache:
+    """Paged keys and values of many sessions: pools [pages, page_rows, heads,
+    head_dim] of float16 or bfloat16 (any strides but the last), table int32
+    [sessions, pages of a session], -1 an empty page.  The first `sinks` tokens
+    of a session stay; with `ring` the others reuse that many slots in turn.
+    v_table: the values' pages, where they are not the keys' (keeps its tensors
+    alive)."""
+
+    def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, table: torch.Tensor,
+                 sinks: int = 0, ring: int = 0, v_table: torch.Tensor = None):
+        if k_pool.dim() != 4 or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() \
+                or k_pool.dtype != v_pool.dtype or not k_pool.is_cuda or not v_pool.is_cuda:
+            raise ValueError("k_pool and v_pool must be CUDA tensors [pages, page_rows, heads, "
+                             "head_dim] of one shape, type and layout")
+        if k_pool.stride(3) != 1 or k_pool.dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError("pools must hold float16 or bfloat16 with contiguous heads")
+        _int32(table, "table", 2)
+        if v_table is not None:
+            _int32(v_table, "v_table", 2)
+            if v_table.shape != table.shape or v_table.stride() != table.stride():
+                raise ValueError("table and v_table must have one shape and layout")
+        n, rows, heads, dim = k_pool.shape
+        ps, rs, hs, _ = k_pool.stride()
+        self.sessions = table.shape[0]
+        self.heads, self.head_dim, self.dtype = heads, dim, k_pool.dtype
+        self.keep = (k_pool, v_pool, table, v_table)
+        self.struct = pcs_kv_cache(
+            _ptr(k_pool), _ptr(v_pool), _ptr(table), _ptr(v_table),
+            max(table.stride(0), table.shape[1]) if self.sessions <= 1 else table.stride(0),
+            ps if n > 1 else rows * heads * dim, rs if rows > 1 else heads * dim,
+            hs if heads > 1 else dim, n, table.shape[1], rows, heads, dim, sinks, ring,
+            _HEAD_DTYPES[k_pool.dtype])
+
+
+class KvBatch:
+    """New tokens of a call: lens int32 [sessions] (each session's length with
+    its new tokens); rows q_off[s] .. q_off[s + 1] of the call's tensors are
+    session s's, or the `tokens` are shared out evenly.  max_new: the most new
+    tokens of a session (needed with q_off); max_len: a hint, the longest
+    session (keeps its tensors alive)."""
+
+    def __init__(self, lens: torch.Tensor, tokens: int, q_off: torch.Tensor = None,
+                 max_new: int = 0, max_len: int = 0):
+        _int32(lens, "lens", 1)
+        if q_off is not None and _int32(q_off, "q_off", 1).numel() != lens.numel() + 1:
+            raise ValueError("q_off must have one element more than lens")
+        self.tokens, self.sessions = tokens, lens.numel()
+        self.keep = (lens, q_off)
+        self.struct = pcs_kv_batch(_ptr(lens), _ptr(q_off), tokens, lens.numel(), max_new, max_len, 0)
 
 
 # --------------------------------------------------------------------------
@@ -654,6 +798,74 @@ class Context:
         if failure:
             raise failure[0]
         check(st, "pcs_prune_global_part")
+
+    # -- paged cache of keys and values ------------------------------------------
+    def rotate(self, xs, rotary: Rotary, out=None, inverse: bool = False, stream=None) -> list:
+        """Rotary positions applied to each tensor [tokens, heads, head_dim] of
+        xs, or with `inverse` taken back (the gradient).  out: the results'
+        tensors (may be xs itself); returns them."""
+        if out is None:
+            out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in xs]
+        n = len(xs)
+        if len(out) != n or any(x.shape != y.shape or x.shape[0] != rotary.tokens
+                                for x, y in zip(xs, out)):
+            raise ValueError("every tensor and its result need the positions' %d tokens"
+                             % rotary.tokens)
+        arr = pcs_heads * max(n, 1)
+        check(self.lib.pcs_rotate(self.h, rotary.inverse if inverse else rotary.forward,
+                                  arr(*[_heads(x, "x") for x in xs]),
+                                  arr(*[_heads(y, "out") for y in out]), n, rotary.tokens,
+                                  _stream_ptr(stream)), "pcs_rotate")
+        return out
+
+    @staticmethod
+    def _check_tokens(cache: KvCache, batch: KvBatch, **tensors) -> None:
+        if batch.sessions > cache.sessions:
+            raise ValueError("%d sessions and %d page tables" % (batch.sessions, cache.sessions))
+        for what, t in tensors.items():
+            if t.shape[0] != batch.tokens:
+                raise ValueError("%s: %d tokens, the batch has %d" % (what, t.shape[0], batch.tokens))
+
+    def kv_append(self, cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor,
+                  q: torch.Tensor = None, rotary: Rotary = None, q_out: torch.Tensor = None,
+                  stream=None):
+        """Write the new tokens' keys (rotated) and values [tokens, heads,
+        head_dim] into the cache; with q, returns it rotated (q_out)."""
+        self._check_tokens(cache, batch, k=k, v=v)
+        if rotary is not None and rotary.tokens != batch.tokens:
+            raise ValueError("%d positions, the batch has %d tokens" % (rotary.tokens, batch.tokens))
+        qs = None
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            self._check_tokens(cache, batch, q=q, q_out=q_out)
+            qs = (_heads(q, "q"), _heads(q_out, "q_out"))
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        check(self.lib.pcs_kv_append(self.h, cache.struct, batch.struct,
+                                     None if rotary is None else rotary.forward, _heads(k, "k"),
+                                     _heads(v, "v"), qs and qs[0], qs and qs[1],
+                                     _stream_ptr(stream)), "pcs_kv_append")
+        return q_out
+
+    def attend(self, cache: KvCache, batch: KvBatch, q: torch.Tensor, out: torch.Tensor = None,
+               lse: torch.Tensor = None, scale: float = 0.0, window: int = 0,
+               return_lse: bool = False, stream=None):
+        """Attention of the new tokens' queries [tokens, q heads, head_dim] over
+        the cache; returns out, or (out, lse) if lse is given or asked for.
+        lse: float32 [tokens, q heads].  scale 0: 1 / sqrt(head_dim)."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        self._check_tokens(cache, batch, q=q, out=out)
+        if lse is None and return_lse:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2]
+                                or not lse.is_cuda or not lse.is_contiguous()):
+            raise ValueError("lse must be a contiguous CUDA float32 [tokens, q heads]")
+        check(self.lib.pcs_attend(self.h, cache.struct, batch.struct,
+                                  pcs_attend_params(scale, window, 0, 0), _heads(q, "q"),
+                                  _heads(out, "out"), _ptr(lse), _stream_ptr(stream)), "pcs_attend")
+        return out if lse is None else (out, lse)
 
     # -- snapshots -------------------------------------------------------------
     def record_bytes(self, session: Session) -> int:
