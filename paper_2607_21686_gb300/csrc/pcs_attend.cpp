@@ -265,32 +265,53 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     a.group = q->heads / cache->heads;
     a.by_group.set(a.group);
 
-    // Tokens a session sees at most, as far as the host knows: a hint for the
-    // split, which is right for any length.
+    const int64_t rows = static_cast<int64_t>(a.batch.max_new) * a.group;
+    const bool few = rows <= kTokenRowsMax;
+    // Tokens that the rows of a block see at most, as far as the host knows: a
+    // hint for the split, which is right for any length.
     int64_t seen = cache->ring ? static_cast<int64_t>(cache->sinks) + cache->ring : a.cache.slots;
     if (batch->max_len) seen = std::min<int64_t>(seen, batch->max_len);
-    if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + a.batch.max_new - 1);
+    const int64_t tokens = few ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
+    if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
     const int64_t pairs = static_cast<int64_t>(a.batch.sessions) * cache->heads;
-    const int64_t rows = static_cast<int64_t>(a.batch.max_new) * a.group;
 
     if ((st = call.begin())) return st;
     a.err = call.errors();
-    if (rows > kTokenRowsMax) return op_fail(PCS_E_INVAL, "too many new tokens");
-    const int64_t resident = static_cast<int64_t>(call.sm_count()) * attend_token_blocks_per_sm(cache->head_dim);
-    const int64_t tiles = (seen + 15) / 16;
-    int64_t splits = 1;
-    if (pairs <= kOpWords)
-      splits = std::max<int64_t>(1, std::min(resident / pairs, (tiles + 2 * kTokenWarps - 1) / (2 * kTokenWarps)));
+    if (few) {
+      const int64_t resident = static_cast<int64_t>(call.sm_count()) * attend_token_blocks_per_sm(cache->head_dim);
+      const int64_t tiles = (seen + 15) / 16;
+      int64_t splits = 1;
+      if (pairs <= kOpWords)
+        splits = std::max<int64_t>(1, std::min(resident / pairs, (tiles + 2 * kTokenWarps - 1) / (2 * kTokenWarps)));
+      a.splits = static_cast<int32_t>(splits);
+      if (pairs * splits > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
+      if (splits > 1) {
+        uint8_t* ws = nullptr;
+        st = call.scratch(4 * token_part_floats(static_cast<int>(rows), cache->head_dim) * pairs * splits, &ws, &a.ticket);
+        if (st) return st;
+        a.part = reinterpret_cast<float*>(ws);
+      }
+      call.before(kOpAttendToken);
+      if ((st = call.after(launch_attend_token(a, cache->dtype, static_cast<int>(rows), call.stream())))) return st;
+      return call.end();
+    }
+    const int64_t blocks = (rows + kBlockRows - 1) / kBlockRows;
+    if (blocks > 0x7FFFFFFFll / pairs) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
+    const int64_t tiles = (seen + kBlockTile - 1) / kBlockTile;
+    int64_t splits = std::max<int64_t>(1, std::min(call.sm_count() / (pairs * blocks), tiles / 4));
     a.splits = static_cast<int32_t>(splits);
-    if (pairs * splits > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
     if (splits > 1) {
       uint8_t* ws = nullptr;
-      st = call.scratch(4 * token_part_floats(static_cast<int>(rows), cache->head_dim) * pairs * splits, &ws, &a.ticket);
+      st = call.scratch(4 * block_part_floats(cache->head_dim) * splits * cache->heads * a.batch.tokens * a.group, &ws, &a.ticket);
       if (st) return st;
       a.part = reinterpret_cast<float*>(ws);
     }
-    call.before(kOpAttendToken);
-    if ((st = call.after(launch_attend_token(a, cache->dtype, static_cast<int>(rows), call.stream())))) return st;
+    call.before(kOpAttendBlock);
+    if ((st = call.after(launch_attend_block(a, cache->dtype, static_cast<int>(blocks), call.stream())))) return st;
+    if (splits > 1) {
+      call.before(kOpAttendJoin);
+      if ((st = call.after(launch_attend_join(a, cache->dtype, call.stream())))) return st;
+    }
     return call.end();
   });
 }

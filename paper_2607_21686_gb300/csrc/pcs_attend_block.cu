@@ -1,0 +1,651 @@
+// pcs_attend_block.cu -- attention of blocks of new tokens (frames, prompts)
+// over a paged cache of keys and values.
+//
+// k_attend_block  The same one-pass softmax as the token kernel's, with enough
+//                 query rows per key head that the matrix products bound it
+//                 (4 head_dim flops per visible pair of row and token): they
+//                 run on the fifth-generation tensor cores.  A block takes one
+//                 session, key head and 256 rows (query heads of a key head
+//                 side by side, then tokens) as two tiles of 128, and walks
+//                 the tokens they see in tiles of 128.  Per tile and row tile
+//                 S = Q K^T goes to tensor memory, four warps turn it into
+//                 weights (a thread per row), write them back as the first
+//                 operand of O += P V, which stays in tensor memory too; while
+//                 one row tile is with its warps the other one has the matrix
+//                 unit.  Four more warps copy keys and values (16-byte
+//                 asynchronous copies, so pages may have any size and end
+//                 anywhere in a tile) into a ring in shared memory, in the
+//                 128-byte swizzled layout the matrix unit reads.
+//                 A tile that some rows see in part may hold infinities or NaN
+//                 in values those rows must not see, and 0 * inf is NaN: there
+//                 the copying warps replace them by zeros, and the rows that
+//                 do see them take them up at the end.
+#include "pcs_attend_dev.cuh"
+
+namespace pcs {
+namespace {
+
+constexpr int kTile = 128;              // rows of a row tile, tokens of a tile
+constexpr int kSoftWarps = 8;           // warps 0-3: row tile 0, 4-7: row tile 1
+constexpr int kMmaWarp = 8;
+constexpr int kCopyWarp = 9;            // warps 9-12
+constexpr int kCopyWarps = 4;
+constexpr int kThreads = 32 * (kCopyWarp + kCopyWarps);
+constexpr int kLag = 2;                 // copies in flight behind the newest
+constexpr int kValid = 8;               // tiles whose masks are kept
+constexpr unsigned kFull = 0xffffffffu;
+constexpr float kSlack = 8.0f;          // as in the token kernel
+constexpr long long kWaitCycles = 4000000000ll;
+
+template <int DP>
+constexpr int kBuffers = DP == 64 ? 8 : 5;  // tiles of keys or values in the ring
+template <int DP>
+constexpr uint32_t kTileBytes = kTile * DP * 2;
+template <int DP>
+constexpr uint32_t kSmemBytes = (2 + kBuffers<DP>) * kTileBytes<DP> + 1024;
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(20000u)
+      : "memory");
+  return ok != 0;
+}
+// Bounded wait for the phase of the given parity; false: it gave up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  if (bar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity))
+    if (clock64() - t0 > kWaitCycles) return false;
+  return true;
+}
+
+// ---- Tensor memory and its matrix instruction ----------------------------------
+
+// Shared-memory operand in 128-byte rows of a 128-byte swizzle: eight rows are
+// 1,024 bytes, `lead` bytes lie between 64-element columns of a transposed one.
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t lead) {
+  return static_cast<uint64_t>((at >> 4) & 0x3fff) | (static_cast<uint64_t>(lead >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// 128 x N products of 16-bit elements into 32-bit floats; b_across: the second
+// operand lies with its columns, not its rows, in 128-byte rows.
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t instruction(uint32_t n, bool b_across) {
+  const uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  return (1u << 4) | (type << 7) | (type << 10) | ((b_across ? 1u : 0u) << 16) | ((n >> 3) << 17) |
+         ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t i, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(i), "r"(add ? 1u : 0u)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t i, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(i), "r"(add ? 1u : 0u)
+      : "memory");
+}
+// The barrier's arrival when everything issued so far has finished.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void fence_before() {
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void fence_after() {
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+// 32 columns of this warp's 32 lanes, a lane per thread.
+__device__ __forceinline__ void tm_load(uint32_t (&r)[32], uint32_t at) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+      "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+        "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+        "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
+        "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store(uint32_t at, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
+      "%26,%27,%28,%29,%30,%31,%32};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Columns of tensor memory: scores (then weights) and sums of the row tiles.
+constexpr uint32_t kScores = 0, kSums = 256;
+
+// What a block's rows see, the same for all its warps.
+struct Work {
+  SessionView all;    // the session
+  SessionView view;   // what these rows see
+  int32_t rows;       // of the session and key head
+  int32_t row0;       // the block's first
+  int32_t tile0, tiles;
+  int32_t pmin, pmax; // positions of the block's rows
+};
+
+__device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, int sp) {
+  Work w;
+  w.all = session_view(a, s);
+  w.rows = max(w.all.m, 0) * a.group;
+  w.row0 = blk * 2 * kTile;
+  w.tiles = 0;
+  if (w.row0 >= w.rows || w.all.m > a.batch.max_new) return w;
+  const int t0 = a.by_group.div(w.row0);
+  const int t1 = a.by_group.div(min(w.row0 + 2 * kTile, w.rows) - 1);
+  w.view = rows_view(a, w.all, t0, t1 + 1);
+  w.pmin = w.all.first + t0;
+  w.pmax = w.all.first + t1;
+  const int n = (w.view.seen + kTile - 1) / kTile;
+  const int per = (n + a.splits - 1) / a.splits;
+  w.tile0 = min(n, sp * per);
+  w.tiles = min(n, w.tile0 + per) - w.tile0;
+  return w;
+}
+
+// Whether rows at positions [pmin, pmax] all see all tokens of tile t, if
+// they are in the cache.
+__device__ __forceinline__ bool seen_whole(const AttendArgs& a, const SessionView& v, int t, int pmin, int pmax) {
+  const int e0 = t * kTile, e1 = e0 + kTile - 1;
+  if (e1 >= v.seen) return false;
+  const int32_t lo = seen_position(v, e0), hi = seen_position(v, e1);
+  return hi <= pmin && (a.window == 0 || lo > pmax - a.window || hi < a.cache.sinks);
+}
+
+// 16-bit elements (two in a word) whose exponent is all ones.
+template <typename T>
+__device__ __forceinline__ uint32_t specials(uint32_t x) {
+  const uint32_t e = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+  return ((x & e) == e ? 0xffffu : 0u) | ((x >> 16 & e) == e ? 0xffff0000u : 0u);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_constant__ AttendArgs a, int blocks) {
+  constexpr int kRing = kBuffers<DP>;
+  constexpr uint32_t kBytes = kTileBytes<DP>;
+  constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
+  constexpr int kChunks = DP / 8;
+  extern __shared__ __align__(16) uint8_t raw[];
+  __shared__ __align__(8) uint64_t bars[1 + 2 * kRing + 2 + 2 + 2];
+  __shared__ uint32_t tmem_at;
+  __shared__ uint32_t valid[kValid][4];
+  __shared__ uint32_t special;
+
+  attend_dependency();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int b = blockIdx.x;
+  const int head = b % a.cache.heads;
+  b /= a.cache.heads;
+  const int sp = b % a.splits;
+  b /= a.splits;
+  const int s = b % a.batch.sessions;
+  const int blk = blocks - 1 - b / a.batch.sessions;  // the longest first
+  const Work w = block_work(a, s, blk, sp);
+  if (w.all.m > a.batch.max_new) {
+    if (tid == 0) atomicOr(a.err, kDevErrIndex);
+    return;
+  }
+  if (w.row0 >= w.rows) return;
+  const int nq = w.rows - w.row0 > kTile ? 2 : 1;  // row tiles
+
+  const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
+  const uint32_t qat = smem, ring = smem + 2 * kBytes;
+  uint8_t* const ring_ptr = raw + (ring - smem_addr(raw));
+  const uint32_t bar0 = smem_addr(bars);
+  const uint32_t q_full = bar0;
+  auto kv_full = [&](int i) { return bar0 + 8 * (1 + i); };
+  auto kv_empty = [&](int i) { return bar0 + 8 * (1 + kRing + i); };
+  auto s_full = [&](int t) { return bar0 + 8 * (1 + 2 * kRing + t); };
+  auto p_full = [&](int t) { return bar0 + 8 * (3 + 2 * kRing + t); };
+  auto o_full = [&](int t) { return bar0 + 8 * (5 + 2 * kRing + t); };
+  if (tid == 0) {
+    bar_init(q_full, 32 * kCopyWarps);
+    for (int i = 0; i < kRing; ++i) {
+      bar_init(kv_full(i), 32 * kCopyWarps);
+      bar_init(kv_empty(i), 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      bar_init(s_full(t), 1);
+      bar_init(p_full(t), kTile);
+      bar_init(o_full(t), 1);
+    }
+    special = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (w.all.first < 0) atomicOr(a.err, kDevErrIndex);
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_at))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_at;
+  bool ok = true;
+
+  if (warp >= kCopyWarp && w.tiles > 0) {
+    // ---- Copying warps: warp c moves rows 32 c .. of each tile ----
+    const int c = warp - kCopyWarp, row0 = 32 * c;
+    constexpr int kAtOnce = 32 / kChunks;  // rows one instruction moves
+    const int chunk = lane % kChunks, sub = lane / kChunks;
+    const bool mine = chunk * 8 < a.cache.head_dim;
+    auto spot = [&](int row) {  // this lane's chunk of a row in a tile
+      return (chunk >> 3) * kPanel + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+    };
+    if (a.cache.head_dim < DP) {  // chunks that no copy writes
+      if (!mine)
+        for (int i = 0; i < 2 + kRing; ++i)
+          for (int r = sub; r < 32; r += kAtOnce)
+            *reinterpret_cast<uint4*>(ring_ptr - 2 * kBytes + i * kBytes + spot(row0 + r)) = make_uint4(0, 0, 0, 0);
+    }
+    // Query rows: zeros behind the last.
+    for (int t = 0; t < nq; ++t)
+#pragma unroll 4
+      for (int i = 0; i < 32 / kAtOnce; ++i) {
+        const int row = row0 + i * kAtOnce + sub, r = w.row0 + t * kTile + row;
+        const bool there = r < w.rows;
+        const uint32_t tok = a.by_group.div(there ? r : 0);
+        const int h = head * a.group + ((there ? r : 0) - tok * a.group);
+        const uint8_t* q = a.q.data + (w.all.q0 + tok) * a.q.token_bytes + h * a.q.head_bytes;
+        if (mine) copy16(qat + t * kBytes + spot(row), q + chunk * 16, there);
+      }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+
+    // Fill i: keys of tile i / 2, or its values.  Fill -1 stands for the
+    // query rows.
+    auto landed = [&](int i) {
+      if (i >= 0 && (i & 1)) {
+        const int t = w.tile0 + i / 2;
+        if (!seen_whole(a, w.view, t, w.pmin, w.pmax) && mine) {
+          uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
+          uint32_t any = 0;
+          for (int r = sub; r < 32; r += kAtOnce) {
+            uint4* x = reinterpret_cast<uint4*>(tile + spot(row0 + r));
+            uint4 v = *x;
+            const uint4 m = make_uint4(specials<T>(v.x), specials<T>(v.y), specials<T>(v.z), specials<T>(v.w));
+            if (m.x | m.y | m.z | m.w) {
+              any = 1;
+              v.x &= ~m.x, v.y &= ~m.y, v.z &= ~m.z, v.w &= ~m.w;
+              *x = v;
+            }
+          }
+          if (any) special = 1;
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive(i < 0 ? q_full : kv_full(i % kRing));
+    };
+    auto look = [&](int t) {
+      RowPlace r = {-1, -1};
+      const int e = t * kTile + row0 + lane;
+      if (e < w.view.seen) r = row_place(a, s, seen_position(w.view, e));
+      return r;
+    };
+    const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes;
+    const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
+    RowPlace place = look(w.tile0), next = place;
+    for (int i = 0; i < 2 * w.tiles && ok; ++i) {
+      const int buf = i % kRing, use = i / kRing;
+      if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
+      ok = __all_sync(kFull, ok);
+      if (!ok) break;
+      if ((i & 1) == 0) {
+        place = next;
+        const uint32_t there = __ballot_sync(kFull, place.k >= 0);
+        if (lane == 0) valid[(i / 2) % kValid][c] = there;
+        if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
+      }
+      const uint8_t* base = i & 1 ? vbase : kbase;
+      const int64_t off = place.k < 0 ? -1 : i & 1 ? place.v : place.k;
+      const uint32_t tile = ring + buf * kBytes;
+#pragma unroll 4
+      for (int r = 0; r < 32 / kAtOnce; ++r) {
+        const int row = r * kAtOnce + sub;
+        const int64_t o = __shfl_sync(kFull, off, row);
+        if (mine) copy16(tile + spot(row0 + row), base + (o < 0 ? 0 : o) + chunk * 16, o >= 0);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+      if (i - kLag >= -1) landed(i - kLag);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (ok)
+      for (int i = max(-1, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
+  } else if (warp == kMmaWarp && w.tiles > 0) {
+    // ---- The warp that feeds the matrix unit, by one of its threads ----
+    if (lane == 0) {
+      constexpr uint32_t kQK = instruction<T>(kTile, false), kPV = instruction<T>(DP, true);
+      auto scores = [&](int t, int i) {  // S = Q K^T of row tile t, keys of fill i
+        const uint32_t q = qat + t * kBytes, k = ring + (i % kRing) * kBytes;
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) {
+          const uint32_t at = (d >> 2) * kPanel + (d & 3) * 32;
+          mma_ss(tmem + kScores + t * kTile, operand(q + at, 16), operand(k + at, 16), kQK, d > 0);
+        }
+      };
+      auto sums = [&](int t, int i, bool add) {  // O += P V, values of fill i
+        const uint32_t v = ring + (i % kRing) * kBytes;
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_ts(tmem + kSums + t * DP, tmem + kScores + t * kTile + k * 8, operand(v + k * 2048, kPanel), kPV,
+                 add || k > 0);
+      };
+      ok = bar_wait(q_full, 0) && bar_wait(kv_full(0), 0);
+      if (ok) {
+        fence_after();
+        for (int t = 0; t < nq; ++t) {
+          scores(t, 0);
+          mma_commit(s_full(t));
+        }
+        mma_commit(kv_empty(0));
+      }
+      for (int j = 0; j < w.tiles && ok; ++j) {
+        const int vi = 2 * j + 1, ki = 2 * j + 2;
+        const bool more = j + 1 < w.tiles;
+        ok = bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
+        if (ok && more) ok = bar_wait(kv_full(ki % kRing), (ki / kRing) & 1);
+        for (int t = 0; t < nq && ok; ++t) {
+          ok = bar_wait(p_full(t), j & 1);
+          if (!ok) break;
+          fence_after();
+          sums(t, vi, j > 0);
+          if (t == nq - 1) mma_commit(kv_empty(vi % kRing));
+          if (more) {
+            scores(t, ki);
+            mma_commit(s_full(t));
+            if (t == nq - 1) mma_commit(kv_empty(ki % kRing));
+          } else {
+            mma_commit(o_full(t));
+          }
+        }
+      }
+    }
+    __syncwarp();
+    ok = __shfl_sync(kFull, ok, 0);
+  } else if (warp < kSoftWarps && (warp >> 2) < nq) {
+    // ---- A thread per row: weights, running maximum and total ----
+    const int t = warp >> 2;
+    const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // its warp's lanes of tensor memory
+    const uint32_t sc = tmem + kScores + t * kTile + lanes, su = tmem + kSums + t * DP + lanes;
+    const int r = w.row0 + t * kTile + (warp & 3) * 32 + lane;
+    const bool there = r < w.rows;
+    const uint32_t tok = a.by_group.div(there ? r : w.rows - 1);
+    const int32_t p = w.all.first + static_cast<int32_t>(tok);
+    // Positions of the row tile.
+    const int32_t pmin = w.all.first + static_cast<int32_t>(a.by_group.div(w.row0 + t * kTile));
+    const int32_t pmax = w.all.first + static_cast<int32_t>(a.by_group.div(min(w.row0 + (t + 1) * kTile, w.rows) - 1));
+    float top = -INFINITY, total = 0.0f;
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int ki = 2 * j;
+      ok = bar_wait(s_full(t), j & 1) && bar_wait(kv_full(ki % kRing), (ki / kRing) & 1);
+      ok = __all_sync(kFull, ok);
+      if (!ok) break;
+      fence_after();
+      const int tile = w.tile0 + j;
+      const uint32_t* in = valid[j % kValid];
+      const bool whole = seen_whole(a, w.view, tile, pmin, pmax) && (in[0] & in[1] & in[2] & in[3]) == kFull;
+      auto fetch = [&](uint32_t (&x)[32], int c) {
+        tm_load(x, sc + c * 32);
+        tm_loaded();
+        if (!whole) {
+          const uint32_t m = in[c];
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (!((m >> k & 1) && sees(a, p, seen_position(w.view, tile * kTile + c * 32 + k))))
+              x[k] = 0xff800000u;  // -inf
+        }
+      };
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t x[32];
+        fetch(x, c);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(x[k]));
+      }
+      const float high = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+      const bool raise = high > top + kSlack;
+      if (__any_sync(kFull, raise)) {
+        const float to = raise ? high : top;
+        const float f = raise ? exp2_fast(top - to) : 1.0f;
+        top = to;
+        total *= f;
+        if (j > 0) {
+#pragma unroll
+          for (int c = 0; c < DP / 32; ++c) {
+            uint32_t x[32];
+            tm_load(x, su + c * 32);
+            tm_loaded();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+            tm_store(su + c * 32, x);
+          }
+        }
+      }
+      const float at = top == -INFINITY ? 0.0f : top;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t y[32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t x[32];
+          fetch(x, 2 * h + c);
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            const float u = exp2_fast(fmaf(__uint_as_float(x[k]), a.scale_log2, -at));
+            const float v = exp2_fast(fmaf(__uint_as_float(x[k + 1]), a.scale_log2, -at));
+            sum[k & 2] += u;
+            sum[(k & 2) + 1] += v;
+            y[c * 16 + k / 2] = pack2<T>(u, v);
+          }
+        }
+        // Weights over the first scores: those this half needs later lie behind.
+        tm_store(sc + h * 32, y);
+      }
+      total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tm_stored();
+      fence_before();
+      bar_arrive(p_full(t));
+    }
+    if (ok && w.tiles > 0) ok = bar_wait(o_full(t), 0);
+    ok = __all_sync(kFull, ok);
+    fence_after();
+    constexpr float kLn2 = 0.693147180559945309f;
+    const int64_t qt = w.all.q0 + tok;
+    const int h = head * a.group + (r - static_cast<int>(tok) * a.group);
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const bool mend = *reinterpret_cast<volatile uint32_t*>(&special) != 0;
+    const int64_t row = (static_cast<int64_t>(sp) * a.cache.heads + head) * a.batch.tokens * a.group +
+                        w.all.q0 * a.group + r;
+    float* part = a.part + row * (DP + 2);
+#pragma unroll 1
+    for (int c = 0; c < DP / 32; ++c) {
+      uint32_t x[32];
+      if (w.tiles > 0) {
+        tm_load(x, su + c * 32);
+        tm_loaded();
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) x[k] = 0;
+      }
+      if (!ok || !there) continue;
+      if (mend) {
+        // Infinities and NaN among the values that this row sees in tiles
+        // where zeros took their place.
+        for (int j = w.tile0; j < w.tile0 + w.tiles; ++j) {
+          if (seen_whole(a, w.view, j, w.pmin, w.pmax)) continue;
+          for (int e = j * kTile; e < min((j + 1) * kTile, w.view.seen); ++e) {
+            const int32_t at = seen_position(w.view, e);
+            if (!sees(a, p, at)) continue;
+            const RowPlace pl = row_place(a, s, at);
+            if (pl.k < 0) continue;
+            const uint8_t* v = a.cache.v + head * a.cache.head_bytes + pl.v + c * 64;
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              if (c * 32 + k >= a.cache.head_dim) continue;
+              const uint32_t y = *reinterpret_cast<const uint32_t*>(v + 2 * k), m = specials<T>(y);
+              T e0, e1;
+              const uint16_t lo = static_cast<uint16_t>(y), hi = static_cast<uint16_t>(y >> 16);
+              memcpy(&e0, &lo, 2);
+              memcpy(&e1, &hi, 2);
+              if (m & 0xffffu) x[k] = __float_as_uint(__uint_as_float(x[k]) + static_cast<float>(e0));
+              if (m >> 16) x[k + 1] = __float_as_uint(__uint_as_float(x[k + 1]) + static_cast<float>(e1));
+            }
+          }
+        }
+      }
+      if (a.splits > 1) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 2)
+          *reinterpret_cast<float2*>(part + c * 32 + k) =
+              make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+      } else {
+        uint8_t* o = a.out.data + qt * a.out.token_bytes + h * a.out.head_bytes + c * 64;
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+          if (c * 32 + k >= a.cache.head_dim) continue;
+          uint4 y;
+          y.x = pack2<T>(__uint_as_float(x[k]) * inv, __uint_as_float(x[k + 1]) * inv);
+          y.y = pack2<T>(__uint_as_float(x[k + 2]) * inv, __uint_as_float(x[k + 3]) * inv);
+          y.z = pack2<T>(__uint_as_float(x[k + 4]) * inv, __uint_as_float(x[k + 5]) * inv);
+          y.w = pack2<T>(__uint_as_float(x[k + 6]) * inv, __uint_as_float(x[k + 7]) * inv);
+          *reinterpret_cast<uint4*>(o + 2 * k) = y;
+        }
+      }
+    }
+    if (ok && there) {
+      if (a.splits > 1) {
+        *reinterpret_cast<float2*>(part + DP) = make_float2(top, total);
+      } else if (a.lse) {
+        a.lse[qt * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
+            total == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(total));
+      }
+    }
+  }
+  if (!ok && lane == 0) atomicOr(a.err, kDevErrTimeout);
+  fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+}
+
+// Joins the parts of every row: a warp each.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ AttendArgs a) {
+  attend_dependency();
+  const int64_t rows = a.batch.tokens * a.group;  // of a key head
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (i >= rows * a.cache.heads) return;
+  const int lane = threadIdx.x & 31;
+  const int head = static_cast<int>(i / rows);
+  const int64_t r = i - head * rows;
+  const int64_t tok = r / a.group;
+  const int h = head * a.group + static_cast<int>(r - tok * a.group);
+  const float* part = a.part + i * (DP + 2);
+  const int64_t step = rows * a.cache.heads * (DP + 2);
+  float top = -INFINITY;
+  for (int w = 0; w < a.splits; ++w) top = fmaxf(top, __ldcg(part + w * step + DP));
+  const float at = top == -INFINITY ? 0.0f : top;
+  float o[DP / 32] = {}, total = 0.0f;
+  for (int w = 0; w < a.splits; ++w) {
+    const float2 x = __ldcg(reinterpret_cast<const float2*>(part + w * step + DP));
+    const float f = exp2_fast(x.x - at);
+    total = fmaf(x.y, f, total);
+#pragma unroll
+    for (int k = 0; k < DP / 64; ++k) {
+      const float2 v = __ldcg(reinterpret_cast<const float2*>(part + w * step + 64 * k + 2 * lane));
+      o[2 * k] = fmaf(v.x, f, o[2 * k]);
+      o[2 * k + 1] = fmaf(v.y, f, o[2 * k + 1]);
+    }
+  }
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  uint8_t* out = a.out.data + tok * a.out.token_bytes + h * a.out.head_bytes;
+#pragma unroll
+  for (int k = 0; k < DP / 64; ++k) {
+    const int d = 64 * k + 2 * lane;
+    if (d < a.cache.head_dim) *reinterpret_cast<uint32_t*>(out + 2 * d) = pack2<T>(o[2 * k] * inv, o[2 * k + 1] * inv);
+  }
+  if (lane == 0 && a.lse)
+    a.lse[tok * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
+        total == 0.0f ? -INFINITY : fmaf(top, 0.693147180559945309f, logf(total));
+}
+
+cudaLaunchConfig_t config(int64_t grid, int threads, uint32_t smem, cudaLaunchAttribute* attr, cudaStream_t stream) {
+  attr->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr->val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
+template <typename T, int DP>
+cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t stream) {
+  auto k = k_attend_block<T, DP>;
+  static SmemLimit limit;
+  if (cudaError_t e = limit.set(k, kSmemBytes<DP>)) return e;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg =
+      config(static_cast<int64_t>(blocks) * a.batch.sessions * a.splits * a.cache.heads, kThreads, kSmemBytes<DP>, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, k, a, blocks);
+}
+
+template <typename T, int DP>
+cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream) {
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = config((a.batch.tokens * a.group * a.cache.heads + 7) / 8, 256, 0, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, k_attend_join<T, DP>, a);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream) {
+  if (dtype == PCS_DT_F16)
+    return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, stream) : launch<__half, 128>(a, blocks, stream);
+  return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, stream)
+                                : launch<__nv_bfloat16, 128>(a, blocks, stream);
+}
+
+cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, cudaStream_t stream) {
+  if (dtype == PCS_DT_F16)
+    return a.cache.head_dim <= 64 ? launch_join<__half, 64>(a, stream) : launch_join<__half, 128>(a, stream);
+  return a.cache.head_dim <= 64 ? launch_join<__nv_bfloat16, 64>(a, stream) : launch_join<__nv_bfloat16, 128>(a, stream);
+}
+
+}  // namespace pcs

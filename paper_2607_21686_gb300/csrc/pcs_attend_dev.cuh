@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cstring>
+#include <type_traits>
 #include <cstdint>
 
 #include "pcs_attend.h"
@@ -116,6 +118,11 @@ __device__ __forceinline__ SessionView rows_view(const AttendArgs& a, const Sess
 // Position of the e-th token of a view.
 __device__ __forceinline__ int32_t seen_position(const SessionView& v, int32_t e) {
   return e < v.sinks ? e : v.lo + (e - v.sinks);
+}
+
+// Whether the token at position p sees the one at position `at`.
+__device__ __forceinline__ bool sees(const AttendArgs& a, int32_t p, int32_t at) {
+  return at <= p && (a.window == 0 || at < a.cache.sinks || at > p - a.window);
 }
 
 // Where position p of session s is in the cache (of head 0): byte offsets of

@@ -220,7 +220,10 @@ __global__ void __launch_bounds__(kThreads)
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[n][i] *= a.scale_log2;
-    if (many || there != 0xffffu) {
+    const int32_t lo = seen_position(view, t * kTile), hi = seen_position(view, t * kTile + kTile - 1);
+    const bool part = many && !(hi <= view.first && (a.window == 0 || hi < a.cache.sinks ||
+                                                     lo > view.first + view.m - 1 - a.window));
+    if (part || there != 0xffffu) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int row = g + 8 * h;
@@ -229,11 +232,8 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const bool sees = in && p <= pos[n][i] &&
-                              (a.window == 0 || p < a.cache.sinks || p > pos[n][i] - a.window);
-            if (!sees) c[n][2 * h + i] = -INFINITY;
-          }
+          for (int i = 0; i < 2; ++i)
+            if (!in || (many && !sees(a, pos[n][i], p))) c[n][2 * h + i] = -INFINITY;
       }
     }
     bool raise = false;
@@ -273,13 +273,50 @@ __global__ void __launch_bounds__(kThreads)
       w[n][0] = transposed(pack2<T>(p0, p1));
       w[n][1] = transposed(pack2<T>(p2, p3));
     }
-#pragma unroll
-    for (int d = 0; d < DP / 16; ++d) {
-      uint32_t f[4];
+    auto values = [&](uint32_t (&f)[4], int d) {
       const int row = (lane & 7) + (lane >> 4) * 8;
       ldm4t(f, vat + row * (DP * 2) + (((d * 2 + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+    };
+    if (!part) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) mma<T>(o[d][n], f, w[n][0], w[n][1]);
+      for (int d = 0; d < DP / 16; ++d) {
+        uint32_t f[4];
+        values(f, d);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma<T>(o[d][n], f, w[n][0], w[n][1]);
+      }
+    } else {
+      // Tokens that some rows see and others do not: a weight of 0 would not
+      // keep an infinity or a NaN out, so each new token's rows take what the
+      // values come to with those it does not see taken out.
+      for (int i = 0; i < view.m; ++i) {
+        uint32_t in[2];  // of tokens 2 q4, +1 and 8 more
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int e = t * kTile + 8 * h + 2 * q4;
+          in[h] = (sees(a, view.first + i, seen_position(view, e)) ? 0xffffu : 0u) |
+                  (sees(a, view.first + i, seen_position(view, e + 1)) ? 0xffff0000u : 0u);
+        }
+        bool mine[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) mine[n][h] = pos[n][h] == view.first + i;
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) {
+          uint32_t f[4];
+          values(f, d);
+          f[0] &= in[0], f[1] &= in[0], f[2] &= in[1], f[3] &= in[1];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            mma<T>(x, f, w[n][0], w[n][1]);
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              if (mine[n][h & 1]) o[d][n][h] += x[h];
+          }
+        }
+      }
     }
     __syncwarp();  // the stage may be filled again
     stage = stage + 1 == kStages ? 0 : stage + 1;
