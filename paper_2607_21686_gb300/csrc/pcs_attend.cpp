@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <numeric>
 
 #include "pcs.h"
 #include "pcs_attend.h"
@@ -77,6 +78,16 @@ pcs_status check_cache(const pcs_kv_cache* c, CacheDev* d) {
   d->page_bytes = 2 * c->page_stride;
   d->row_bytes = 2 * c->row_stride;
   d->head_bytes = 2 * c->head_stride;
+  const uint64_t unit = std::gcd(static_cast<uint64_t>(d->page_bytes), static_cast<uint64_t>(d->row_bytes));
+  d->unit = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(unit, 16), 0x7FFFFFF0u));
+  if (d->page_bytes % d->unit || d->row_bytes % d->unit) d->unit = 16;
+  const uint64_t pu = d->page_bytes / d->unit, ru = d->row_bytes / d->unit;
+  if (pu > 0xFFFFFFFEull || ru > 0xFFFFFFFEull ||
+      pu * (c->n_pages - 1) > 0xFFFFFFFEull - std::min<uint64_t>(ru * (c->page_rows - 1), 0xFFFFFFFEull))
+    return op_fail(PCS_E_INVAL, "cache: rows lie more than 2^32 common divisors (%u bytes) of their strides apart",
+                   d->unit);
+  d->page_units = static_cast<uint32_t>(pu);
+  d->row_units = static_cast<uint32_t>(ru);
   d->page_rows.set(c->page_rows);
   if (c->ring) d->ring.set(c->ring);
   d->n_pages = c->n_pages;

@@ -78,6 +78,8 @@ struct CacheDev {
   const int32_t* v_table;  // null: the K pages' table
   int64_t table_stride;
   int64_t page_bytes, row_bytes, head_bytes;  // strides
+  uint32_t unit, page_units, row_units;       // page and row strides in units of `unit` bytes,
+                                              // in which every row's offset has 32 bits
   FastDiv page_rows, ring;
   int32_t n_pages, slots;   // slots a table has room for
   int32_t heads, head_dim;

@@ -28,8 +28,11 @@ namespace {
 constexpr int kTile = 128;              // rows of a row tile, tokens of a tile
 constexpr int kSoftWarps = 8;           // warps 0-3: row tile 0, 4-7: row tile 1
 constexpr int kMmaWarp = 8;
-constexpr int kCopyWarp = 9;            // warps 9-12
+constexpr int kCopyWarp = 12;           // warps 12-15 (9-11 make up the fours that registers go by)
 constexpr int kCopyWarps = 4;
+// Registers of a thread: the launch's 128 shared out anew, 2 x 128 x 184 +
+// 2 x 128 x 72 = 512 x 128.
+constexpr int kSoftRegs = 184, kOtherRegs = 72;
 constexpr int kThreads = 32 * (kCopyWarp + kCopyWarps);
 constexpr int kLag = 2;                 // copies in flight behind the newest
 constexpr int kValid = 8;               // tiles whose masks are kept
@@ -139,6 +142,31 @@ __device__ __forceinline__ void tm_store(uint32_t at, const uint32_t (&r)[32]) {
 __device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Two floats side by side, and operations on both.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& x, float& y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+
 // Columns of tensor memory: scores (then weights) and sums of the row tiles.
 constexpr uint32_t kScores = 0, kSums = 256;
 
@@ -171,13 +199,29 @@ __device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, 
   return w;
 }
 
-// Whether rows at positions [pmin, pmax] all see all tokens of tile t, if
-// they are in the cache.
-__device__ __forceinline__ bool seen_whole(const AttendArgs& a, const SessionView& v, int t, int pmin, int pmax) {
-  const int e0 = t * kTile, e1 = e0 + kTile - 1;
-  if (e1 >= v.seen) return false;
-  const int32_t lo = seen_position(v, e0), hi = seen_position(v, e1);
-  return hi <= pmin && (a.window == 0 || lo > pmax - a.window || hi < a.cache.sinks);
+// What the rows of a block or of a row tile see, at positions [pmin, pmax].
+struct RowsRange {
+  int32_t hi_min, hi_max, lo_min, lo_max, first;
+  // They all see all tokens of tile t, if those are in the cache.
+  __device__ __forceinline__ bool whole(int t) const {
+    const int e0 = t * kTile, e1 = e0 + kTile - 1;
+    return e1 <= hi_min && (e0 >= lo_max || e1 < first);
+  }
+  // Some row sees some token of it.
+  __device__ __forceinline__ bool some(int t) const {
+    const int e0 = t * kTile, e1 = e0 + kTile - 1;
+    return e0 <= hi_max && (e1 >= lo_min || e0 < first);
+  }
+};
+__device__ __forceinline__ RowsRange rows_range(const AttendArgs& a, const SessionView& v, int pmin, int pmax) {
+  const RowRange x = row_range(a, v, pmin), y = row_range(a, v, pmax);
+  return {x.hi, y.hi, x.lo, y.lo, x.first};
+}
+// Of row tile t.
+__device__ __forceinline__ RowsRange tile_range(const AttendArgs& a, const Work& w, int t) {
+  const int r0 = w.row0 + t * kTile, r1 = min(r0 + kTile, w.rows) - 1;
+  return rows_range(a, w.view, w.all.first + static_cast<int>(a.by_group.div(r0)),
+                    w.all.first + static_cast<int>(a.by_group.div(r1)));
 }
 
 // 16-bit elements (two in a word) whose exponent is all ones.
@@ -196,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
   extern __shared__ __align__(16) uint8_t raw[];
   __shared__ __align__(8) uint64_t bars[1 + 2 * kRing + 2 + 2 + 2];
   __shared__ uint32_t tmem_at;
-  __shared__ uint32_t valid[kValid][4];
+  __shared__ __align__(16) uint32_t valid[kValid][4];
   __shared__ uint32_t special;
 
   attend_dependency();
@@ -252,7 +296,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
   const uint32_t tmem = tmem_at;
   bool ok = true;
 
-  if (warp >= kCopyWarp && w.tiles > 0) {
+  if (warp >= kCopyWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (w.tiles > 0) {
     // ---- Copying warps: warp c moves rows 32 c .. of each tile ----
     const int c = warp - kCopyWarp, row0 = 32 * c;
     constexpr int kAtOnce = 32 / kChunks;  // rows one instruction moves
@@ -280,12 +326,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
       }
     asm volatile("cp.async.commit_group;" ::: "memory");
 
+    const RowsRange range = rows_range(a, w.view, w.pmin, w.pmax);
     // Fill i: keys of tile i / 2, or its values.  Fill -1 stands for the
     // query rows.
     auto landed = [&](int i) {
       if (i >= 0 && (i & 1)) {
-        const int t = w.tile0 + i / 2;
-        if (!seen_whole(a, w.view, t, w.pmin, w.pmax) && mine) {
+        if (!range.whole(w.tile0 + i / 2) && mine) {
           uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
           uint32_t any = 0;
           for (int r = sub; r < 32; r += kAtOnce) {
@@ -305,13 +351,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
       bar_arrive(i < 0 ? q_full : kv_full(i % kRing));
     };
     auto look = [&](int t) {
-      RowPlace r = {-1, -1};
+      RowPlace r = {kNoRow, kNoRow};
       const int e = t * kTile + row0 + lane;
       if (e < w.view.seen) r = row_place(a, s, seen_position(w.view, e));
       return r;
     };
-    const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes;
-    const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
+    const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes + chunk * 16;
+    const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes + chunk * 16;
     RowPlace place = look(w.tile0), next = place;
     for (int i = 0; i < 2 * w.tiles && ok; ++i) {
       const int buf = i % kRing, use = i / kRing;
@@ -320,18 +366,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
       if (!ok) break;
       if ((i & 1) == 0) {
         place = next;
-        const uint32_t there = __ballot_sync(kFull, place.k >= 0);
+        const uint32_t there = __ballot_sync(kFull, place.k != kNoRow);
         if (lane == 0) valid[(i / 2) % kValid][c] = there;
         if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
       }
       const uint8_t* base = i & 1 ? vbase : kbase;
-      const int64_t off = place.k < 0 ? -1 : i & 1 ? place.v : place.k;
+      const uint32_t off = i & 1 ? place.v : place.k;
       const uint32_t tile = ring + buf * kBytes;
 #pragma unroll 4
       for (int r = 0; r < 32 / kAtOnce; ++r) {
         const int row = r * kAtOnce + sub;
-        const int64_t o = __shfl_sync(kFull, off, row);
-        if (mine) copy16(tile + spot(row0 + row), base + (o < 0 ? 0 : o) + chunk * 16, o >= 0);
+        const uint32_t o = __shfl_sync(kFull, off, row);
+        const bool in = o != kNoRow;
+        if (mine) copy16(tile + spot(row0 + row), row_at(a, base, in ? o : 0), in);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
       asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
@@ -340,9 +387,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (ok)
       for (int i = max(-1, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
-  } else if (warp == kMmaWarp && w.tiles > 0) {
+    }
+  } else if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     // ---- The warp that feeds the matrix unit, by one of its threads ----
-    if (lane == 0) {
+    if (warp == kMmaWarp && lane == 0 && w.tiles > 0) {
       constexpr uint32_t kQK = instruction<T>(kTile, false), kPV = instruction<T>(DP, true);
       auto scores = [&](int t, int i) {  // S = Q K^T of row tile t, keys of fill i
         const uint32_t q = qat + t * kBytes, k = ring + (i % kRing) * kBytes;
@@ -359,39 +408,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
           mma_ts(tmem + kSums + t * DP, tmem + kScores + t * kTile + k * 8, operand(v + k * 2048, kPanel), kPV,
                  add || k > 0);
       };
-      ok = bar_wait(q_full, 0) && bar_wait(kv_full(0), 0);
-      if (ok) {
-        fence_after();
-        for (int t = 0; t < nq; ++t) {
-          scores(t, 0);
-          mma_commit(s_full(t));
-        }
-        mma_commit(kv_empty(0));
+      RowsRange range[2];
+      int done[2] = {0, 0}, end[2] = {-1, -1};  // tiles taken, the last one
+      for (int t = 0; t < nq; ++t) {
+        range[t] = tile_range(a, w, t);
+        for (int j = 0; j < w.tiles; ++j)
+          if (range[t].some(w.tile0 + j)) end[t] = j;
       }
-      for (int j = 0; j < w.tiles && ok; ++j) {
+      ok = bar_wait(q_full, 0);
+      for (int j = -1; j < w.tiles && ok; ++j) {  // values of tile j, keys of the next
         const int vi = 2 * j + 1, ki = 2 * j + 2;
         const bool more = j + 1 < w.tiles;
-        ok = bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
+        if (j >= 0) ok = bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
         if (ok && more) ok = bar_wait(kv_full(ki % kRing), (ki / kRing) & 1);
+        fence_after();
         for (int t = 0; t < nq && ok; ++t) {
-          ok = bar_wait(p_full(t), j & 1);
-          if (!ok) break;
-          fence_after();
-          sums(t, vi, j > 0);
-          if (t == nq - 1) mma_commit(kv_empty(vi % kRing));
-          if (more) {
+          if (j >= 0 && range[t].some(w.tile0 + j)) {
+            ok = bar_wait(p_full(t), done[t] & 1);
+            if (!ok) break;
+            fence_after();
+            sums(t, vi, done[t] > 0);
+            done[t] += 1;
+            if (j == end[t]) mma_commit(o_full(t));
+          }
+          if (j >= 0 && t == nq - 1) mma_commit(kv_empty(vi % kRing));
+          if (more && range[t].some(w.tile0 + j + 1)) {
             scores(t, ki);
             mma_commit(s_full(t));
-            if (t == nq - 1) mma_commit(kv_empty(ki % kRing));
-          } else {
-            mma_commit(o_full(t));
           }
+          if (more && t == nq - 1) mma_commit(kv_empty(ki % kRing));
         }
       }
     }
     __syncwarp();
     ok = __shfl_sync(kFull, ok, 0);
-  } else if (warp < kSoftWarps && (warp >> 2) < nq) {
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    if ((warp >> 2) < nq) {
     // ---- A thread per row: weights, running maximum and total ----
     const int t = warp >> 2;
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // its warp's lanes of tensor memory
@@ -399,85 +452,91 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
     const int r = w.row0 + t * kTile + (warp & 3) * 32 + lane;
     const bool there = r < w.rows;
     const uint32_t tok = a.by_group.div(there ? r : w.rows - 1);
-    const int32_t p = w.all.first + static_cast<int32_t>(tok);
-    // Positions of the row tile.
-    const int32_t pmin = w.all.first + static_cast<int32_t>(a.by_group.div(w.row0 + t * kTile));
-    const int32_t pmax = w.all.first + static_cast<int32_t>(a.by_group.div(min(w.row0 + (t + 1) * kTile, w.rows) - 1));
+    const RowRange sees = row_range(a, w.view, w.all.first + static_cast<int32_t>(tok));
+    const RowsRange range = tile_range(a, w, t);
     float top = -INFINITY, total = 0.0f;
+    int done = 0;
     for (int j = 0; j < w.tiles && ok; ++j) {
-      const int ki = 2 * j;
-      ok = bar_wait(s_full(t), j & 1) && bar_wait(kv_full(ki % kRing), (ki / kRing) & 1);
+      const int tile = w.tile0 + j;
+      if (!range.some(tile)) continue;
+      ok = bar_wait(s_full(t), done & 1);
       ok = __all_sync(kFull, ok);
       if (!ok) break;
       fence_after();
-      const int tile = w.tile0 + j;
-      const uint32_t* in = valid[j % kValid];
-      const bool whole = seen_whole(a, w.view, tile, pmin, pmax) && (in[0] & in[1] & in[2] & in[3]) == kFull;
-      auto fetch = [&](uint32_t (&x)[32], int c) {
-        tm_load(x, sc + c * 32);
-        tm_loaded();
-        if (!whole) {
-          const uint32_t m = in[c];
+      uint32_t x[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tm_load(x[c], sc + c * 32);
+      tm_loaded();
+      const uint4 in = *reinterpret_cast<const uint4*>(valid[j % kValid]);
+      if (!(range.whole(tile) && (in.x & in.y & in.z & in.w) == kFull)) {
+        const uint32_t m4[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t m = m4[c] & sees.bits(tile * kTile + c * 32);
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (!((m >> k & 1) && sees(a, p, seen_position(w.view, tile * kTile + c * 32 + k))))
-              x[k] = 0xff800000u;  // -inf
+            if (!(m >> k & 1)) x[c][k] = 0xff800000u;  // -inf
         }
-      };
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t x[32];
-        fetch(x, c);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(x[k]));
       }
-      const float high = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+      float high = -INFINITY;
+      {
+        float mx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          mx[c] = __uint_as_float(x[c][0]);
+#pragma unroll
+          for (int k = 1; k < 31; k += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
+          mx[c] = fmaxf(mx[c], __uint_as_float(x[c][31]));
+        }
+        high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
+      }
       const bool raise = high > top + kSlack;
       if (__any_sync(kFull, raise)) {
         const float to = raise ? high : top;
         const float f = raise ? exp2_fast(top - to) : 1.0f;
         top = to;
         total *= f;
-        if (j > 0) {
-#pragma unroll
+        if (done > 0) {
+#pragma unroll 1
           for (int c = 0; c < DP / 32; ++c) {
-            uint32_t x[32];
-            tm_load(x, su + c * 32);
+            uint32_t y[32];
+            tm_load(y, su + c * 32);
             tm_loaded();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-            tm_store(su + c * 32, x);
+            for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+            tm_store(su + c * 32, y);
           }
         }
       }
       const float at = top == -INFINITY ? 0.0f : top;
-      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), at2 = pair(-at, -at);
+      uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t y[32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t x[32];
-          fetch(x, 2 * h + c);
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            const float u = exp2_fast(fmaf(__uint_as_float(x[k]), a.scale_log2, -at));
-            const float v = exp2_fast(fmaf(__uint_as_float(x[k + 1]), a.scale_log2, -at));
-            sum[k & 2] += u;
-            sum[(k & 2) + 1] += v;
-            y[c * 16 + k / 2] = pack2<T>(u, v);
-          }
+        for (int k = 0; k < 32; ++k) {
+          const uint32_t* z = &x[2 * h + k / 16][k % 16 * 2];
+          float u, v;
+          unpair(fma2(pair(__uint_as_float(z[0]), __uint_as_float(z[1])), scale2, at2), u, v);
+          u = exp2_fast(u);
+          v = exp2_fast(v);
+          sum[k & 1] = add2(sum[k & 1], pair(u, v));
+          y[k] = pack2<T>(u, v);
         }
-        // Weights over the first scores: those this half needs later lie behind.
+        // Weights over the first half of the scores, all of which are in
+        // registers by now.
         tm_store(sc + h * 32, y);
       }
-      total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      float u, v;
+      unpair(add2(sum[0], sum[1]), u, v);
+      total += u + v;
       tm_stored();
       fence_before();
       bar_arrive(p_full(t));
+      done += 1;
     }
-    if (ok && w.tiles > 0) ok = bar_wait(o_full(t), 0);
+    if (ok && done > 0) ok = bar_wait(o_full(t), 0);
     ok = __all_sync(kFull, ok);
     fence_after();
     constexpr float kLn2 = 0.693147180559945309f;
@@ -491,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
 #pragma unroll 1
     for (int c = 0; c < DP / 32; ++c) {
       uint32_t x[32];
-      if (w.tiles > 0) {
+      if (done > 0) {
         tm_load(x, su + c * 32);
         tm_loaded();
       } else {
@@ -502,14 +561,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
       if (mend) {
         // Infinities and NaN among the values that this row sees in tiles
         // where zeros took their place.
+        const RowsRange block = rows_range(a, w.view, w.pmin, w.pmax);
         for (int j = w.tile0; j < w.tile0 + w.tiles; ++j) {
-          if (seen_whole(a, w.view, j, w.pmin, w.pmax)) continue;
+          if (block.whole(j)) continue;
           for (int e = j * kTile; e < min((j + 1) * kTile, w.view.seen); ++e) {
-            const int32_t at = seen_position(w.view, e);
-            if (!sees(a, p, at)) continue;
-            const RowPlace pl = row_place(a, s, at);
-            if (pl.k < 0) continue;
-            const uint8_t* v = a.cache.v + head * a.cache.head_bytes + pl.v + c * 64;
+            if (!(sees.bits(e) & 1)) continue;
+            const RowPlace pl = row_place(a, s, seen_position(w.view, e));
+            if (pl.k == kNoRow) continue;
+            const uint8_t* v = row_at(a, a.cache.v + head * a.cache.head_bytes, pl.v) + c * 64;
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
               if (c * 32 + k >= a.cache.head_dim) continue;
@@ -551,6 +610,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
             total == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(total));
       }
     }
+  }
   }
   if (!ok && lane == 0) atomicOr(a.err, kDevErrTimeout);
   fence_before();

@@ -120,26 +120,22 @@ __device__ __forceinline__ int32_t seen_position(const SessionView& v, int32_t e
   return e < v.sinks ? e : v.lo + (e - v.sinks);
 }
 
-// Whether the token at position p sees the one at position `at`.
-__device__ __forceinline__ bool sees(const AttendArgs& a, int32_t p, int32_t at) {
-  return at <= p && (a.window == 0 || at < a.cache.sinks || at > p - a.window);
-}
-
-// Where position p of session s is in the cache (of head 0): byte offsets of
-// its key and value, or k = -1 if it is in no page.
+// Where position p of session s is in the cache (of head 0): offsets of its
+// key and value in units, kNoRow if it is in no page.
+constexpr uint32_t kNoRow = 0xffffffffu;
 struct RowPlace {
-  int64_t k, v;
+  uint32_t k, v;
 };
 __device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_t p) {
   const CacheDev& c = a.cache;
-  RowPlace r = {-1, -1};
+  RowPlace r = {kNoRow, kNoRow};
   const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
   if (slot >= static_cast<uint32_t>(c.slots)) {
     atomicOr(a.err, kDevErrIndex);
     return r;
   }
   const uint32_t page = c.page_rows.div(slot);
-  const int64_t row = static_cast<int64_t>(slot - page * c.page_rows.d) * c.row_bytes;
+  const uint32_t row = (slot - page * c.page_rows.d) * c.row_units;
   const int64_t e = s * c.table_stride + page;
   const int32_t kp = __ldg(c.table + e);
   const int32_t vp = c.v_table ? __ldg(c.v_table + e) : kp;
@@ -147,8 +143,31 @@ __device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_
     if (kp < -1 || kp >= c.n_pages || vp < -1 || vp >= c.n_pages) atomicOr(a.err, kDevErrIndex);
     return r;
   }
-  r.k = kp * c.page_bytes + row;
-  r.v = vp * c.page_bytes + row;
+  r.k = kp * c.page_units + row;
+  r.v = vp * c.page_units + row;
+  return r;
+}
+__device__ __forceinline__ const uint8_t* row_at(const AttendArgs& a, const uint8_t* base, uint32_t off) {
+  return base + static_cast<uint64_t>(off) * a.cache.unit;
+}
+
+// What a row at position p sees of a view's tokens: e with e <= hi and (e <
+// first or e >= lo).
+struct RowRange {
+  int32_t hi, lo, first;
+  // The tokens [b, b + 32) it sees, as bits.
+  __device__ __forceinline__ uint32_t bits(int32_t b) const {
+    return upto(hi + 1 - b) & (upto(first - b) | ~upto(lo - b));
+  }
+  static __device__ __forceinline__ uint32_t upto(int32_t n) {
+    return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1;
+  }
+};
+__device__ __forceinline__ RowRange row_range(const AttendArgs& a, const SessionView& v, int32_t p) {
+  RowRange r;
+  r.hi = p >= v.lo ? v.sinks + (p - v.lo) : min(p, v.sinks - 1);
+  r.first = v.lo > 0 ? v.sinks : a.cache.sinks;
+  r.lo = a.window ? v.sinks + max(p - a.window + 1 - v.lo, 0) : 0;
   return r;
 }
 

@@ -126,24 +126,25 @@ __global__ void __launch_bounds__(kThreads)
   const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
   // Lanes 0..15 (and again 16..31) look up a row each.
   auto look = [&](int t) {
-    RowPlace r = {-1, -1};
+    RowPlace r = {kNoRow, kNoRow};
     const int e = t * kTile + (lane & 15);
     if (t < t_end && e < view.seen) r = row_place(a, s, seen_position(view, e));
     return r;
   };
   const int chunk = lane % kChunks, row0 = lane / kChunks;
   auto copy = [&](const RowPlace& r, int stage) {
-    const uint32_t there = __ballot_sync(kFull, r.k >= 0) & 0xffffu;
+    const uint32_t there = __ballot_sync(kFull, r.k != kNoRow) & 0xffffu;
     if (lane == 0) valid[warp][stage] = there;
     const uint32_t base = ring + stage * kStage;
 #pragma unroll
     for (int i = 0; i < kTile / kRowsAtOnce; ++i) {
       const int row = i * kRowsAtOnce + row0;
-      const int64_t ko = __shfl_sync(kFull, r.k, row), vo = __shfl_sync(kFull, r.v, row);
+      const uint32_t ko = __shfl_sync(kFull, r.k, row), vo = __shfl_sync(kFull, r.v, row);
+      const bool in = ko != kNoRow;
       if (chunk * 8 < head_dim) {
         const uint32_t at = base + row * (DP * 2) + ((chunk ^ (row & 7)) << 4);
-        copy16(at, kbase + (ko < 0 ? 0 : ko) + chunk * 16, ko >= 0);
-        copy16(at + kStage / 2, vbase + (ko < 0 ? 0 : vo) + chunk * 16, ko >= 0);
+        copy16(at, row_at(a, kbase, in ? ko : 0) + chunk * 16, in);
+        copy16(at + kStage / 2, row_at(a, vbase, in ? vo : 0) + chunk * 16, in);
       }
     }
   };
@@ -181,6 +182,9 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       pos[n][i] = view.first + static_cast<int>(a.by_group.div(n * 8 + q4 * 2 + i));
+
+  // Ranges of the first and the last new token.
+  const RowRange low = row_range(a, view, view.first), high = row_range(a, view, view.first + view.m - 1);
 
   float o[DP / 16][NT][4];
   float top[NT][2], total[NT][2];
@@ -220,21 +224,17 @@ __global__ void __launch_bounds__(kThreads)
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[n][i] *= a.scale_log2;
-    const int32_t lo = seen_position(view, t * kTile), hi = seen_position(view, t * kTile + kTile - 1);
-    const bool part = many && !(hi <= view.first && (a.window == 0 || hi < a.cache.sinks ||
-                                                     lo > view.first + view.m - 1 - a.window));
+    const int e0 = t * kTile;
+    const bool part = many && !(e0 + kTile - 1 <= low.hi && (e0 >= high.lo || e0 + kTile <= low.first));
     if (part || there != 0xffffu) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int row = g + 8 * h;
-        const bool in = there >> row & 1;
-        const int32_t p = seen_position(view, t * kTile + row);
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            if (!in || (many && !sees(a, pos[n][i], p))) c[n][2 * h + i] = -INFINITY;
-      }
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t m = there & (part ? row_range(a, view, pos[n][i]).bits(e0) : kFull);
+          if (!(m >> g & 1)) c[n][i] = -INFINITY;
+          if (!(m >> (g + 8) & 1)) c[n][2 + i] = -INFINITY;
+        }
     }
     bool raise = false;
 #pragma unroll
@@ -290,13 +290,11 @@ __global__ void __launch_bounds__(kThreads)
       // keep an infinity or a NaN out, so each new token's rows take what the
       // values come to with those it does not see taken out.
       for (int i = 0; i < view.m; ++i) {
+        const uint32_t m = row_range(a, view, view.first + i).bits(e0) >> (2 * q4);
         uint32_t in[2];  // of tokens 2 q4, +1 and 8 more
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int e = t * kTile + 8 * h + 2 * q4;
-          in[h] = (sees(a, view.first + i, seen_position(view, e)) ? 0xffffu : 0u) |
-                  (sees(a, view.first + i, seen_position(view, e + 1)) ? 0xffff0000u : 0u);
-        }
+        for (int h = 0; h < 2; ++h)
+          in[h] = (m >> (8 * h) & 1 ? 0xffffu : 0u) | (m >> (8 * h + 1) & 1 ? 0xffff0000u : 0u);
         bool mine[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
