@@ -2,8 +2,11 @@
 // values: checks of arguments, the choice of a kernel and of its split.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <numeric>
+
+#include <cuda.h>
 
 #include "pcs.h"
 #include "pcs_attend.h"
@@ -11,6 +14,53 @@
 using namespace pcs;
 
 namespace {
+
+// The driver's tensor map encoder; null if there is none.
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encoder() {
+  static const EncodeFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<EncodeFn>(p);
+  }();
+  return fn;
+}
+
+// A pool as elements, heads, rows and pages, copied by boxes of 64 elements of
+// `rows` rows of a page, 128-byte swizzled.
+bool encode_pool(const pcs_kv_cache& c, void* pool, int rows, uint8_t* map) {
+  const EncodeFn fn = encoder();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.heads),
+                              static_cast<cuuint64_t>(c.page_rows), static_cast<cuuint64_t>(c.n_pages)};
+  const cuuint64_t strides[3] = {2 * static_cast<cuuint64_t>(c.head_stride), 2 * static_cast<cuuint64_t>(c.row_stride),
+                                 2 * static_cast<cuuint64_t>(c.page_stride)};
+  const cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(rows), 1}, step[4] = {1, 1, 1, 1};
+  CUtensorMap m;
+  static_assert(sizeof m == 128, "tensor map");
+  if (fn(&m, c.dtype == PCS_DT_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool, dims,
+         strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return false;
+  std::memcpy(map, &m, sizeof m);
+  return true;
+}
+
+// Rows of the boxes that tensor copies can move: a power of two that divides a
+// page (so that a tile's boxes never leave theirs), and with a ring its length
+// and beginning too.  0: rows are copied one by one.
+int box_rows(const pcs_kv_cache& c) {
+  for (int r = 128; r >= 8; r /= 2)
+    if (c.page_rows % r == 0 && (c.ring == 0 || (c.ring % r == 0 && c.sinks % r == 0))) return r;
+  return 0;
+}
 
 bool aligned(const void* p, uint64_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -317,8 +367,12 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
       if (st) return st;
       a.part = reinterpret_cast<float*>(ws);
     }
+    TensorMaps maps = {};
+    a.box_rows = box_rows(*cache);
+    if (a.box_rows && !(encode_pool(*cache, cache->k, a.box_rows, maps.k) && encode_pool(*cache, cache->v, a.box_rows, maps.v)))
+      a.box_rows = 0;
     call.before(kOpAttendBlock);
-    if ((st = call.after(launch_attend_block(a, cache->dtype, static_cast<int>(blocks), call.stream())))) return st;
+    if ((st = call.after(launch_attend_block(a, cache->dtype, static_cast<int>(blocks), maps, call.stream())))) return st;
     if (splits > 1) {
       call.before(kOpAttendJoin);
       if ((st = call.after(launch_attend_join(a, cache->dtype, call.stream())))) return st;

@@ -153,6 +153,7 @@ struct AttendArgs {
   int32_t splits;          // parts of a session's visible tokens
   float* part;             // partial results (splits > 1)
   uint32_t* ticket;        // zero on entry and on exit
+  int32_t box_rows;        // block kernel: rows of a tensor copy, 0: rows are copied one by one
   uint32_t* err;
 };
 
@@ -175,7 +176,12 @@ int attend_token_blocks_per_sm(int head_dim);
 constexpr int kBlockRows = 256;
 constexpr int kBlockTile = 128;  // tokens of a tile
 inline uint64_t block_part_floats(int head_dim) { return (head_dim <= 64 ? 64 : 128) + 2; }
-cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream);
+// maps: the keys' and the values' tensor maps (box_rows > 0), 128 bytes each.
+struct alignas(64) TensorMaps {
+  uint8_t k[128], v[128];
+};
+cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
+                                cudaStream_t stream);
 cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, cudaStream_t stream);
 
 }  // namespace pcs

@@ -73,13 +73,36 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   return true;
 }
 
+// A barrier expects `bytes`; a box of rows of a pool for them.
+__device__ __forceinline__ void fill_begins(uint32_t bar, uint32_t bytes, uint32_t one) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t"
+      "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+      "r"(bytes), "r"(one)
+      : "memory");
+}
+__device__ __forceinline__ void copy_box(uint32_t to, uint64_t map, int d, int head, int row, int page, uint32_t bar,
+                                         uint32_t one) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %7, 0;\n\t"
+      "@q cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(to),
+      "l"(map), "r"(d), "r"(head), "r"(row), "r"(page), "r"(bar), "r"(one)
+      : "memory");
+}
+
 // ---- Tensor memory and its matrix instruction ----------------------------------
 
-// Shared-memory operand in 128-byte rows of a 128-byte swizzle: eight rows are
-// 1,024 bytes, `lead` bytes lie between 64-element columns of a transposed one.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t lead) {
-  return static_cast<uint64_t>((at >> 4) & 0x3fff) | (static_cast<uint64_t>(lead >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+// Shared-memory operand in 128-byte rows of a 128-byte swizzle: the low word of
+// its descriptor (`lead` bytes lie between 64-element columns of a transposed
+// one) and the high one (eight rows are 1,024 bytes).
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t lead) { return (at >> 4) | (lead >> 4) << 16; }
+constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+// One thread of a warp.
+__device__ __forceinline__ uint32_t elected() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is;
 }
 // 128 x N products of 16-bit elements into 32-bit floats; b_across: the second
 // operand lies with its columns, not its rows, in 128-byte rows.
@@ -89,24 +112,34 @@ __device__ __forceinline__ constexpr uint32_t instruction(uint32_t n, bool b_acr
   return (1u << 4) | (type << 7) | (type << 10) | ((b_across ? 1u : 0u) << 16) | ((n >> 3) << 17) |
          ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t i, bool add) {
+// The matrix instruction and its commit are run by the whole warp and take
+// effect in the one thread that `one` is set in: its operands then stay in
+// uniform registers, where it wants them.  Issued by one thread of a branch of
+// its own, every instruction took some 120 cycles instead of the 64 it keeps
+// the unit busy for.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t i, bool add, uint32_t one) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(i), "r"(add ? 1u : 0u)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %6};\n\tmov.b64 b, {%2, %6};\n\t"
+      "setp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(i), "r"(add ? 1u : 0u), "r"(one), "n"(kOperandHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t i, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t i, bool add, uint32_t one) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(i), "r"(add ? 1u : 0u)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 b;\n\tmov.b64 b, {%2, %6};\n\t"
+      "setp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(i), "r"(add ? 1u : 0u), "r"(one), "n"(kOperandHigh)
       : "memory");
 }
 // The barrier's arrival when everything issued so far has finished.
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-               : "memory");
+__device__ __forceinline__ void mma_commit(uint32_t bar, uint32_t one) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(one)
+      : "memory");
 }
 __device__ __forceinline__ void fence_before() {
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -189,7 +222,8 @@ __device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, 
   if (w.row0 >= w.rows || w.all.m > a.batch.max_new) return w;
   const int t0 = a.by_group.div(w.row0);
   const int t1 = a.by_group.div(min(w.row0 + 2 * kTile, w.rows) - 1);
-  w.view = rows_view(a, w.all, t0, t1 + 1);
+  w.view = w.all;
+  narrow(a, w.view, t0, t1 + 1, a.box_rows > 0 ? a.box_rows : 1);
   w.pmin = w.all.first + t0;
   w.pmax = w.all.first + t1;
   const int n = (w.view.seen + kTile - 1) / kTile;
@@ -231,20 +265,54 @@ __device__ __forceinline__ uint32_t specials(uint32_t x) {
   return ((x & e) == e ? 0xffffu : 0u) | ((x >> 16 & e) == e ? 0xffff0000u : 0u);
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_constant__ AttendArgs a, int blocks) {
+// Pages and row of the box of rows that begins at position p; what is not in
+// the cache stays as it was.
+__device__ __forceinline__ void box_place(const AttendArgs& a, int s, int32_t p, int32_t& k, int32_t& v, int32_t& row) {
+  const CacheDev& c = a.cache;
+  const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
+  if (slot >= static_cast<uint32_t>(c.slots)) {
+    atomicOr(a.err, kDevErrIndex);
+    return;
+  }
+  const uint32_t page = c.page_rows.div(slot);
+  const int64_t e = s * c.table_stride + page;
+  const int32_t kp = __ldg(c.table + e);
+  const int32_t vp = c.v_table ? __ldg(c.v_table + e) : kp;
+  if (kp < 0 || kp >= c.n_pages || vp < 0 || vp >= c.n_pages) {
+    if (kp < -1 || kp >= c.n_pages || vp < -1 || vp >= c.n_pages) atomicOr(a.err, kDevErrIndex);
+    return;
+  }
+  k = kp;
+  v = vp;
+  row = slot - page * c.page_rows.d;
+}
+
+// Zeros for the infinities and NaN among eight elements; whether there were any.
+template <typename T>
+__device__ __forceinline__ bool take_out(uint4* at) {
+  uint4 v = *at;
+  const uint4 m = make_uint4(specials<T>(v.x), specials<T>(v.y), specials<T>(v.z), specials<T>(v.w));
+  if (!(m.x | m.y | m.z | m.w)) return false;
+  v.x &= ~m.x, v.y &= ~m.y, v.z &= ~m.z, v.w &= ~m.w;
+  *at = v;
+  return true;
+}
+
+template <typename T, int DP, bool BOX>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {
   constexpr int kRing = kBuffers<DP>;
   constexpr uint32_t kBytes = kTileBytes<DP>;
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[1 + 2 * kRing + 2 + 2 + 2];
+  __shared__ __align__(8) uint64_t bars[7 + 3 * kRing];
   __shared__ uint32_t tmem_at;
   __shared__ __align__(16) uint32_t valid[kValid][4];
   __shared__ uint32_t special;
 
   attend_dependency();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
   int b = blockIdx.x;
   const int head = b % a.cache.heads;
   b /= a.cache.heads;
@@ -270,11 +338,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
   auto s_full = [&](int t) { return bar0 + 8 * (1 + 2 * kRing + t); };
   auto p_full = [&](int t) { return bar0 + 8 * (3 + 2 * kRing + t); };
   auto o_full = [&](int t) { return bar0 + 8 * (5 + 2 * kRing + t); };
+  // BOX: the values of tile j are looked over.  (By tiles: an odd ring has keys
+  // and values in a buffer in turn.)
+  auto v_fine = [&](int j) { return bar0 + 8 * (7 + 2 * kRing + j % kRing); };
   if (tid == 0) {
     bar_init(q_full, 32 * kCopyWarps);
     for (int i = 0; i < kRing; ++i) {
-      bar_init(kv_full(i), 32 * kCopyWarps);
+      bar_init(kv_full(i), BOX ? 1 : 32 * kCopyWarps);
       bar_init(kv_empty(i), 1);
+      bar_init(v_fine(i), 32 * (kCopyWarps - 1));
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(s_full(t), 1);
@@ -309,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
     };
     if (a.cache.head_dim < DP) {  // chunks that no copy writes
       if (!mine)
-        for (int i = 0; i < 2 + kRing; ++i)
+        for (int i = 0; i < (BOX ? 2 : 2 + kRing); ++i)
           for (int r = sub; r < 32; r += kAtOnce)
             *reinterpret_cast<uint4*>(ring_ptr - 2 * kBytes + i * kBytes + spot(row0 + r)) = make_uint4(0, 0, 0, 0);
     }
@@ -327,86 +399,145 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
     asm volatile("cp.async.commit_group;" ::: "memory");
 
     const RowsRange range = rows_range(a, w.view, w.pmin, w.pmax);
-    // Fill i: keys of tile i / 2, or its values.  Fill -1 stands for the
-    // query rows.
-    auto landed = [&](int i) {
-      if (i >= 0 && (i & 1)) {
-        if (!range.whole(w.tile0 + i / 2) && mine) {
-          uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
-          uint32_t any = 0;
-          for (int r = sub; r < 32; r += kAtOnce) {
-            uint4* x = reinterpret_cast<uint4*>(tile + spot(row0 + r));
-            uint4 v = *x;
-            const uint4 m = make_uint4(specials<T>(v.x), specials<T>(v.y), specials<T>(v.z), specials<T>(v.w));
-            if (m.x | m.y | m.z | m.w) {
-              any = 1;
-              v.x &= ~m.x, v.y &= ~m.y, v.z &= ~m.z, v.w &= ~m.w;
-              *x = v;
+    if constexpr (BOX) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive(q_full);
+      if (c == 0) {
+        // One warp fills the ring, a lane per box of rows.
+        const int rows = a.box_rows, boxes = kTile / rows;
+        const uint32_t one = elected();
+        const uint64_t kmap = reinterpret_cast<uint64_t>(maps.k), vmap = reinterpret_cast<uint64_t>(maps.v);
+        struct Box {
+          int32_t k, v, row;  // pages (n_pages: none, zeros are filled in), first row in them
+        };
+        auto look = [&](int t) {
+          Box x = {a.cache.n_pages, a.cache.n_pages, 0};
+          const int e = t * kTile + lane * rows;
+          if (lane < boxes && e < w.view.seen) box_place(a, s, seen_position(w.view, e), x.k, x.v, x.row);
+          return x;
+        };
+        Box box = look(w.tile0), next = box;
+        for (int i = 0; i < 2 * w.tiles && ok; ++i) {
+          const int buf = i % kRing, use = i / kRing;
+          if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
+          ok = __all_sync(kFull, ok);
+          if (!ok) break;
+          if ((i & 1) == 0) {
+            box = next;
+            // A bit per token of the tile: its box is in the cache.
+            const uint32_t there = __ballot_sync(kFull, lane < boxes && box.k < a.cache.n_pages);
+            if (lane < 4) {
+              uint32_t m = 0;
+              for (int k = 0; k < 32; k += 8)
+                if (there >> ((lane * 32 + k) / rows) & 1) m |= 0xffu << k;
+              valid[(i / 2) % kValid][lane] = m;
             }
+            __syncwarp();
+            if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
           }
-          if (any) special = 1;
+          fill_begins(kv_full(buf), kBytes, one);
+          for (int k = 0; k < boxes; ++k) {
+            const int row = __shfl_sync(kFull, box.row, k), page = __shfl_sync(kFull, i & 1 ? box.v : box.k, k);
+#pragma unroll
+            for (int d = 0; d < DP / 64; ++d)
+              copy_box(ring + buf * kBytes + d * kPanel + k * rows * 128, i & 1 ? vmap : kmap, d * 64, head, row, page,
+                       kv_full(buf), one);
+          }
+        }
+      } else {
+        // The other three look values over.
+        for (int i = 1; i < 2 * w.tiles && ok; i += 2) {
+          const int buf = i % kRing;
+          ok = bar_wait(kv_full(buf), (i / kRing) & 1);
+          ok = __all_sync(kFull, ok);
+          if (!ok) break;
+          if (!range.whole(w.tile0 + i / 2)) {
+            uint4* tile = reinterpret_cast<uint4*>(ring_ptr + buf * kBytes);
+            bool any = false;
+            for (int k = (c - 1) * 32 + lane; k < static_cast<int>(kBytes / 16); k += 32 * (kCopyWarps - 1))
+              any |= take_out<T>(tile + k);
+            if (any) special = 1;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          bar_arrive(v_fine(i / 2));
         }
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      bar_arrive(i < 0 ? q_full : kv_full(i % kRing));
-    };
-    auto look = [&](int t) {
-      RowPlace r = {kNoRow, kNoRow};
-      const int e = t * kTile + row0 + lane;
-      if (e < w.view.seen) r = row_place(a, s, seen_position(w.view, e));
-      return r;
-    };
-    const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes + chunk * 16;
-    const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes + chunk * 16;
-    RowPlace place = look(w.tile0), next = place;
-    for (int i = 0; i < 2 * w.tiles && ok; ++i) {
-      const int buf = i % kRing, use = i / kRing;
-      if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
-      ok = __all_sync(kFull, ok);
-      if (!ok) break;
-      if ((i & 1) == 0) {
-        place = next;
-        const uint32_t there = __ballot_sync(kFull, place.k != kNoRow);
-        if (lane == 0) valid[(i / 2) % kValid][c] = there;
-        if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
-      }
-      const uint8_t* base = i & 1 ? vbase : kbase;
-      const uint32_t off = i & 1 ? place.v : place.k;
-      const uint32_t tile = ring + buf * kBytes;
+    } else {
+      // Fill i: keys of tile i / 2, or its values.  Fill -1 stands for the
+      // query rows.
+      auto landed = [&](int i) {
+        if (i >= 0 && (i & 1)) {
+          if (!range.whole(w.tile0 + i / 2) && mine) {
+            uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
+            bool any = false;
+            for (int r = sub; r < 32; r += kAtOnce)
+              any |= take_out<T>(reinterpret_cast<uint4*>(tile + spot(row0 + r)));
+            if (any) special = 1;
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        bar_arrive(i < 0 ? q_full : kv_full(i % kRing));
+      };
+      auto look = [&](int t) {
+        RowPlace r = {kNoRow, kNoRow};
+        const int e = t * kTile + row0 + lane;
+        if (e < w.view.seen) r = row_place(a, s, seen_position(w.view, e));
+        return r;
+      };
+      const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes + chunk * 16;
+      const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes + chunk * 16;
+      RowPlace place = look(w.tile0), next = place;
+      for (int i = 0; i < 2 * w.tiles && ok; ++i) {
+        const int buf = i % kRing, use = i / kRing;
+        if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
+        if ((i & 1) == 0) {
+          place = next;
+          const uint32_t there = __ballot_sync(kFull, place.k != kNoRow);
+          if (lane == 0) valid[(i / 2) % kValid][c] = there;
+          if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
+        }
+        const uint8_t* base = i & 1 ? vbase : kbase;
+        const uint32_t off = i & 1 ? place.v : place.k;
+        const uint32_t tile = ring + buf * kBytes;
 #pragma unroll 4
-      for (int r = 0; r < 32 / kAtOnce; ++r) {
-        const int row = r * kAtOnce + sub;
-        const uint32_t o = __shfl_sync(kFull, off, row);
-        const bool in = o != kNoRow;
-        if (mine) copy16(tile + spot(row0 + row), row_at(a, base, in ? o : 0), in);
+        for (int r = 0; r < 32 / kAtOnce; ++r) {
+          const int row = r * kAtOnce + sub;
+          const uint32_t o = __shfl_sync(kFull, off, row);
+          const bool in = o != kNoRow;
+          if (mine) copy16(tile + spot(row0 + row), row_at(a, base, in ? o : 0), in);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+        if (i - kLag >= -1) landed(i - kLag);
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-      if (i - kLag >= -1) landed(i - kLag);
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (ok)
+        for (int i = max(-1, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    if (ok)
-      for (int i = max(-1, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
     }
   } else if (warp >= kMmaWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    // ---- The warp that feeds the matrix unit, by one of its threads ----
-    if (warp == kMmaWarp && lane == 0 && w.tiles > 0) {
+    // ---- The warp that feeds the matrix unit ----
+    if (warp == kMmaWarp && w.tiles > 0) {
+      const uint32_t one = elected(), mem = __shfl_sync(kFull, tmem, 0);
       constexpr uint32_t kQK = instruction<T>(kTile, false), kPV = instruction<T>(DP, true);
       auto scores = [&](int t, int i) {  // S = Q K^T of row tile t, keys of fill i
         const uint32_t q = qat + t * kBytes, k = ring + (i % kRing) * kBytes;
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
           const uint32_t at = (d >> 2) * kPanel + (d & 3) * 32;
-          mma_ss(tmem + kScores + t * kTile, operand(q + at, 16), operand(k + at, 16), kQK, d > 0);
+          mma_ss(mem + kScores + t * kTile, operand(q + at, 16), operand(k + at, 16), kQK, d > 0, one);
         }
       };
       auto sums = [&](int t, int i, bool add) {  // O += P V, values of fill i
         const uint32_t v = ring + (i % kRing) * kBytes;
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
-          mma_ts(tmem + kSums + t * DP, tmem + kScores + t * kTile + k * 8, operand(v + k * 2048, kPanel), kPV,
-                 add || k > 0);
+          mma_ts(mem + kSums + t * DP, mem + kScores + t * kTile + k * 8, operand(v + k * 2048, kPanel), kPV,
+                 add || k > 0, one);
       };
       RowsRange range[2];
       int done[2] = {0, 0}, end[2] = {-1, -1};  // tiles taken, the last one
@@ -415,33 +546,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_block(const __grid_const
         for (int j = 0; j < w.tiles; ++j)
           if (range[t].some(w.tile0 + j)) end[t] = j;
       }
-      ok = bar_wait(q_full, 0);
+      ok = __all_sync(kFull, bar_wait(q_full, 0));
       for (int j = -1; j < w.tiles && ok; ++j) {  // values of tile j, keys of the next
         const int vi = 2 * j + 1, ki = 2 * j + 2;
         const bool more = j + 1 < w.tiles;
         if (j >= 0) ok = bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
+        if (BOX && j >= 0 && ok) ok = bar_wait(v_fine(j), (j / kRing) & 1);
         if (ok && more) ok = bar_wait(kv_full(ki % kRing), (ki / kRing) & 1);
+        ok = __all_sync(kFull, ok);
         fence_after();
         for (int t = 0; t < nq && ok; ++t) {
           if (j >= 0 && range[t].some(w.tile0 + j)) {
-            ok = bar_wait(p_full(t), done[t] & 1);
+            ok = __all_sync(kFull, bar_wait(p_full(t), done[t] & 1));
             if (!ok) break;
             fence_after();
             sums(t, vi, done[t] > 0);
             done[t] += 1;
-            if (j == end[t]) mma_commit(o_full(t));
+            if (j == end[t]) mma_commit(o_full(t), one);
           }
-          if (j >= 0 && t == nq - 1) mma_commit(kv_empty(vi % kRing));
+          if (j >= 0 && t == nq - 1) mma_commit(kv_empty(vi % kRing), one);
           if (more && range[t].some(w.tile0 + j + 1)) {
             scores(t, ki);
-            mma_commit(s_full(t));
+            mma_commit(s_full(t), one);
           }
-          if (more && t == nq - 1) mma_commit(kv_empty(ki % kRing));
+          if (more && t == nq - 1) mma_commit(kv_empty(ki % kRing), one);
         }
       }
     }
-    __syncwarp();
-    ok = __shfl_sync(kFull, ok, 0);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     if ((warp >> 2) < nq) {
@@ -675,15 +806,20 @@ cudaLaunchConfig_t config(int64_t grid, int threads, uint32_t smem, cudaLaunchAt
   return cfg;
 }
 
-template <typename T, int DP>
-cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t stream) {
-  auto k = k_attend_block<T, DP>;
+template <typename T, int DP, bool BOX>
+cudaError_t launch_form(const AttendArgs& a, int blocks, const TensorMaps& maps, cudaStream_t stream) {
+  auto k = k_attend_block<T, DP, BOX>;
   static SmemLimit limit;
   if (cudaError_t e = limit.set(k, kSmemBytes<DP>)) return e;
   cudaLaunchAttribute attr;
   const cudaLaunchConfig_t cfg =
       config(static_cast<int64_t>(blocks) * a.batch.sessions * a.splits * a.cache.heads, kThreads, kSmemBytes<DP>, &attr, stream);
-  return cudaLaunchKernelEx(&cfg, k, a, blocks);
+  return cudaLaunchKernelEx(&cfg, k, a, maps, blocks);
+}
+template <typename T, int DP>
+cudaError_t launch(const AttendArgs& a, int blocks, const TensorMaps& maps, cudaStream_t stream) {
+  return a.box_rows > 0 ? launch_form<T, DP, true>(a, blocks, maps, stream)
+                        : launch_form<T, DP, false>(a, blocks, maps, stream);
 }
 
 template <typename T, int DP>
@@ -695,11 +831,12 @@ cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream) {
+cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
+                                cudaStream_t stream) {
   if (dtype == PCS_DT_F16)
-    return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, stream) : launch<__half, 128>(a, blocks, stream);
-  return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, stream)
-                                : launch<__nv_bfloat16, 128>(a, blocks, stream);
+    return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, maps, stream) : launch<__half, 128>(a, blocks, maps, stream);
+  return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, maps, stream)
+                                : launch<__nv_bfloat16, 128>(a, blocks, maps, stream);
 }
 
 cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, cudaStream_t stream) {

@@ -70,15 +70,30 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
                : "memory");
 }
 
-// The new tokens of a session and what they see together.
+// The new tokens of a session, and what some of them see together: the first
+// `sinks` tokens (`pad` places of which the last ones are nobody's) and the run
+// [lo, lo + seen - pad), or, not apart, one run from position 0.
 struct SessionView {
   int64_t q0;       // the first new token's row
   int32_t m;        // new tokens
   int32_t first;    // position of the first one (negative: before the session)
-  int32_t sinks;    // first tokens seen besides the run
-  int32_t lo;       // the run: [lo, first + m)
-  int32_t seen;     // sinks + run
+  int32_t sinks, pad, lo, seen;
+  bool apart;
 };
+
+// Narrows a view to what new tokens [t0, t1) see; the run and the places before
+// it begin at multiples of `align`.
+__device__ __forceinline__ void narrow(const AttendArgs& a, SessionView& v, int t0, int t1, int align) {
+  const int32_t len = v.first + v.m;
+  int32_t lo = a.window ? v.first + t0 - a.window + 1 : 0;
+  if (a.cache.ring_rows) lo = max(lo, len - a.cache.ring_rows);
+  const int32_t end = max(v.first + t1, 0);
+  v.apart = lo > a.cache.sinks;
+  v.sinks = v.apart ? min(a.cache.sinks, end) : 0;
+  v.pad = (v.sinks + align - 1) & -align;
+  v.lo = v.apart ? lo & -align : 0;
+  v.seen = v.pad + max(end - v.lo, 0);
+}
 
 __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) {
   SessionView v;
@@ -90,34 +105,14 @@ __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) 
     v.q0 = static_cast<int64_t>(s) * b.each;
     v.m = b.each;
   }
-  const int32_t len = __ldg(b.lens + s);
-  v.first = len - v.m;
-  int32_t lo = a.window ? v.first - a.window + 1 : 0;
-  if (a.cache.ring_rows) lo = max(lo, len - a.cache.ring_rows);
-  const bool apart = lo > a.cache.sinks;
-  v.sinks = apart ? a.cache.sinks : 0;
-  v.lo = apart ? lo : 0;
-  v.seen = max(len, 0) - v.lo + v.sinks;
-  return v;
-}
-
-// Narrows the view of a whole session to what rows of new tokens [t0, t1) see.
-__device__ __forceinline__ SessionView rows_view(const AttendArgs& a, const SessionView& s, int t0,
-                                                 int t1) {
-  SessionView v = s;
-  int32_t lo = a.window ? s.first + t0 - a.window + 1 : 0;
-  if (a.cache.ring_rows) lo = max(lo, s.first + s.m - a.cache.ring_rows);
-  const int32_t end = max(s.first + t1, 0);
-  const bool apart = lo > a.cache.sinks;
-  v.sinks = apart ? min(a.cache.sinks, end) : 0;
-  v.lo = apart ? lo : 0;
-  v.seen = max(end - v.lo, 0) + v.sinks;
+  v.first = __ldg(b.lens + s) - v.m;
+  narrow(a, v, 0, v.m, 1);
   return v;
 }
 
 // Position of the e-th token of a view.
 __device__ __forceinline__ int32_t seen_position(const SessionView& v, int32_t e) {
-  return e < v.sinks ? e : v.lo + (e - v.sinks);
+  return e < v.pad ? e : v.lo + (e - v.pad);
 }
 
 // Where position p of session s is in the cache (of head 0): offsets of its
@@ -164,10 +159,12 @@ struct RowRange {
   }
 };
 __device__ __forceinline__ RowRange row_range(const AttendArgs& a, const SessionView& v, int32_t p) {
+  int32_t low = a.window ? max(p - a.window + 1, 0) : 0;
+  if (a.cache.ring_rows) low = max(low, v.first + v.m - a.cache.ring_rows);
   RowRange r;
-  r.hi = p >= v.lo ? v.sinks + (p - v.lo) : min(p, v.sinks - 1);
-  r.first = v.lo > 0 ? v.sinks : a.cache.sinks;
-  r.lo = a.window ? v.sinks + max(p - a.window + 1 - v.lo, 0) : 0;
+  r.hi = p >= v.lo ? v.pad + (p - v.lo) : min(p, v.pad - 1);
+  r.first = v.apart ? v.sinks : a.cache.sinks;
+  r.lo = v.apart ? v.pad + max(low - v.lo, 0) : max(low, 0);
   return r;
 }
 
