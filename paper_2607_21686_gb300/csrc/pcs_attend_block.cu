@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[7 + 3 * kRing];
+  __shared__ __align__(8) uint64_t bars[9 + 3 * kRing];
   __shared__ uint32_t tmem_at;
   __shared__ __align__(16) uint32_t valid[kValid][4];
   __shared__ uint32_t special;
@@ -336,11 +336,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto kv_full = [&](int i) { return bar0 + 8 * (1 + i); };
   auto kv_empty = [&](int i) { return bar0 + 8 * (1 + kRing + i); };
   auto s_full = [&](int t) { return bar0 + 8 * (1 + 2 * kRing + t); };
-  auto p_full = [&](int t) { return bar0 + 8 * (3 + 2 * kRing + t); };
-  auto o_full = [&](int t) { return bar0 + 8 * (5 + 2 * kRing + t); };
+  // The weights of a tile's first half of tokens, and of its second.
+  auto p_full = [&](int t, int half) { return bar0 + 8 * (3 + 2 * kRing + 2 * t + half); };
+  auto o_full = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };
   // BOX: the values of tile j are looked over.  (By tiles: an odd ring has keys
   // and values in a buffer in turn.)
-  auto v_fine = [&](int j) { return bar0 + 8 * (7 + 2 * kRing + j % kRing); };
+  auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kRing); };
   if (tid == 0) {
     bar_init(q_full, 32 * kCopyWarps);
     for (int i = 0; i < kRing; ++i) {
@@ -350,7 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(s_full(t), 1);
-      bar_init(p_full(t), kTile);
+      bar_init(p_full(t, 0), kTile);
+      bar_init(p_full(t, 1), kTile);
       bar_init(o_full(t), 1);
     }
     special = 0;
@@ -532,12 +534,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           mma_ss(mem + kScores + t * kTile, operand(q + at, 16), operand(k + at, 16), kQK, d > 0, one);
         }
       };
-      auto sums = [&](int t, int i, bool add) {  // O += P V, values of fill i
+      auto sums = [&](int t, int i, int half, bool add) {  // O += P V, values of fill i
         const uint32_t v = ring + (i % kRing) * kBytes;
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_ts(mem + kSums + t * DP, mem + kScores + t * kTile + k * 8, operand(v + k * 2048, kPanel), kPV,
+        for (int k = 0; k < kTile / 32; ++k) {
+          const int at = half * (kTile / 32) + k;
+          mma_ts(mem + kSums + t * DP, mem + kScores + t * kTile + at * 8, operand(v + at * 2048, kPanel), kPV,
                  add || k > 0, one);
+        }
       };
       RowsRange range[2];
       int done[2] = {0, 0}, end[2] = {-1, -1};  // tiles taken, the last one
@@ -557,10 +561,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_after();
         for (int t = 0; t < nq && ok; ++t) {
           if (j >= 0 && range[t].some(w.tile0 + j)) {
-            ok = __all_sync(kFull, bar_wait(p_full(t), done[t] & 1));
+            ok = __all_sync(kFull, bar_wait(p_full(t, 0), done[t] & 1));
             if (!ok) break;
             fence_after();
-            sums(t, vi, done[t] > 0);
+            sums(t, vi, 0, done[t] > 0);
+            ok = __all_sync(kFull, bar_wait(p_full(t, 1), done[t] & 1));
+            if (!ok) break;
+            fence_after();
+            sums(t, vi, 1, true);
             done[t] += 1;
             if (j == end[t]) mma_commit(o_full(t), one);
           }
@@ -595,11 +603,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       fence_after();
       uint32_t x[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tm_load(x[c], sc + c * 32);
+      tm_load(x[0], sc);
+      tm_load(x[1], sc + 32);
       tm_loaded();
+      tm_load(x[2], sc + 64);
+      tm_load(x[3], sc + 96);
+      float mx[4];
+      auto highest = [&](int c) {
+        mx[c] = __uint_as_float(x[c][0]);
+#pragma unroll
+        for (int k = 1; k < 31; k += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
+        mx[c] = fmaxf(mx[c], __uint_as_float(x[c][31]));
+      };
       const uint4 in = *reinterpret_cast<const uint4*>(valid[j % kValid]);
-      if (!(range.whole(tile) && (in.x & in.y & in.z & in.w) == kFull)) {
+      if (range.whole(tile) && (in.x & in.y & in.z & in.w) == kFull) {
+        highest(0);
+        highest(1);
+        tm_loaded();
+      } else {
+        tm_loaded();
         const uint32_t m4[4] = {in.x, in.y, in.z, in.w};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -608,19 +630,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int k = 0; k < 32; ++k)
             if (!(m >> k & 1)) x[c][k] = 0xff800000u;  // -inf
         }
+        highest(0);
+        highest(1);
       }
-      float high = -INFINITY;
-      {
-        float mx[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          mx[c] = __uint_as_float(x[c][0]);
-#pragma unroll
-          for (int k = 1; k < 31; k += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
-          mx[c] = fmaxf(mx[c], __uint_as_float(x[c][31]));
-        }
-        high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
-      }
+      highest(2);
+      highest(3);
+      const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
       const bool raise = high > top + kSlack;
       if (__any_sync(kFull, raise)) {
         const float to = raise ? high : top;
@@ -658,13 +673,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         // Weights over the first half of the scores, all of which are in
         // registers by now.
         tm_store(sc + h * 32, y);
+        tm_stored();
+        fence_before();
+        bar_arrive(p_full(t, h));
       }
       float u, v;
       unpair(add2(sum[0], sum[1]), u, v);
       total += u + v;
-      tm_stored();
-      fence_before();
-      bar_arrive(p_full(t));
       done += 1;
     }
     if (ok && done > 0) ok = bar_wait(o_full(t), 0);
