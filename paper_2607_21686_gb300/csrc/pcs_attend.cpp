@@ -363,7 +363,7 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     a.splits = static_cast<int32_t>(splits);
     if (splits > 1) {
       uint8_t* ws = nullptr;
-      st = call.scratch(4 * block_part_floats(cache->head_dim) * splits * cache->heads * a.batch.tokens * a.group, &ws, &a.ticket);
+      st = call.scratch(4 * block_part_floats(cache->head_dim) * splits * pairs * blocks, &ws, &a.ticket);
       if (st) return st;
       a.part = reinterpret_cast<float*>(ws);
     }
@@ -375,7 +375,7 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     if ((st = call.after(launch_attend_block(a, cache->dtype, static_cast<int>(blocks), maps, call.stream())))) return st;
     if (splits > 1) {
       call.before(kOpAttendJoin);
-      if ((st = call.after(launch_attend_join(a, cache->dtype, call.stream())))) return st;
+      if ((st = call.after(launch_attend_join(a, cache->dtype, static_cast<int>(blocks), call.stream())))) return st;
     }
     return call.end();
   });

@@ -171,17 +171,17 @@ cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, c
 int attend_token_blocks_per_sm(int head_dim);
 
 // The block kernel: a session and key head's rows in blocks of kBlockRows,
-// `blocks` of them at most.  With splits > 1 a row's part is its sums, maximum
-// and total, by part, key head and row; launch_attend_join joins them.
+// `blocks` of them at most.  With splits > 1 a block's part is its rows' sums,
+// maxima and totals; launch_attend_join joins them.
 constexpr int kBlockRows = 256;
 constexpr int kBlockTile = 128;  // tokens of a tile
-inline uint64_t block_part_floats(int head_dim) { return (head_dim <= 64 ? 64 : 128) + 2; }
+inline uint64_t block_part_floats(int head_dim) { return kBlockRows * ((head_dim <= 64 ? 64 : 128) + 2); }
 // maps: the keys' and the values' tensor maps (box_rows > 0), 128 bytes each.
 struct alignas(64) TensorMaps {
   uint8_t k[128], v[128];
 };
 cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
                                 cudaStream_t stream);
-cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, cudaStream_t stream);
+cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream);
 
 }  // namespace pcs

@@ -26,26 +26,29 @@ namespace pcs {
 namespace {
 
 constexpr int kTile = 128;              // rows of a row tile, tokens of a tile
-constexpr int kSoftWarps = 8;           // warps 0-3: row tile 0, 4-7: row tile 1
-constexpr int kMmaWarp = 8;
-constexpr int kCopyWarp = 12;           // warps 12-15 (9-11 make up the fours that registers go by)
-constexpr int kCopyWarps = 4;
-// Registers of a thread: the launch's 128 shared out anew, 2 x 128 x 184 +
-// 2 x 128 x 72 = 512 x 128.
-constexpr int kSoftRegs = 184, kOtherRegs = 72;
+constexpr int kHalf = kTile / 2;        // tokens a softmax thread has of a tile
+// Warps 0-7 and 8-15: a row tile each, two threads a row; 16: matrix products;
+// 17-19: copies.
+constexpr int kSoftWarps = 16;
+constexpr int kMmaWarp = 16;
+constexpr int kCopyWarp = 17;
+constexpr int kCopyWarps = 3;
 constexpr int kThreads = 32 * (kCopyWarp + kCopyWarps);
+// Registers of a thread: the launch's 96 shared out anew, 512 x 104 + 128 x 64
+// = 640 x 96.
+constexpr int kSoftRegs = 104, kOtherRegs = 64;
 constexpr int kLag = 2;                 // copies in flight behind the newest
 constexpr int kValid = 8;               // tiles whose masks are kept
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kSlack = 8.0f;          // as in the token kernel
 constexpr long long kWaitCycles = 4000000000ll;
 
-template <int DP>
-constexpr int kBuffers = DP == 64 ? 8 : 5;  // tiles of keys or values in the ring
+template <int DP, bool BOX>
+constexpr int kBuffers = DP == 64 ? 8 : BOX ? 5 : 4;  // tiles of keys or values in the ring
 template <int DP>
 constexpr uint32_t kTileBytes = kTile * DP * 2;
-template <int DP>
-constexpr uint32_t kSmemBytes = (2 + kBuffers<DP>) * kTileBytes<DP> + 1024;
+template <int DP, bool BOX>
+constexpr uint32_t kSmemBytes = (2 + kBuffers<DP, BOX>) * kTileBytes<DP> + 1024;
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -172,6 +175,29 @@ __device__ __forceinline__ void tm_store(uint32_t at, const uint32_t (&r)[32]) {
       "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+// Barriers of the 32 * 8 threads of a row tile, and of the copying warps.
+__device__ __forceinline__ void row_tile_sync(int t) { asm volatile("barrier.cta.sync %0, 256;" ::"r"(1 + t) : "memory"); }
+__device__ __forceinline__ bool row_tile_any(int t, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(x ? 1u : 0u), "r"(1 + t)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void copy_sync() {
+  asm volatile("barrier.cta.sync 3, %0;" ::"n"(32 * kCopyWarps) : "memory");
+}
 __device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -200,8 +226,17 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
   return r;
 }
 
-// Columns of tensor memory: scores (then weights) and sums of the row tiles.
+// Columns of tensor memory: scores, sums and weights of the row tiles.  Heads of
+// 64 leave room for weights beside the scores, so that the next tile's scores
+// are made while this one's weights are (kAhead); with heads of 128 the weights
+// lie over the scores they came from.
 constexpr uint32_t kScores = 0, kSums = 256;
+template <int DP>
+constexpr bool kAhead = DP == 64;
+template <int DP>
+constexpr uint32_t kWeights = DP == 64 ? 384 : 0;
+template <int DP>
+constexpr uint32_t kWeightsStep = DP == 64 ? 64 : kTile;
 
 // What a block's rows see, the same for all its warps.
 struct Work {
@@ -265,26 +300,33 @@ __device__ __forceinline__ uint32_t specials(uint32_t x) {
   return ((x & e) == e ? 0xffffu : 0u) | ((x >> 16 & e) == e ? 0xffff0000u : 0u);
 }
 
-// Pages and row of the box of rows that begins at position p; what is not in
-// the cache stays as it was.
-__device__ __forceinline__ void box_place(const AttendArgs& a, int s, int32_t p, int32_t& k, int32_t& v, int32_t& row) {
+// A box of rows: pages of its keys and values as the table has them, the first
+// row in them.  The page ids are on their way from memory until settle().
+struct Box {
+  int32_t k, v, row;
+};
+__device__ __forceinline__ Box box_place(const AttendArgs& a, int s, int32_t p) {
   const CacheDev& c = a.cache;
   const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
   if (slot >= static_cast<uint32_t>(c.slots)) {
     atomicOr(a.err, kDevErrIndex);
-    return;
+    return {-1, -1, 0};
   }
   const uint32_t page = c.page_rows.div(slot);
   const int64_t e = s * c.table_stride + page;
-  const int32_t kp = __ldg(c.table + e);
-  const int32_t vp = c.v_table ? __ldg(c.v_table + e) : kp;
-  if (kp < 0 || kp >= c.n_pages || vp < 0 || vp >= c.n_pages) {
-    if (kp < -1 || kp >= c.n_pages || vp < -1 || vp >= c.n_pages) atomicOr(a.err, kDevErrIndex);
-    return;
+  Box x;
+  x.k = __ldg(c.table + e);
+  x.v = __ldg((c.v_table ? c.v_table : c.table) + e);
+  x.row = slot - page * c.page_rows.d;
+  return x;
+}
+// Page n_pages, whose rows come out as zeros, for what is not in the cache.
+__device__ __forceinline__ void settle(const AttendArgs& a, Box& x) {
+  const int32_t n = a.cache.n_pages;
+  if (x.k < 0 || x.k >= n || x.v < 0 || x.v >= n) {
+    if (x.k < -1 || x.k >= n || x.v < -1 || x.v >= n) atomicOr(a.err, kDevErrIndex);
+    x.k = x.v = n;
   }
-  k = kp;
-  v = vp;
-  row = slot - page * c.page_rows.d;
 }
 
 // Zeros for the infinities and NaN among eight elements; whether there were any.
@@ -301,15 +343,17 @@ __device__ __forceinline__ bool take_out(uint4* at) {
 template <typename T, int DP, bool BOX>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {
-  constexpr int kRing = kBuffers<DP>;
+  constexpr int kRing = kBuffers<DP, BOX>;
   constexpr uint32_t kBytes = kTileBytes<DP>;
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[9 + 3 * kRing];
+  __shared__ __align__(8) uint64_t bars[11 + 3 * kRing];
   __shared__ uint32_t tmem_at;
-  __shared__ __align__(16) uint32_t valid[kValid][4];
+  __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
   __shared__ uint32_t special;
+  __shared__ float swap[2][kTile];                        // what a row's two threads tell one another
+  __shared__ uint32_t places[2][2][BOX ? 1 : kTile];      // tile, keys or values, row: offsets (not BOX)
 
   attend_dependency();
   const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
@@ -341,9 +385,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto o_full = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };
   // BOX: the values of tile j are looked over.  (By tiles: an odd ring has keys
   // and values in a buffer in turn.)
-  auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kRing); };
+  auto s_read = [&](int t) { return bar0 + 8 * (9 + 2 * kRing + t); };  // kAhead: scores are in registers
+  auto v_fine = [&](int j) { return bar0 + 8 * (11 + 2 * kRing + j % kRing); };
   if (tid == 0) {
-    bar_init(q_full, 32 * kCopyWarps);
+    bar_init(q_full, 32 * kSoftWarps / 2 * nq);
     for (int i = 0; i < kRing; ++i) {
       bar_init(kv_full(i), BOX ? 1 : 32 * kCopyWarps);
       bar_init(kv_empty(i), 1);
@@ -354,6 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(p_full(t, 0), kTile);
       bar_init(p_full(t, 1), kTile);
       bar_init(o_full(t), 1);
+      bar_init(s_read(t), 1);
     }
     special = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -370,56 +416,31 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = tmem_at;
   bool ok = true;
 
-  if (warp >= kCopyWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (w.tiles > 0) {
-    // ---- Copying warps: warp c moves rows 32 c .. of each tile ----
-    const int c = warp - kCopyWarp, row0 = 32 * c;
-    constexpr int kAtOnce = 32 / kChunks;  // rows one instruction moves
-    const int chunk = lane % kChunks, sub = lane / kChunks;
-    const bool mine = chunk * 8 < a.cache.head_dim;
-    auto spot = [&](int row) {  // this lane's chunk of a row in a tile
-      return (chunk >> 3) * kPanel + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-    };
-    if (a.cache.head_dim < DP) {  // chunks that no copy writes
-      if (!mine)
-        for (int i = 0; i < (BOX ? 2 : 2 + kRing); ++i)
-          for (int r = sub; r < 32; r += kAtOnce)
-            *reinterpret_cast<uint4*>(ring_ptr - 2 * kBytes + i * kBytes + spot(row0 + r)) = make_uint4(0, 0, 0, 0);
-    }
-    // Query rows: zeros behind the last.
-    for (int t = 0; t < nq; ++t)
-#pragma unroll 4
-      for (int i = 0; i < 32 / kAtOnce; ++i) {
-        const int row = row0 + i * kAtOnce + sub, r = w.row0 + t * kTile + row;
-        const bool there = r < w.rows;
-        const uint32_t tok = a.by_group.div(there ? r : 0);
-        const int h = head * a.group + ((there ? r : 0) - tok * a.group);
-        const uint8_t* q = a.q.data + (w.all.q0 + tok) * a.q.token_bytes + h * a.q.head_bytes;
-        if (mine) copy16(qat + t * kBytes + spot(row), q + chunk * 16, there);
-      }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+  // This lane's 16-byte chunk of a row of a tile: kAtOnce rows an instruction.
+  constexpr int kAtOnce = 32 / kChunks;
+  const int chunk = lane % kChunks, sub = lane / kChunks;
+  const bool mine = chunk * 8 < a.cache.head_dim;
+  auto spot = [](int row, int c) { return (c >> 3) * kPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4); };
 
+  if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp >= kCopyWarp && w.tiles > 0) {
+    // ---- Copying warps.  Fill i: keys of tile i / 2, or its values ----
+    const int c = warp - kCopyWarp;
     const RowsRange range = rows_range(a, w.view, w.pmin, w.pmax);
     if constexpr (BOX) {
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      bar_arrive(q_full);
       if (c == 0) {
         // One warp fills the ring, a lane per box of rows.
-        const int rows = a.box_rows, boxes = kTile / rows;
         const uint32_t one = elected();
         const uint64_t kmap = reinterpret_cast<uint64_t>(maps.k), vmap = reinterpret_cast<uint64_t>(maps.v);
-        struct Box {
-          int32_t k, v, row;  // pages (n_pages: none, zeros are filled in), first row in them
-        };
+        const int rows = a.box_rows, boxes = kTile / rows;
         auto look = [&](int t) {
-          Box x = {a.cache.n_pages, a.cache.n_pages, 0};
+          Box x = {-1, -1, 0};
           const int e = t * kTile + lane * rows;
-          if (lane < boxes && e < w.view.seen) box_place(a, s, seen_position(w.view, e), x.k, x.v, x.row);
+          if (lane < boxes && e < w.view.seen) x = box_place(a, s, seen_position(w.view, e));
           return x;
         };
-        Box box = look(w.tile0), next = box;
+        Box box, next = look(w.tile0);
         for (int i = 0; i < 2 * w.tiles && ok; ++i) {
           const int buf = i % kRing, use = i / kRing;
           if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
@@ -427,6 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           if ((i & 1) == 0) {
             box = next;
+            if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
+            settle(a, box);
             // A bit per token of the tile: its box is in the cache.
             const uint32_t there = __ballot_sync(kFull, lane < boxes && box.k < a.cache.n_pages);
             if (lane < 4) {
@@ -436,7 +459,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               valid[(i / 2) % kValid][lane] = m;
             }
             __syncwarp();
-            if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
           }
           fill_begins(kv_full(buf), kBytes, one);
           for (int k = 0; k < boxes; ++k) {
@@ -448,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else {
-        // The other three look values over.
+        // The others look values over.
         for (int i = 1; i < 2 * w.tiles && ok; i += 2) {
           const int buf = i % kRing;
           ok = bar_wait(kv_full(buf), (i / kRing) & 1);
@@ -457,6 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!range.whole(w.tile0 + i / 2)) {
             uint4* tile = reinterpret_cast<uint4*>(ring_ptr + buf * kBytes);
             bool any = false;
+#pragma unroll 4
             for (int k = (c - 1) * 32 + lane; k < static_cast<int>(kBytes / 16); k += 32 * (kCopyWarps - 1))
               any |= take_out<T>(tile + k);
             if (any) special = 1;
@@ -466,297 +489,369 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     } else {
-      // Fill i: keys of tile i / 2, or its values.  Fill -1 stands for the
-      // query rows.
+      constexpr int kGroups = kTile / kAtOnce;  // warp c moves every kCopyWarps-th
+      if (!mine)                                // chunks that no copy writes
+        for (int i = 0; i < kRing; ++i)
+          for (int g = c; g < kGroups; g += kCopyWarps)
+            *reinterpret_cast<uint4*>(ring_ptr + i * kBytes + spot(g * kAtOnce + sub, chunk)) = make_uint4(0, 0, 0, 0);
       auto landed = [&](int i) {
-        if (i >= 0 && (i & 1)) {
-          if (!range.whole(w.tile0 + i / 2) && mine) {
-            uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
-            bool any = false;
-            for (int r = sub; r < 32; r += kAtOnce)
-              any |= take_out<T>(reinterpret_cast<uint4*>(tile + spot(row0 + r)));
-            if (any) special = 1;
-          }
+        if ((i & 1) && !range.whole(w.tile0 + i / 2) && mine) {
+          uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
+          bool any = false;
+          for (int g = c; g < kGroups; g += kCopyWarps)
+            any |= take_out<T>(reinterpret_cast<uint4*>(tile + spot(g * kAtOnce + sub, chunk)));
+          if (any) special = 1;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(i < 0 ? q_full : kv_full(i % kRing));
+        bar_arrive(kv_full(i % kRing));
       };
+      // Rows' places of tile t, of the call's tile w.tile0 + t.
       auto look = [&](int t) {
-        RowPlace r = {kNoRow, kNoRow};
-        const int e = t * kTile + row0 + lane;
-        if (e < w.view.seen) r = row_place(a, s, seen_position(w.view, e));
-        return r;
+        for (int r = c * 32 + lane; r < kTile; r += 32 * kCopyWarps) {
+          RowPlace x = {kNoRow, kNoRow};
+          const int e = (w.tile0 + t) * kTile + r;
+          if (e < w.view.seen) x = row_place(a, s, seen_position(w.view, e));
+          places[t & 1][0][r] = x.k;
+          places[t & 1][1][r] = x.v;
+          const uint32_t there = __ballot_sync(kFull, x.k != kNoRow);
+          if (lane == 0) valid[t % kValid][r >> 5] = there;
+        }
       };
+      look(0);
       const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes + chunk * 16;
       const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes + chunk * 16;
-      RowPlace place = look(w.tile0), next = place;
       for (int i = 0; i < 2 * w.tiles && ok; ++i) {
         const int buf = i % kRing, use = i / kRing;
         if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
         ok = __all_sync(kFull, ok);
-        if (!ok) break;
-        if ((i & 1) == 0) {
-          place = next;
-          const uint32_t there = __ballot_sync(kFull, place.k != kNoRow);
-          if (lane == 0) valid[(i / 2) % kValid][c] = there;
-          if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
-        }
+        if ((i & 1) == 0) copy_sync();  // the tile's places are written, the ones before the last are used up
+        if (!ok) continue;
         const uint8_t* base = i & 1 ? vbase : kbase;
-        const uint32_t off = i & 1 ? place.v : place.k;
+        const uint32_t* place = places[(i / 2) & 1][i & 1];
         const uint32_t tile = ring + buf * kBytes;
 #pragma unroll 4
-        for (int r = 0; r < 32 / kAtOnce; ++r) {
-          const int row = r * kAtOnce + sub;
-          const uint32_t o = __shfl_sync(kFull, off, row);
+        for (int g = c; g < kGroups; g += kCopyWarps) {
+          const uint32_t o = place[g * kAtOnce + sub];
           const bool in = o != kNoRow;
-          if (mine) copy16(tile + spot(row0 + row), row_at(a, base, in ? o : 0), in);
+          if (mine) copy16(tile + spot(g * kAtOnce + sub, chunk), row_at(a, base, in ? o : 0), in);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
+        if ((i & 1) == 0 && i / 2 + 1 < w.tiles) look(i / 2 + 1);
         asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-        if (i - kLag >= -1) landed(i - kLag);
+        if (i >= kLag) landed(i - kLag);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       if (ok)
-        for (int i = max(-1, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
+        for (int i = max(0, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
     }
     }
-  } else if (warp >= kMmaWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     // ---- The warp that feeds the matrix unit ----
     if (warp == kMmaWarp && w.tiles > 0) {
-      const uint32_t one = elected(), mem = __shfl_sync(kFull, tmem, 0);
+      // Everything an instruction's operands and this loop go by is the same in
+      // all lanes, and made so that it is seen to be (a reduction over the
+      // warp): operands then lie in uniform registers.  Moved there one by one
+      // they held the instructions 80 cycles apart.
+      const uint32_t one = elected(), mem = __reduce_max_sync(kFull, tmem);
+      const int tiles = static_cast<int>(__reduce_max_sync(kFull, static_cast<uint32_t>(w.tiles)));
+      const int row_tiles = static_cast<int>(__reduce_max_sync(kFull, static_cast<uint32_t>(nq)));
       constexpr uint32_t kQK = instruction<T>(kTile, false), kPV = instruction<T>(DP, true);
+      const uint32_t q0 = operand(qat, 16), k0 = operand(ring, 16), v0 = operand(ring, kPanel);
       auto scores = [&](int t, int i) {  // S = Q K^T of row tile t, keys of fill i
-        const uint32_t q = qat + t * kBytes, k = ring + (i % kRing) * kBytes;
+        const uint32_t q = q0 + t * (kBytes >> 4), k = k0 + (i % kRing) * (kBytes >> 4);
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
-          const uint32_t at = (d >> 2) * kPanel + (d & 3) * 32;
-          mma_ss(mem + kScores + t * kTile, operand(q + at, 16), operand(k + at, 16), kQK, d > 0, one);
+          const uint32_t at = ((d >> 2) * kPanel + (d & 3) * 32) >> 4;
+          mma_ss(mem + kScores + t * kTile, q + at, k + at, kQK, d > 0, one);
         }
       };
       auto sums = [&](int t, int i, int half, bool add) {  // O += P V, values of fill i
-        const uint32_t v = ring + (i % kRing) * kBytes;
+        const uint32_t v = v0 + (i % kRing) * (kBytes >> 4);
 #pragma unroll
         for (int k = 0; k < kTile / 32; ++k) {
           const int at = half * (kTile / 32) + k;
-          mma_ts(mem + kSums + t * DP, mem + kScores + t * kTile + at * 8, operand(v + at * 2048, kPanel), kPV,
+          mma_ts(mem + kSums + t * DP, mem + kWeights<DP> + t * kWeightsStep<DP> + at * 8, v + at * (2048 >> 4), kPV,
                  add || k > 0, one);
         }
       };
-      RowsRange range[2];
-      int done[2] = {0, 0}, end[2] = {-1, -1};  // tiles taken, the last one
-      for (int t = 0; t < nq; ++t) {
-        range[t] = tile_range(a, w, t);
-        for (int j = 0; j < w.tiles; ++j)
-          if (range[t].some(w.tile0 + j)) end[t] = j;
-      }
+      const RowsRange range0 = tile_range(a, w, 0), range1 = tile_range(a, w, nq - 1);
+      auto some = [&](int t, int j) { return __any_sync(kFull, (t ? range1 : range0).some(w.tile0 + j)); };
+      int done[2] = {0, 0};  // tiles taken
       ok = __all_sync(kFull, bar_wait(q_full, 0));
-      for (int j = -1; j < w.tiles && ok; ++j) {  // values of tile j, keys of the next
-        const int vi = 2 * j + 1, ki = 2 * j + 2;
-        const bool more = j + 1 < w.tiles;
-        if (j >= 0) ok = bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
-        if (BOX && j >= 0 && ok) ok = bar_wait(v_fine(j), (j / kRing) & 1);
-        if (ok && more) ok = bar_wait(kv_full(ki % kRing), (ki / kRing) & 1);
-        ok = __all_sync(kFull, ok);
+      int given[2] = {0, 0};  // scores made
+      // S of row tile t and tile j, whose keys are there.
+      auto next_scores = [&](int t, int j) {
+        if (some(t, j)) {
+          if (kAhead<DP> && given[t] > 0) ok = __all_sync(kFull, bar_wait(s_read(t), (given[t] - 1) & 1));
+          if (!ok) return;
+          fence_after();
+          scores(t, 2 * j);
+          mma_commit(s_full(t), one);
+          given[t] += 1;
+        }
+      };
+      // O += P V of row tile t and tile j, whose values are there.
+      auto next_sums = [&](int t, int j) {
+        if (some(t, j)) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            ok = __all_sync(kFull, bar_wait(p_full(t, half), done[t] & 1));
+            if (!ok) return;
+            fence_after();
+            sums(t, 2 * j + 1, half, half > 0 || done[t] > 0);
+          }
+          done[t] += 1;
+          mma_commit(o_full(t), one);
+        }
+      };
+      auto keys = [&](int j) {
+        ok = __all_sync(kFull, ok && bar_wait(kv_full(2 * j % kRing), (2 * j / kRing) & 1));
         fence_after();
-        for (int t = 0; t < nq && ok; ++t) {
-          if (j >= 0 && range[t].some(w.tile0 + j)) {
-            ok = __all_sync(kFull, bar_wait(p_full(t, 0), done[t] & 1));
-            if (!ok) break;
-            fence_after();
-            sums(t, vi, 0, done[t] > 0);
-            ok = __all_sync(kFull, bar_wait(p_full(t, 1), done[t] & 1));
-            if (!ok) break;
-            fence_after();
-            sums(t, vi, 1, true);
-            done[t] += 1;
-            if (j == end[t]) mma_commit(o_full(t), one);
+      };
+      if (ok) keys(0);
+      for (int t = 0; t < row_tiles && ok; ++t) next_scores(t, 0);
+      if (ok) mma_commit(kv_empty(0), one);
+      for (int j = 0; j < tiles && ok; ++j) {
+        const int vi = 2 * j + 1, ki = 2 * j + 2;
+        const bool more = j + 1 < tiles;
+        if (kAhead<DP> && more) {
+          keys(j + 1);
+          for (int t = 0; t < row_tiles && ok; ++t) next_scores(t, j + 1);
+          mma_commit(kv_empty(ki % kRing), one);
+        }
+        ok = ok && bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
+        if (BOX) ok = ok && bar_wait(v_fine(j), (j / kRing) & 1);
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
+        next_sums(0, j);
+        if (row_tiles == 1) mma_commit(kv_empty(vi % kRing), one);
+        if (!kAhead<DP> && more && ok) {
+          keys(j + 1);
+          if (ok) next_scores(0, j + 1);
+          if (row_tiles == 1) mma_commit(kv_empty(ki % kRing), one);
+        }
+        if (row_tiles == 2 && ok) {
+          next_sums(1, j);
+          mma_commit(kv_empty(vi % kRing), one);
+          if (!kAhead<DP> && more && ok) {
+            next_scores(1, j + 1);
+            mma_commit(kv_empty(ki % kRing), one);
           }
-          if (j >= 0 && t == nq - 1) mma_commit(kv_empty(vi % kRing), one);
-          if (more && range[t].some(w.tile0 + j + 1)) {
-            scores(t, ki);
-            mma_commit(s_full(t), one);
-          }
-          if (more && t == nq - 1) mma_commit(kv_empty(ki % kRing), one);
         }
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    if ((warp >> 2) < nq) {
-    // ---- A thread per row: weights, running maximum and total ----
-    const int t = warp >> 2;
-    const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // its warp's lanes of tensor memory
-    const uint32_t sc = tmem + kScores + t * kTile + lanes, su = tmem + kSums + t * DP + lanes;
-    const int r = w.row0 + t * kTile + (warp & 3) * 32 + lane;
-    const bool there = r < w.rows;
-    const uint32_t tok = a.by_group.div(there ? r : w.rows - 1);
-    const RowRange sees = row_range(a, w.view, w.all.first + static_cast<int32_t>(tok));
-    const RowsRange range = tile_range(a, w, t);
-    float top = -INFINITY, total = 0.0f;
-    int done = 0;
-    for (int j = 0; j < w.tiles && ok; ++j) {
-      const int tile = w.tile0 + j;
-      if (!range.some(tile)) continue;
-      ok = bar_wait(s_full(t), done & 1);
-      ok = __all_sync(kFull, ok);
-      if (!ok) break;
-      fence_after();
-      uint32_t x[4][32];
-      tm_load(x[0], sc);
-      tm_load(x[1], sc + 32);
-      tm_loaded();
-      tm_load(x[2], sc + 64);
-      tm_load(x[3], sc + 96);
-      float mx[4];
-      auto highest = [&](int c) {
-        mx[c] = __uint_as_float(x[c][0]);
+    // ---- Two threads per row: weights, running maximum and totals ----
+    const int t = warp >> 3, half = (warp >> 2) & 1;
+    if (t < nq) {
+      const int row = (warp & 3) * 32 + lane, r = w.row0 + t * kTile + row;
+      const bool there = r < w.rows;
+      const uint32_t tok = a.by_group.div(there ? r : w.rows - 1);
+      // Query rows, zeros behind the last: kAtOnce rows an instruction.
 #pragma unroll
-        for (int k = 1; k < 31; k += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
-        mx[c] = fmaxf(mx[c], __uint_as_float(x[c][31]));
-      };
-      const uint4 in = *reinterpret_cast<const uint4*>(valid[j % kValid]);
-      if (range.whole(tile) && (in.x & in.y & in.z & in.w) == kFull) {
-        highest(0);
-        highest(1);
-        tm_loaded();
-      } else {
-        tm_loaded();
-        const uint32_t m4[4] = {in.x, in.y, in.z, in.w};
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t m = m4[c] & sees.bits(tile * kTile + c * 32);
-#pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (!(m >> k & 1)) x[c][k] = 0xff800000u;  // -inf
-        }
-        highest(0);
-        highest(1);
+      for (int g = 0; g < kTile / kAtOnce / 8; ++g) {
+        const int i = (g * 8 + (warp & 7)) * kAtOnce + sub, ri = w.row0 + t * kTile + i;
+        const bool in = ri < w.rows;
+        const uint32_t ti = a.by_group.div(in ? ri : 0);
+        const int h = head * a.group + (in ? ri - static_cast<int>(ti) * a.group : 0);
+        const bool live = mine && in;
+        copy16(qat + t * kBytes + spot(i, chunk),
+               a.q.data + (live ? (w.all.q0 + ti) * a.q.token_bytes + h * a.q.head_bytes + chunk * 16 : 0), live);
       }
-      highest(2);
-      highest(3);
-      const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
-      const bool raise = high > top + kSlack;
-      if (__any_sync(kFull, raise)) {
-        const float to = raise ? high : top;
-        const float f = raise ? exp2_fast(top - to) : 1.0f;
-        top = to;
-        total *= f;
-        if (done > 0) {
-#pragma unroll 1
-          for (int c = 0; c < DP / 32; ++c) {
-            uint32_t y[32];
-            tm_load(y, su + c * 32);
-            tm_loaded();
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive(q_full);
+      const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // its warp's lanes of tensor memory
+      const uint32_t sc = tmem + kScores + t * kTile + lanes, su = tmem + kSums + t * DP + half * (DP / 2) + lanes,
+                     we = tmem + kWeights<DP> + t * kWeightsStep<DP> + lanes;
+      const RowRange sees = row_range(a, w.view, w.all.first + static_cast<int32_t>(tok));
+      const RowsRange range = tile_range(a, w, t);
+      float top = -INFINITY, total = 0.0f;
+      int done = 0;
+      for (int j = 0; j < w.tiles; ++j) {
+        const int tile = w.tile0 + j;
+        if (!range.some(tile)) continue;
+        ok = ok && bar_wait(s_full(t), done & 1);
+        __syncwarp();
+        fence_after();
+        uint32_t x[2][32];
+        tm_load(x[0], sc + half * kHalf);
+        tm_load(x[1], sc + half * kHalf + 32);
+        tm_loaded();
+        const uint2 in = *reinterpret_cast<const uint2*>(&valid[j % kValid][2 * half]);
+        if (!(range.whole(tile) && (in.x & in.y) == kFull)) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
-            tm_store(su + c * 32, y);
+          for (int c = 0; c < 2; ++c) {
+            // (Most 32 by 32 pieces of a tile on the diagonal are seen whole.)
+            const uint32_t m = (c ? in.y : in.x) & sees.bits(tile * kTile + half * kHalf + c * 32);
+            if (__all_sync(kFull, m == kFull)) continue;
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (!(m >> k & 1)) x[c][k] = 0xff800000u;  // -inf
           }
         }
-      }
-      const float at = top == -INFINITY ? 0.0f : top;
-      const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), at2 = pair(-at, -at);
-      uint64_t sum[2] = {0, 0};
+        float mx[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t y[32];
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t* y = &x[c >> 1][(c & 1) * 16];
+          mx[c] = __uint_as_float(y[0]);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const uint32_t* z = &x[2 * h + k / 16][k % 16 * 2];
-          float u, v;
-          unpair(fma2(pair(__uint_as_float(z[0]), __uint_as_float(z[1])), scale2, at2), u, v);
-          u = exp2_fast(u);
-          v = exp2_fast(v);
-          sum[k & 1] = add2(sum[k & 1], pair(u, v));
-          y[k] = pack2<T>(u, v);
+          for (int k = 1; k < 15; k += 2) mx[c] = max3(mx[c], __uint_as_float(y[k]), __uint_as_float(y[k + 1]));
+          mx[c] = fmaxf(mx[c], __uint_as_float(y[15]));
         }
-        // Weights over the first half of the scores, all of which are in
-        // registers by now.
-        tm_store(sc + h * 32, y);
-        tm_stored();
-        fence_before();
-        bar_arrive(p_full(t, h));
-      }
-      float u, v;
-      unpair(add2(sum[0], sum[1]), u, v);
-      total += u + v;
-      done += 1;
-    }
-    if (ok && done > 0) ok = bar_wait(o_full(t), 0);
-    ok = __all_sync(kFull, ok);
-    fence_after();
-    constexpr float kLn2 = 0.693147180559945309f;
-    const int64_t qt = w.all.q0 + tok;
-    const int h = head * a.group + (r - static_cast<int>(tok) * a.group);
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const bool mend = *reinterpret_cast<volatile uint32_t*>(&special) != 0;
-    const int64_t row = (static_cast<int64_t>(sp) * a.cache.heads + head) * a.batch.tokens * a.group +
-                        w.all.q0 * a.group + r;
-    float* part = a.part + row * (DP + 2);
+        float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
+        // All scores of the row tile are in registers behind this barrier.
+        const bool any = row_tile_any(t, high > top + kSlack);
+        if (kAhead<DP>) {
+          if ((warp & 7) == 0 && lane == 0) {
+            fence_before();
+            bar_arrive(s_read(t));
+          }
+          // The weights before these are used up, and the sums may be changed.
+          if (done > 0) ok = ok && bar_wait(o_full(t), (done - 1) & 1);
+          __syncwarp();
+          fence_after();
+        }
+        if (any) {
+          if (half == 0) swap[t][row] = high;
+          row_tile_sync(t);
+          if (half == 1) {
+            high = fmaxf(high, swap[t][row]);
+            swap[t][row] = high;
+          }
+          row_tile_sync(t);
+          high = swap[t][row];
+          const bool raise = high > top + kSlack;
+          const float to = raise ? high : top;
+          const float f = raise ? exp2_fast(top - to) : 1.0f;
+          top = to;
+          total *= f;
+          if (done > 0) {
 #pragma unroll 1
-    for (int c = 0; c < DP / 32; ++c) {
-      uint32_t x[32];
-      if (done > 0) {
-        tm_load(x, su + c * 32);
-        tm_loaded();
-      } else {
+            for (int c = 0; c < DP / 64; ++c) {
+              uint32_t y[32];
+              tm_load(y, su + c * 32);
+              tm_loaded();
 #pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = 0;
-      }
-      if (!ok || !there) continue;
-      if (mend) {
-        // Infinities and NaN among the values that this row sees in tiles
-        // where zeros took their place.
-        const RowsRange block = rows_range(a, w.view, w.pmin, w.pmax);
-        for (int j = w.tile0; j < w.tile0 + w.tiles; ++j) {
-          if (block.whole(j)) continue;
-          for (int e = j * kTile; e < min((j + 1) * kTile, w.view.seen); ++e) {
-            if (!(sees.bits(e) & 1)) continue;
-            const RowPlace pl = row_place(a, s, seen_position(w.view, e));
-            if (pl.k == kNoRow) continue;
-            const uint8_t* v = row_at(a, a.cache.v + head * a.cache.head_bytes, pl.v) + c * 64;
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              if (c * 32 + k >= a.cache.head_dim) continue;
-              const uint32_t y = *reinterpret_cast<const uint32_t*>(v + 2 * k), m = specials<T>(y);
-              T e0, e1;
-              const uint16_t lo = static_cast<uint16_t>(y), hi = static_cast<uint16_t>(y >> 16);
-              memcpy(&e0, &lo, 2);
-              memcpy(&e1, &hi, 2);
-              if (m & 0xffffu) x[k] = __float_as_uint(__uint_as_float(x[k]) + static_cast<float>(e0));
-              if (m >> 16) x[k + 1] = __float_as_uint(__uint_as_float(x[k + 1]) + static_cast<float>(e1));
+              for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+              tm_store(su + c * 32, y);
             }
           }
         }
+        const float at = top == -INFINITY ? 0.0f : top;
+        const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), at2 = pair(-at, -at);
+        uint64_t sum[2] = {0, 0};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t y[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float u, v;
+            unpair(fma2(pair(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), scale2, at2), u, v);
+            u = exp2_fast(u);
+            v = exp2_fast(v);
+            sum[k & 1] = add2(sum[k & 1], pair(u, v));
+            y[k] = pack2<T>(u, v);
+          }
+          tm_store16(we + half * 32 + c * 16, y);
+        }
+        float u, v;
+        unpair(add2(sum[0], sum[1]), u, v);
+        total += u + v;
+        tm_stored();
+        fence_before();
+        bar_arrive(p_full(t, half));
+        done += 1;
+      }
+      // (The sums before the last ones were done when the last scores were.)
+      if (ok && done > 0) ok = bar_wait(o_full(t), (done - 1) & 1);
+      __syncwarp();
+      fence_after();
+      if (half == 0) swap[t][row] = total;
+      row_tile_sync(t);
+      if (half == 1) {
+        total += swap[t][row];
+        swap[t][row] = total;
+      }
+      row_tile_sync(t);
+      total = swap[t][row];
+      constexpr float kLn2 = 0.693147180559945309f;
+      const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+      const bool mend = *reinterpret_cast<volatile uint32_t*>(&special) != 0;
+      float* part = a.part + (static_cast<int64_t>(blockIdx.x) * 2 + t) * (DP + 2) * kTile + row;
+#pragma unroll 1
+      for (int c = 0; c < DP / 64; ++c) {
+        const int d0 = half * (DP / 2) + c * 32;
+        uint32_t x[32];
+        if (done > 0) {
+          tm_load(x, su + c * 32);
+          tm_loaded();
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = 0;
+        }
+        if (mend && there) {
+          // Infinities and NaN among the values that this row sees in tiles
+          // where zeros took their place.
+          const RowsRange block = rows_range(a, w.view, w.pmin, w.pmax);
+          for (int j = w.tile0; j < w.tile0 + w.tiles; ++j) {
+            if (block.whole(j)) continue;
+            for (int e = j * kTile; e < min((j + 1) * kTile, w.view.seen); ++e) {
+              if (!(sees.bits(e) & 1)) continue;
+              const RowPlace pl = row_place(a, s, seen_position(w.view, e));
+              if (pl.k == kNoRow) continue;
+              const uint8_t* v = row_at(a, a.cache.v + head * a.cache.head_bytes, pl.v) + d0 * 2;
+#pragma unroll
+              for (int k = 0; k < 32; k += 2) {
+                if (d0 + k >= a.cache.head_dim) continue;
+                const uint32_t y = *reinterpret_cast<const uint32_t*>(v + 2 * k), m = specials<T>(y);
+                T e0, e1;
+                const uint16_t lo = static_cast<uint16_t>(y), hi = static_cast<uint16_t>(y >> 16);
+                memcpy(&e0, &lo, 2);
+                memcpy(&e1, &hi, 2);
+                if (m & 0xffffu) x[k] = __float_as_uint(__uint_as_float(x[k]) + static_cast<float>(e0));
+                if (m >> 16) x[k + 1] = __float_as_uint(__uint_as_float(x[k + 1]) + static_cast<float>(e1));
+              }
+            }
+          }
+        }
+        if (a.splits > 1) {  // a column at a time: a warp's rows lie side by side
+#pragma unroll
+          for (int k = 0; k < 32; ++k) part[(d0 + k) * kTile] = __uint_as_float(x[k]);
+        } else {  // over the query rows, which are used up
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {
+            uint4 y;
+            y.x = pack2<T>(__uint_as_float(x[k]) * inv, __uint_as_float(x[k + 1]) * inv);
+            y.y = pack2<T>(__uint_as_float(x[k + 2]) * inv, __uint_as_float(x[k + 3]) * inv);
+            y.z = pack2<T>(__uint_as_float(x[k + 4]) * inv, __uint_as_float(x[k + 5]) * inv);
+            y.w = pack2<T>(__uint_as_float(x[k + 6]) * inv, __uint_as_float(x[k + 7]) * inv);
+            *reinterpret_cast<uint4*>(ring_ptr - (2 - t) * kBytes + spot(row, (d0 + k) >> 3)) = y;
+          }
+        }
       }
       if (a.splits > 1) {
-#pragma unroll
-        for (int k = 0; k < 32; k += 2)
-          *reinterpret_cast<float2*>(part + c * 32 + k) =
-              make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+        if (half == 0) {
+          part[DP * kTile] = top;
+          part[(DP + 1) * kTile] = total;
+        }
       } else {
-        uint8_t* o = a.out.data + qt * a.out.token_bytes + h * a.out.head_bytes + c * 64;
-#pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-          if (c * 32 + k >= a.cache.head_dim) continue;
-          uint4 y;
-          y.x = pack2<T>(__uint_as_float(x[k]) * inv, __uint_as_float(x[k + 1]) * inv);
-          y.y = pack2<T>(__uint_as_float(x[k + 2]) * inv, __uint_as_float(x[k + 3]) * inv);
-          y.z = pack2<T>(__uint_as_float(x[k + 4]) * inv, __uint_as_float(x[k + 5]) * inv);
-          y.w = pack2<T>(__uint_as_float(x[k + 6]) * inv, __uint_as_float(x[k + 7]) * inv);
-          *reinterpret_cast<uint4*>(o + 2 * k) = y;
+        row_tile_sync(t);
+        for (int g = warp & 7; g < kTile / kAtOnce; g += 8) {  // whole rows to memory
+          const int i = g * kAtOnce + sub, ri = w.row0 + t * kTile + i;
+          if (ri >= w.rows || !mine || !ok) continue;
+          const uint32_t ti = a.by_group.div(ri);
+          const int h = head * a.group + (ri - static_cast<int>(ti) * a.group);
+          *reinterpret_cast<uint4*>(a.out.data + (w.all.q0 + ti) * a.out.token_bytes + h * a.out.head_bytes + chunk * 16) =
+              *reinterpret_cast<const uint4*>(ring_ptr - (2 - t) * kBytes + spot(i, chunk));
+        }
+        if (ok && there && half == 0 && a.lse) {
+          const int h = head * a.group + (r - static_cast<int>(tok) * a.group);
+          a.lse[(w.all.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
+              total == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(total));
         }
       }
     }
-    if (ok && there) {
-      if (a.splits > 1) {
-        *reinterpret_cast<float2*>(part + DP) = make_float2(top, total);
-      } else if (a.lse) {
-        a.lse[qt * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
-            total == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(total));
-      }
-    }
-  }
   }
   if (!ok && lane == 0) atomicOr(a.err, kDevErrTimeout);
   fence_before();
@@ -767,44 +862,51 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Joins the parts of every row: a warp each.
+// Joins the parts of a row tile: a thread per row, 32 of its dims a block.
 template <typename T, int DP>
-__global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kTile) k_attend_join(const __grid_constant__ AttendArgs a, int blocks) {
   attend_dependency();
-  const int64_t rows = a.batch.tokens * a.group;  // of a key head
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (i >= rows * a.cache.heads) return;
-  const int lane = threadIdx.x & 31;
-  const int head = static_cast<int>(i / rows);
-  const int64_t r = i - head * rows;
-  const int64_t tok = r / a.group;
-  const int h = head * a.group + static_cast<int>(r - tok * a.group);
-  const float* part = a.part + i * (DP + 2);
-  const int64_t step = rows * a.cache.heads * (DP + 2);
+  int b = blockIdx.x;
+  const int d0 = b % (DP / 32) * 32;
+  b /= DP / 32;
+  const int t = b % 2;
+  b /= 2;
+  const int head = b % a.cache.heads;
+  b /= a.cache.heads;
+  const int s = b % a.batch.sessions, blk = blocks - 1 - b / a.batch.sessions;
+  const SessionView v = session_view(a, s);
+  const int row = threadIdx.x, r = blk * 2 * kTile + t * kTile + row;
+  if (v.m > a.batch.max_new || r >= v.m * a.group) return;
+  // The parts of the blocks that the block kernel's numbering puts side by side.
+  const int64_t first = static_cast<int64_t>(b) * a.splits * a.cache.heads + head;
+  const int64_t step = static_cast<int64_t>(a.cache.heads) * 2 * (DP + 2) * kTile;
+  const float* part = a.part + (first * 2 + t) * (DP + 2) * kTile + row;
   float top = -INFINITY;
-  for (int w = 0; w < a.splits; ++w) top = fmaxf(top, __ldcg(part + w * step + DP));
+  for (int w = 0; w < a.splits; ++w) top = fmaxf(top, __ldcg(part + w * step + DP * kTile));
   const float at = top == -INFINITY ? 0.0f : top;
-  float o[DP / 32] = {}, total = 0.0f;
+  float o[32] = {}, total = 0.0f;
   for (int w = 0; w < a.splits; ++w) {
-    const float2 x = __ldcg(reinterpret_cast<const float2*>(part + w * step + DP));
-    const float f = exp2_fast(x.x - at);
-    total = fmaf(x.y, f, total);
+    const float f = exp2_fast(__ldcg(part + w * step + DP * kTile) - at);
+    total = fmaf(__ldcg(part + w * step + (DP + 1) * kTile), f, total);
 #pragma unroll
-    for (int k = 0; k < DP / 64; ++k) {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(part + w * step + 64 * k + 2 * lane));
-      o[2 * k] = fmaf(v.x, f, o[2 * k]);
-      o[2 * k + 1] = fmaf(v.y, f, o[2 * k + 1]);
-    }
+    for (int k = 0; k < 32; ++k) o[k] = fmaf(__ldcg(part + w * step + (d0 + k) * kTile), f, o[k]);
   }
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-  uint8_t* out = a.out.data + tok * a.out.token_bytes + h * a.out.head_bytes;
+  const uint32_t tok = a.by_group.div(r);
+  const int h = head * a.group + (r - static_cast<int>(tok) * a.group);
+  uint8_t* out = a.out.data + (v.q0 + tok) * a.out.token_bytes + h * a.out.head_bytes + d0 * 2;
 #pragma unroll
-  for (int k = 0; k < DP / 64; ++k) {
-    const int d = 64 * k + 2 * lane;
-    if (d < a.cache.head_dim) *reinterpret_cast<uint32_t*>(out + 2 * d) = pack2<T>(o[2 * k] * inv, o[2 * k + 1] * inv);
+  for (int k = 0; k < 32; k += 8) {
+    if (d0 + k >= a.cache.head_dim) continue;
+    uint4 y;
+    y.x = pack2<T>(o[k] * inv, o[k + 1] * inv);
+    y.y = pack2<T>(o[k + 2] * inv, o[k + 3] * inv);
+    y.z = pack2<T>(o[k + 4] * inv, o[k + 5] * inv);
+    y.w = pack2<T>(o[k + 6] * inv, o[k + 7] * inv);
+    *reinterpret_cast<uint4*>(out + 2 * k) = y;
   }
-  if (lane == 0 && a.lse)
-    a.lse[tok * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
+  if (d0 == 0 && a.lse)
+    a.lse[(v.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
         total == 0.0f ? -INFINITY : fmaf(top, 0.693147180559945309f, logf(total));
 }
 
@@ -825,10 +927,10 @@ template <typename T, int DP, bool BOX>
 cudaError_t launch_form(const AttendArgs& a, int blocks, const TensorMaps& maps, cudaStream_t stream) {
   auto k = k_attend_block<T, DP, BOX>;
   static SmemLimit limit;
-  if (cudaError_t e = limit.set(k, kSmemBytes<DP>)) return e;
+  if (cudaError_t e = limit.set(k, kSmemBytes<DP, BOX>)) return e;
   cudaLaunchAttribute attr;
   const cudaLaunchConfig_t cfg =
-      config(static_cast<int64_t>(blocks) * a.batch.sessions * a.splits * a.cache.heads, kThreads, kSmemBytes<DP>, &attr, stream);
+      config(static_cast<int64_t>(blocks) * a.batch.sessions * a.splits * a.cache.heads, kThreads, kSmemBytes<DP, BOX>, &attr, stream);
   return cudaLaunchKernelEx(&cfg, k, a, maps, blocks);
 }
 template <typename T, int DP>
@@ -838,10 +940,11 @@ cudaError_t launch(const AttendArgs& a, int blocks, const TensorMaps& maps, cuda
 }
 
 template <typename T, int DP>
-cudaError_t launch_join(const AttendArgs& a, cudaStream_t stream) {
+cudaError_t launch_join(const AttendArgs& a, int blocks, cudaStream_t stream) {
   cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = config((a.batch.tokens * a.group * a.cache.heads + 7) / 8, 256, 0, &attr, stream);
-  return cudaLaunchKernelEx(&cfg, k_attend_join<T, DP>, a);
+  const cudaLaunchConfig_t cfg =
+      config(static_cast<int64_t>(blocks) * a.batch.sessions * a.cache.heads * 2 * (DP / 32), kTile, 0, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, k_attend_join<T, DP>, a, blocks);
 }
 
 }  // namespace
@@ -854,10 +957,10 @@ cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks,
                                 : launch<__nv_bfloat16, 128>(a, blocks, maps, stream);
 }
 
-cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, cudaStream_t stream) {
+cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream) {
   if (dtype == PCS_DT_F16)
-    return a.cache.head_dim <= 64 ? launch_join<__half, 64>(a, stream) : launch_join<__half, 128>(a, stream);
-  return a.cache.head_dim <= 64 ? launch_join<__nv_bfloat16, 64>(a, stream) : launch_join<__nv_bfloat16, 128>(a, stream);
+    return a.cache.head_dim <= 64 ? launch_join<__half, 64>(a, blocks, stream) : launch_join<__half, 128>(a, blocks, stream);
+  return a.cache.head_dim <= 64 ? launch_join<__nv_bfloat16, 64>(a, blocks, stream) : launch_join<__nv_bfloat16, 128>(a, blocks, stream);
 }
 
 }  // namespace pcs

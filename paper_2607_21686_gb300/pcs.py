@@ -423,18 +423,25 @@ def kv_session(session_id: int, meta: torch.Tensor, k_pool: torch.Tensor, v_pool
 _HEAD_DTYPES = {torch.float16: PCS_DT_F16, torch.bfloat16: PCS_DT_BF16, torch.float32: PCS_DT_F32}
 
 
-def _heads(t: torch.Tensor, what: str) -> pcs_heads:
+def _heads(t: torch.Tensor, what: str, tokens: int) -> pcs_heads:
     """pcs_heads of a [tokens, heads, head_dim] tensor."""
-    if t.dim() != 3 or not t.is_cuda or t.dtype not in _HEAD_DTYPES:
+    dtype = _HEAD_DTYPES.get(t.dtype)
+    if t.dim() != 3 or dtype is None or not t.is_cuda:
         raise ValueError("%s: a CUDA tensor [tokens, heads, head_dim] of float16, bfloat16 or "
                          "float32 is wanted" % what)
     n, h, d = t.shape
+    if n != tokens:
+        raise ValueError("%s: %d tokens, %d are wanted" % (what, n, tokens))
     ts, hs, es = t.stride()
     if es != 1 and d > 1:
         raise ValueError("%s: the elements of a head must be contiguous" % what)
     # A stride over one item is never taken and may be anything.
-    return pcs_heads(t.data_ptr(), ts if n > 1 else h * d, hs if h > 1 else d, h, d,
-                     _HEAD_DTYPES[t.dtype], 0)
+    return pcs_heads(t.data_ptr(), ts if n > 1 else h * d, hs if h > 1 else d, h, d, dtype, 0)
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor of t's shape and type."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _int32(t: torch.Tensor, what: str, dim: int) -> torch.Tensor:
@@ -805,46 +812,41 @@ class Context:
         xs, or with `inverse` taken back (the gradient).  out: the results'
         tensors (may be xs itself); returns them."""
         if out is None:
-            out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in xs]
-        n = len(xs)
-        if len(out) != n or any(x.shape != y.shape or x.shape[0] != rotary.tokens
-                                for x, y in zip(xs, out)):
-            raise ValueError("every tensor and its result need the positions' %d tokens"
-                             % rotary.tokens)
+            out = [_like(x) for x in xs]
+        n, tokens = len(xs), rotary.tokens
+        if len(out) != n:
+            raise ValueError("%d tensors and %d results" % (n, len(out)))
         arr = pcs_heads * max(n, 1)
         check(self.lib.pcs_rotate(self.h, rotary.inverse if inverse else rotary.forward,
-                                  arr(*[_heads(x, "x") for x in xs]),
-                                  arr(*[_heads(y, "out") for y in out]), n, rotary.tokens,
+                                  arr(*[_heads(x, "x", tokens) for x in xs]),
+                                  arr(*[_heads(y, "out", tokens) for y in out]), n, tokens,
                                   _stream_ptr(stream)), "pcs_rotate")
         return out
 
     @staticmethod
-    def _check_tokens(cache: KvCache, batch: KvBatch, **tensors) -> None:
+    def _check_tables(cache: KvCache, batch: KvBatch) -> None:
         if batch.sessions > cache.sessions:
             raise ValueError("%d sessions and %d page tables" % (batch.sessions, cache.sessions))
-        for what, t in tensors.items():
-            if t.shape[0] != batch.tokens:
-                raise ValueError("%s: %d tokens, the batch has %d" % (what, t.shape[0], batch.tokens))
 
     def kv_append(self, cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor,
                   q: torch.Tensor = None, rotary: Rotary = None, q_out: torch.Tensor = None,
                   stream=None):
         """Write the new tokens' keys (rotated) and values [tokens, heads,
         head_dim] into the cache; with q, returns it rotated (q_out)."""
-        self._check_tokens(cache, batch, k=k, v=v)
-        if rotary is not None and rotary.tokens != batch.tokens:
-            raise ValueError("%d positions, the batch has %d tokens" % (rotary.tokens, batch.tokens))
-        qs = None
+        self._check_tables(cache, batch)
+        n = batch.tokens
+        if rotary is not None and rotary.tokens != n:
+            raise ValueError("%d positions, the batch has %d tokens" % (rotary.tokens, n))
+        qs = ys = None
         if q is not None:
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            self._check_tokens(cache, batch, q=q, q_out=q_out)
-            qs = (_heads(q, "q"), _heads(q_out, "q_out"))
+                q_out = _like(q)
+            qs, ys = _heads(q, "q", n), _heads(q_out, "q_out", n)
         elif q_out is not None:
             raise ValueError("q_out without q")
         check(self.lib.pcs_kv_append(self.h, cache.struct, batch.struct,
-                                     None if rotary is None else rotary.forward, _heads(k, "k"),
-                                     _heads(v, "v"), qs and qs[0], qs and qs[1],
+                                     None if rotary is None else rotary.forward,
+                                     _heads(k, "k", n), _heads(v, "v", n), qs, ys,
                                      _stream_ptr(stream)), "pcs_kv_append")
         return q_out
 
@@ -854,17 +856,20 @@ class Context:
         """Attention of the new tokens' queries [tokens, q heads, head_dim] over
         the cache; returns out, or (out, lse) if lse is given or asked for.
         lse: float32 [tokens, q heads].  scale 0: 1 / sqrt(head_dim)."""
+        self._check_tables(cache, batch)
+        n = batch.tokens
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        self._check_tokens(cache, batch, q=q, out=out)
-        if lse is None and return_lse:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2]
-                                or not lse.is_cuda or not lse.is_contiguous()):
-            raise ValueError("lse must be a contiguous CUDA float32 [tokens, q heads]")
+            out = _like(q)
+        qs, ys = _heads(q, "q", n), _heads(out, "out", n)
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_cuda \
+                    or not lse.is_contiguous():
+                raise ValueError("lse must be a contiguous CUDA float32 [tokens, q heads]")
+        elif return_lse:
+            lse = torch.empty((n, qs.heads), dtype=torch.float32, device=q.device)
         check(self.lib.pcs_attend(self.h, cache.struct, batch.struct,
-                                  pcs_attend_params(scale, window, 0, 0), _heads(q, "q"),
-                                  _heads(out, "out"), _ptr(lse), _stream_ptr(stream)), "pcs_attend")
+                                  pcs_attend_params(scale, window, 0, 0), qs, ys, _ptr(lse),
+                                  _stream_ptr(stream)), "pcs_attend")
         return out if lse is None else (out, lse)
 
     # -- snapshots -------------------------------------------------------------
