@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[11 + 3 * kRing];
+  __shared__ __align__(8) uint64_t bars[9 + 3 * kRing];
   __shared__ uint32_t tmem_at;
   __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
   __shared__ uint32_t special;
@@ -380,13 +380,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto kv_full = [&](int i) { return bar0 + 8 * (1 + i); };
   auto kv_empty = [&](int i) { return bar0 + 8 * (1 + kRing + i); };
   auto s_full = [&](int t) { return bar0 + 8 * (1 + 2 * kRing + t); };
-  // The weights of a tile's first half of tokens, and of its second.
-  auto p_full = [&](int t, int half) { return bar0 + 8 * (3 + 2 * kRing + 2 * t + half); };
-  auto o_full = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };
+  auto p_full = [&](int t) { return bar0 + 8 * (3 + 2 * kRing + t); };
+  auto o_full = [&](int t) { return bar0 + 8 * (5 + 2 * kRing + t); };
   // BOX: the values of tile j are looked over.  (By tiles: an odd ring has keys
   // and values in a buffer in turn.)
-  auto s_read = [&](int t) { return bar0 + 8 * (9 + 2 * kRing + t); };  // kAhead: scores are in registers
-  auto v_fine = [&](int j) { return bar0 + 8 * (11 + 2 * kRing + j % kRing); };
+  auto s_read = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };  // kAhead: scores are in registers
+  auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kRing); };
   if (tid == 0) {
     bar_init(q_full, 32 * kSoftWarps / 2 * nq);
     for (int i = 0; i < kRing; ++i) {
@@ -396,8 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(s_full(t), 1);
-      bar_init(p_full(t, 0), kTile);
-      bar_init(p_full(t, 1), kTile);
+      bar_init(p_full(t), 2 * kTile);
       bar_init(o_full(t), 1);
       bar_init(s_read(t), 1);
     }
@@ -564,14 +562,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           mma_ss(mem + kScores + t * kTile, q + at, k + at, kQK, d > 0, one);
         }
       };
-      auto sums = [&](int t, int i, int half, bool add) {  // O += P V, values of fill i
+      auto sums = [&](int t, int i, bool add) {  // O += P V, values of fill i
         const uint32_t v = v0 + (i % kRing) * (kBytes >> 4);
 #pragma unroll
-        for (int k = 0; k < kTile / 32; ++k) {
-          const int at = half * (kTile / 32) + k;
-          mma_ts(mem + kSums + t * DP, mem + kWeights<DP> + t * kWeightsStep<DP> + at * 8, v + at * (2048 >> 4), kPV,
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_ts(mem + kSums + t * DP, mem + kWeights<DP> + t * kWeightsStep<DP> + k * 8, v + k * (2048 >> 4), kPV,
                  add || k > 0, one);
-        }
       };
       const RowsRange range0 = tile_range(a, w, 0), range1 = tile_range(a, w, nq - 1);
       auto some = [&](int t, int j) { return __any_sync(kFull, (t ? range1 : range0).some(w.tile0 + j)); };
@@ -592,13 +588,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       // O += P V of row tile t and tile j, whose values are there.
       auto next_sums = [&](int t, int j) {
         if (some(t, j)) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            ok = __all_sync(kFull, bar_wait(p_full(t, half), done[t] & 1));
-            if (!ok) return;
-            fence_after();
-            sums(t, 2 * j + 1, half, half > 0 || done[t] > 0);
-          }
+          ok = __all_sync(kFull, bar_wait(p_full(t), done[t] & 1));
+          if (!ok) return;
+          fence_after();
+          sums(t, 2 * j + 1, done[t] > 0);
           done[t] += 1;
           mma_commit(o_full(t), one);
         }
@@ -613,8 +606,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < tiles && ok; ++j) {
         const int vi = 2 * j + 1, ki = 2 * j + 2;
         const bool more = j + 1 < tiles;
+        // Everything that is not on the way from weights to scores is waited
+        // for before them: a wait takes some 200 cycles even if it is over.
+        if (more) keys(j + 1);
         if (kAhead<DP> && more) {
-          keys(j + 1);
           for (int t = 0; t < row_tiles && ok; ++t) next_scores(t, j + 1);
           mma_commit(kv_empty(ki % kRing), one);
         }
@@ -625,8 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         next_sums(0, j);
         if (row_tiles == 1) mma_commit(kv_empty(vi % kRing), one);
         if (!kAhead<DP> && more && ok) {
-          keys(j + 1);
-          if (ok) next_scores(0, j + 1);
+          next_scores(0, j + 1);
           if (row_tiles == 1) mma_commit(kv_empty(ki % kRing), one);
         }
         if (row_tiles == 2 && ok) {
@@ -760,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         total += u + v;
         tm_stored();
         fence_before();
-        bar_arrive(p_full(t, half));
+        bar_arrive(p_full(t));
         done += 1;
       }
       // (The sums before the last ones were done when the last scores were.)
