@@ -26,17 +26,16 @@ namespace pcs {
 namespace {
 
 constexpr int kTile = 128;              // rows of a row tile, tokens of a tile
-constexpr int kHalf = kTile / 2;        // tokens a softmax thread has of a tile
-// Warps 0-7 and 8-15: a row tile each, two threads a row; 16: matrix products;
-// 17-19: copies.
-constexpr int kSoftWarps = 16;
-constexpr int kMmaWarp = 16;
-constexpr int kCopyWarp = 17;
+// Warps 0-3 and 4-7: a row tile each, a thread a row; 8: matrix products; 9-11:
+// copies.
+constexpr int kSoftWarps = 8;
+constexpr int kMmaWarp = 8;
+constexpr int kCopyWarp = 9;
 constexpr int kCopyWarps = 3;
 constexpr int kThreads = 32 * (kCopyWarp + kCopyWarps);
-// Registers of a thread: the launch's 96 shared out anew, 512 x 104 + 128 x 64
-// = 640 x 96.
-constexpr int kSoftRegs = 104, kOtherRegs = 64;
+// Registers of a thread: the launch's 168 shared out anew, 256 x 216 + 128 x 72
+// = 384 x 168.
+constexpr int kSoftRegs = 216, kOtherRegs = 72;
 constexpr int kLag = 2;                 // copies in flight behind the newest
 constexpr int kValid = 8;               // tiles whose masks are kept
 constexpr unsigned kFull = 0xffffffffu;
@@ -60,10 +59,10 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(20000u)
+      : "r"(bar), "r"(parity)
       : "memory");
   return ok != 0;
 }
@@ -175,26 +174,8 @@ __device__ __forceinline__ void tm_store(uint32_t at, const uint32_t (&r)[32]) {
       "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
-__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-// Barriers of the 32 * 8 threads of a row tile, and of the copying warps.
-__device__ __forceinline__ void row_tile_sync(int t) { asm volatile("barrier.cta.sync %0, 256;" ::"r"(1 + t) : "memory"); }
-__device__ __forceinline__ bool row_tile_any(int t, bool x) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"(x ? 1u : 0u), "r"(1 + t)
-      : "memory");
-  return r != 0;
-}
+// Barriers of the threads of a row tile, and of the copying warps.
+__device__ __forceinline__ void row_tile_sync(int t) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + t) : "memory"); }
 __device__ __forceinline__ void copy_sync() {
   asm volatile("barrier.cta.sync 3, %0;" ::"n"(32 * kCopyWarps) : "memory");
 }
@@ -352,7 +333,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ uint32_t tmem_at;
   __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
   __shared__ uint32_t special;
-  __shared__ float swap[2][kTile];                        // what a row's two threads tell one another
   __shared__ uint32_t places[2][2][BOX ? 1 : kTile];      // tile, keys or values, row: offsets (not BOX)
 
   attend_dependency();
@@ -395,9 +375,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(s_full(t), 1);
-      bar_init(p_full(t), 2 * kTile);
+      bar_init(p_full(t), kTile);
       bar_init(o_full(t), 1);
-      bar_init(s_read(t), 1);
+      bar_init(s_read(t), kTile);
     }
     special = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -420,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const bool mine = chunk * 8 < a.cache.head_dim;
   auto spot = [](int row, int c) { return (c >> 3) * kPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4); };
 
-  if (warp >= kMmaWarp) {
+  if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp >= kCopyWarp && w.tiles > 0) {
     // ---- Copying warps.  Fill i: keys of tile i / 2, or its values ----
@@ -635,16 +615,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    // ---- Two threads per row: weights, running maximum and totals ----
-    const int t = warp >> 3, half = (warp >> 2) & 1;
+    // ---- A thread per row: weights, running maximum and total ----
+    const int t = warp >> 2;
     if (t < nq) {
       const int row = (warp & 3) * 32 + lane, r = w.row0 + t * kTile + row;
       const bool there = r < w.rows;
       const uint32_t tok = a.by_group.div(there ? r : w.rows - 1);
       // Query rows, zeros behind the last: kAtOnce rows an instruction.
 #pragma unroll
-      for (int g = 0; g < kTile / kAtOnce / 8; ++g) {
-        const int i = (g * 8 + (warp & 7)) * kAtOnce + sub, ri = w.row0 + t * kTile + i;
+      for (int g = 0; g < kTile / kAtOnce / 4; ++g) {
+        const int i = (g * 4 + (warp & 3)) * kAtOnce + sub, ri = w.row0 + t * kTile + i;
         const bool in = ri < w.rows;
         const uint32_t ti = a.by_group.div(in ? ri : 0);
         const int h = head * a.group + (in ? ri - static_cast<int>(ti) * a.group : 0);
@@ -656,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       bar_arrive(q_full);
       const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // its warp's lanes of tensor memory
-      const uint32_t sc = tmem + kScores + t * kTile + lanes, su = tmem + kSums + t * DP + half * (DP / 2) + lanes,
+      const uint32_t sc = tmem + kScores + t * kTile + lanes, su = tmem + kSums + t * DP + lanes,
                      we = tmem + kWeights<DP> + t * kWeightsStep<DP> + lanes;
       const RowRange sees = row_range(a, w.view, w.all.first + static_cast<int32_t>(tok));
       const RowsRange range = tile_range(a, w, t);
@@ -668,61 +648,60 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = ok && bar_wait(s_full(t), done & 1);
         __syncwarp();
         fence_after();
-        uint32_t x[2][32];
-        tm_load(x[0], sc + half * kHalf);
-        tm_load(x[1], sc + half * kHalf + 32);
+        uint32_t x[4][32];
+        tm_load(x[0], sc);
+        tm_load(x[1], sc + 32);
         tm_loaded();
-        const uint2 in = *reinterpret_cast<const uint2*>(&valid[j % kValid][2 * half]);
-        if (!(range.whole(tile) && (in.x & in.y) == kFull)) {
+        tm_load(x[2], sc + 64);
+        tm_load(x[3], sc + 96);
+        float mx[4];
+        auto highest = [&](int c) {
+          mx[c] = __uint_as_float(x[c][0]);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          for (int k = 1; k < 31; k += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
+          mx[c] = fmaxf(mx[c], __uint_as_float(x[c][31]));
+        };
+        const uint4 in = *reinterpret_cast<const uint4*>(valid[j % kValid]);
+        if (range.whole(tile) && (in.x & in.y & in.z & in.w) == kFull) {
+          highest(0);
+          highest(1);
+          tm_loaded();
+        } else {
+          tm_loaded();
+          const uint32_t m4[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
             // (Most 32 by 32 pieces of a tile on the diagonal are seen whole.)
-            const uint32_t m = (c ? in.y : in.x) & sees.bits(tile * kTile + half * kHalf + c * 32);
+            const uint32_t m = m4[c] & sees.bits(tile * kTile + c * 32);
             if (__all_sync(kFull, m == kFull)) continue;
 #pragma unroll
             for (int k = 0; k < 32; ++k)
               if (!(m >> k & 1)) x[c][k] = 0xff800000u;  // -inf
           }
+          highest(0);
+          highest(1);
         }
-        float mx[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t* y = &x[c >> 1][(c & 1) * 16];
-          mx[c] = __uint_as_float(y[0]);
-#pragma unroll
-          for (int k = 1; k < 15; k += 2) mx[c] = max3(mx[c], __uint_as_float(y[k]), __uint_as_float(y[k + 1]));
-          mx[c] = fmaxf(mx[c], __uint_as_float(y[15]));
-        }
-        float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
-        // All scores of the row tile are in registers behind this barrier.
-        const bool any = row_tile_any(t, high > top + kSlack);
         if (kAhead<DP>) {
-          if ((warp & 7) == 0 && lane == 0) {
-            fence_before();
-            bar_arrive(s_read(t));
-          }
-          // The weights before these are used up, and the sums may be changed.
-          if (done > 0) ok = ok && bar_wait(o_full(t), (done - 1) & 1);
+          fence_before();
+          bar_arrive(s_read(t));
+        }
+        highest(2);
+        highest(3);
+        const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2;
+        if (kAhead<DP> && done > 0) {  // the weights before these are used up, the sums may be changed
+          ok = ok && bar_wait(o_full(t), (done - 1) & 1);
           __syncwarp();
           fence_after();
         }
-        if (any) {
-          if (half == 0) swap[t][row] = high;
-          row_tile_sync(t);
-          if (half == 1) {
-            high = fmaxf(high, swap[t][row]);
-            swap[t][row] = high;
-          }
-          row_tile_sync(t);
-          high = swap[t][row];
-          const bool raise = high > top + kSlack;
+        const bool raise = high > top + kSlack;
+        if (__any_sync(kFull, raise)) {
           const float to = raise ? high : top;
           const float f = raise ? exp2_fast(top - to) : 1.0f;
           top = to;
           total *= f;
           if (done > 0) {
 #pragma unroll 1
-            for (int c = 0; c < DP / 64; ++c) {
+            for (int c = 0; c < DP / 32; ++c) {
               uint32_t y[32];
               tm_load(y, su + c * 32);
               tm_loaded();
@@ -736,18 +715,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), at2 = pair(-at, -at);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t y[16];
+        for (int h = 0; h < 2; ++h) {
+          uint32_t y[32];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
+          for (int k = 0; k < 32; ++k) {
+            const uint32_t* z = &x[2 * h + k / 16][k % 16 * 2];
             float u, v;
-            unpair(fma2(pair(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), scale2, at2), u, v);
+            unpair(fma2(pair(__uint_as_float(z[0]), __uint_as_float(z[1])), scale2, at2), u, v);
             u = exp2_fast(u);
             v = exp2_fast(v);
             sum[k & 1] = add2(sum[k & 1], pair(u, v));
             y[k] = pack2<T>(u, v);
           }
-          tm_store16(we + half * 32 + c * 16, y);
+          // (Heads of 128: over the first half of the scores, all of which are
+          // in registers by now.)
+          tm_store(we + h * 32, y);
         }
         float u, v;
         unpair(add2(sum[0], sum[1]), u, v);
@@ -761,21 +743,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok && done > 0) ok = bar_wait(o_full(t), (done - 1) & 1);
       __syncwarp();
       fence_after();
-      if (half == 0) swap[t][row] = total;
-      row_tile_sync(t);
-      if (half == 1) {
-        total += swap[t][row];
-        swap[t][row] = total;
-      }
-      row_tile_sync(t);
-      total = swap[t][row];
       constexpr float kLn2 = 0.693147180559945309f;
       const float inv = total == 0.0f ? 0.0f : 1.0f / total;
       const bool mend = *reinterpret_cast<volatile uint32_t*>(&special) != 0;
       float* part = a.part + (static_cast<int64_t>(blockIdx.x) * 2 + t) * (DP + 2) * kTile + row;
 #pragma unroll 1
-      for (int c = 0; c < DP / 64; ++c) {
-        const int d0 = half * (DP / 2) + c * 32;
+      for (int c = 0; c < DP / 32; ++c) {
+        const int d0 = c * 32;
         uint32_t x[32];
         if (done > 0) {
           tm_load(x, su + c * 32);
@@ -825,13 +799,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (a.splits > 1) {
-        if (half == 0) {
-          part[DP * kTile] = top;
-          part[(DP + 1) * kTile] = total;
-        }
+        part[DP * kTile] = top;
+        part[(DP + 1) * kTile] = total;
       } else {
         row_tile_sync(t);
-        for (int g = warp & 7; g < kTile / kAtOnce; g += 8) {  // whole rows to memory
+#pragma unroll 4
+        for (int g = warp & 3; g < kTile / kAtOnce; g += 4) {  // whole rows to memory
           const int i = g * kAtOnce + sub, ri = w.row0 + t * kTile + i;
           if (ri >= w.rows || !mine || !ok) continue;
           const uint32_t ti = a.by_group.div(ri);
@@ -839,7 +812,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           *reinterpret_cast<uint4*>(a.out.data + (w.all.q0 + ti) * a.out.token_bytes + h * a.out.head_bytes + chunk * 16) =
               *reinterpret_cast<const uint4*>(ring_ptr - (2 - t) * kBytes + spot(i, chunk));
         }
-        if (ok && there && half == 0 && a.lse) {
+        if (ok && there && a.lse) {
           const int h = head * a.group + (r - static_cast<int>(tok) * a.group);
           a.lse[(w.all.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
               total == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(total));
