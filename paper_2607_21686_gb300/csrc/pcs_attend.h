@@ -152,7 +152,7 @@ struct AttendArgs {
   FastDiv by_group;
   int32_t splits;          // parts of a session's visible tokens
   float* part;             // partial results (splits > 1)
-  uint32_t* ticket;        // zero on entry and on exit
+  uint32_t* ticket;        // token kernel: zero on entry and on exit; null: parts are joined later
   int32_t box_rows;        // block kernel: rows of a tensor copy, 0: rows are copied one by one
   uint32_t* err;
 };
@@ -166,7 +166,10 @@ inline uint64_t token_part_floats(int rows, int head_dim) {
   const uint64_t padded = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   return padded * ((head_dim <= 64 ? 64 : 128) + 2);
 }
-cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, cudaStream_t stream);
+// Parts are joined by the block that ends last while there are at most
+// kTokenOwnJoin of them (a.ticket), else by a second launch (`join`).
+constexpr int kTokenOwnJoin = 16;
+cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream);
 // Blocks of the token kernel that one SM holds.
 int attend_token_blocks_per_sm(int head_dim);
 

@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kThreads)
       }
     }
   }
-  if (a.splits == 1) return;
+  if (a.splits == 1 || a.ticket == nullptr) return;
 
   // The part that ends last joins all, in the parts' order.
   __threadfence();
@@ -403,27 +403,95 @@ __global__ void __launch_bounds__(kThreads)
   __syncthreads();
   if (!last) return;
   __threadfence();
-  for (int i = tid; i < rows * (DP / 2); i += kThreads) {
-    const int row = i / (DP / 2), d = i % (DP / 2) * 2;
+  constexpr int kMine = kRows * DP / 2 / kThreads;  // pairs of dims a thread joins at most
+  float* factors = sums;                            // [part][row]: 2^(its maximum - the row's)
+  for (int row = tid; row < rows; row += kThreads) {
     float m = -INFINITY;
     for (int w = 0; w < a.splits; ++w) m = fmaxf(m, __ldcg(part + w * part_floats + kRows * DP + row));
     const float at = m == -INFINITY ? 0.0f : m;
-    Joined j = {0.0f, 0.0f, m, 0.0f};
-#pragma unroll 4
+    float total = 0.0f;
     for (int w = 0; w < a.splits; ++w) {
-      const float* p = part + w * part_floats;
-      const float f = exp2_fast(__ldcg(p + kRows * DP + row) - at);
-      const float2 x = __ldcg(reinterpret_cast<const float2*>(p + row * DP + d));
-      j.x = fmaf(x.x, f, j.x);
-      j.y = fmaf(x.y, f, j.y);
-      j.total = fmaf(__ldcg(p + kRows * DP + kRows + row), f, j.total);
+      const float* p = part + w * part_floats + kRows * DP + row;
+      const float f = exp2_fast(__ldcg(p) - at);
+      factors[w * kRows + row] = f;
+      total = fmaf(__ldcg(p + kRows), f, total);
     }
-    write(row, d, j);
+    tops[row] = m;
+    totals[row] = total;
+  }
+  __syncthreads();
+  float2 x[kMine];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) x[k] = make_float2(0.0f, 0.0f);
+#pragma unroll 2
+  for (int w = 0; w < a.splits; ++w) {
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      const int i = tid + k * kThreads, row = i / (DP / 2), d = i % (DP / 2) * 2;
+      if (row >= rows) continue;
+      const float2 y = __ldcg(reinterpret_cast<const float2*>(part + w * part_floats + row * DP + d));
+      const float f = factors[w * kRows + row];
+      x[k].x = fmaf(y.x, f, x[k].x);
+      x[k].y = fmaf(y.y, f, x[k].y);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = tid + k * kThreads, row = i / (DP / 2), d = i % (DP / 2) * 2;
+    if (row < rows) write(row, d, Joined{x[k].x, x[k].y, tops[row], totals[row]});
   }
 }
 
+// Joins many parts: a warp per row, its parts by lane for maximum and total,
+// then its dims.
 template <typename T, int DP, int NT>
-cudaError_t launch(const AttendArgs& a, cudaStream_t stream) {
+__global__ void __launch_bounds__(kThreads) k_attend_token_join(const __grid_constant__ AttendArgs a) {
+  constexpr int kRows = 8 * NT;
+  attend_dependency();
+  const int lane = threadIdx.x & 31;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t pair = i / kRows;
+  const int row = static_cast<int>(i % kRows);
+  const int s = static_cast<int>(pair / a.cache.heads), head = static_cast<int>(pair % a.cache.heads);
+  if (s >= a.batch.sessions) return;
+  const SessionView view = session_view(a, s);
+  if (row >= view.m * a.group || view.m * a.group > kRows || view.m > a.batch.max_new) return;
+  const int64_t part_floats = static_cast<int64_t>(kRows) * (DP + 2);
+  const float* part = a.part + pair * a.splits * part_floats;
+  float m = -INFINITY;
+  for (int w = lane; w < a.splits; w += 32) m = fmaxf(m, __ldcg(part + w * part_floats + kRows * DP + row));
+#pragma unroll
+  for (int k = 16; k > 0; k /= 2) m = fmaxf(m, __shfl_xor_sync(kFull, m, k));
+  const float at = m == -INFINITY ? 0.0f : m;
+  float x[DP / 32] = {}, total = 0.0f;
+#pragma unroll 8
+  for (int w = 0; w < a.splits; ++w) {
+    const float* p = part + w * part_floats;
+    const float f = exp2_fast(__ldcg(p + kRows * DP + row) - at);
+    total = fmaf(__ldcg(p + kRows * DP + kRows + row), f, total);
+#pragma unroll
+    for (int k = 0; k < DP / 64; ++k) {
+      const float2 y = __ldcg(reinterpret_cast<const float2*>(p + row * DP + 64 * k + 2 * lane));
+      x[2 * k] = fmaf(y.x, f, x[2 * k]);
+      x[2 * k + 1] = fmaf(y.y, f, x[2 * k + 1]);
+    }
+  }
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  const uint32_t tok = a.by_group.div(row);
+  const int h = head * a.group + (row - static_cast<int>(tok) * a.group);
+  uint8_t* out = a.out.data + (view.q0 + tok) * a.out.token_bytes + h * a.out.head_bytes;
+#pragma unroll
+  for (int k = 0; k < DP / 64; ++k) {
+    const int d = 64 * k + 2 * lane;
+    if (d < a.cache.head_dim) *reinterpret_cast<uint32_t*>(out + d * 2) = pack2<T>(x[2 * k] * inv, x[2 * k + 1] * inv);
+  }
+  if (lane == 0 && a.lse)
+    a.lse[(view.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
+        total == 0.0f ? -INFINITY : fmaf(m, 0.693147180559945309f, logf(total));
+}
+
+template <typename T, int DP, int NT>
+cudaError_t launch(const AttendArgs& a, bool join, cudaStream_t stream) {
   auto k = k_attend_token<T, DP, NT>;
   static SmemLimit limit;
   if (cudaError_t e = limit.set(k, kRingBytes<DP>)) return e;
@@ -437,16 +505,21 @@ cudaError_t launch(const AttendArgs& a, cudaStream_t stream) {
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  if (join) {
+    cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(a.batch.sessions) * a.cache.heads * 8 * NT / kWarps));
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, k_attend_token_join<T, DP, NT>, a);
+  }
   return cudaLaunchKernelEx(&cfg, k, a);
 }
 
 template <typename T>
-cudaError_t by_size(const AttendArgs& a, int rows, cudaStream_t stream) {
+cudaError_t by_size(const AttendArgs& a, int rows, bool join, cudaStream_t stream) {
   if (a.cache.head_dim <= 64)
-    return rows <= 8 ? launch<T, 64, 1>(a, stream) : rows <= 16 ? launch<T, 64, 2>(a, stream)
-                                                               : launch<T, 64, 4>(a, stream);
-  return rows <= 8 ? launch<T, 128, 1>(a, stream) : rows <= 16 ? launch<T, 128, 2>(a, stream)
-                                                              : launch<T, 128, 4>(a, stream);
+    return rows <= 8 ? launch<T, 64, 1>(a, join, stream) : rows <= 16 ? launch<T, 64, 2>(a, join, stream)
+                                                               : launch<T, 64, 4>(a, join, stream);
+  return rows <= 8 ? launch<T, 128, 1>(a, join, stream) : rows <= 16 ? launch<T, 128, 2>(a, join, stream)
+                                                              : launch<T, 128, 4>(a, join, stream);
 }
 
 }  // namespace
@@ -456,8 +529,8 @@ int attend_token_blocks_per_sm(int head_dim) {
   return static_cast<int>(227 * 1024 / ((head_dim <= 64 ? kRingBytes<64> : kRingBytes<128>) + 2048));
 }
 
-cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, cudaStream_t stream) {
-  return dtype == PCS_DT_F16 ? by_size<__half>(a, rows, stream) : by_size<__nv_bfloat16>(a, rows, stream);
+cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream) {
+  return dtype == PCS_DT_F16 ? by_size<__half>(a, rows, join, stream) : by_size<__nv_bfloat16>(a, rows, join, stream);
 }
 
 }  // namespace pcs

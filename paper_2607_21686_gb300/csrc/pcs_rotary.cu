@@ -27,7 +27,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTokens = 8;     // tokens of a block at most
 constexpr int kPairs = 128;    // pairs of a head at most
-constexpr int kUnroll = 4;     // units in flight per thread
 
 __device__ __forceinline__ void grid_dependency() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -75,19 +74,32 @@ struct Place {
   int64_t k, v;
 };
 
-__device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t) {
+// The last of the sessions whose first token is at most t, by one warp: 32
+// probes at a time.
+__device__ __forceinline__ int session_of(const BatchDev& b, int64_t t, int lane) {
+  int lo = 0, n = b.sessions;  // it is among [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const int i = lo + lane * step;
+    const unsigned m = __ballot_sync(0xffffffffu, lane * step < n && __ldg(b.q_off + i) <= t);
+    const int k = m ? 31 - __clz(m) : 0;
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
+__device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t, int s) {
   const BatchDev& b = a.batch;
-  int s, at, m;
+  int at, m;
   if (b.q_off) {
-    int lo = 0, hi = b.sessions;  // the last session whose first token is at most t
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (__ldg(b.q_off + mid) <= t) lo = mid;
-      else hi = mid;
+    int32_t o = __ldg(b.q_off + s), end = __ldg(b.q_off + s + 1);
+    while (t >= end && s + 1 < b.sessions) {
+      ++s;
+      o = end;
+      end = __ldg(b.q_off + s + 1);
     }
-    s = lo;
-    const int32_t o = __ldg(b.q_off + s);
-    m = __ldg(b.q_off + s + 1) - o;
+    m = end - o;
     at = static_cast<int>(t - o);
     if (at < 0 || at >= m) return {-1, -1};
   } else {
@@ -120,19 +132,112 @@ __device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t) {
   return r;
 }
 
-// Units of a turned head: `turn` units of VE pairs' worth, then the elements
-// behind them; of a copied head: elements.  VE elements a unit (1: one pair or
-// one element).
+// How a block's threads share out the heads [first, first + heads) of its
+// tokens: `units` threads side by side to a head of a token, `at_once` heads.
+struct Share {
+  int32_t first, heads, units, at_once;
+  FastDiv by_units, by_heads;
+  void set(int first_, int heads_, int units_) {
+    first = first_;
+    heads = heads_;
+    units = units_;
+    at_once = units_ > kThreads ? 1 : kThreads / units_;
+    by_units.set(units_);
+    by_heads.set(heads_ > 0 ? heads_ : 1);
+  }
+};
+
+// A unit in flight: its elements (of both halves of its pairs) and where they go.
+template <typename V>
+struct Unit {
+  V x, y;
+  uint8_t* dst;
+  int pair;  // the first pair of a turned unit, -1: copied, -2: nothing
+};
+
+// Units are VE elements, or with halves (a pair's elements lie in two runs) VE
+// of each; VE 1: one pair or one element.
 template <typename T, int VE, bool IL, bool PAGED>
-__global__ void __launch_bounds__(kThreads)
-    k_rotate(const __grid_constant__ RotArgs a, int per_block, int turn, int units_turned,
-             int units_plain, FastDiv by_units, FastDiv by_turned, FastDiv by_plain) {
+__device__ __forceinline__ void load_unit(Unit<Run<T, VE>>& u, const RotArgs& a, const Place* place, int64_t t0,
+                                          int nt, const Share& sh, int turn, int r, int p) {
+  using V = Run<T, VE>;
+  u.pair = -2;
+  const int t = sh.by_heads.div(p);
+  if (t >= nt) return;
+  const int head = sh.first + p - t * sh.heads;
+  int n = 0;
+  while (head >= a.t[n].heads) ++n;
+  const RotSlot& z = a.t[n];
+  const int h = head - (n ? a.t[n - 1].heads : 0);
+  int e, w = -1;
+  if (r < turn) {
+    if (VE == 1) w = r, e = IL ? 2 * r : r;
+    else w = IL ? r * (VE / 2) : r * VE, e = r * VE;
+  } else {
+    e = (turn ? 2 * a.pairs : 0) + (r - turn) * VE;
+  }
+  const uint8_t* src = z.src + (t0 + t) * z.src_token + h * z.src_head + e * sizeof(T);
+  if (PAGED && z.role) {
+    const int64_t row = z.role == 1 ? place[t].k : place[t].v;
+    if (row < 0) return;
+    u.dst = (z.role == 1 ? a.cache.k : a.cache.v) + row + h * a.cache.head_bytes + e * sizeof(T);
+  } else {
+    u.dst = z.dst + (t0 + t) * z.dst_token + h * z.dst_head + e * sizeof(T);
+  }
+  u.x = *reinterpret_cast<const V*>(src);
+  if (w >= 0) {
+    if (!IL) u.y = *reinterpret_cast<const V*>(src + a.pairs * sizeof(T));
+    else if (VE == 1) u.y = *reinterpret_cast<const V*>(src + sizeof(T));
+    w += t * a.pairs;
+  }
+  u.pair = w;
+}
+
+template <typename T, int VE, bool IL>
+__device__ __forceinline__ void turn_unit(Unit<Run<T, VE>>& u, const RotArgs& a, const float2* cs) {
+  using V = Run<T, VE>;
+  if (u.pair == -2) return;
+  if (u.pair >= 0) {
+    if (!IL || VE == 1) {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const float2 c = cs[u.pair + i];
+        const float p = to_float(u.x.e[i]), q = to_float(u.y.e[i]);
+        u.x.e[i] = from_float<T>(p * c.x - q * c.y);
+        u.y.e[i] = from_float<T>(p * c.y + q * c.x);
+      }
+      *reinterpret_cast<V*>(u.dst + (IL ? 1 : a.pairs) * sizeof(T)) = u.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VE; i += 2) {
+        const float2 c = cs[u.pair + i / 2];
+        const int k = i + 1 < VE ? i + 1 : i;
+        const float p = to_float(u.x.e[i]), q = to_float(u.x.e[k]);
+        u.x.e[i] = from_float<T>(p * c.x - q * c.y);
+        u.x.e[k] = from_float<T>(p * c.y + q * c.x);
+      }
+    }
+  }
+  *reinterpret_cast<V*>(u.dst) = u.x;
+}
+
+template <typename T, int VE, bool IL, bool PAGED>
+__global__ void __launch_bounds__(kThreads, 4)
+    k_rotate(const __grid_constant__ RotArgs a, const __grid_constant__ Share turned, const __grid_constant__ Share plain,
+             int per_block, int turn) {
+  constexpr int kUnits = IL ? 4 : 2;  // units a thread has in flight
+  using U = Unit<Run<T, VE>>;
   __shared__ float2 cs[kTokens * kPairs];
   __shared__ Place place[kTokens];
   grid_dependency();
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * per_block;
   const int nt = static_cast<int>(a.tokens - t0 < per_block ? a.tokens - t0 : per_block);
-  for (int i = threadIdx.x; i < nt * a.pairs; i += kThreads) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (PAGED && tid >= kThreads - 32) {  // the last warp looks the tokens up
+    const int s = a.batch.q_off ? session_of(a.batch, t0, lane) : 0;
+    if (lane < nt) place[lane] = place_of(a, t0 + lane, s);
+  }
+  for (int i = tid; i < nt * a.pairs; i += kThreads) {
     const int t = i / a.pairs, p = i - t * a.pairs;
     int axis = 0;
     while (axis < a.axes - 1 && p >= a.axis_end[axis]) ++axis;
@@ -140,100 +245,34 @@ __global__ void __launch_bounds__(kThreads)
     if (a.inverse) x.y = -x.y;
     cs[i] = x;
   }
-  if (PAGED && threadIdx.x < nt) place[threadIdx.x] = place_of(a, t0 + threadIdx.x);
   __syncthreads();
-
-  constexpr bool kPairRuns = !IL;  // the halves of a pair lie in two runs
-  using V = Run<T, VE>;
-  const int turned_heads = a.plain ? a.t[a.plain - 1].heads : 0;
-  const uint32_t units_head = turned_heads * units_turned;
-  const uint32_t total = nt * by_units.d;
-  for (uint32_t u0 = threadIdx.x; u0 < total; u0 += kThreads * kUnroll) {
-    V x[kUnroll], y[kUnroll];
-    uint8_t* dst[kUnroll];
-    int what[kUnroll];  // the first pair of a turned unit, -1: copied, -2: nothing
+  auto pass = [&](const Share& sh, int tn) {
+    if (sh.heads == 0) return;
+    const int h0 = sh.by_units.div(tid), r0 = tid - h0 * sh.units;
+    const int total = nt * sh.heads;
+    if (h0 >= sh.at_once) return;
+    // (A head of more units than threads takes them in turns.)
+    for (int r = r0; r < sh.units; r += kThreads) {
+      for (int p = h0; p < total; p += kUnits * sh.at_once) {
+        U u[kUnits];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      const uint32_t u = u0 + k * kThreads;
-      what[k] = -2;
-      if (u >= total) continue;
-      const uint32_t t = by_units.div(u);
-      uint32_t r = u - t * by_units.d;
-      int head, e, w = -1;  // head of the call, first element, first pair
-      if (r < units_head) {
-        head = by_turned.div(r);
-        r -= head * units_turned;
-        if (static_cast<int>(r) < turn) {
-          if (VE == 1) w = r, e = IL ? 2 * r : r;
-          else w = IL ? r * (VE / 2) : r * VE, e = r * VE;
-        } else {
-          e = 2 * a.pairs + (r - turn) * VE;
-        }
-      } else {
-        r -= units_head;
-        const uint32_t h = by_plain.div(r);
-        head = turned_heads + h;
-        e = (r - h * units_plain) * VE;
+        for (int k = 0; k < kUnits; ++k) load_unit<T, VE, IL, PAGED>(u[k], a, place, t0, nt, sh, tn, r, p + k * sh.at_once);
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) turn_unit<T, VE, IL>(u[k], a, cs);
       }
-      int n = 0;
-      while (head >= a.t[n].heads) ++n;
-      const RotSlot& z = a.t[n];
-      const int h = head - (n ? a.t[n - 1].heads : 0);
-      const uint8_t* src = z.src + (t0 + t) * z.src_token + h * z.src_head + e * sizeof(T);
-      if (PAGED && z.role) {
-        const int64_t row = z.role == 1 ? place[t].k : place[t].v;
-        if (row < 0) continue;
-        dst[k] = (z.role == 1 ? a.cache.k : a.cache.v) + row + h * a.cache.head_bytes + e * sizeof(T);
-      } else {
-        dst[k] = z.dst + (t0 + t) * z.dst_token + h * z.dst_head + e * sizeof(T);
-      }
-      x[k] = *reinterpret_cast<const V*>(src);
-      if (w >= 0) {
-        if (kPairRuns) y[k] = *reinterpret_cast<const V*>(src + a.pairs * sizeof(T));
-        else if (VE == 1) y[k] = *reinterpret_cast<const V*>(src + sizeof(T));
-        w += t * a.pairs;
-      }
-      what[k] = w;
     }
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      if (what[k] == -2) continue;
-      if (what[k] >= 0) {
-        if (kPairRuns || VE == 1) {
-#pragma unroll
-          for (int i = 0; i < VE; ++i) {
-            const float2 c = cs[what[k] + i];
-            const float p = to_float(x[k].e[i]), q = to_float(y[k].e[i]);
-            x[k].e[i] = from_float<T>(p * c.x - q * c.y);
-            y[k].e[i] = from_float<T>(p * c.y + q * c.x);
-          }
-          *reinterpret_cast<V*>(dst[k] + (kPairRuns ? a.pairs : 1) * sizeof(T)) = y[k];
-        } else {
-#pragma unroll
-          for (int i = 0; i < VE; i += 2) {
-            const float2 c = cs[what[k] + i / 2];
-            const float p = to_float(x[k].e[i]), q = to_float(x[k].e[i + 1 < VE ? i + 1 : i]);
-            x[k].e[i] = from_float<T>(p * c.x - q * c.y);
-            x[k].e[i + 1 < VE ? i + 1 : i] = from_float<T>(p * c.y + q * c.x);
-          }
-        }
-      }
-      *reinterpret_cast<V*>(dst[k]) = x[k];
-    }
-  }
+  };
+  pass(turned, turn);
+  if (PAGED) pass(plain, 0);
 }
 
 template <typename T, int VE, bool IL, bool PAGED>
 cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
   const int turn = a.pairs == 0 ? 0 : VE == 1 ? a.pairs : IL ? 2 * a.pairs / VE : a.pairs / VE;
-  const int units_turned = turn + (a.head_dim - 2 * a.pairs) / VE;
-  const int units_plain = a.head_dim / VE;
   const int turned_heads = a.plain ? a.t[a.plain - 1].heads : 0;
-  const int plain_heads = a.t[a.n - 1].heads - turned_heads;
-  FastDiv by_units, by_turned, by_plain;
-  by_units.set(turned_heads * units_turned + plain_heads * units_plain);
-  by_turned.set(units_turned);
-  by_plain.set(units_plain);
+  Share turned, plain;
+  turned.set(0, turned_heads, turn + (a.head_dim - 2 * a.pairs) / VE);
+  plain.set(turned_heads, a.t[a.n - 1].heads - turned_heads, a.head_dim / VE);
   // Few tokens: a block each, for latency; many: up to kTokens a block, which
   // shares the setup among them while every SM still has two blocks.
   const int64_t share = a.tokens / (2 * sm_count);
@@ -248,8 +287,7 @@ cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_rotate<T, VE, IL, PAGED>, a, per_block, turn, units_turned,
-                            units_plain, by_units, by_turned, by_plain);
+  return cudaLaunchKernelEx(&cfg, k_rotate<T, VE, IL, PAGED>, a, turned, plain, per_block, turn);
 }
 
 template <typename T>
