@@ -132,149 +132,142 @@ __device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t, int s) {
   return r;
 }
 
-// How a block's threads share out the heads [first, first + heads) of its
-// tokens: `units` threads side by side to a head of a token, `at_once` heads.
+// How a block's threads share out a head: `units` side by side, `at_once` heads.
 struct Share {
-  int32_t first, heads, units, at_once;
-  FastDiv by_units, by_heads;
-  void set(int first_, int heads_, int units_) {
-    first = first_;
-    heads = heads_;
+  int32_t units, at_once;
+  FastDiv by_units;
+  void set(int units_) {
     units = units_;
     at_once = units_ > kThreads ? 1 : kThreads / units_;
     by_units.set(units_);
-    by_heads.set(heads_ > 0 ? heads_ : 1);
   }
 };
-
-// A unit in flight: its elements (of both halves of its pairs) and where they go.
-template <typename V>
-struct Unit {
-  V x, y;
-  uint8_t* dst;
-  int pair;  // the first pair of a turned unit, -1: copied, -2: nothing
+struct Shares {
+  Share turned, plain;             // heads that are turned, that are copied
+  FastDiv by_heads[kRotTensors];   // by a tensor's heads
 };
 
-// Units are VE elements, or with halves (a pair's elements lie in two runs) VE
-// of each; VE 1: one pair or one element.
-template <typename T, int VE, bool IL, bool PAGED>
-__device__ __forceinline__ void load_unit(Unit<Run<T, VE>>& u, const RotArgs& a, const Place* place, int64_t t0,
-                                          int nt, const Share& sh, int turn, int r, int p) {
-  using V = Run<T, VE>;
-  u.pair = -2;
-  const int t = sh.by_heads.div(p);
-  if (t >= nt) return;
-  const int head = sh.first + p - t * sh.heads;
-  int n = 0;
-  while (head >= a.t[n].heads) ++n;
-  const RotSlot& z = a.t[n];
-  const int h = head - (n ? a.t[n - 1].heads : 0);
-  int e, w = -1;
-  if (r < turn) {
-    if (VE == 1) w = r, e = IL ? 2 * r : r;
-    else w = IL ? r * (VE / 2) : r * VE, e = r * VE;
-  } else {
-    e = (turn ? 2 * a.pairs : 0) + (r - turn) * VE;
-  }
-  const uint8_t* src = z.src + (t0 + t) * z.src_token + h * z.src_head + e * sizeof(T);
-  if (PAGED && z.role) {
-    const int64_t row = z.role == 1 ? place[t].k : place[t].v;
-    if (row < 0) return;
-    u.dst = (z.role == 1 ? a.cache.k : a.cache.v) + row + h * a.cache.head_bytes + e * sizeof(T);
-  } else {
-    u.dst = z.dst + (t0 + t) * z.dst_token + h * z.dst_head + e * sizeof(T);
-  }
-  u.x = *reinterpret_cast<const V*>(src);
-  if (w >= 0) {
-    if (!IL) u.y = *reinterpret_cast<const V*>(src + a.pairs * sizeof(T));
-    else if (VE == 1) u.y = *reinterpret_cast<const V*>(src + sizeof(T));
-    w += t * a.pairs;
-  }
-  u.pair = w;
+__device__ __forceinline__ int64_t times(uint32_t n, int64_t stride) {
+  return static_cast<int64_t>(static_cast<uint64_t>(n) * static_cast<uint64_t>(stride));
 }
 
+// Units of VE elements, or with halves (a pair's elements lie in two runs) VE
+// of each; VE 1: one pair or one element.  Turns the pairs from `cs` on.
 template <typename T, int VE, bool IL>
-__device__ __forceinline__ void turn_unit(Unit<Run<T, VE>>& u, const RotArgs& a, const float2* cs) {
-  using V = Run<T, VE>;
-  if (u.pair == -2) return;
-  if (u.pair >= 0) {
-    if (!IL || VE == 1) {
+__device__ __forceinline__ void turn_unit(Run<T, VE>& x, Run<T, VE>& y, const float2* cs) {
+  if constexpr (VE == 1) {
+    const float2 c = cs[0];
+    const float p = to_float(x.e[0]), q = to_float(y.e[0]);
+    x.e[0] = from_float<T>(p * c.x - q * c.y);
+    y.e[0] = from_float<T>(p * c.y + q * c.x);
+  } else {
+    const float4* c4 = reinterpret_cast<const float4*>(cs);
+    constexpr int kPairsHere = IL ? VE / 2 : VE;
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const float2 c = cs[u.pair + i];
-        const float p = to_float(u.x.e[i]), q = to_float(u.y.e[i]);
-        u.x.e[i] = from_float<T>(p * c.x - q * c.y);
-        u.y.e[i] = from_float<T>(p * c.y + q * c.x);
-      }
-      *reinterpret_cast<V*>(u.dst + (IL ? 1 : a.pairs) * sizeof(T)) = u.y;
-    } else {
+    for (int i = 0; i < kPairsHere; i += 2) {
+      const float4 c = c4[i / 2];
 #pragma unroll
-      for (int i = 0; i < VE; i += 2) {
-        const float2 c = cs[u.pair + i / 2];
-        const int k = i + 1 < VE ? i + 1 : i;
-        const float p = to_float(u.x.e[i]), q = to_float(u.x.e[k]);
-        u.x.e[i] = from_float<T>(p * c.x - q * c.y);
-        u.x.e[k] = from_float<T>(p * c.y + q * c.x);
+      for (int k = 0; k < 2; ++k) {
+        const float co = k ? c.z : c.x, si = k ? c.w : c.y;
+        T& u = IL ? x.e[2 * (i + k)] : x.e[i + k];
+        T& v = IL ? x.e[2 * (i + k) + 1] : y.e[i + k];
+        const float p = to_float(u), q = to_float(v);
+        u = from_float<T>(p * co - q * si);
+        v = from_float<T>(p * si + q * co);
       }
     }
   }
-  *reinterpret_cast<V*>(u.dst) = u.x;
 }
 
 template <typename T, int VE, bool IL, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 4)
-    k_rotate(const __grid_constant__ RotArgs a, const __grid_constant__ Share turned, const __grid_constant__ Share plain,
-             int per_block, int turn) {
-  constexpr int kUnits = IL ? 4 : 2;  // units a thread has in flight
-  using U = Unit<Run<T, VE>>;
-  __shared__ float2 cs[kTokens * kPairs];
+    k_rotate(const __grid_constant__ RotArgs a, const __grid_constant__ Shares shares, int per_block, int turn) {
+  using V = Run<T, VE>;
+  constexpr int kUnits = IL && VE > 1 ? 4 : 2;  // units a thread has in flight
+  constexpr bool kTwo = !IL || VE == 1;         // a turned unit has two runs
+  __shared__ __align__(16) float2 cs[kTokens * kPairs];
   __shared__ Place place[kTokens];
   grid_dependency();
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * per_block;
   const int nt = static_cast<int>(a.tokens - t0 < per_block ? a.tokens - t0 : per_block);
   const int tid = threadIdx.x, lane = tid & 31;
-  if (PAGED && tid >= kThreads - 32) {  // the last warp looks the tokens up
+  // All tensors, or this block's.
+  const int n0 = gridDim.y > 1 ? blockIdx.y : 0, n1 = gridDim.y > 1 ? n0 + 1 : a.n;
+  if (PAGED && tid >= kThreads - 32 && a.t[n1 - 1].role) {  // the last warp looks the tokens up
     const int s = a.batch.q_off ? session_of(a.batch, t0, lane) : 0;
     if (lane < nt) place[lane] = place_of(a, t0 + lane, s);
   }
-  for (int i = tid; i < nt * a.pairs; i += kThreads) {
-    const int t = i / a.pairs, p = i - t * a.pairs;
-    int axis = 0;
-    while (axis < a.axes - 1 && p >= a.axis_end[axis]) ++axis;
-    float2 x = cos_sin(__ldg(a.pos + (t0 + t) * a.axes + axis), __ldg(a.freq + p));
-    if (a.inverse) x.y = -x.y;
-    cs[i] = x;
-  }
+  if (n0 < a.plain)
+    for (int i = tid; i < nt * a.pairs; i += kThreads) {
+      const int t = i / a.pairs, p = i - t * a.pairs;
+      int axis = 0;
+      while (axis < a.axes - 1 && p >= a.axis_end[axis]) ++axis;
+      float2 x = cos_sin(__ldg(a.pos + (t0 + t) * a.axes + axis), __ldg(a.freq + p));
+      if (a.inverse) x.y = -x.y;
+      cs[i] = x;
+    }
   __syncthreads();
-  auto pass = [&](const Share& sh, int tn) {
-    if (sh.heads == 0) return;
+  const int64_t second = (IL ? 1 : a.pairs) * static_cast<int64_t>(sizeof(T));  // from a pair's first element
+  for (int n = n0; n < n1; ++n) {
+    const RotSlot& z = a.t[n];
+    const Share& sh = n < a.plain ? shares.turned : shares.plain;
+    const int turned = n < a.plain ? turn : 0;
+    const int heads = z.heads - (n ? a.t[n - 1].heads : 0), total = nt * heads;
     const int h0 = sh.by_units.div(tid), r0 = tid - h0 * sh.units;
-    const int total = nt * sh.heads;
-    if (h0 >= sh.at_once) return;
+    if (h0 >= sh.at_once) continue;
+    const uint8_t* const src0 = z.src + t0 * z.src_token;
     // (A head of more units than threads takes them in turns.)
     for (int r = r0; r < sh.units; r += kThreads) {
-      for (int p = h0; p < total; p += kUnits * sh.at_once) {
-        U u[kUnits];
+      const bool turns = r < turned;
+      const int pair = VE == 1 ? r : IL ? r * (VE / 2) : r * VE;
+      const int e = (turns ? (VE == 1 && IL ? 2 * r : r * VE) : (turned ? 2 * a.pairs : 0) + (r - turned) * VE) *
+                    static_cast<int>(sizeof(T));
+      for (int p0 = h0; p0 < total; p0 += kUnits * sh.at_once) {
+        V x[kUnits], y[kUnits];
+        int at[kUnits];  // the token, -1: nothing to do
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) load_unit<T, VE, IL, PAGED>(u[k], a, place, t0, nt, sh, tn, r, p + k * sh.at_once);
+        for (int k = 0; k < kUnits; ++k) {
+          const uint32_t p = p0 + k * sh.at_once;
+          const uint32_t t = shares.by_heads[n].div(p), h = p - t * heads;
+          at[k] = static_cast<int>(p) < total ? static_cast<int>(t) : -1;
+          if (at[k] < 0) continue;
+          const uint8_t* src = src0 + times(t, z.src_token) + times(h, z.src_head) + e;
+          x[k] = *reinterpret_cast<const V*>(src);
+          if (kTwo && turns) y[k] = *reinterpret_cast<const V*>(src + second);
+        }
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) turn_unit<T, VE, IL>(u[k], a, cs);
+        for (int k = 0; k < kUnits; ++k) {
+          if (at[k] < 0) continue;
+          const uint32_t t = at[k], h = p0 + k * sh.at_once - t * heads;
+          uint8_t* dst;
+          if (PAGED && z.role) {
+            const int64_t row = z.role == 1 ? place[t].k : place[t].v;
+            if (row < 0) continue;
+            dst = (z.role == 1 ? a.cache.k : a.cache.v) + row + times(h, a.cache.head_bytes) + e;
+          } else {
+            dst = z.dst + (t0 + t) * z.dst_token + times(h, z.dst_head) + e;
+          }
+          if (turns) {
+            turn_unit<T, VE, IL>(x[k], y[k], cs + t * a.pairs + pair);
+            if (kTwo) *reinterpret_cast<V*>(dst + second) = y[k];
+          }
+          *reinterpret_cast<V*>(dst) = x[k];
+        }
       }
     }
-  };
-  pass(turned, turn);
-  if (PAGED) pass(plain, 0);
+  }
 }
 
 template <typename T, int VE, bool IL, bool PAGED>
 cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
   const int turn = a.pairs == 0 ? 0 : VE == 1 ? a.pairs : IL ? 2 * a.pairs / VE : a.pairs / VE;
-  const int turned_heads = a.plain ? a.t[a.plain - 1].heads : 0;
-  Share turned, plain;
-  turned.set(0, turned_heads, turn + (a.head_dim - 2 * a.pairs) / VE);
-  plain.set(turned_heads, a.t[a.n - 1].heads - turned_heads, a.head_dim / VE);
-  // Few tokens: a block each, for latency; many: up to kTokens a block, which
-  // shares the setup among them while every SM still has two blocks.
+  Shares shares;
+  shares.turned.set(turn + (a.head_dim - 2 * a.pairs) / VE);
+  shares.plain.set(a.head_dim / VE);
+  for (int n = 0; n < a.n; ++n) shares.by_heads[n].set(a.t[n].heads - (n ? a.t[n - 1].heads : 0));
+  // Few tokens: a block for each and each tensor, for latency; many: up to
+  // kTokens a block, which shares the setup among them and all tensors while
+  // every SM still has two blocks.
   const int64_t share = a.tokens / (2 * sm_count);
   const int per_block = static_cast<int>(share < 1 ? 1 : share > kTokens ? kTokens : share);
   const int64_t grid = (a.tokens + per_block - 1) / per_block;
@@ -282,12 +275,12 @@ cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.gridDim = dim3(static_cast<unsigned>(grid), share < 2 ? a.n : 1);
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_rotate<T, VE, IL, PAGED>, a, turned, plain, per_block, turn);
+  return cudaLaunchKernelEx(&cfg, k_rotate<T, VE, IL, PAGED>, a, shares, per_block, turn);
 }
 
 template <typename T>
