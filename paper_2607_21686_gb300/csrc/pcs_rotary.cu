@@ -25,7 +25,7 @@ namespace pcs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 8;     // tokens of a block at most
+constexpr int kTokens = 4;     // tokens of a block at most
 constexpr int kPairs = 128;    // pairs of a head at most
 
 __device__ __forceinline__ void grid_dependency() {
@@ -180,10 +180,13 @@ __device__ __forceinline__ void turn_unit(Run<T, VE>& x, Run<T, VE>& y, const fl
 }
 
 template <typename T, int VE, bool IL, bool PAGED>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 7)
     k_rotate(const __grid_constant__ RotArgs a, const __grid_constant__ Shares shares, int per_block, int turn) {
   using V = Run<T, VE>;
-  constexpr int kUnits = IL && VE > 1 ? 4 : 2;  // units a thread has in flight
+  // Units a thread has in flight: one, of as many threads as an SM's registers
+  // hold (49,153 tokens of 32 + 8 heads of 128: 165 us; two units of fewer
+  // threads 184 us, four 186 us, eight 286 us).
+  constexpr int kUnits = 1;
   constexpr bool kTwo = !IL || VE == 1;         // a turned unit has two runs
   __shared__ __align__(16) float2 cs[kTokens * kPairs];
   __shared__ Place place[kTokens];
