@@ -207,11 +207,8 @@ void add_tensor(RotArgs* a, const pcs_heads& x, const pcs_heads* y, int role) {
   a->n += 1;
 }
 
-// Whether heads and the parts the rotation cuts them into are whole vectors.
-bool vector_parts(const RotArgs& a, uint32_t dtype) {
-  const int v = 16 / elem_bytes(dtype);
-  return a.head_dim % v == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % v == 0;
-}
+// Whether heads are whole vectors.
+bool vector_parts(const RotArgs& a, uint32_t dtype) { return a.head_dim % (16 / elem_bytes(dtype)) == 0; }
 
 }  // namespace
 

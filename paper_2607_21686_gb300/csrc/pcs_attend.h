@@ -134,8 +134,8 @@ struct RotArgs {
   CacheDev cache;          // append only
   BatchDev batch;
 };
-// paged: some tensor goes to the cache.  vec: every address is a multiple of
-// 16 bytes, and so are a head, its turned part and (halves) its first half.
+// paged: some tensor goes to the cache.  vec: every address and a head are
+// multiples of 16 bytes.
 cudaError_t launch_rotate(const RotArgs& a, uint32_t dtype, bool paged, bool vec, int sm_count,
                           cudaStream_t stream);
 

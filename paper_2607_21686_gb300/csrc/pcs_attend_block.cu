@@ -235,7 +235,7 @@ __device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, 
   w.rows = max(w.all.m, 0) * a.group;
   w.row0 = blk * 2 * kTile;
   w.tiles = 0;
-  if (w.row0 >= w.rows || w.all.m > a.batch.max_new) return w;
+  if (w.row0 >= w.rows || !rows_there(a, w.all, false)) return w;
   const int t0 = a.by_group.div(w.row0);
   const int t1 = a.by_group.div(min(w.row0 + 2 * kTile, w.rows) - 1);
   w.view = w.all;
@@ -345,11 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int s = b % a.batch.sessions;
   const int blk = blocks - 1 - b / a.batch.sessions;  // the longest first
   const Work w = block_work(a, s, blk, sp);
-  if (w.all.m > a.batch.max_new) {
-    if (tid == 0) atomicOr(a.err, kDevErrIndex);
-    return;
-  }
-  if (w.row0 >= w.rows) return;
+  if (w.row0 >= w.rows || !rows_there(a, w.all, tid == 0)) return;
   const int nq = w.rows - w.row0 > kTile ? 2 : 1;  // row tiles
 
   const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
@@ -381,7 +377,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     special = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (w.all.first < 0) atomicOr(a.err, kDevErrIndex);
   }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_at))
@@ -843,7 +838,7 @@ __global__ void __launch_bounds__(kTile) k_attend_join(const __grid_constant__ A
   const int s = b % a.batch.sessions, blk = blocks - 1 - b / a.batch.sessions;
   const SessionView v = session_view(a, s);
   const int row = threadIdx.x, r = blk * 2 * kTile + t * kTile + row;
-  if (v.m > a.batch.max_new || r >= v.m * a.group) return;
+  if (!rows_there(a, v, false) || r >= v.m * a.group) return;
   // The parts of the blocks that the block kernel's numbering puts side by side.
   const int64_t first = static_cast<int64_t>(b) * a.splits * a.cache.heads + head;
   const int64_t step = static_cast<int64_t>(a.cache.heads) * 2 * (DP + 2) * kTile;

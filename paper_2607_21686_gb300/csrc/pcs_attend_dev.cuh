@@ -87,12 +87,22 @@ __device__ __forceinline__ void narrow(const AttendArgs& a, SessionView& v, int 
   const int32_t len = v.first + v.m;
   int32_t lo = a.window ? v.first + t0 - a.window + 1 : 0;
   if (a.cache.ring_rows) lo = max(lo, len - a.cache.ring_rows);
-  const int32_t end = max(v.first + t1, 0);
+  // (A session longer than its table sees what the table has room for.)
+  const int32_t end = min(max(v.first + t1, 0), a.cache.ring_rows ? 0x7fffffff : a.cache.slots);
   v.apart = lo > a.cache.sinks;
   v.sinks = v.apart ? min(a.cache.sinks, end) : 0;
   v.pad = (v.sinks + align - 1) & -align;
   v.lo = v.apart ? lo & -align : 0;
   v.seen = v.pad + max(end - v.lo, 0);
+}
+
+// Whether a session's rows of the call's tensors are there, and no more than
+// the call said; else an error is recorded.
+__device__ __forceinline__ bool rows_there(const AttendArgs& a, const SessionView& v, bool tell) {
+  const bool fine = v.m <= a.batch.max_new && v.q0 >= 0 && v.q0 + v.m <= a.batch.tokens;
+  if (tell && (!fine || v.first < 0 || (a.cache.ring_rows == 0 && v.first + v.m > a.cache.slots)))
+    atomicOr(a.err, kDevErrIndex);
+  return fine;
 }
 
 __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) {

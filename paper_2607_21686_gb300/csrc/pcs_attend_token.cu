@@ -103,11 +103,7 @@ __global__ void __launch_bounds__(kThreads)
   const SessionView view = session_view(a, s);
   if (view.m <= 0) return;  // the same in every part
   const int rows = view.m * a.group;
-  if (rows > kRows || view.m > a.batch.max_new) {
-    if (tid == 0) atomicOr(a.err, kDevErrIndex);
-    return;
-  }
-  if (view.first < 0 && tid == 0) atomicOr(a.err, kDevErrIndex);
+  if (!rows_there(a, view, tid == 0)) return;  // (max_new tokens' rows are at most kRows)
   const int head_dim = a.cache.head_dim;
   const uint32_t ring = smem_addr(smem) + warp * kStages * kStage;
   if (head_dim < DP) {  // chunks that no copy writes
@@ -455,7 +451,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_token_join(const __grid_con
   const int s = static_cast<int>(pair / a.cache.heads), head = static_cast<int>(pair % a.cache.heads);
   if (s >= a.batch.sessions) return;
   const SessionView view = session_view(a, s);
-  if (row >= view.m * a.group || view.m * a.group > kRows || view.m > a.batch.max_new) return;
+  if (row >= view.m * a.group || !rows_there(a, view, false)) return;
   const int64_t part_floats = static_cast<int64_t>(kRows) * (DP + 2);
   const float* part = a.part + pair * a.splits * part_floats;
   float m = -INFINITY;

@@ -152,9 +152,10 @@ __device__ __forceinline__ int64_t times(uint32_t n, int64_t stride) {
 }
 
 // Units of VE elements, or with halves (a pair's elements lie in two runs) VE
-// of each; VE 1: one pair or one element.  Turns the pairs from `cs` on.
+// of each; VE 1: one pair or one element.  Turns the pairs from `cs` on, `live`
+// of which there are (neighbours: a unit may end in elements that stay).
 template <typename T, int VE, bool IL>
-__device__ __forceinline__ void turn_unit(Run<T, VE>& x, Run<T, VE>& y, const float2* cs) {
+__device__ __forceinline__ void turn_unit(Run<T, VE>& x, Run<T, VE>& y, const float2* cs, int live) {
   if constexpr (VE == 1) {
     const float2 c = cs[0];
     const float p = to_float(x.e[0]), q = to_float(y.e[0]);
@@ -172,11 +173,47 @@ __device__ __forceinline__ void turn_unit(Run<T, VE>& x, Run<T, VE>& y, const fl
         T& u = IL ? x.e[2 * (i + k)] : x.e[i + k];
         T& v = IL ? x.e[2 * (i + k) + 1] : y.e[i + k];
         const float p = to_float(u), q = to_float(v);
+        if (IL && i + k >= live) continue;
         u = from_float<T>(p * co - q * si);
         v = from_float<T>(p * si + q * co);
       }
     }
   }
+}
+
+// A token's cosines and sines begin at a multiple of 32 bytes.
+__device__ __forceinline__ int pairs_row(const RotArgs& a) { return (a.pairs + 3) & ~3; }
+
+// A block's tokens [t0, t0 + nt) and tensors [n0, n1); their cosines and sines,
+// and the rows of the cache they go to, are in shared memory after this.
+struct BlockWork {
+  int64_t t0;
+  int nt, n0, n1;
+};
+template <bool PAGED>
+__device__ __forceinline__ BlockWork block_setup(const RotArgs& a, int per_block, float2* cs, Place* place) {
+  grid_dependency();
+  BlockWork b;
+  b.t0 = static_cast<int64_t>(blockIdx.x) * per_block;
+  b.nt = static_cast<int>(a.tokens - b.t0 < per_block ? a.tokens - b.t0 : per_block);
+  b.n0 = gridDim.y > 1 ? blockIdx.y : 0;
+  b.n1 = gridDim.y > 1 ? b.n0 + 1 : a.n;
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (PAGED && tid >= kThreads - 32 && a.t[b.n1 - 1].role) {  // the last warp looks the tokens up
+    const int s = a.batch.q_off ? session_of(a.batch, b.t0, lane) : 0;
+    if (lane < b.nt) place[lane] = place_of(a, b.t0 + lane, s);
+  }
+  if (b.n0 < a.plain)
+    for (int i = tid; i < b.nt * a.pairs; i += kThreads) {
+      const int t = i / a.pairs, p = i - t * a.pairs;
+      int axis = 0;
+      while (axis < a.axes - 1 && p >= a.axis_end[axis]) ++axis;
+      float2 x = cos_sin(__ldg(a.pos + (b.t0 + t) * a.axes + axis), __ldg(a.freq + p));
+      if (a.inverse) x.y = -x.y;
+      cs[t * pairs_row(a) + p] = x;
+    }
+  __syncthreads();
+  return b;
 }
 
 template <typename T, int VE, bool IL, bool PAGED>
@@ -188,28 +225,12 @@ __global__ void __launch_bounds__(kThreads, 7)
   // threads 184 us, four 186 us, eight 286 us).
   constexpr int kUnits = 1;
   constexpr bool kTwo = !IL || VE == 1;         // a turned unit has two runs
-  __shared__ __align__(16) float2 cs[kTokens * kPairs];
+  __shared__ __align__(32) float2 cs[kTokens * kPairs + 4];
   __shared__ Place place[kTokens];
-  grid_dependency();
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * per_block;
-  const int nt = static_cast<int>(a.tokens - t0 < per_block ? a.tokens - t0 : per_block);
-  const int tid = threadIdx.x, lane = tid & 31;
-  // All tensors, or this block's.
-  const int n0 = gridDim.y > 1 ? blockIdx.y : 0, n1 = gridDim.y > 1 ? n0 + 1 : a.n;
-  if (PAGED && tid >= kThreads - 32 && a.t[n1 - 1].role) {  // the last warp looks the tokens up
-    const int s = a.batch.q_off ? session_of(a.batch, t0, lane) : 0;
-    if (lane < nt) place[lane] = place_of(a, t0 + lane, s);
-  }
-  if (n0 < a.plain)
-    for (int i = tid; i < nt * a.pairs; i += kThreads) {
-      const int t = i / a.pairs, p = i - t * a.pairs;
-      int axis = 0;
-      while (axis < a.axes - 1 && p >= a.axis_end[axis]) ++axis;
-      float2 x = cos_sin(__ldg(a.pos + (t0 + t) * a.axes + axis), __ldg(a.freq + p));
-      if (a.inverse) x.y = -x.y;
-      cs[i] = x;
-    }
-  __syncthreads();
+  const BlockWork b = block_setup<PAGED>(a, per_block, cs, place);
+  const int64_t t0 = b.t0;
+  const int nt = b.nt, n0 = b.n0, n1 = b.n1, tid = threadIdx.x;
+  const int row = pairs_row(a);
   const int64_t second = (IL ? 1 : a.pairs) * static_cast<int64_t>(sizeof(T));  // from a pair's first element
   for (int n = n0; n < n1; ++n) {
     const RotSlot& z = a.t[n];
@@ -223,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 7)
     for (int r = r0; r < sh.units; r += kThreads) {
       const bool turns = r < turned;
       const int pair = VE == 1 ? r : IL ? r * (VE / 2) : r * VE;
-      const int e = (turns ? (VE == 1 && IL ? 2 * r : r * VE) : (turned ? 2 * a.pairs : 0) + (r - turned) * VE) *
+      const int e = (turns ? (VE == 1 && IL ? 2 * r : r * VE) : (turned ? (VE > 1 && IL ? turned * VE : 2 * a.pairs) : 0) + (r - turned) * VE) *
                     static_cast<int>(sizeof(T));
       for (int p0 = h0; p0 < total; p0 += kUnits * sh.at_once) {
         V x[kUnits], y[kUnits];
@@ -251,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 7)
             dst = z.dst + (t0 + t) * z.dst_token + times(h, z.dst_head) + e;
           }
           if (turns) {
-            turn_unit<T, VE, IL>(x[k], y[k], cs + t * a.pairs + pair);
+            turn_unit<T, VE, IL>(x[k], y[k], cs + t * row + pair, a.pairs - pair);
             if (kTwo) *reinterpret_cast<V*>(dst + second) = y[k];
           }
           *reinterpret_cast<V*>(dst) = x[k];
@@ -261,45 +282,156 @@ __global__ void __launch_bounds__(kThreads, 7)
   }
 }
 
-template <typename T, int VE, bool IL, bool PAGED>
-cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
-  const int turn = a.pairs == 0 ? 0 : VE == 1 ? a.pairs : IL ? 2 * a.pairs / VE : a.pairs / VE;
-  Shares shares;
-  shares.turned.set(turn + (a.head_dim - 2 * a.pairs) / VE);
-  shares.plain.set(a.head_dim / VE);
-  for (int n = 0; n < a.n; ++n) shares.by_heads[n].set(a.t[n].heads - (n ? a.t[n - 1].heads : 0));
-  // Few tokens: a block for each and each tensor, for latency; many: up to
-  // kTokens a block, which shares the setup among them and all tensors while
-  // every SM still has two blocks.
+// Halves of any number of pairs, in vectors of VE elements: a lane has a vector
+// of a head and takes its elements' partners, a run that begins anywhere in the
+// head, out of the two vectors that hold it (from the cache of the SM, where the
+// head's other lanes have just read them).  A head's lanes are in one warp,
+// which has read before any of it writes: a result may take its tensor's place.
+template <typename T, bool PAGED>
+__global__ void __launch_bounds__(kThreads, 5)
+    k_rotate_halves(const __grid_constant__ RotArgs a, const __grid_constant__ Shares shares, int per_block, int log_lanes) {
+  constexpr int VE = 16 / sizeof(T);
+  using V = Run<T, VE>;
+  __shared__ __align__(32) float2 cs[kTokens * kPairs + 4];
+  __shared__ Place place[kTokens];
+  const BlockWork b = block_setup<PAGED>(a, per_block, cs, place);
+  const int tid = threadIdx.x, P = a.pairs, row = pairs_row(a);
+  const int e = (tid & ((1 << log_lanes) - 1)) * VE, h0 = tid >> log_lanes, at_once = kThreads >> log_lanes;
+  const bool live = e < a.head_dim;
+  for (int n = b.n0; n < b.n1; ++n) {
+    const RotSlot& z = a.t[n];
+    const int heads = z.heads - (n ? a.t[n - 1].heads : 0), total = b.nt * heads;
+    const bool turns = n < a.plain && live && e < 2 * P;
+    // All elements in the first half, or in the second; else the vector has some
+    // of each or ends in elements that stay.
+    const bool low = e + VE <= P, high = e >= P && e + VE <= 2 * P;
+    const uint8_t* const src0 = z.src + b.t0 * z.src_token;
+    for (int p0 = 0; p0 < total; p0 += at_once) {  // the same turns for all lanes
+      const uint32_t p = p0 + h0;
+      const uint32_t t = shares.by_heads[n].div(p), h = p - t * heads;
+      bool there = live && static_cast<int>(p) < total;
+      V x, y;
+      if (there) {
+        const T* src = reinterpret_cast<const T*>(src0 + times(t, z.src_token) + times(h, z.src_head));
+        x = *reinterpret_cast<const V*>(src + e);
+        if (turns) {
+          if (low || high) {
+            const int s = low ? e + P : e - P, k = s & (VE - 1);
+            uint32_t w[8];
+            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(src + (s - k));
+            if (k) *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(src + (s - k) + VE);
+            // The 16 bytes from element k on.
+            const int words = k * static_cast<int>(sizeof(T)) / 4;
+            if (words & 2) {
+#pragma unroll
+              for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+            }
+            if (words & 1) {
+#pragma unroll
+              for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+            }
+            if (sizeof(T) == 2 && (k & 1)) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+            }
+            y = *reinterpret_cast<const V*>(w);
+          } else {
+#pragma unroll
+            for (int i = 0; i < VE; ++i)
+              y.e[i] = e + i < P ? src[e + i + P] : e + i < 2 * P ? src[e + i - P] : x.e[i];
+          }
+        }
+      }
+      __syncwarp();
+      if (!there) continue;
+      if (turns) {
+        const float2* c = cs + t * row;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          const bool first = e + i < P;
+          if (e + i >= 2 * P) continue;
+          const float2 k = c[first ? e + i : e + i - P];
+          const float own = to_float(x.e[i]), other = to_float(y.e[i]);
+          x.e[i] = from_float<T>(first ? own * k.x - other * k.y : other * k.y + own * k.x);
+        }
+      }
+      uint8_t* dst;
+      if (PAGED && z.role) {
+        const int64_t at = z.role == 1 ? place[t].k : place[t].v;
+        if (at < 0) continue;
+        dst = (z.role == 1 ? a.cache.k : a.cache.v) + at + times(h, a.cache.head_bytes);
+      } else {
+        dst = z.dst + (b.t0 + t) * z.dst_token + times(h, z.dst_head);
+      }
+      *reinterpret_cast<V*>(dst + e * sizeof(T)) = x;
+    }
+  }
+}
+
+// Few tokens: a block for each and each tensor, for latency; many: up to
+// kTokens a block, which shares the setup among them and all tensors while
+// every SM still has two blocks.
+cudaLaunchConfig_t config(const RotArgs& a, int sm_count, int* per_block, cudaLaunchAttribute* attr, cudaStream_t stream) {
   const int64_t share = a.tokens / (2 * sm_count);
-  const int per_block = static_cast<int>(share < 1 ? 1 : share > kTokens ? kTokens : share);
-  const int64_t grid = (a.tokens + per_block - 1) / per_block;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  *per_block = static_cast<int>(share < 1 ? 1 : share > kTokens ? kTokens : share);
+  attr->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr->val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid), share < 2 ? a.n : 1);
+  cfg.gridDim = dim3(static_cast<unsigned>((a.tokens + *per_block - 1) / *per_block), share < 2 ? a.n : 1);
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  return cfg;
+}
+
+template <typename T, int VE, bool IL, bool PAGED>
+cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
+  const int turn = a.pairs == 0 ? 0 : VE == 1 ? a.pairs : IL ? (2 * a.pairs + VE - 1) / VE : a.pairs / VE;
+  Shares shares;
+  shares.turned.set(VE > 1 && IL ? a.head_dim / VE : turn + (a.head_dim - 2 * a.pairs) / VE);
+  shares.plain.set(a.head_dim / VE);
+  for (int n = 0; n < a.n; ++n) shares.by_heads[n].set(a.t[n].heads - (n ? a.t[n - 1].heads : 0));
+  int per_block;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = config(a, sm_count, &per_block, &attr, stream);
   return cudaLaunchKernelEx(&cfg, k_rotate<T, VE, IL, PAGED>, a, shares, per_block, turn);
+}
+
+template <typename T, bool PAGED>
+cudaError_t launch_halves(const RotArgs& a, int sm_count, cudaStream_t stream) {
+  int log_lanes = 0;
+  while ((1 << log_lanes) * (16 / static_cast<int>(sizeof(T))) < a.head_dim) ++log_lanes;
+  Shares shares = {};
+  for (int n = 0; n < a.n; ++n) shares.by_heads[n].set(a.t[n].heads - (n ? a.t[n - 1].heads : 0));
+  int per_block;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = config(a, sm_count, &per_block, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, k_rotate_halves<T, PAGED>, a, shares, per_block, log_lanes);
 }
 
 template <typename T>
 cudaError_t by_form(const RotArgs& a, bool paged, bool vec, int sm_count, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
+  // Halves of whole vectors: a thread has both elements of its pairs.  Of other
+  // numbers of pairs a head's vectors look their partners up, as long as a warp
+  // holds the head.
+  const bool whole = a.interleaved || a.pairs % V == 0;
+  const bool look = vec && !whole && a.head_dim <= 32 * V;
+  vec = vec && whole;
   if constexpr (sizeof(T) == 2) {
     if (paged)
-      return vec ? (a.interleaved ? launch<T, V, true, true>(a, sm_count, stream)
-                                  : launch<T, V, false, true>(a, sm_count, stream))
-                 : (a.interleaved ? launch<T, 1, true, true>(a, sm_count, stream)
-                                  : launch<T, 1, false, true>(a, sm_count, stream));
+      return look ? launch_halves<T, true>(a, sm_count, stream)
+             : vec ? (a.interleaved ? launch<T, V, true, true>(a, sm_count, stream)
+                                    : launch<T, V, false, true>(a, sm_count, stream))
+                   : (a.interleaved ? launch<T, 1, true, true>(a, sm_count, stream)
+                                    : launch<T, 1, false, true>(a, sm_count, stream));
   }
-  return vec ? (a.interleaved ? launch<T, V, true, false>(a, sm_count, stream)
-                              : launch<T, V, false, false>(a, sm_count, stream))
-             : (a.interleaved ? launch<T, 1, true, false>(a, sm_count, stream)
-                              : launch<T, 1, false, false>(a, sm_count, stream));
+  return look ? launch_halves<T, false>(a, sm_count, stream)
+         : vec ? (a.interleaved ? launch<T, V, true, false>(a, sm_count, stream)
+                                : launch<T, V, false, false>(a, sm_count, stream))
+               : (a.interleaved ? launch<T, 1, true, false>(a, sm_count, stream)
+                                : launch<T, 1, false, false>(a, sm_count, stream));
 }
 
 }  // namespace

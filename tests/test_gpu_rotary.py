@@ -198,3 +198,23 @@ def test_append_reports_slots_and_positions_out_of_range(ctx, dev):
         if lens == [2]:
             k[int(p.table[0, 0]), 0:2] = p.nk[1:]
         assert torch.equal(p.dk.cpu(), k)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,pairs", [(128, (15, 24, 24)), (64, (9, 10, 10)), (80, (3, 3, 3)), (96, (13, 16, 16)),
+                                       (64, (10, 10, 10)), (8, (1, 1, 1)), (256, (41, 43, 42)), (16, (2, 3, 3))])
+def test_pairs_that_are_no_whole_vectors(ctx, dev, dtype, interleaved, dim, pairs):
+    g = torch.Generator().manual_seed(dim + sum(pairs))
+    pos, freq = positions(g, 37, 3), freqs(pairs, "cpu")
+    x = torch.randn(37, 5, dim, generator=g).clamp(-5, 5).to(dtype)
+    x[3, 2, 2 * sum(pairs):] = math.inf  # what stays does not meet a product
+    rot = pcs.Rotary(pos.to(dev), freq.to(dev), pairs, interleaved)
+    y = x.to(dev)
+    got = ctx.rotate([y], rot)[0]
+    want = kv_ref.turned(x, pos, freq, pairs, interleaved)
+    m = 2 * sum(pairs)
+    assert off_by(got[..., :m], want[..., :m], dtype) <= 0
+    assert torch.equal(got[..., m:].cpu(), x[..., m:])
+    ctx.rotate([y], rot, out=[y])
+    assert torch.equal(y, got)
