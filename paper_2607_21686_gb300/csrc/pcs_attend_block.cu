@@ -249,23 +249,24 @@ __device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, 
   return w;
 }
 
-// What the rows of a block or of a row tile see, at positions [pmin, pmax].
+// What the rows of a block or of a row tile see, at positions [pmin, pmax], in
+// tiles: they all see all of tiles [.., all_to) from all_from on, or before
+// all_first; some of them see some of tiles [.., some_to] from some_from on, or
+// before some_first; tiles [gap_from, gap_to) have places that are nobody's.
 struct RowsRange {
-  int32_t hi_min, hi_max, lo_min, lo_max, first;
-  // They all see all tokens of tile t, if those are in the cache.
-  __device__ __forceinline__ bool whole(int t) const {
-    const int e0 = t * kTile, e1 = e0 + kTile - 1;
-    return e1 <= hi_min && (e0 >= lo_max || e1 < first);
-  }
+  int32_t all_to, all_from, all_first, some_to, some_from, some_first, gap_from, gap_to;
+  // They all see all tokens of tile t that are in the cache.
+  __device__ __forceinline__ bool whole(int t) const { return t < all_to && (t >= all_from || t < all_first); }
+  __device__ __forceinline__ bool whole_and_filled(int t) const { return whole(t) && (t < gap_from || t >= gap_to); }
   // Some row sees some token of it.
-  __device__ __forceinline__ bool some(int t) const {
-    const int e0 = t * kTile, e1 = e0 + kTile - 1;
-    return e0 <= hi_max && (e1 >= lo_min || e0 < first);
-  }
+  __device__ __forceinline__ bool some(int t) const { return t <= some_to && (t >= some_from || t < some_first); }
 };
 __device__ __forceinline__ RowsRange rows_range(const AttendArgs& a, const SessionView& v, int pmin, int pmax) {
+  static_assert(kTile == 128, "shifts");
   const RowRange x = row_range(a, v, pmin), y = row_range(a, v, pmax);
-  return {x.hi, y.hi, x.lo, y.lo, x.first};
+  return {(x.hi + 1) >> 7, static_cast<int32_t>((static_cast<uint32_t>(y.lo) + 127) >> 7), x.first >> 7, y.hi >> 7, x.lo >> 7,
+          static_cast<int32_t>((static_cast<uint32_t>(x.first) + 127) >> 7), v.gap0 >> 7,
+          static_cast<int32_t>((static_cast<uint32_t>(v.gap1) + 127) >> 7)};
 }
 // Of row tile t.
 __device__ __forceinline__ RowsRange tile_range(const AttendArgs& a, const Work& w, int t) {
@@ -286,18 +287,19 @@ __device__ __forceinline__ uint32_t specials(uint32_t x) {
 struct Box {
   int32_t k, v, row;
 };
-__device__ __forceinline__ Box box_place(const AttendArgs& a, int s, int32_t p) {
+// The box at place e of a view.
+__device__ __forceinline__ Box box_place(const AttendArgs& a, int s, const SessionView& w, int32_t e) {
   const CacheDev& c = a.cache;
-  const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
+  const uint32_t slot = e < w.pad ? e : e >= w.gap0 ? c.sinks + (e - w.gap1) : w.slot + (e - w.pad);
   if (slot >= static_cast<uint32_t>(c.slots)) {
     atomicOr(a.err, kDevErrIndex);
     return {-1, -1, 0};
   }
   const uint32_t page = c.page_rows.div(slot);
-  const int64_t e = s * c.table_stride + page;
+  const int64_t at = s * c.table_stride + page;
   Box x;
-  x.k = __ldg(c.table + e);
-  x.v = __ldg((c.v_table ? c.v_table : c.table) + e);
+  x.k = __ldg(c.table + at);
+  x.v = __ldg((c.v_table ? c.v_table : c.table) + at);
   x.row = slot - page * c.page_rows.d;
   return x;
 }
@@ -410,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto look = [&](int t) {
           Box x = {-1, -1, 0};
           const int e = t * kTile + lane * rows;
-          if (lane < boxes && e < w.view.seen) x = box_place(a, s, seen_position(w.view, e));
+          if (lane < boxes && e < w.view.seen) x = box_place(a, s, w.view, e);
           return x;
         };
         Box box, next = look(w.tile0);
@@ -429,6 +431,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint32_t m = 0;
               for (int k = 0; k < 32; k += 8)
                 if (there >> ((lane * 32 + k) / rows) & 1) m |= 0xffu << k;
+              const int32_t e = (w.tile0 + i / 2) * kTile + lane * 32;
+              m &= ~(RowRange::upto(w.view.gap1 - e) & ~RowRange::upto(w.view.gap0 - e));
               valid[(i / 2) % kValid][lane] = m;
             }
             __syncwarp();
@@ -449,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = bar_wait(kv_full(buf), (i / kRing) & 1);
           ok = __all_sync(kFull, ok);
           if (!ok) break;
-          if (!range.whole(w.tile0 + i / 2)) {
+          if (!range.whole_and_filled(w.tile0 + i / 2)) {
             uint4* tile = reinterpret_cast<uint4*>(ring_ptr + buf * kBytes);
             bool any = false;
 #pragma unroll 4
@@ -468,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int g = c; g < kGroups; g += kCopyWarps)
             *reinterpret_cast<uint4*>(ring_ptr + i * kBytes + spot(g * kAtOnce + sub, chunk)) = make_uint4(0, 0, 0, 0);
       auto landed = [&](int i) {
-        if ((i & 1) && !range.whole(w.tile0 + i / 2) && mine) {
+        if ((i & 1) && !range.whole_and_filled(w.tile0 + i / 2) && mine) {
           uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
           bool any = false;
           for (int g = c; g < kGroups; g += kCopyWarps)
@@ -758,9 +762,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           // where zeros took their place.
           const RowsRange block = rows_range(a, w.view, w.pmin, w.pmax);
           for (int j = w.tile0; j < w.tile0 + w.tiles; ++j) {
-            if (block.whole(j)) continue;
+            if (block.whole_and_filled(j)) continue;
             for (int e = j * kTile; e < min((j + 1) * kTile, w.view.seen); ++e) {
-              if (!(sees.bits(e) & 1)) continue;
+              if (!(sees.bits(e) & 1) || (e >= w.view.gap0 && e < w.view.gap1)) continue;
               const RowPlace pl = row_place(a, s, seen_position(w.view, e));
               if (pl.k == kNoRow) continue;
               const uint8_t* v = row_at(a, a.cache.v + head * a.cache.head_bytes, pl.v) + d0 * 2;

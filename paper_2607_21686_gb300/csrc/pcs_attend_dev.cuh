@@ -70,30 +70,54 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
                : "memory");
 }
 
-// The new tokens of a session, and what some of them see together: the first
-// `sinks` tokens (`pad` places of which the last ones are nobody's) and the run
-// [lo, lo + seen - pad), or, not apart, one run from position 0.
+// The new tokens of a session, and the places of what some of them see together:
+// [0, pad) the first `sinks` tokens (the last places are nobody's), then from
+// position `lo` on; not apart, one run from position 0.
+// Copies of whole boxes of `align` rows need a place's distance from its slot to
+// be a multiple of align.  So the run begins at such a position, and where it
+// goes over the end of a ring (position `wrap` has slot `sinks` again) the places
+// [gap0, gap1) are nobody's.  With align 1 there is no gap (wrap: none).
 struct SessionView {
   int64_t q0;       // the first new token's row
   int32_t m;        // new tokens
   int32_t first;    // position of the first one (negative: before the session)
   int32_t sinks, pad, lo, seen;
+  int32_t slot;     // of place `pad`
+  int32_t wrap, gap0, gap1;
   bool apart;
+  __device__ __forceinline__ int32_t place(int32_t p) const { return p >= wrap ? gap1 + (p - wrap) : pad + (p - lo); }
 };
+constexpr int32_t kNever = 0x7fffffff;
 
-// Narrows a view to what new tokens [t0, t1) see; the run and the places before
-// it begin at multiples of `align`.
+// Narrows a view to what new tokens [t0, t1) see.
 __device__ __forceinline__ void narrow(const AttendArgs& a, SessionView& v, int t0, int t1, int align) {
+  const CacheDev& c = a.cache;
   const int32_t len = v.first + v.m;
   int32_t lo = a.window ? v.first + t0 - a.window + 1 : 0;
-  if (a.cache.ring_rows) lo = max(lo, len - a.cache.ring_rows);
+  if (c.ring_rows) lo = max(lo, len - c.ring_rows);
   // (A session longer than its table sees what the table has room for.)
-  const int32_t end = min(max(v.first + t1, 0), a.cache.ring_rows ? 0x7fffffff : a.cache.slots);
-  v.apart = lo > a.cache.sinks;
-  v.sinks = v.apart ? min(a.cache.sinks, end) : 0;
+  const int32_t end = min(max(v.first + t1, 0), c.ring_rows ? kNever : c.slots);
+  v.apart = lo > c.sinks;
+  v.sinks = v.apart ? min(c.sinks, end) : 0;
   v.pad = (v.sinks + align - 1) & -align;
-  v.lo = v.apart ? lo & -align : 0;
-  v.seen = v.pad + max(end - v.lo, 0);
+  v.wrap = v.gap0 = v.gap1 = kNever;
+  v.slot = 0;
+  if (!v.apart) {
+    v.lo = 0;
+  } else if (align == 1) {
+    v.lo = lo;
+  } else {
+    const int32_t slot = c.slot_of(lo);
+    v.slot = slot & -align;
+    v.lo = lo - (slot - v.slot);
+    const int32_t wrap = lo + (c.sinks + c.ring_rows - slot);
+    if (c.ring_rows && wrap < end) {
+      v.wrap = wrap;
+      v.gap0 = v.pad + (wrap - v.lo);
+      v.gap1 = ((v.gap0 + align - 1) & -align) + (c.sinks & (align - 1));
+    }
+  }
+  v.seen = end > lo ? v.place(end - 1) + 1 : v.pad;
 }
 
 // Whether a session's rows of the call's tensors are there, and no more than
@@ -120,9 +144,9 @@ __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) 
   return v;
 }
 
-// Position of the e-th token of a view.
+// Position of place e of a view, of a place that is somebody's.
 __device__ __forceinline__ int32_t seen_position(const SessionView& v, int32_t e) {
-  return e < v.pad ? e : v.lo + (e - v.pad);
+  return e < v.pad ? e : e >= v.gap1 ? v.wrap + (e - v.gap1) : v.lo + (e - v.pad);
 }
 
 // Where position p of session s is in the cache (of head 0): offsets of its
@@ -172,9 +196,9 @@ __device__ __forceinline__ RowRange row_range(const AttendArgs& a, const Session
   int32_t low = a.window ? max(p - a.window + 1, 0) : 0;
   if (a.cache.ring_rows) low = max(low, v.first + v.m - a.cache.ring_rows);
   RowRange r;
-  r.hi = p >= v.lo ? v.pad + (p - v.lo) : min(p, v.pad - 1);
+  r.hi = p >= v.lo ? v.place(p) : min(p, v.pad - 1);
   r.first = v.apart ? v.sinks : a.cache.sinks;
-  r.lo = v.apart ? v.pad + max(low - v.lo, 0) : max(low, 0);
+  r.lo = v.apart ? v.place(max(low, v.lo)) : max(low, 0);
   return r;
 }
 

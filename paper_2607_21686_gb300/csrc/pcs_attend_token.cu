@@ -438,30 +438,32 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// Joins many parts: a warp per row, its parts by lane for maximum and total,
-// then its dims.
+// Joins many parts: a block per row, whose warps take every kWarps-th part.
 template <typename T, int DP, int NT>
 __global__ void __launch_bounds__(kThreads) k_attend_token_join(const __grid_constant__ AttendArgs a) {
   constexpr int kRows = 8 * NT;
+  __shared__ float sums[kWarps][DP], tops[kWarps], totals[kWarps];
   attend_dependency();
-  const int lane = threadIdx.x & 31;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  const int64_t pair = i / kRows;
-  const int row = static_cast<int>(i % kRows);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t pair = blockIdx.x / kRows;
+  const int row = static_cast<int>(blockIdx.x % kRows);
   const int s = static_cast<int>(pair / a.cache.heads), head = static_cast<int>(pair % a.cache.heads);
-  if (s >= a.batch.sessions) return;
   const SessionView view = session_view(a, s);
   if (row >= view.m * a.group || !rows_there(a, view, false)) return;
   const int64_t part_floats = static_cast<int64_t>(kRows) * (DP + 2);
   const float* part = a.part + pair * a.splits * part_floats;
   float m = -INFINITY;
-  for (int w = lane; w < a.splits; w += 32) m = fmaxf(m, __ldcg(part + w * part_floats + kRows * DP + row));
+  for (int w = threadIdx.x; w < a.splits; w += kThreads) m = fmaxf(m, __ldcg(part + w * part_floats + kRows * DP + row));
 #pragma unroll
   for (int k = 16; k > 0; k /= 2) m = fmaxf(m, __shfl_xor_sync(kFull, m, k));
+  if (lane == 0) tops[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) m = fmaxf(m, tops[w]);
   const float at = m == -INFINITY ? 0.0f : m;
   float x[DP / 32] = {}, total = 0.0f;
 #pragma unroll 8
-  for (int w = 0; w < a.splits; ++w) {
+  for (int w = warp; w < a.splits; w += kWarps) {
     const float* p = part + w * part_floats;
     const float f = exp2_fast(__ldcg(p + kRows * DP + row) - at);
     total = fmaf(__ldcg(p + kRows * DP + kRows + row), f, total);
@@ -472,16 +474,28 @@ __global__ void __launch_bounds__(kThreads) k_attend_token_join(const __grid_con
       x[2 * k + 1] = fmaf(y.y, f, x[2 * k + 1]);
     }
   }
+#pragma unroll
+  for (int k = 0; k < DP / 64; ++k)
+    *reinterpret_cast<float2*>(&sums[warp][64 * k + 2 * lane]) = make_float2(x[2 * k], x[2 * k + 1]);
+  if (lane == 0) totals[warp] = total;
+  __syncthreads();
+  total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) total += totals[w];
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   const uint32_t tok = a.by_group.div(row);
   const int h = head * a.group + (row - static_cast<int>(tok) * a.group);
-  uint8_t* out = a.out.data + (view.q0 + tok) * a.out.token_bytes + h * a.out.head_bytes;
+  for (int d = 2 * threadIdx.x; d < a.cache.head_dim; d += 2 * kThreads) {
+    float2 y = make_float2(0.0f, 0.0f);
 #pragma unroll
-  for (int k = 0; k < DP / 64; ++k) {
-    const int d = 64 * k + 2 * lane;
-    if (d < a.cache.head_dim) *reinterpret_cast<uint32_t*>(out + d * 2) = pack2<T>(x[2 * k] * inv, x[2 * k + 1] * inv);
+    for (int w = 0; w < kWarps; ++w) {
+      y.x += sums[w][d];
+      y.y += sums[w][d + 1];
+    }
+    *reinterpret_cast<uint32_t*>(a.out.data + (view.q0 + tok) * a.out.token_bytes + h * a.out.head_bytes + d * 2) =
+        pack2<T>(y.x * inv, y.y * inv);
   }
-  if (lane == 0 && a.lse)
+  if (threadIdx.x == 0 && a.lse)
     a.lse[(view.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
         total == 0.0f ? -INFINITY : fmaf(m, 0.693147180559945309f, logf(total));
 }
@@ -502,7 +516,7 @@ cudaError_t launch(const AttendArgs& a, bool join, cudaStream_t stream) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if (join) {
-    cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(a.batch.sessions) * a.cache.heads * 8 * NT / kWarps));
+    cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(a.batch.sessions) * a.cache.heads * 8 * NT));
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, k_attend_token_join<T, DP, NT>, a);
   }

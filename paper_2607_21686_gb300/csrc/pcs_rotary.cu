@@ -413,9 +413,12 @@ cudaError_t launch_halves(const RotArgs& a, int sm_count, cudaStream_t stream) {
 template <typename T>
 cudaError_t by_form(const RotArgs& a, bool paged, bool vec, int sm_count, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
-  // Halves of whole vectors: a thread has both elements of its pairs.  Of other
-  // numbers of pairs a head's vectors look their partners up, as long as a warp
-  // holds the head.
+  // Halves of whole vectors: a thread has both elements of its pairs; so of whole
+  // half vectors, in 8-byte units.  Of other numbers of pairs a head's vectors
+  // look their partners up, as long as a warp holds the head.
+  if constexpr (sizeof(T) == 2)
+    if (vec && !a.interleaved && a.pairs % V == 4)
+      return paged ? launch<T, 4, false, true>(a, sm_count, stream) : launch<T, 4, false, false>(a, sm_count, stream);
   const bool whole = a.interleaved || a.pairs % V == 0;
   const bool look = vec && !whole && a.head_dim <= 32 * V;
   vec = vec && whole;

@@ -165,3 +165,25 @@ def test_bad_ids_and_short_sessions(ctx, dev):
     assert e.value.status == pcs.PCS_E_RANGE
     kv_ref.check_attend(p, out, lse)
     assert (out[50:80] == 0).all() and (lse[50:80] == -math.inf).all()
+
+
+@pytest.mark.parametrize("sinks,ring", [(0, 301), (0, 200), (5, 200), (16, 333), (7, 129), (130, 190), (3, 500)])
+@pytest.mark.parametrize("rows", [8, 16, 24, 64])
+def test_rings_that_wrap_anywhere(ctx, sinks, ring, rows):
+    # Lengths that put the ring's end at every place of a box and a tile.
+    lens = [ring + sinks + d for d in (-1, 0, 1, 7, 40, 100, ring // 2)]
+    new = [40, 100, 120, 33, 128, 90, 50]
+    p = kv_ref.Population(ring + rows, lens, new, 1, 1, 64, page_rows=rows, sinks=sinks, ring=ring, dtype=torch.float16)
+    check(ctx, p)
+    check(ctx, p, window=77)
+
+
+def test_junk_past_the_end_of_a_ring(ctx):
+    # Rows of the last page behind the ring, and of the page of the first tokens.
+    p = kv_ref.Population(20, [400], [60], 1, 1, 64, page_rows=16, sinks=5, ring=203)
+    out, lse = check(ctx, p)
+    for at in range(208, 16 * p.pages):
+        p.k[int(p.table[0, at // 16]), at % 16] = math.nan
+        p.v[int(p.table[0, at // 16]), at % 16] = math.inf
+    again, lse2 = attend(ctx, p)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
