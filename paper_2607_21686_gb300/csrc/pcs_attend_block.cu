@@ -33,9 +33,9 @@ constexpr int kMmaWarp = 8;
 constexpr int kCopyWarp = 9;
 constexpr int kCopyWarps = 3;
 constexpr int kThreads = 32 * (kCopyWarp + kCopyWarps);
-// Registers of a thread: the launch's 168 shared out anew, 256 x 216 + 128 x 72
+// Registers of a thread: the launch's 168 shared out anew, 256 x 224 + 128 x 56
 // = 384 x 168.
-constexpr int kSoftRegs = 216, kOtherRegs = 72;
+constexpr int kSoftRegs = 224, kOtherRegs = 56;
 constexpr int kLag = 2;                 // copies in flight behind the newest
 constexpr int kValid = 8;               // tiles whose masks are kept
 constexpr unsigned kFull = 0xffffffffu;
@@ -179,6 +179,14 @@ __device__ __forceinline__ void row_tile_sync(int t) { asm volatile("barrier.cta
 __device__ __forceinline__ void copy_sync() {
   asm volatile("barrier.cta.sync 3, %0;" ::"n"(32 * kCopyWarps) : "memory");
 }
+__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -231,7 +239,7 @@ struct Work {
 
 __device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, int sp) {
   Work w;
-  w.all = session_view(a, s);
+  w.all = session_rows(a, s);
   w.rows = max(w.all.m, 0) * a.group;
   w.row0 = blk * 2 * kTile;
   w.tiles = 0;
@@ -714,11 +722,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), at2 = pair(-at, -at);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t y[32];
+        for (int h = 0; h < 4; ++h) {
+          uint32_t y[16];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const uint32_t* z = &x[2 * h + k / 16][k % 16 * 2];
+          for (int k = 0; k < 16; ++k) {
+            const uint32_t* z = &x[h][2 * k];
             float u, v;
             unpair(fma2(pair(__uint_as_float(z[0]), __uint_as_float(z[1])), scale2, at2), u, v);
             u = exp2_fast(u);
@@ -728,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           // (Heads of 128: over the first half of the scores, all of which are
           // in registers by now.)
-          tm_store(we + h * 32, y);
+          tm_store16(we + h * 16, y);
         }
         float u, v;
         unpair(add2(sum[0], sum[1]), u, v);
@@ -840,7 +848,7 @@ __global__ void __launch_bounds__(kTile) k_attend_join(const __grid_constant__ A
   const int head = b % a.cache.heads;
   b /= a.cache.heads;
   const int s = b % a.batch.sessions, blk = blocks - 1 - b / a.batch.sessions;
-  const SessionView v = session_view(a, s);
+  const SessionView v = session_rows(a, s);
   const int row = threadIdx.x, r = blk * 2 * kTile + t * kTile + row;
   if (!rows_there(a, v, false) || r >= v.m * a.group) return;
   // The parts of the blocks that the block kernel's numbering puts side by side.

@@ -129,7 +129,8 @@ __device__ __forceinline__ bool rows_there(const AttendArgs& a, const SessionVie
   return fine;
 }
 
-__device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) {
+// A session's new tokens; what they see is left to narrow().
+__device__ __forceinline__ SessionView session_rows(const AttendArgs& a, int s) {
   SessionView v;
   const BatchDev& b = a.batch;
   if (b.q_off) {
@@ -140,6 +141,11 @@ __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) 
     v.m = b.each;
   }
   v.first = __ldg(b.lens + s) - v.m;
+  return v;
+}
+// And what they see together.
+__device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) {
+  SessionView v = session_rows(a, s);
   narrow(a, v, 0, v.m, 1);
   return v;
 }

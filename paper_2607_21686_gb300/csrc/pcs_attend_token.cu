@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_token_join(const __grid_con
   const int64_t pair = blockIdx.x / kRows;
   const int row = static_cast<int>(blockIdx.x % kRows);
   const int s = static_cast<int>(pair / a.cache.heads), head = static_cast<int>(pair % a.cache.heads);
-  const SessionView view = session_view(a, s);
+  const SessionView view = session_rows(a, s);
   if (row >= view.m * a.group || !rows_there(a, view, false)) return;
   const int64_t part_floats = static_cast<int64_t>(kRows) * (DP + 2);
   const float* part = a.part + pair * a.splits * part_floats;
