@@ -42,8 +42,17 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr float kSlack = 8.0f;          // as in the token kernel
 constexpr long long kWaitCycles = 4000000000ll;
 
+// Tiles of keys and of values in shared memory, each a ring of its own: a warp
+// that waits for values alone then sees every phase of their barriers.  (In one
+// ring of five, keys and values took turns in a buffer; a warp that waited for
+// its values while the keys before them were still on their way took the phase
+// before those for its own.)
+template <int DP>
+constexpr int kKeyTiles = DP == 64 ? 4 : 2;
 template <int DP, bool BOX>
-constexpr int kBuffers = DP == 64 ? 8 : BOX ? 5 : 4;  // tiles of keys or values in the ring
+constexpr int kValueTiles = DP == 64 ? 4 : BOX ? 3 : 2;
+template <int DP, bool BOX>
+constexpr int kBuffers = kKeyTiles<DP> + kValueTiles<DP, BOX>;
 template <int DP>
 constexpr uint32_t kTileBytes = kTile * DP * 2;
 template <int DP, bool BOX>
@@ -334,7 +343,11 @@ __device__ __forceinline__ bool take_out(uint4* at) {
 template <typename T, int DP, bool BOX>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {
-  constexpr int kRing = kBuffers<DP, BOX>;
+  constexpr int kRing = kBuffers<DP, BOX>, kKeys = kKeyTiles<DP>, kValues = kValueTiles<DP, BOX>;
+  // The buffer of fill i -- keys of tile i / 2, or its values -- and how often it
+  // has been filled before.
+  auto buf_of = [](int i) { return i & 1 ? kKeys + (i >> 1) % kValues : (i >> 1) % kKeys; };
+  auto use_of = [](int i) { return i & 1 ? (i >> 1) / kValues : (i >> 1) / kKeys; };
   constexpr uint32_t kBytes = kTileBytes<DP>;
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
@@ -368,10 +381,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto s_full = [&](int t) { return bar0 + 8 * (1 + 2 * kRing + t); };
   auto p_full = [&](int t) { return bar0 + 8 * (3 + 2 * kRing + t); };
   auto o_full = [&](int t) { return bar0 + 8 * (5 + 2 * kRing + t); };
-  // BOX: the values of tile j are looked over.  (By tiles: an odd ring has keys
-  // and values in a buffer in turn.)
+  // BOX: the values of tile j are looked over.
   auto s_read = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };  // kAhead: scores are in registers
-  auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kRing); };
+  auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kValues); };
   if (tid == 0) {
     bar_init(q_full, 32 * kSoftWarps / 2 * nq);
     for (int i = 0; i < kRing; ++i) {
@@ -425,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         Box box, next = look(w.tile0);
         for (int i = 0; i < 2 * w.tiles && ok; ++i) {
-          const int buf = i % kRing, use = i / kRing;
+          const int buf = buf_of(i), use = use_of(i);
           if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
           ok = __all_sync(kFull, ok);
           if (!ok) break;
@@ -457,8 +469,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         // The others look values over.
         for (int i = 1; i < 2 * w.tiles && ok; i += 2) {
-          const int buf = i % kRing;
-          ok = bar_wait(kv_full(buf), (i / kRing) & 1);
+          const int buf = buf_of(i);
+          ok = bar_wait(kv_full(buf), use_of(i) & 1);
           ok = __all_sync(kFull, ok);
           if (!ok) break;
           if (!range.whole_and_filled(w.tile0 + i / 2)) {
@@ -481,14 +493,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             *reinterpret_cast<uint4*>(ring_ptr + i * kBytes + spot(g * kAtOnce + sub, chunk)) = make_uint4(0, 0, 0, 0);
       auto landed = [&](int i) {
         if ((i & 1) && !range.whole_and_filled(w.tile0 + i / 2) && mine) {
-          uint8_t* tile = ring_ptr + (i % kRing) * kBytes;
+          uint8_t* tile = ring_ptr + buf_of(i) * kBytes;
           bool any = false;
           for (int g = c; g < kGroups; g += kCopyWarps)
             any |= take_out<T>(reinterpret_cast<uint4*>(tile + spot(g * kAtOnce + sub, chunk)));
           if (any) special = 1;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(kv_full(i % kRing));
+        bar_arrive(kv_full(buf_of(i)));
       };
       // Rows' places of tile t, of the call's tile w.tile0 + t.
       auto look = [&](int t) {
@@ -506,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes + chunk * 16;
       const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes + chunk * 16;
       for (int i = 0; i < 2 * w.tiles && ok; ++i) {
-        const int buf = i % kRing, use = i / kRing;
+        const int buf = buf_of(i), use = use_of(i);
         if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
         ok = __all_sync(kFull, ok);
         if ((i & 1) == 0) copy_sync();  // the tile's places are written, the ones before the last are used up
@@ -542,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t kQK = instruction<T>(kTile, false), kPV = instruction<T>(DP, true);
       const uint32_t q0 = operand(qat, 16), k0 = operand(ring, 16), v0 = operand(ring, kPanel);
       auto scores = [&](int t, int i) {  // S = Q K^T of row tile t, keys of fill i
-        const uint32_t q = q0 + t * (kBytes >> 4), k = k0 + (i % kRing) * (kBytes >> 4);
+        const uint32_t q = q0 + t * (kBytes >> 4), k = k0 + buf_of(i) * (kBytes >> 4);
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
           const uint32_t at = ((d >> 2) * kPanel + (d & 3) * 32) >> 4;
@@ -550,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       };
       auto sums = [&](int t, int i, bool add) {  // O += P V, values of fill i
-        const uint32_t v = v0 + (i % kRing) * (kBytes >> 4);
+        const uint32_t v = v0 + buf_of(i) * (kBytes >> 4);
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
           mma_ts(mem + kSums + t * DP, mem + kWeights<DP> + t * kWeightsStep<DP> + k * 8, v + k * (2048 >> 4), kPV,
@@ -584,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       };
       auto keys = [&](int j) {
-        ok = __all_sync(kFull, ok && bar_wait(kv_full(2 * j % kRing), (2 * j / kRing) & 1));
+        ok = __all_sync(kFull, ok && bar_wait(kv_full(buf_of(2 * j)), use_of(2 * j) & 1));
         fence_after();
       };
       if (ok) keys(0);
@@ -598,24 +610,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (more) keys(j + 1);
         if (kAhead<DP> && more) {
           for (int t = 0; t < row_tiles && ok; ++t) next_scores(t, j + 1);
-          mma_commit(kv_empty(ki % kRing), one);
+          mma_commit(kv_empty(buf_of(ki)), one);
         }
-        ok = ok && bar_wait(kv_full(vi % kRing), (vi / kRing) & 1);
-        if (BOX) ok = ok && bar_wait(v_fine(j), (j / kRing) & 1);
+        ok = ok && bar_wait(kv_full(buf_of(vi)), use_of(vi) & 1);
+        if (BOX) ok = ok && bar_wait(v_fine(j), (j / kValues) & 1);
         ok = __all_sync(kFull, ok);
         if (!ok) break;
         next_sums(0, j);
-        if (row_tiles == 1) mma_commit(kv_empty(vi % kRing), one);
+        if (row_tiles == 1) mma_commit(kv_empty(buf_of(vi)), one);
         if (!kAhead<DP> && more && ok) {
           next_scores(0, j + 1);
-          if (row_tiles == 1) mma_commit(kv_empty(ki % kRing), one);
+          if (row_tiles == 1) mma_commit(kv_empty(buf_of(ki)), one);
         }
         if (row_tiles == 2 && ok) {
           next_sums(1, j);
-          mma_commit(kv_empty(vi % kRing), one);
+          mma_commit(kv_empty(buf_of(vi)), one);
           if (!kAhead<DP> && more && ok) {
             next_scores(1, j + 1);
-            mma_commit(kv_empty(ki % kRing), one);
+            mma_commit(kv_empty(buf_of(ki)), one);
           }
         }
       }

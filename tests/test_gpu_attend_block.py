@@ -187,3 +187,29 @@ def test_junk_past_the_end_of_a_ring(ctx):
         p.v[int(p.table[0, at // 16]), at % 16] = math.inf
     again, lse2 = attend(ctx, p)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dim,new,page_rows", [(128, 2, 16), (128, 40, 16), (64, 40, 8), (128, 40, 13), (64, 300, 24)])
+def test_again_and_again(ctx, dev, dim, new, page_rows):
+    # Many ragged sessions whose keys and values come from far and near, over and
+    # over: every pass gives the same bits, and no wait runs out.
+    n = 48
+    g = torch.Generator().manual_seed(dim + new)
+    lens = torch.randint(new, 3000, (n,), generator=g, dtype=torch.int32)
+    pages = -(-3000 // page_rows)
+    dk, dv = (torch.randn(n * pages + 5, page_rows, 4, dim, device=dev, dtype=torch.bfloat16) for _ in range(2))
+    table = torch.randperm(n * pages + 5, generator=g)[:n * pages].reshape(n, pages).int().to(dev)
+    cache = pcs.KvCache(dk, dv, table)
+    batch = pcs.KvBatch(lens.to(dev), n * new)
+    q = torch.randn(n * new, 72 if new == 2 else 4, dim, device=dev, dtype=torch.bfloat16)
+    far = torch.empty(64 << 20, dtype=torch.int32, device=dev)
+    first = None
+    for i in range(60):
+        if i % 3 == 0:
+            far.fill_(i)  # the pools leave the cache
+        out, lse = ctx.attend(cache, batch, q, window=1000, return_lse=True)
+        if first is None:
+            first = (out, lse)
+        else:
+            assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), i
+    ctx.sync()
