@@ -325,17 +325,21 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     a.by_group.set(a.group);
 
     const int64_t rows = static_cast<int64_t>(a.batch.max_new) * a.group;
-    const bool few = rows <= kTokenRowsMax;
+    // Few rows of a key head, bound by HBM, go to the token kernel: up to 16, and
+    // up to 32 where sessions and heads alone would leave SMs without a block of
+    // the other one.  (64 sessions of 500 to 4,000 tokens, 4 key heads of 128:
+    // 8 rows 62 us, and 79 us by blocks; 16 rows 75 and 79; 32 rows 116 and 81.
+    // One session of 100,000 tokens, 32 rows: 62 and 114 us.)
+    const int64_t pairs = static_cast<int64_t>(a.batch.sessions) * cache->heads;
+    if ((st = call.begin())) return st;
+    a.err = call.errors();
+    const bool few = rows <= 16 || (rows <= kTokenRowsMax && pairs < call.sm_count());
     // Tokens that the rows of a block see at most, as far as the host knows: a
     // hint for the split, which is right for any length.
     int64_t seen = cache->ring ? static_cast<int64_t>(cache->sinks) + cache->ring : a.cache.slots;
     if (batch->max_len) seen = std::min<int64_t>(seen, batch->max_len);
     const int64_t tokens = few ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
     if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
-    const int64_t pairs = static_cast<int64_t>(a.batch.sessions) * cache->heads;
-
-    if ((st = call.begin())) return st;
-    a.err = call.errors();
     if (few) {
       const int64_t resident = static_cast<int64_t>(call.sm_count()) * attend_token_blocks_per_sm(cache->head_dim);
       const int64_t tiles = (seen + 15) / 16;

@@ -8,10 +8,15 @@
 //            A block takes a few tokens: their cosines and sines are computed
 //            once into shared memory and serve all heads of all tensors, which
 //            is what keeps the trigonometry (some 40 instructions a pair) off
-//            the critical path; then each thread moves units of 16 bytes, or
-//            of one pair where something is not aligned to 16 bytes.
-//            With a cache (PAGED) the rows of keys and values go to the slots
-//            of the tokens' positions.
+//            the critical path; then each thread moves units of 16 bytes, of 8
+//            or 4 where the pairs' halves are no whole vectors, or of one pair
+//            where something is not aligned.  With a cache (PAGED) the rows of
+//            keys and values go to the slots of the tokens' positions.
+//            49,153 tokens of 32 + 8 heads of 128 in float16: 165 us, 6.1 TB/s
+//            (91 % of the measured copy rate); 23,000 new tokens of 24 sessions,
+//            16 heads of 64: 50 us, 5.7 TB/s.  What is left is instructions (68 %
+//            of the issue slots are taken) and a block's look-ups before its
+//            first load.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -282,92 +287,6 @@ __global__ void __launch_bounds__(kThreads, 7)
   }
 }
 
-// Halves of any number of pairs, in vectors of VE elements: a lane has a vector
-// of a head and takes its elements' partners, a run that begins anywhere in the
-// head, out of the two vectors that hold it (from the cache of the SM, where the
-// head's other lanes have just read them).  A head's lanes are in one warp,
-// which has read before any of it writes: a result may take its tensor's place.
-template <typename T, bool PAGED>
-__global__ void __launch_bounds__(kThreads, 5)
-    k_rotate_halves(const __grid_constant__ RotArgs a, const __grid_constant__ Shares shares, int per_block, int log_lanes) {
-  constexpr int VE = 16 / sizeof(T);
-  using V = Run<T, VE>;
-  __shared__ __align__(32) float2 cs[kTokens * kPairs + 4];
-  __shared__ Place place[kTokens];
-  const BlockWork b = block_setup<PAGED>(a, per_block, cs, place);
-  const int tid = threadIdx.x, P = a.pairs, row = pairs_row(a);
-  const int e = (tid & ((1 << log_lanes) - 1)) * VE, h0 = tid >> log_lanes, at_once = kThreads >> log_lanes;
-  const bool live = e < a.head_dim;
-  for (int n = b.n0; n < b.n1; ++n) {
-    const RotSlot& z = a.t[n];
-    const int heads = z.heads - (n ? a.t[n - 1].heads : 0), total = b.nt * heads;
-    const bool turns = n < a.plain && live && e < 2 * P;
-    // All elements in the first half, or in the second; else the vector has some
-    // of each or ends in elements that stay.
-    const bool low = e + VE <= P, high = e >= P && e + VE <= 2 * P;
-    const uint8_t* const src0 = z.src + b.t0 * z.src_token;
-    for (int p0 = 0; p0 < total; p0 += at_once) {  // the same turns for all lanes
-      const uint32_t p = p0 + h0;
-      const uint32_t t = shares.by_heads[n].div(p), h = p - t * heads;
-      bool there = live && static_cast<int>(p) < total;
-      V x, y;
-      if (there) {
-        const T* src = reinterpret_cast<const T*>(src0 + times(t, z.src_token) + times(h, z.src_head));
-        x = *reinterpret_cast<const V*>(src + e);
-        if (turns) {
-          if (low || high) {
-            const int s = low ? e + P : e - P, k = s & (VE - 1);
-            uint32_t w[8];
-            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(src + (s - k));
-            if (k) *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(src + (s - k) + VE);
-            // The 16 bytes from element k on.
-            const int words = k * static_cast<int>(sizeof(T)) / 4;
-            if (words & 2) {
-#pragma unroll
-              for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-            }
-            if (words & 1) {
-#pragma unroll
-              for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-            }
-            if (sizeof(T) == 2 && (k & 1)) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-            }
-            y = *reinterpret_cast<const V*>(w);
-          } else {
-#pragma unroll
-            for (int i = 0; i < VE; ++i)
-              y.e[i] = e + i < P ? src[e + i + P] : e + i < 2 * P ? src[e + i - P] : x.e[i];
-          }
-        }
-      }
-      __syncwarp();
-      if (!there) continue;
-      if (turns) {
-        const float2* c = cs + t * row;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          const bool first = e + i < P;
-          if (e + i >= 2 * P) continue;
-          const float2 k = c[first ? e + i : e + i - P];
-          const float own = to_float(x.e[i]), other = to_float(y.e[i]);
-          x.e[i] = from_float<T>(first ? own * k.x - other * k.y : other * k.y + own * k.x);
-        }
-      }
-      uint8_t* dst;
-      if (PAGED && z.role) {
-        const int64_t at = z.role == 1 ? place[t].k : place[t].v;
-        if (at < 0) continue;
-        dst = (z.role == 1 ? a.cache.k : a.cache.v) + at + times(h, a.cache.head_bytes);
-      } else {
-        dst = z.dst + (b.t0 + t) * z.dst_token + times(h, z.dst_head);
-      }
-      *reinterpret_cast<V*>(dst + e * sizeof(T)) = x;
-    }
-  }
-}
-
 // Few tokens: a block for each and each tensor, for latency; many: up to
 // kTokens a block, which shares the setup among them and all tensors while
 // every SM still has two blocks.
@@ -398,43 +317,27 @@ cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, k_rotate<T, VE, IL, PAGED>, a, shares, per_block, turn);
 }
 
+// The widest units of whole vectors (neighbours: of vectors that may end in
+// elements that stay; halves: a half is a number of whole units, for a thread has
+// both elements of its pairs).  49,153 tokens of 32 + 8 heads of 128: 64 pairs, in
+// units of 16 bytes, 165 us; 60 pairs, of 8 bytes, 178 us; pair by pair 393 us.
 template <typename T, bool PAGED>
-cudaError_t launch_halves(const RotArgs& a, int sm_count, cudaStream_t stream) {
-  int log_lanes = 0;
-  while ((1 << log_lanes) * (16 / static_cast<int>(sizeof(T))) < a.head_dim) ++log_lanes;
-  Shares shares = {};
-  for (int n = 0; n < a.n; ++n) shares.by_heads[n].set(a.t[n].heads - (n ? a.t[n - 1].heads : 0));
-  int per_block;
-  cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = config(a, sm_count, &per_block, &attr, stream);
-  return cudaLaunchKernelEx(&cfg, k_rotate_halves<T, PAGED>, a, shares, per_block, log_lanes);
+cudaError_t by_unit(const RotArgs& a, bool vec, int sm_count, cudaStream_t stream) {
+  constexpr int V = 16 / sizeof(T);
+  if (a.interleaved)
+    return vec ? launch<T, V, true, PAGED>(a, sm_count, stream) : launch<T, 1, true, PAGED>(a, sm_count, stream);
+  if (vec && a.pairs % V == 0) return launch<T, V, false, PAGED>(a, sm_count, stream);
+  if constexpr (V == 8)
+    if (vec && a.pairs % 4 == 0) return launch<T, 4, false, PAGED>(a, sm_count, stream);
+  if (vec && a.pairs % 2 == 0) return launch<T, 2, false, PAGED>(a, sm_count, stream);
+  return launch<T, 1, false, PAGED>(a, sm_count, stream);
 }
 
 template <typename T>
 cudaError_t by_form(const RotArgs& a, bool paged, bool vec, int sm_count, cudaStream_t stream) {
-  constexpr int V = 16 / sizeof(T);
-  // Halves of whole vectors: a thread has both elements of its pairs; so of whole
-  // half vectors, in 8-byte units.  Of other numbers of pairs a head's vectors
-  // look their partners up, as long as a warp holds the head.
   if constexpr (sizeof(T) == 2)
-    if (vec && !a.interleaved && a.pairs % V == 4)
-      return paged ? launch<T, 4, false, true>(a, sm_count, stream) : launch<T, 4, false, false>(a, sm_count, stream);
-  const bool whole = a.interleaved || a.pairs % V == 0;
-  const bool look = vec && !whole && a.head_dim <= 32 * V;
-  vec = vec && whole;
-  if constexpr (sizeof(T) == 2) {
-    if (paged)
-      return look ? launch_halves<T, true>(a, sm_count, stream)
-             : vec ? (a.interleaved ? launch<T, V, true, true>(a, sm_count, stream)
-                                    : launch<T, V, false, true>(a, sm_count, stream))
-                   : (a.interleaved ? launch<T, 1, true, true>(a, sm_count, stream)
-                                    : launch<T, 1, false, true>(a, sm_count, stream));
-  }
-  return look ? launch_halves<T, false>(a, sm_count, stream)
-         : vec ? (a.interleaved ? launch<T, V, true, false>(a, sm_count, stream)
-                                : launch<T, V, false, false>(a, sm_count, stream))
-               : (a.interleaved ? launch<T, 1, true, false>(a, sm_count, stream)
-                                : launch<T, 1, false, false>(a, sm_count, stream));
+    if (paged) return by_unit<T, true>(a, vec, sm_count, stream);
+  return by_unit<T, false>(a, vec, sm_count, stream);
 }
 
 }  // namespace
