@@ -339,20 +339,33 @@ __device__ __forceinline__ void settle(const AttendArgs& a, Box& x) {
   }
 }
 
-// Zeros for the infinities and NaN among eight elements; whether there were any.
+// Whether some of eight elements are infinite or NaN: the lowest bit of an
+// exponent added to one of all ones carries into the sign's place.
 template <typename T>
-__device__ __forceinline__ bool take_out(uint4* at) {
-  uint4 v = *at;
+__device__ __forceinline__ bool has_specials(const uint4& v) {
+  constexpr uint32_t e = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
+  constexpr uint32_t one = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+  return ((((v.x & e) + one) | ((v.y & e) + one) | ((v.z & e) + one) | ((v.w & e) + one)) & 0x80008000u) != 0;
+}
+// Zeros for them; whether there were any.
+template <typename T>
+__device__ __forceinline__ bool take_out(uint4* at, uint4 v) {
+  if (!has_specials<T>(v)) return false;
   const uint4 m = make_uint4(specials<T>(v.x), specials<T>(v.y), specials<T>(v.z), specials<T>(v.w));
-  if (!(m.x | m.y | m.z | m.w)) return false;
   v.x &= ~m.x, v.y &= ~m.y, v.z &= ~m.z, v.w &= ~m.w;
   *at = v;
   return true;
 }
 
-template <typename T, int DP, bool BOX>
+// MAKERS: warps that send tensor copies of boxes of rows (the other copying warps
+// look values over); 0: rows are copied one by one.  Boxes of eight rows are
+// sixteen or thirty-two a tile, more than one warp can send in a tile's time: two
+// warps take keys and values (8,000-token prompt in pages of 8: 407 us by one,
+// 357 us by two; in pages of 16: 350 and 353 us).
+template <typename T, int DP, int MAKERS>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {
+  constexpr bool BOX = MAKERS > 0;
   constexpr int kRing = kBuffers<DP, BOX>, kKeys = kKeyTiles<DP>, kValues = kValueTiles<DP, BOX>;
   // The buffer of fill i -- keys of tile i / 2, or its values -- and how often it
   // has been filled before.
@@ -399,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kRing; ++i) {
       bar_init(kv_full(i), BOX ? 1 : 32 * kCopyWarps);
       bar_init(kv_empty(i), 1);
-      bar_init(v_fine(i), 32 * (kCopyWarps - 1));
+      bar_init(v_fine(i), 32 * (kCopyWarps - MAKERS));
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(s_full(t), 1);
@@ -434,8 +447,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int c = warp - kCopyWarp;
     const RowsRange range = rows_range(a, w.view, w.pmin, w.pmax);
     if constexpr (BOX) {
-      if (c == 0) {
-        // One warp fills the ring, a lane per box of rows.
+      if (c < MAKERS) {
+        // Fills the rings, a lane per box of rows.
         const uint32_t one = elected();
         const uint64_t kmap = reinterpret_cast<uint64_t>(maps.k), vmap = reinterpret_cast<uint64_t>(maps.v);
         const int rows = a.box_rows, boxes = kTile / rows;
@@ -446,18 +459,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           return x;
         };
         Box box, next = look(w.tile0);
-        for (int i = 0; i < 2 * w.tiles && ok; ++i) {
+        for (int i = c; i < 2 * w.tiles && ok; i += MAKERS) {
           const int buf = buf_of(i), use = use_of(i);
           if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
           ok = __all_sync(kFull, ok);
           if (!ok) break;
-          if ((i & 1) == 0) {
+          if (MAKERS == 2 || (i & 1) == 0) {
             box = next;
             if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
             settle(a, box);
             // A bit per token of the tile: its box is in the cache.
             const uint32_t there = __ballot_sync(kFull, lane < boxes && box.k < a.cache.n_pages);
-            if (lane < 4) {
+            if (lane < 4 && (i & 1) == 0) {
               uint32_t m = 0;
               for (int k = 0; k < 32; k += 8)
                 if (there >> ((lane * 32 + k) / rows) & 1) m |= 0xffu << k;
@@ -486,9 +499,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!range.whole_and_filled(w.tile0 + i / 2)) {
             uint4* tile = reinterpret_cast<uint4*>(ring_ptr + buf * kBytes);
             bool any = false;
-#pragma unroll 4
-            for (int k = (c - 1) * 32 + lane; k < static_cast<int>(kBytes / 16); k += 32 * (kCopyWarps - 1))
-              any |= take_out<T>(tile + k);
+            constexpr int kFlight = 8;  // vectors in flight
+            constexpr int step = 32 * (kCopyWarps - MAKERS);
+            for (int k = (c - MAKERS) * 32 + lane; k < static_cast<int>(kBytes / 16); k += kFlight * step) {
+              uint4 v[kFlight];
+#pragma unroll
+              for (int u = 0; u < kFlight; ++u) v[u] = tile[k + u * step];
+#pragma unroll
+              for (int u = 0; u < kFlight; ++u) any |= take_out<T>(tile + k + u * step, v[u]);
+            }
             if (any) special = 1;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
@@ -506,7 +525,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint8_t* tile = ring_ptr + buf_of(i) * kBytes;
           bool any = false;
           for (int g = c; g < kGroups; g += kCopyWarps)
-            any |= take_out<T>(reinterpret_cast<uint4*>(tile + spot(g * kAtOnce + sub, chunk)));
+            any |= take_out<T>(reinterpret_cast<uint4*>(tile + spot(g * kAtOnce + sub, chunk)),
+                               *reinterpret_cast<const uint4*>(tile + spot(g * kAtOnce + sub, chunk)));
           if (any) special = 1;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -919,20 +939,22 @@ cudaLaunchConfig_t config(int64_t grid, int threads, uint32_t smem, cudaLaunchAt
   return cfg;
 }
 
-template <typename T, int DP, bool BOX>
+template <typename T, int DP, int MAKERS>
 cudaError_t launch_form(const AttendArgs& a, int blocks, const TensorMaps& maps, cudaStream_t stream) {
-  auto k = k_attend_block<T, DP, BOX>;
+  auto k = k_attend_block<T, DP, MAKERS>;
+  constexpr uint32_t smem = kSmemBytes<DP, (MAKERS > 0)>;
   static SmemLimit limit;
-  if (cudaError_t e = limit.set(k, kSmemBytes<DP, BOX>)) return e;
+  if (cudaError_t e = limit.set(k, smem)) return e;
   cudaLaunchAttribute attr;
   const cudaLaunchConfig_t cfg =
-      config(static_cast<int64_t>(blocks) * a.batch.sessions * a.splits * a.cache.heads, kThreads, kSmemBytes<DP, BOX>, &attr, stream);
+      config(static_cast<int64_t>(blocks) * a.batch.sessions * a.splits * a.cache.heads, kThreads, smem, &attr, stream);
   return cudaLaunchKernelEx(&cfg, k, a, maps, blocks);
 }
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs& a, int blocks, const TensorMaps& maps, cudaStream_t stream) {
-  return a.box_rows > 0 ? launch_form<T, DP, true>(a, blocks, maps, stream)
-                        : launch_form<T, DP, false>(a, blocks, maps, stream);
+  return a.box_rows == 0   ? launch_form<T, DP, 0>(a, blocks, maps, stream)
+         : a.box_rows == 8 ? launch_form<T, DP, 2>(a, blocks, maps, stream)
+                           : launch_form<T, DP, 1>(a, blocks, maps, stream);
 }
 
 template <typename T, int DP>
