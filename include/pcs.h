@@ -14,7 +14,8 @@
  * This library implements those operations for many sessions per call, plus
  * the content fingerprint that decides must-snapshot vs derivable (Sec. 4,
  * procedure FINGERPRINT, step 1 at epsilon = 0) and the relevance-keyed
- * pruning of memory banks (Sec. 5 "The two semantic decisions"; Sec. 7.5).
+ * pruning of memory banks (Sec. 5 "The two semantic decisions"; Sec. 7.5),
+ * and the operators that a session's model runs on its paged keys and values.
  *
  * Conventions for every call
  *   - Return value: PCS_OK (0) or a negative pcs_status.  pcs_last_error()
