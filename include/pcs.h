@@ -756,8 +756,8 @@ pcs_status pcs_kv_append(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_b
  * log sum exp(scale * q.k_j) (-inf if it sees nothing), by which results over
  * several caches can be joined.  Sums are in 32 bits, weights are rounded to
  * the cache's type before they multiply values.  What is in slots that no new
- * token sees (infinities, NaN) does not matter.  q and out: 16-byte multiples
- * (else PCS_E_ALIGN).  Page ids outside the pool, slots beyond the table, more
+ * token sees (infinities, NaN) does not matter.  out may be q.  q and out:
+ * 16-byte multiples (else PCS_E_ALIGN).  Page ids outside the pool, slots beyond the table, more
  * new tokens than max_new or than lens says -> PCS_E_RANGE at the next
  * pcs_sync (unseen; sessions over max_new are skipped).
  */

@@ -15,7 +15,7 @@ using namespace pcs;
 
 namespace {
 
-// The driver's tensor map encoder; null if there is none.
+// CUDA's tensor map encoder; null if there is none.
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);

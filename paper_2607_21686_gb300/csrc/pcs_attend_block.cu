@@ -23,14 +23,15 @@
 //                 do see them take them up at the end.
 //                 A prompt of 8,000 tokens, 32 query heads over 8 of 128 in
 //                 bfloat16: 350 us, 1.50 PFLOP/s (79 % of the measured matrix
-//                 rate; by rows 867 us).  The matrix unit is busy 52 % of a
+//                 rate; 366 us where passes take turns on three sets of inputs;
+//                 by rows 867 us).  The matrix unit is busy 52 % of a
 //                 4,096-token prompt's 112 us: without the warps' work on the
 //                 scores it took 98 us, without the products 113 us, so what
 //                 bounds it is the chain of both with the hand-overs between
 //                 them, and at windows and short sessions the 6 us a block
 //                 takes to its first scores and from its last ones.
 // k_attend_join   joins the parts of rows whose tokens were split over blocks.
-#include "pcs_attend_dev.cuh"
+#include "pcs_attend_dev.h"
 
 namespace pcs {
 namespace {
@@ -383,6 +384,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   attend_dependency();
   const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
+  if (BOX && warp == kCopyWarp && lane < 2)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? maps.v : maps.k)) : "memory");
   int b = blockIdx.x;
   const int head = b % a.cache.heads;
   b /= a.cache.heads;
@@ -787,6 +790,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before();
         bar_arrive(p_full(t));
         done += 1;
+      }
+      // Whatever the copying warps took out of the values is known when they have
+      // handed over the last ones.
+      if (ok && w.tiles > 0) {
+        const int last = w.tiles - 1, i = 2 * last + 1;
+        ok = BOX ? bar_wait(v_fine(last), (last / kValues) & 1) : bar_wait(kv_full(buf_of(i)), use_of(i) & 1);
       }
       // (The sums before the last ones were done when the last scores were.)
       if (ok && done > 0) ok = bar_wait(o_full(t), (done - 1) & 1);

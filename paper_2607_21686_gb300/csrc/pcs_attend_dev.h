@@ -1,4 +1,4 @@
-// pcs_attend_dev.cuh -- device code that the attention kernels share.
+// pcs_attend_dev.h -- device code that the attention kernels share.
 #pragma once
 
 #include <cuda_bf16.h>

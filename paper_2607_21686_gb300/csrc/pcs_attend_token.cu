@@ -23,7 +23,7 @@
 //                 bfloat16: 169 us, 6.36 TB/s (95 % of the measured copy rate);
 //                 four tokens over 200,001, 8 key heads of 128: 126 us, 6.5 TB/s.
 //                 k_attend_token_join joins more parts than kTokenOwnJoin.
-#include "pcs_attend_dev.cuh"
+#include "pcs_attend_dev.h"
 
 namespace pcs {
 namespace {

@@ -441,7 +441,8 @@ def _heads(t: torch.Tensor, what: str, tokens: int) -> pcs_heads:
 
 def _like(t: torch.Tensor) -> torch.Tensor:
     """A new contiguous tensor of t's shape and type."""
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return torch.empty_like(t) if t.is_contiguous() else \
+        torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _int32(t: torch.Tensor, what: str, dim: int) -> torch.Tensor:
@@ -854,7 +855,8 @@ class Context:
                lse: torch.Tensor = None, scale: float = 0.0, window: int = 0,
                return_lse: bool = False, stream=None):
         """Attention of the new tokens' queries [tokens, q heads, head_dim] over
-        the cache; returns out, or (out, lse) if lse is given or asked for.
+        the cache; returns out (which may be q), or (out, lse) if lse is given
+        or asked for.
         lse: float32 [tokens, q heads].  scale 0: 1 / sqrt(head_dim)."""
         self._check_tables(cache, batch)
         n = batch.tokens

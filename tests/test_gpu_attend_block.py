@@ -213,3 +213,12 @@ def test_again_and_again(ctx, dev, dim, new, page_rows):
         else:
             assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), i
     ctx.sync()
+
+
+@pytest.mark.parametrize("lens,new,hq", [([70, 400], [1, 1], 2), ([5000], [2], 8), ([300, 200], [90, 40], 2), ([2500], [60], 2)])
+def test_results_in_place_of_the_queries(ctx, dev, lens, new, hq):
+    p = kv_ref.Population(21, lens, new, hq, 2, 128)
+    out, lse = check(ctx, p)
+    cache, batch, q = kv_ref.on_gpu(pcs, p)
+    ctx.attend(cache, batch, q, out=q)
+    assert torch.equal(q, out)
