@@ -22,8 +22,8 @@
 //                 the copying warps replace them by zeros, and the rows that
 //                 do see them take them up at the end.
 //                 A prompt of 8,000 tokens, 32 query heads over 8 of 128 in
-//                 bfloat16: 350 us, 1.50 PFLOP/s (79 % of the measured matrix
-//                 rate; 366 us where passes take turns on three sets of inputs;
+//                 bfloat16: 345 us, 1.52 PFLOP/s (80 % of the measured matrix
+//                 rate; 368 us where passes take turns on three sets of inputs;
 //                 by rows 867 us).  The matrix unit is busy 52 % of a
 //                 4,096-token prompt's 112 us: without the warps' work on the
 //                 scores it took 98 us, without the products 113 us, so what

@@ -20,8 +20,8 @@
 //                 generation tensor cores, which want 128 rows, have nothing to
 //                 add here.)
 //                 256 sessions over windows of 1,024 tokens, 16 heads of 64 in
-//                 bfloat16: 169 us, 6.36 TB/s (95 % of the measured copy rate);
-//                 four tokens over 200,001, 8 key heads of 128: 126 us, 6.5 TB/s.
+//                 bfloat16: 167 us, 6.4 TB/s (96 % of the measured copy rate);
+//                 four tokens over 200,001, 8 key heads of 128: 123 us, 6.7 TB/s.
 //                 k_attend_token_join joins more parts than kTokenOwnJoin.
 #include "pcs_attend_dev.h"
 
