@@ -25,11 +25,12 @@
 //                 bfloat16: 345 us, 1.52 PFLOP/s (80 % of the measured matrix
 //                 rate; 368 us where passes take turns on three sets of inputs;
 //                 by rows 867 us).  The matrix unit is busy 52 % of a
-//                 4,096-token prompt's 112 us: without the warps' work on the
-//                 scores it took 98 us, without the products 113 us, so what
-//                 bounds it is the chain of both with the hand-overs between
-//                 them, and at windows and short sessions the 6 us a block
-//                 takes to its first scores and from its last ones.
+//                 4,096-token prompt's 112 us.  When that took 129 us, leaving
+//                 out the warps' work on the scores saved 31 us, the products
+//                 15 us and the exponentials 5 us: what bounds it is the chain
+//                 of both with the hand-overs between them, and at windows and
+//                 short sessions the 6 us a block takes to its first scores and
+//                 from its last ones.
 // k_attend_join   joins the parts of rows whose tokens were split over blocks.
 #include "pcs_attend_dev.h"
 
