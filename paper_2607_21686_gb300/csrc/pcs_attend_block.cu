@@ -278,25 +278,6 @@ __device__ __forceinline__ Work block_work(const AttendArgs& a, int s, int blk, 
   return w;
 }
 
-// What the rows of a block or of a row tile see, at positions [pmin, pmax], in
-// tiles: they all see all of tiles [.., all_to) from all_from on, or before
-// all_first; some of them see some of tiles [.., some_to] from some_from on, or
-// before some_first; tiles [gap_from, gap_to) have places that are nobody's.
-struct RowsRange {
-  int32_t all_to, all_from, all_first, some_to, some_from, some_first, gap_from, gap_to;
-  // They all see all tokens of tile t that are in the cache.
-  __device__ __forceinline__ bool whole(int t) const { return t < all_to && (t >= all_from || t < all_first); }
-  __device__ __forceinline__ bool whole_and_filled(int t) const { return whole(t) && (t < gap_from || t >= gap_to); }
-  // Some row sees some token of it.
-  __device__ __forceinline__ bool some(int t) const { return t <= some_to && (t >= some_from || t < some_first); }
-};
-__device__ __forceinline__ RowsRange rows_range(const AttendArgs& a, const SessionView& v, int pmin, int pmax) {
-  static_assert(kTile == 128, "shifts");
-  const RowRange x = row_range(a, v, pmin), y = row_range(a, v, pmax);
-  return {(x.hi + 1) >> 7, static_cast<int32_t>((static_cast<uint32_t>(y.lo) + 127) >> 7), x.first >> 7, y.hi >> 7, x.lo >> 7,
-          static_cast<int32_t>((static_cast<uint32_t>(x.first) + 127) >> 7), v.gap0 >> 7,
-          static_cast<int32_t>((static_cast<uint32_t>(v.gap1) + 127) >> 7)};
-}
 // Of row tile t.
 __device__ __forceinline__ RowsRange tile_range(const AttendArgs& a, const Work& w, int t) {
   const int r0 = w.row0 + t * kTile, r1 = min(r0 + kTile, w.rows) - 1;
@@ -319,7 +300,7 @@ struct Box {
 // The box at place e of a view.
 __device__ __forceinline__ Box box_place(const AttendArgs& a, int s, const SessionView& w, int32_t e) {
   const CacheDev& c = a.cache;
-  const uint32_t slot = e < w.pad ? e : e >= w.gap0 ? c.sinks + (e - w.gap1) : w.slot + (e - w.pad);
+  const uint32_t slot = box_slot(a, w, e);
   if (slot >= static_cast<uint32_t>(c.slots)) {
     atomicOr(a.err, kDevErrIndex);
     return {-1, -1, 0};

@@ -11,6 +11,7 @@
 #include <cstdint>
 
 #include "pcs_attend.h"
+#include "pcs_attend_view.h"
 #include "pcs_internal.h"
 
 namespace pcs {
@@ -70,56 +71,6 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
                : "memory");
 }
 
-// The new tokens of a session, and the places of what some of them see together:
-// [0, pad) the first `sinks` tokens (the last places are nobody's), then from
-// position `lo` on; not apart, one run from position 0.
-// Copies of whole boxes of `align` rows need a place's distance from its slot to
-// be a multiple of align.  So the run begins at such a position, and where it
-// goes over the end of a ring (position `wrap` has slot `sinks` again) the places
-// [gap0, gap1) are nobody's.  With align 1 there is no gap (wrap: none).
-struct SessionView {
-  int64_t q0;       // the first new token's row
-  int32_t m;        // new tokens
-  int32_t first;    // position of the first one (negative: before the session)
-  int32_t sinks, pad, lo, seen;
-  int32_t slot;     // of place `pad`
-  int32_t wrap, gap0, gap1;
-  bool apart;
-  __device__ __forceinline__ int32_t place(int32_t p) const { return p >= wrap ? gap1 + (p - wrap) : pad + (p - lo); }
-};
-constexpr int32_t kNever = 0x7fffffff;
-
-// Narrows a view to what new tokens [t0, t1) see.
-__device__ __forceinline__ void narrow(const AttendArgs& a, SessionView& v, int t0, int t1, int align) {
-  const CacheDev& c = a.cache;
-  const int32_t len = v.first + v.m;
-  int32_t lo = a.window ? v.first + t0 - a.window + 1 : 0;
-  if (c.ring_rows) lo = max(lo, len - c.ring_rows);
-  // (A session longer than its table sees what the table has room for.)
-  const int32_t end = min(max(v.first + t1, 0), c.ring_rows ? kNever : c.slots);
-  v.apart = lo > c.sinks;
-  v.sinks = v.apart ? min(c.sinks, end) : 0;
-  v.pad = (v.sinks + align - 1) & -align;
-  v.wrap = v.gap0 = v.gap1 = kNever;
-  v.slot = 0;
-  if (!v.apart) {
-    v.lo = 0;
-  } else if (align == 1) {
-    v.lo = lo;
-  } else {
-    const int32_t slot = c.slot_of(lo);
-    v.slot = slot & -align;
-    v.lo = lo - (slot - v.slot);
-    const int32_t wrap = lo + (c.sinks + c.ring_rows - slot);
-    if (c.ring_rows && wrap < end) {
-      v.wrap = wrap;
-      v.gap0 = v.pad + (wrap - v.lo);
-      v.gap1 = ((v.gap0 + align - 1) & -align) + (c.sinks & (align - 1));
-    }
-  }
-  v.seen = end > lo ? v.place(end - 1) + 1 : v.pad;
-}
-
 // Whether a session's rows of the call's tensors are there, and no more than
 // the call said; else an error is recorded.
 __device__ __forceinline__ bool rows_there(const AttendArgs& a, const SessionView& v, bool tell) {
@@ -148,11 +99,6 @@ __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) 
   SessionView v = session_rows(a, s);
   narrow(a, v, 0, v.m, 1);
   return v;
-}
-
-// Position of place e of a view, of a place that is somebody's.
-__device__ __forceinline__ int32_t seen_position(const SessionView& v, int32_t e) {
-  return e < v.pad ? e : e >= v.gap1 ? v.wrap + (e - v.gap1) : v.lo + (e - v.pad);
 }
 
 // Where position p of session s is in the cache (of head 0): offsets of its
@@ -184,28 +130,6 @@ __device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_
 }
 __device__ __forceinline__ const uint8_t* row_at(const AttendArgs& a, const uint8_t* base, uint32_t off) {
   return base + static_cast<uint64_t>(off) * a.cache.unit;
-}
-
-// What a row at position p sees of a view's tokens: e with e <= hi and (e <
-// first or e >= lo).
-struct RowRange {
-  int32_t hi, lo, first;
-  // The tokens [b, b + 32) it sees, as bits.
-  __device__ __forceinline__ uint32_t bits(int32_t b) const {
-    return upto(hi + 1 - b) & (upto(first - b) | ~upto(lo - b));
-  }
-  static __device__ __forceinline__ uint32_t upto(int32_t n) {
-    return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1;
-  }
-};
-__device__ __forceinline__ RowRange row_range(const AttendArgs& a, const SessionView& v, int32_t p) {
-  int32_t low = a.window ? max(p - a.window + 1, 0) : 0;
-  if (a.cache.ring_rows) low = max(low, v.first + v.m - a.cache.ring_rows);
-  RowRange r;
-  r.hi = p >= v.lo ? v.place(p) : min(p, v.pad - 1);
-  r.first = v.apart ? v.sinks : a.cache.sinks;
-  r.lo = v.apart ? v.place(max(low, v.lo)) : max(low, 0);
-  return r;
 }
 
 }  // namespace pcs
