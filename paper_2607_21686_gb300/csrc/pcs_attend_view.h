@@ -88,7 +88,9 @@ __host__ __device__ __forceinline__ RowRange row_range(const AttendArgs& a, cons
   int32_t low = a.window ? larger(p - a.window + 1, 0) : 0;
   if (a.cache.ring_rows) low = larger(low, v.first + v.m - a.cache.ring_rows);
   RowRange r;
-  r.hi = p >= v.lo ? v.place(p) : smaller(p, v.pad - 1);
+  // (A run of boxes may begin below `sinks`: a row of a first token sees no
+  // further than itself all the same.)
+  r.hi = p >= v.lo && !(v.apart && p < v.sinks) ? v.place(p) : smaller(p, v.pad - 1);
   r.first = v.apart ? v.sinks : a.cache.sinks;
   r.lo = v.apart ? v.place(larger(low, v.lo)) : larger(low, 0);
   return r;

@@ -1,0 +1,28 @@
+"""GPU: attention of blocks of new tokens that lap the ring they are written to
+(more new tokens than it has slots), with first tokens that stay, against the
+definition in 64 bits."""
+import pytest
+import torch
+
+import kv_ref
+from paper_2607_21686_gb300 import pcs
+from test_gpu_attend import TYPES, check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, TYPES[0]), (128, TYPES[1])])
+@pytest.mark.parametrize("sinks,ring,rows", [(4, 64, 16), (16, 203, 8), (64, 128, 128), (100, 64, 16), (130, 150, 32),
+                                             (5, 90, 17)])
+def test_prompts_that_lap_their_ring(ctx, dim, dtype, sinks, ring, rows):
+    # Lengths a little over sinks + ring: the run behind the first tokens begins
+    # in a box that it shares with them.
+    lens = [sinks + ring + d for d in (1, 7, rows, rows + 1)]
+    p = kv_ref.Population(sinks + rows, lens, lens, 2, 1, dim, page_rows=rows, sinks=sinks, ring=ring, dtype=dtype)
+    check(ctx, p)
+    check(ctx, p, window=50)
+
+
+def test_a_prompt_of_a_wide_page(ctx):
+    p = kv_ref.Population(1, [700], [700], 1, 1, 64, page_rows=128, sinks=4, ring=600)
+    check(ctx, p)
