@@ -59,7 +59,9 @@ __host__ __device__ __forceinline__ void narrow(const AttendArgs& a, SessionView
       v.gap1 = ((v.gap0 + align - 1) & -align) + (c.sinks & (align - 1));
     }
   }
-  v.seen = end > lo ? v.place(end - 1) + 1 : v.pad;
+  // (Rows that a ring has left behind see first tokens alone; those of one run
+  // are places of it.)
+  v.seen = end > (v.apart ? lo : 0) ? v.place(end - 1) + 1 : v.pad;
 }
 
 // Position of place e of a view, of a place that is somebody's.

@@ -26,3 +26,12 @@ def test_prompts_that_lap_their_ring(ctx, dim, dtype, sinks, ring, rows):
 def test_a_prompt_of_a_wide_page(ctx):
     p = kv_ref.Population(1, [700], [700], 1, 1, 64, page_rows=128, sinks=4, ring=600)
     check(ctx, p)
+
+
+@pytest.mark.parametrize("dim,rows", [(64, 16), (128, 8), (128, 13)])
+def test_blocks_of_first_tokens_alone(ctx, dim, rows):
+    # Blocks of rows that see nothing of the ring, which begins behind them.
+    p = kv_ref.Population(dim + rows, [600, 570], [600, 490], 1, 1, dim, page_rows=rows, sinks=300, ring=300)
+    check(ctx, p)
+    p = kv_ref.Population(rows, [24, 20], [24, 9], 64, 1, dim, page_rows=rows, sinks=8, ring=16)
+    check(ctx, p)

@@ -39,3 +39,18 @@ def test_first_tokens_of_a_block_that_laps_its_ring(checker, sinks, ring, box, g
         n = sinks + ring + beyond
         run(checker, sinks, ring, 0, n, n, box, group, 0)
         run(checker, sinks, ring, 40, n, n - 1, box, group, 1)
+
+
+@pytest.mark.parametrize("sinks,ring,n,new,box,group", [(300, 300, 600, 600, 16, 1), (8, 16, 24, 24, 8, 64),
+                                                        (588, 71, 579, 474, 1, 1), (700, 40, 740, 740, 128, 1),
+                                                        (300, 290, 588, 588, 1, 2), (40, 20, 60, 60, 8, 40)])
+def test_a_block_of_rows_at_first_positions_alone(checker, sinks, ring, n, new, box, group):
+    # The ring's last positions begin at or below `sinks`, and behind the block.
+    run(checker, sinks, ring, 0, n, new, box, group, 0)
+    run(checker, sinks, ring, 77, n, new, box, group, 1)
+
+
+@pytest.mark.parametrize("kind", [0, 1])
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_what_rows_see(checker, seed, kind):
+    run(checker, seed, 1500, kind)
