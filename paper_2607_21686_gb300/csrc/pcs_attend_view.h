@@ -52,10 +52,11 @@ __host__ __device__ __forceinline__ void narrow(const AttendArgs& a, SessionView
     const int32_t slot = c.slot_of(lo);
     v.slot = slot & -align;
     v.lo = lo - (slot - v.slot);
-    const int32_t wrap = lo + (c.sinks + c.ring_rows - slot);
-    if (c.ring_rows && wrap < end) {
-      v.wrap = wrap;
-      v.gap0 = v.pad + (wrap - v.lo);
+    // (Differences, not positions: those may end at 2^31 - 1.)
+    const int32_t left = c.sinks + c.ring_rows - slot;
+    if (c.ring_rows && left < end - lo) {
+      v.wrap = lo + left;
+      v.gap0 = v.pad + (v.wrap - v.lo);
       v.gap1 = ((v.gap0 + align - 1) & -align) + (c.sinks & (align - 1));
     }
   }

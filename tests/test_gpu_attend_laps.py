@@ -35,3 +35,27 @@ def test_blocks_of_first_tokens_alone(ctx, dim, rows):
     check(ctx, p)
     p = kv_ref.Population(rows, [24, 20], [24, 9], 64, 1, dim, page_rows=rows, sinks=8, ring=16)
     check(ctx, p)
+
+
+class Far(kv_ref.Population):
+    """Sessions too long to be walked from their first token."""
+
+    def seen(self, s, p, window):
+        n = self.lens[s]
+        low = max(n - self.ring, p - window + 1 if window else 0)
+        assert low >= self.sinks
+        out = []
+        for j in list(range(self.sinks)) + list(range(low, p + 1)):
+            at = kv_ref.slot_of(j, self.sinks, self.ring)
+            page = int(self.table[s, at // self.rows])
+            out.append((j, page, page, at % self.rows))
+        return out
+
+
+@pytest.mark.parametrize("new", [2, 150])
+@pytest.mark.parametrize("rows", [16, 13])
+def test_sessions_of_two_billion_tokens(ctx, new, rows):
+    lens = [2 ** 31 - 1, 2 ** 31 - 60, 2 ** 31 - 301]
+    p = Far(new + rows, lens, [new] * 3, 2, 1, 64, page_rows=rows, sinks=9, ring=260)
+    check(ctx, p)
+    check(ctx, p, window=77)

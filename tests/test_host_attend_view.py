@@ -54,3 +54,9 @@ def test_a_block_of_rows_at_first_positions_alone(checker, sinks, ring, n, new, 
 @pytest.mark.parametrize("seed", [1, 2, 3])
 def test_what_rows_see(checker, seed, kind):
     run(checker, seed, 1500, kind)
+
+
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_sessions_of_two_billion_tokens(checker, seed):
+    # The next lap of the ring would begin beyond 2^31.
+    run(checker, seed, 1500, 2)
