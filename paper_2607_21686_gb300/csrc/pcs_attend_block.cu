@@ -33,6 +33,7 @@
 //                 from its last ones.
 // k_attend_join   joins the parts of rows whose tokens were split over blocks.
 #include "pcs_attend_dev.h"
+#include "pcs_attend_rounds.h"
 
 namespace pcs {
 namespace {
@@ -197,8 +198,16 @@ __device__ __forceinline__ void tm_store(uint32_t at, const uint32_t (&r)[32]) {
 }
 // Barriers of the threads of a row tile, and of the copying warps.
 __device__ __forceinline__ void row_tile_sync(int t) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + t) : "memory"); }
-__device__ __forceinline__ void copy_sync() {
-  asm volatile("barrier.cta.sync 3, %0;" ::"n"(32 * kCopyWarps) : "memory");
+// The copying warps meet; whether all of them are fine.
+__device__ __forceinline__ bool copy_sync(bool fine) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.and.pred q, 3, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(fine ? 1u : 0u), "n"(32 * kCopyWarps)
+      : "memory");
+  return all != 0;
 }
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile(
@@ -532,26 +541,29 @@ __global__ void __launch_bounds__(kThreads, 1)
       look(0);
       const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes + chunk * 16;
       const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes + chunk * 16;
-      for (int i = 0; i < 2 * w.tiles && ok; ++i) {
-        const int buf = buf_of(i), use = use_of(i);
-        if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
-        ok = __all_sync(kFull, ok);
-        if ((i & 1) == 0) copy_sync();  // the tile's places are written, the ones before the last are used up
-        if (!ok) continue;
-        const uint8_t* base = i & 1 ? vbase : kbase;
-        const uint32_t* place = places[(i / 2) & 1][i & 1];
-        const uint32_t tile = ring + buf * kBytes;
+      ok = in_rounds(
+          2 * w.tiles,
+          [&](int i) {
+            const int use = use_of(i);
+            return __all_sync(kFull, use == 0 || bar_wait(kv_empty(buf_of(i)), (use - 1) & 1)) != 0;
+          },
+          // The tile's places are written, the ones before the last are used up.
+          [&](bool fine) { return copy_sync(fine); },
+          [&](int i) {
+            const uint8_t* base = i & 1 ? vbase : kbase;
+            const uint32_t* place = places[(i / 2) & 1][i & 1];
+            const uint32_t tile = ring + buf_of(i) * kBytes;
 #pragma unroll 4
-        for (int g = c; g < kGroups; g += kCopyWarps) {
-          const uint32_t o = place[g * kAtOnce + sub];
-          const bool in = o != kNoRow;
-          if (mine) copy16(tile + spot(g * kAtOnce + sub, chunk), row_at(a, base, in ? o : 0), in);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        if ((i & 1) == 0 && i / 2 + 1 < w.tiles) look(i / 2 + 1);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-        if (i >= kLag) landed(i - kLag);
-      }
+            for (int g = c; g < kGroups; g += kCopyWarps) {
+              const uint32_t o = place[g * kAtOnce + sub];
+              const bool in = o != kNoRow;
+              if (mine) copy16(tile + spot(g * kAtOnce + sub, chunk), row_at(a, base, in ? o : 0), in);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if ((i & 1) == 0 && i / 2 + 1 < w.tiles) look(i / 2 + 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+            if (i >= kLag) landed(i - kLag);
+          });
       asm volatile("cp.async.wait_all;" ::: "memory");
       if (ok)
         for (int i = max(0, 2 * w.tiles - kLag); i < 2 * w.tiles; ++i) landed(i);
