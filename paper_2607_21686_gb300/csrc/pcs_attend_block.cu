@@ -198,16 +198,8 @@ __device__ __forceinline__ void tm_store(uint32_t at, const uint32_t (&r)[32]) {
 }
 // Barriers of the threads of a row tile, and of the copying warps.
 __device__ __forceinline__ void row_tile_sync(int t) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + t) : "memory"); }
-// The copying warps meet; whether all of them are fine.
-__device__ __forceinline__ bool copy_sync(bool fine) {
-  uint32_t all;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.and.pred q, 3, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(all)
-      : "r"(fine ? 1u : 0u), "n"(32 * kCopyWarps)
-      : "memory");
-  return all != 0;
+__device__ __forceinline__ void copy_sync() {
+  asm volatile("barrier.cta.sync 3, %0;" ::"n"(32 * kCopyWarps) : "memory");
 }
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile(
@@ -548,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             return __all_sync(kFull, use == 0 || bar_wait(kv_empty(buf_of(i)), (use - 1) & 1)) != 0;
           },
           // The tile's places are written, the ones before the last are used up.
-          [&](bool fine) { return copy_sync(fine); },
+          [&] { copy_sync(); },
           [&](int i) {
             const uint8_t* base = i & 1 ? vbase : kbase;
             const uint32_t* place = places[(i / 2) & 1][i & 1];

@@ -11,17 +11,15 @@
 namespace pcs {
 
 // Fills 0 .. n - 1, two a round.  Every warp waits for a fill's place (`wait`, with
-// a limit; false: it ran out), and all meet at the beginning of each round:
-// `meet` gives every one of them the same answer, whether all of them are fine.
-// So they leave at the same meeting, or after the last one: a warp whose wait ran
-// out inside a round fills no more and goes to the next meeting, where nobody
-// waits for it in vain.  Whether all fills were made.
+// a limit; false: it ran out), and all meet at the beginning of each round.  A warp
+// whose wait ran out fills and waits no more, but comes to every meeting, so that
+// nobody waits for it in vain.  Whether all fills were made.
 template <typename Wait, typename Meet, typename Fill>
 PCS_ROUNDS bool in_rounds(int n, Wait&& wait, Meet&& meet, Fill&& fill) {
   bool ok = true;
   for (int i = 0; i < n; ++i) {
     ok = ok && wait(i);
-    if ((i & 1) == 0 && !meet(ok)) return false;
+    if ((i & 1) == 0) meet();
     if (ok) fill(i);
   }
   return ok;

@@ -2,6 +2,7 @@
 // (csrc/pcs_attend_rounds.h) with a thread per warp: whichever warp's wait runs
 // out, and at whichever fill, all of them leave, and none is left waiting at a
 // meeting.  Prints "ok" or the first failure.
+#include <atomic>
 #include <chrono>
 #include <condition_variable>
 #include <cstdio>
@@ -19,47 +20,44 @@ constexpr int kWarps = 3;
 // left alone is found out.
 class Meeting {
  public:
-  // 1: all were fine, 0: not all, -1: the others did not come.
-  int meet(bool fine) {
+  // Whether the others came.
+  bool meet() {
     std::unique_lock<std::mutex> l(mu_);
-    if (alone_) return -1;
-    all_ = (here_ == 0 || all_) && fine;
+    if (alone_) return false;
     if (++here_ == kWarps) {
       here_ = 0;
-      answer_ = all_;
       ++round_;
       cv_.notify_all();
-      return answer_;
+      return true;
     }
     const int round = round_;
     if (!cv_.wait_for(l, std::chrono::milliseconds(500), [&] { return round_ != round || alone_; }) || alone_) {
       alone_ = true;
       cv_.notify_all();
-      return -1;
+      return false;
     }
-    return answer_;
+    return true;
   }
 
  private:
   std::mutex mu_;
   std::condition_variable cv_;
   int here_ = 0, round_ = 0;
-  bool all_ = true, answer_ = true, alone_ = false;
+  bool alone_ = false;
 };
 
 bool run(int n, int bad_warp, int bad_fill) {
   Meeting meeting;
-  bool left_alone = false, ok[kWarps] = {};
+  std::atomic<bool> left_alone{false};
+  bool ok[kWarps] = {};
   int filled[kWarps] = {};
   std::vector<std::thread> warps;
   for (int w = 0; w < kWarps; ++w)
     warps.emplace_back([&, w] {
       ok[w] = pcs::in_rounds(
           n, [&](int i) { return !(w == bad_warp && i == bad_fill); },
-          [&](bool fine) {
-            const int r = meeting.meet(fine);
-            if (r < 0) left_alone = true;
-            return r == 1;
+          [&] {
+            if (!meeting.meet()) left_alone = true;
           },
           [&](int i) { filled[w] += i + 1; });
     });
@@ -69,7 +67,7 @@ bool run(int n, int bad_warp, int bad_fill) {
   for (int w = 0; w < kWarps; ++w) {
     const bool whole = bad_warp < 0 || bad_fill >= n;
     if (whole) fine = fine && ok[w] && filled[w] == all;
-    else fine = fine && !(w == bad_warp && (ok[w] || filled[w] != bad_fill * (bad_fill + 1) / 2));
+    else fine = fine && ok[w] == (w != bad_warp) && filled[w] == (w == bad_warp ? bad_fill * (bad_fill + 1) / 2 : all);
   }
   if (!fine) std::printf("%d fills, warp %d's wait for fill %d: %s\n", n, bad_warp, bad_fill, left_alone ? "a warp is left waiting" : "wrong fills");
   return fine;
