@@ -351,15 +351,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {
   constexpr bool BOX = MAKERS > 0;
   constexpr int kRing = kBuffers<DP, BOX>, kKeys = kKeyTiles<DP>, kValues = kValueTiles<DP, BOX>;
-  // The buffer of fill i -- keys of tile i / 2, or its values -- and how often it
-  // has been filled before.
-  auto buf_of = [](int i) { return i & 1 ? kKeys + (i >> 1) % kValues : (i >> 1) % kKeys; };
-  auto use_of = [](int i) { return i & 1 ? (i >> 1) / kValues : (i >> 1) / kKeys; };
+  using Fills = Rings<kKeys, kValues>;
+  auto buf_of = [](int i) { return Fills::buffer(i); };
+  auto use_of = [](int i) { return Fills::use(i); };
   constexpr uint32_t kBytes = kTileBytes<DP>;
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[9 + 3 * kRing];
+  __shared__ __align__(8) uint64_t bars[10 + 3 * kRing];
   __shared__ uint32_t tmem_at;
   __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
   __shared__ uint32_t special;
@@ -393,7 +392,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   // BOX: the values of tile j are looked over.
   auto s_read = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };  // kAhead: scores are in registers
   auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kValues); };
+  const uint32_t drained = bar0 + 8 * (9 + 3 * kRing);  // every product is done
   if (tid == 0) {
+    bar_init(drained, 1);
     bar_init(q_full, 32 * kSoftWarps / 2 * nq);
     for (int i = 0; i < kRing; ++i) {
       bar_init(kv_full(i), BOX ? 1 : 32 * kCopyWarps);
@@ -445,11 +446,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           return x;
         };
         Box box, next = look(w.tile0);
-        for (int i = c; i < 2 * w.tiles && ok; i += MAKERS) {
+        int sent = 2 * w.tiles;
+        for (int i = c; i < 2 * w.tiles; i += MAKERS) {
           const int buf = buf_of(i), use = use_of(i);
           if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
           ok = __all_sync(kFull, ok);
-          if (!ok) break;
+          if (!ok) {
+            sent = i;
+            break;
+          }
           if (MAKERS == 2 || (i & 1) == 0) {
             box = next;
             if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
@@ -475,6 +480,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                        kv_full(buf), one);
           }
         }
+        // No copy is on its way into a block that has ended, whoever gave up.
+        const bool landed =
+            Fills::drain(c, MAKERS, sent, [&](int f) { return bar_wait(kv_full(buf_of(f)), use_of(f) & 1); });
+        ok = ok && landed;
       } else {
         // The others look values over.
         for (int i = 1; i < 2 * w.tiles && ok; i += 2) {
@@ -650,6 +659,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
+      // Nor are products or their arrivals at barriers, when tensor memory is
+      // given back.
+      mma_commit(drained, one);
+      const bool finished = bar_wait(drained, 0);
+      ok = ok && finished;
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));

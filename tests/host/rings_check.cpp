@@ -1,0 +1,54 @@
+// Check of what warps that send copies wait for before they end
+// (csrc/pcs_attend_rounds.h): barriers of two phases told apart by parity, as the
+// kernel has them.  After n fills, wherever the warps stopped, the waits return
+// once all copies have landed, and not before.  Prints "ok" or the first failure.
+#include <cstdio>
+#include <vector>
+
+#include "pcs_attend_rounds.h"
+
+namespace {
+
+template <int KEYS, int VALUES>
+bool run(int step, int c, int sent) {
+  using R = pcs::Rings<KEYS, VALUES>;
+  // The warp's fills c, c + step, .. below `sent`; each buffer's, in order.
+  std::vector<int> newest(KEYS + VALUES, -1), times(KEYS + VALUES, 0);
+  int n = c;
+  for (; n < sent; n += step) {
+    if (R::use(n) != times[R::buffer(n)]) return false;
+    newest[R::buffer(n)] = n;
+    times[R::buffer(n)] += 1;
+  }
+  // A barrier whose phase x is in progress lets a wait for parity p through
+  // where x and p differ in parity.
+  for (int late = -1; late < KEYS + VALUES; ++late) {  // the buffer whose last copy has not landed
+    if (late >= 0 && newest[late] < 0) continue;
+    int waits = 0;
+    const bool over = R::drain(c, step, n, [&](int i) {
+      const int b = R::buffer(i), phase = times[b] - (b == late);
+      ++waits;
+      return ((phase ^ R::use(i)) & 1) != 0;
+    });
+    if (over != (late < 0) || waits > KEYS + VALUES) {
+      std::printf("rings of %d and %d, step %d from %d, %d sent: buffer %d late, %d waits, %s\n", KEYS, VALUES, step, c, sent,
+                  late, waits, over ? "over" : "not over");
+      return false;
+    }
+  }
+  return true;
+}
+
+template <int KEYS, int VALUES>
+bool all() {
+  for (int sent = 0; sent < 60; ++sent)
+    if (!run<KEYS, VALUES>(1, 0, sent) || !run<KEYS, VALUES>(2, 0, sent) || !run<KEYS, VALUES>(2, 1, sent)) return false;
+  return true;
+}
+
+}  // namespace
+
+int main() {
+  if (!all<4, 4>() || !all<2, 3>() || !all<2, 2>() || !all<3, 2>()) return 1;
+  std::puts("ok");
+}
