@@ -352,13 +352,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr bool BOX = MAKERS > 0;
   constexpr int kRing = kBuffers<DP, BOX>, kKeys = kKeyTiles<DP>, kValues = kValueTiles<DP, BOX>;
   using Fills = Rings<kKeys, kValues>;
+  using Bars = Barriers<kKeys, kValues, BOX>;
   auto buf_of = [](int i) { return Fills::buffer(i); };
   auto use_of = [](int i) { return Fills::use(i); };
   constexpr uint32_t kBytes = kTileBytes<DP>;
   constexpr uint32_t kPanel = kTile * 128;  // 64 columns of a tile
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[10 + 3 * kRing];
+  __shared__ __align__(8) uint64_t bars[Bars::kCount];
   __shared__ uint32_t tmem_at;
   __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
   __shared__ uint32_t special;
@@ -383,30 +384,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t qat = smem, ring = smem + 2 * kBytes;
   uint8_t* const ring_ptr = raw + (ring - smem_addr(raw));
   const uint32_t bar0 = smem_addr(bars);
-  const uint32_t q_full = bar0;
-  auto kv_full = [&](int i) { return bar0 + 8 * (1 + i); };
-  auto kv_empty = [&](int i) { return bar0 + 8 * (1 + kRing + i); };
-  auto s_full = [&](int t) { return bar0 + 8 * (1 + 2 * kRing + t); };
-  auto p_full = [&](int t) { return bar0 + 8 * (3 + 2 * kRing + t); };
-  auto o_full = [&](int t) { return bar0 + 8 * (5 + 2 * kRing + t); };
-  // BOX: the values of tile j are looked over.
-  auto s_read = [&](int t) { return bar0 + 8 * (7 + 2 * kRing + t); };  // kAhead: scores are in registers
-  auto v_fine = [&](int j) { return bar0 + 8 * (9 + 2 * kRing + j % kValues); };
-  const uint32_t drained = bar0 + 8 * (9 + 3 * kRing);  // every product is done
+  const uint32_t q_full = bar0 + 8 * Bars::q_full(), drained = bar0 + 8 * Bars::drained();
+  auto kv_full = [&](int i) { return bar0 + 8 * Bars::kv_full(i); };
+  auto kv_empty = [&](int i) { return bar0 + 8 * Bars::kv_empty(i); };
+  auto s_full = [&](int t) { return bar0 + 8 * Bars::s_full(t); };
+  auto p_full = [&](int t) { return bar0 + 8 * Bars::p_full(t); };
+  auto o_full = [&](int t) { return bar0 + 8 * Bars::o_full(t); };
+  auto s_read = [&](int t) { return bar0 + 8 * Bars::s_read(t); };  // kAhead: scores are in registers
+  auto v_fine = [&](int j) { return bar0 + 8 * Bars::v_fine(j); };  // BOX: the values of tile j are looked over
   if (tid == 0) {
-    bar_init(drained, 1);
-    bar_init(q_full, 32 * kSoftWarps / 2 * nq);
-    for (int i = 0; i < kRing; ++i) {
-      bar_init(kv_full(i), BOX ? 1 : 32 * kCopyWarps);
-      bar_init(kv_empty(i), 1);
-      bar_init(v_fine(i), 32 * (kCopyWarps - MAKERS));
-    }
-    for (int t = 0; t < 2; ++t) {
-      bar_init(s_full(t), 1);
-      bar_init(p_full(t), kTile);
-      bar_init(o_full(t), 1);
-      bar_init(s_read(t), kTile);
-    }
+    Bars::each(kTile, 32 * kSoftWarps / 2 * nq, BOX ? 1 : 32 * kCopyWarps, 32 * (kCopyWarps - MAKERS),
+               [&](int i, int count) { bar_init(bar0 + 8 * i, count); });
     special = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }

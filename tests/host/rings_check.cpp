@@ -1,7 +1,7 @@
 // Check of what warps that send copies wait for before they end
 // (csrc/pcs_attend_rounds.h): barriers of two phases told apart by parity, as the
 // kernel has them.  After n fills, wherever the warps stopped, the waits return
-// once all copies have landed, and not before.  Prints "ok" or the first failure.
+// once all copies have landed, and not before.  And of the barriers' numbers.  Prints "ok" or the first failure.
 #include <cstdio>
 #include <vector>
 
@@ -46,9 +46,31 @@ bool all() {
   return true;
 }
 
+// Every barrier is made once, and each name has one of its own.
+template <int KEYS, int VALUES, bool LOOK>
+bool barriers() {
+  using B = pcs::Barriers<KEYS, VALUES, LOOK>;
+  std::vector<int> made(B::kCount, 0), named(B::kCount, 0);
+  bool fine = true;
+  B::each(128, 256, 1, 64, [&](int i, int count) {
+    if (i < 0 || i >= B::kCount || count < 1) fine = false;
+    else made[i] += 1;
+  });
+  named[B::q_full()] += 1;
+  named[B::drained()] += 1;
+  for (int t = 0; t < 2; ++t)
+    for (int i : {B::s_full(t), B::s_read(t), B::p_full(t), B::o_full(t)}) named[i] += 1;
+  for (int i = 0; i < KEYS + VALUES; ++i) named[B::kv_full(i)] += 1, named[B::kv_empty(i)] += 1;
+  for (int j = 0; LOOK && j < 3 * VALUES; ++j) named[B::v_fine(j)] += j < VALUES;
+  for (int i = 0; i < B::kCount; ++i) fine = fine && made[i] == 1 && named[i] == 1;
+  if (!fine) std::printf("barriers of rings of %d and %d are not made once each\n", KEYS, VALUES);
+  return fine;
+}
+
 }  // namespace
 
 int main() {
+  if (!barriers<4, 4, true>() || !barriers<2, 3, true>() || !barriers<2, 2, false>() || !barriers<4, 4, false>()) return 1;
   if (!all<4, 4>() || !all<2, 3>() || !all<2, 2>() || !all<3, 2>()) return 1;
   std::puts("ok");
 }
