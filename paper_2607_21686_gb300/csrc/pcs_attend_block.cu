@@ -751,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        const float at = top == -INFINITY ? 0.0f : top;
+        const float at = top == -INFINITY ? 0.0f : top - kLift<T>;
         const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), at2 = pair(-at, -at);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -861,7 +861,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ok && there && a.lse) {
           const int h = head * a.group + (r - static_cast<int>(tok) * a.group);
           a.lse[(w.all.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
-              total == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(total));
+              total == 0.0f ? -INFINITY : fmaf(top - kLift<T>, kLn2, logf(total));
         }
       }
     }
@@ -920,7 +920,7 @@ __global__ void __launch_bounds__(kTile) k_attend_join(const __grid_constant__ A
   }
   if (d0 == 0 && a.lse)
     a.lse[(v.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
-        total == 0.0f ? -INFINITY : fmaf(top, 0.693147180559945309f, logf(total));
+        total == 0.0f ? -INFINITY : fmaf(top - kLift<T>, 0.693147180559945309f, logf(total));
 }
 
 cudaLaunchConfig_t config(int64_t grid, int threads, uint32_t smem, cudaLaunchAttribute* attr, cudaStream_t stream) {

@@ -51,6 +51,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // The weights of a softmax are rounded to the cache's type for the matrix
 // instruction, each by at most 2^-8 (bf16) or 2^-11 of itself, which is what
 // the rounding of the result itself costs; their sum stays in 32 bits.
+// float16 holds numbers below 2^-14 to 2^-25 and no better: many small weights
+// beside a large one would be lost, while the total counts them.  So its weights
+// are 2^kLift times exp(score - maximum) -- at most 2^15 with a maximum that is
+// raised by steps of 2^8 -- and keep 11 bits down to 2^-21 of the largest, and
+// 2^-32 below.  The total is taken over the same weights and takes the factor out.
+template <typename T>
+constexpr float kLift = std::is_same<T, __half>::value ? 7.0f : 0.0f;
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi);
 template <>

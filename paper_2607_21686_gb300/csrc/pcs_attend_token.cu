@@ -33,7 +33,7 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kTile = 16;
 constexpr unsigned kFull = 0xffffffffu;
 // A row's running maximum is raised only when a score exceeds it by 2^8: the
-// weights stay below 256, and raising it (a reduction over the warp and a
+// weights stay below 256 (times 2^kLift), and raising it (a reduction over the warp and a
 // pass over the sums) is rare.
 constexpr float kSlack = 8.0f;
 
@@ -265,8 +265,8 @@ __global__ void __launch_bounds__(kThreads)
     uint32_t w[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float m0 = top[n][0] == -INFINITY ? 0.0f : top[n][0];
-      const float m1 = top[n][1] == -INFINITY ? 0.0f : top[n][1];
+      const float m0 = top[n][0] == -INFINITY ? 0.0f : top[n][0] - kLift<T>;
+      const float m1 = top[n][1] == -INFINITY ? 0.0f : top[n][1] - kLift<T>;
       const float p0 = exp2_fast(c[n][0] - m0), p1 = exp2_fast(c[n][1] - m1);
       const float p2 = exp2_fast(c[n][2] - m0), p3 = exp2_fast(c[n][3] - m1);
       total[n][0] += p0 + p2;
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kThreads)
           pack2<T>(j.x * inv, j.y * inv);
     if (d == 0 && a.lse)
       a.lse[t * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
-          j.total == 0.0f ? -INFINITY : fmaf(j.top, kLn2, logf(j.total));
+          j.total == 0.0f ? -INFINITY : fmaf(j.top - kLift<T>, kLn2, logf(j.total));
   };
   const int64_t pair = static_cast<int64_t>(s) * a.cache.heads + head;
   const int64_t part_floats = static_cast<int64_t>(kRows) * (DP + 2);
@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_token_join(const __grid_con
   }
   if (threadIdx.x == 0 && a.lse)
     a.lse[(view.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + h] =
-        total == 0.0f ? -INFINITY : fmaf(m, 0.693147180559945309f, logf(total));
+        total == 0.0f ? -INFINITY : fmaf(m - kLift<T>, 0.693147180559945309f, logf(total));
 }
 
 template <typename T, int DP, int NT>
