@@ -341,7 +341,8 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     const int64_t tokens = few ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
     if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
     if (few) {
-      const int64_t resident = static_cast<int64_t>(call.sm_count()) * attend_token_blocks_per_sm(cache->head_dim);
+      const int64_t resident =
+          static_cast<int64_t>(call.sm_count()) * attend_token_blocks_per_sm(cache->head_dim, static_cast<int>(rows));
       const int64_t tiles = (seen + 15) / 16;
       // Parts for a wave of blocks, of two tiles a warp at least; and of several
       // sessions, whose lengths may differ, up to four waves of parts of eight

@@ -170,8 +170,8 @@ inline uint64_t token_part_floats(int rows, int head_dim) {
 // kTokenOwnJoin of them (a.ticket), else by a second launch (`join`).
 constexpr int kTokenOwnJoin = 16;
 cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream);
-// Blocks of the token kernel that one SM holds.
-int attend_token_blocks_per_sm(int head_dim);
+// Blocks of the token kernel that one SM holds, for `rows` rows a key head.
+int attend_token_blocks_per_sm(int head_dim, int rows);
 
 // The block kernel: a session and key head's rows in blocks of kBlockRows,
 // `blocks` of them at most.  With splits > 1 a block's part is its rows' sums,

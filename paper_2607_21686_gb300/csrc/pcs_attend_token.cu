@@ -80,13 +80,22 @@ constexpr uint32_t kStageBytes = 2 * kTile * DP * 2;
 template <int DP>
 constexpr uint32_t kRingBytes = kWarps * kStagesOf<DP> * kStageBytes<DP>;
 
+// Blocks that one SM holds: as many rings as its 227 KB of shared memory take
+// (2 KB a block for the rest), and as its registers do -- 32 rows of 64 dims want
+// some 250 a thread, two blocks' worth.  The compiler is held to it, so that what
+// the host takes for one wave of parts is one.  (One session of 100,000 tokens,
+// 32 rows of 64 dims: 36 us; 47 us when three blocks were counted on.)  32 rows of
+// 128 dims take all 255 registers, and 68 bytes of a thread's values spill.
+template <int DP, int NT>
+constexpr int kResident = DP == 64 && NT == 4 ? 2 : static_cast<int>(227 * 1024 / (kRingBytes<DP> + 2048));
+
 // Joined sums of one row pair of dims; `w` parts with maxima m, totals l.
 struct Joined {
   float x, y, top, total;
 };
 
 template <typename T, int DP, int NT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, (kResident<DP, NT>))
     k_attend_token(const __grid_constant__ AttendArgs a) {
   constexpr int kStages = kStagesOf<DP>;
   constexpr uint32_t kStage = kStageBytes<DP>;
@@ -539,9 +548,9 @@ cudaError_t by_size(const AttendArgs& a, int rows, bool join, cudaStream_t strea
 
 }  // namespace
 
-int attend_token_blocks_per_sm(int head_dim) {
-  // As many rings as the 227 KB of shared memory hold.
-  return static_cast<int>(227 * 1024 / ((head_dim <= 64 ? kRingBytes<64> : kRingBytes<128>) + 2048));
+int attend_token_blocks_per_sm(int head_dim, int rows) {
+  if (head_dim <= 64) return rows <= 16 ? kResident<64, 2> : kResident<64, 4>;
+  return kResident<128, 4>;
 }
 
 cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream) {
