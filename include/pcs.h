@@ -643,7 +643,8 @@ pcs_status pcs_snapshot_read_file(pcs_ctx *ctx, const char *path, uint32_t place
  * next checkpoint: give new tokens their positions, write them into the pages
  * of the window, attend over it.  (The paper's runtime leaves the model to its
  * caller, Sec. 3 "Boundary"; the pages are those of Sec. 7.2's addressable KV
- * and of the copy-on-write pool above.)
+ * and of the copy-on-write pool above.)  Fields said to be 0 that are not, and
+ * flags that are not named here -> PCS_E_INVAL.
  */
 
 /* Heads of tokens: element d of head h of token t is at

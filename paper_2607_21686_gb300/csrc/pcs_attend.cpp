@@ -83,6 +83,7 @@ pcs_status guarded(F&& f) {
 
 pcs_status check_heads(const pcs_heads* h, const char* what, uint32_t dtype, int32_t head_dim) {
   if (!h) return op_fail(PCS_E_INVAL, "%s is null", what);
+  if (h->reserved) return op_fail(PCS_E_INVAL, "%s: reserved must be 0", what);
   if (h->heads < 1 || h->heads > 65535) return op_fail(PCS_E_INVAL, "%s: %d heads", what, h->heads);
   if (h->dtype != dtype) return op_fail(PCS_E_INVAL, "%s: element type %u, expected %u", what, h->dtype, dtype);
   if (h->head_dim != head_dim)
@@ -152,6 +153,7 @@ pcs_status check_cache(const pcs_kv_cache* c, CacheDev* d) {
 
 pcs_status check_batch(const pcs_kv_batch* b, BatchDev* d) {
   if (!b) return op_fail(PCS_E_INVAL, "batch is null");
+  if (b->reserved) return op_fail(PCS_E_INVAL, "batch: reserved must be 0");
   if (b->sessions < 0 || b->tokens < 0 || b->tokens > 0x7FFFFFFFll || b->max_new < 0 || b->max_len < 0)
     return op_fail(PCS_E_INVAL, "batch: negative or too large counts");
   if (b->sessions == 0 && b->tokens > 0) return op_fail(PCS_E_INVAL, "batch: tokens without sessions");
@@ -303,6 +305,8 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     if (!st) st = check_batch(batch, &a.batch);
     if (st) return st;
     if (!params) return op_fail(PCS_E_INVAL, "params is null");
+    if (params->flags || params->reserved)
+      return op_fail(PCS_E_INVAL, "params: flags (0x%x) and reserved must be 0", params->flags);
     if (params->window < 0) return op_fail(PCS_E_INVAL, "negative window");
     if (!(params->scale >= 0.0f) || std::isinf(params->scale))
       return op_fail(PCS_E_INVAL, "scale must be finite and positive (0: 1 / sqrt(head_dim))");
