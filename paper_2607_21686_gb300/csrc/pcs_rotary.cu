@@ -38,22 +38,36 @@ __device__ __forceinline__ void grid_dependency() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// x + y as a float and what its rounding left (Knuth's two-sum).
+__device__ __forceinline__ float two_sum(float x, float y, float& left) {
+  const float s = x + y, t = s - x;
+  left = (x - (s - t)) + (y - t);
+  return s;
+}
+
 // Cosine and sine of position times frequency, the product in two floats: the
 // position is split so that both parts are exact floats, each product's
-// rounding error comes from a fused multiply-add, and the sum's from Knuth's
-// two-sum.  (One rounding of a position of 10^5 would cost 0.004 rad.)  The
-// rest turns the result: by two terms of its series while it is below 2^-8
-// (what is left out is below 2^-26), by its own sine and cosine at positions
-// beyond.
+// rounding error comes from a fused multiply-add, and the sums' from two_sum.
+// (One rounding of a position of 10^5 would cost 0.004 rad.)  The rest turns the
+// result: by two terms of its series while it is below 2^-8 (what is left out is
+// below 2^-26), by its own sine and cosine at positions beyond, where its
+// rounding (2^-17 rad at 2^31) turns them by one term.
 __device__ __forceinline__ float2 cos_sin(int32_t pos, float f) {
   const float hi = static_cast<float>(pos & ~0xfff), lo = static_cast<float>(pos & 0xfff);
-  const float a = hi * f, ae = fmaf(hi, f, -a);
-  const float b = lo * f, be = fmaf(lo, f, -b);
-  const float s = a + b, t = s - a;
-  const float rest = (((a - (s - t)) + (b - t)) + ae) + be;
+  const float a = __fmul_rn(hi, f), ae = fmaf(hi, f, -a);
+  const float b = __fmul_rn(lo, f), be = fmaf(lo, f, -b);
+  float e, left_e, left;
+  const float s = two_sum(a, b, e);
+  const float rest = two_sum(two_sum(e, ae, left_e), be, left);
   float sn, cs, rs = rest, rc = fmaf(-0.5f * rest, rest, 1.0f);
   sincosf(s, &sn, &cs);
-  if (fabsf(rest) > 0.00390625f) sincosf(rest, &rs, &rc);
+  if (fabsf(rest) > 0.00390625f) {
+    float rs1, rc1;
+    sincosf(rest, &rs1, &rc1);
+    left += left_e;
+    rs = fmaf(rc1, left, rs1);
+    rc = fmaf(-rs1, left, rc1);
+  }
   return make_float2(fmaf(cs, rc, -sn * rs), fmaf(sn, rc, cs * rs));
 }
 
