@@ -152,12 +152,13 @@ __device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t, int s) {
 }
 
 // How a block's threads share out a head: `units` side by side, `at_once` heads.
+// (A head has at most 256 elements, so no more units than there are threads.)
 struct Share {
   int32_t units, at_once;
   FastDiv by_units;
   void set(int units_) {
     units = units_;
-    at_once = units_ > kThreads ? 1 : kThreads / units_;
+    at_once = kThreads / units_;
     by_units.set(units_);
   }
 };
@@ -239,10 +240,6 @@ template <typename T, int VE, bool IL, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 7)
     k_rotate(const __grid_constant__ RotArgs a, const __grid_constant__ Shares shares, int per_block, int turn) {
   using V = Run<T, VE>;
-  // Units a thread has in flight: one, of as many threads as an SM's registers
-  // hold (49,153 tokens of 32 + 8 heads of 128: 165 us; two units of fewer
-  // threads 184 us, four 186 us, eight 286 us).
-  constexpr int kUnits = 1;
   constexpr bool kTwo = !IL || VE == 1;         // a turned unit has two runs
   __shared__ __align__(32) float2 cs[kTokens * kPairs + 4];
   __shared__ Place place[kTokens];
@@ -256,47 +253,38 @@ __global__ void __launch_bounds__(kThreads, 7)
     const Share& sh = n < a.plain ? shares.turned : shares.plain;
     const int turned = n < a.plain ? turn : 0;
     const int heads = z.heads - (n ? a.t[n - 1].heads : 0), total = nt * heads;
-    const int h0 = sh.by_units.div(tid), r0 = tid - h0 * sh.units;
+    const int h0 = sh.by_units.div(tid), r = tid - h0 * sh.units;
     if (h0 >= sh.at_once) continue;
+    const bool turns = r < turned;
+    const int pair = VE == 1 ? r : IL ? r * (VE / 2) : r * VE;
+    const int e = (turns ? (VE == 1 && IL ? 2 * r : r * VE) : (turned ? (VE > 1 && IL ? turned * VE : 2 * a.pairs) : 0) + (r - turned) * VE) *
+                  static_cast<int>(sizeof(T));
     const uint8_t* const src0 = z.src + t0 * z.src_token;
-    // (A head of more units than threads takes them in turns.)
-    for (int r = r0; r < sh.units; r += kThreads) {
-      const bool turns = r < turned;
-      const int pair = VE == 1 ? r : IL ? r * (VE / 2) : r * VE;
-      const int e = (turns ? (VE == 1 && IL ? 2 * r : r * VE) : (turned ? (VE > 1 && IL ? turned * VE : 2 * a.pairs) : 0) + (r - turned) * VE) *
-                    static_cast<int>(sizeof(T));
-      for (int p0 = h0; p0 < total; p0 += kUnits * sh.at_once) {
-        V x[kUnits], y[kUnits];
-        int at[kUnits];  // the token, -1: nothing to do
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-          const uint32_t p = p0 + k * sh.at_once;
-          const uint32_t t = shares.by_heads[n].div(p), h = p - t * heads;
-          at[k] = static_cast<int>(p) < total ? static_cast<int>(t) : -1;
-          if (at[k] < 0) continue;
-          const uint8_t* src = src0 + times(t, z.src_token) + times(h, z.src_head) + e;
-          x[k] = *reinterpret_cast<const V*>(src);
-          if (kTwo && turns) y[k] = *reinterpret_cast<const V*>(src + second);
-        }
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-          if (at[k] < 0) continue;
-          const uint32_t t = at[k], h = p0 + k * sh.at_once - t * heads;
-          uint8_t* dst;
-          if (PAGED && z.role) {
-            const int64_t row = z.role == 1 ? place[t].k : place[t].v;
-            if (row < 0) continue;
-            dst = (z.role == 1 ? a.cache.k : a.cache.v) + row + times(h, a.cache.head_bytes) + e;
-          } else {
-            dst = z.dst + (t0 + t) * z.dst_token + times(h, z.dst_head) + e;
-          }
-          if (turns) {
-            turn_unit<T, VE, IL>(x[k], y[k], cs + t * row + pair, a.pairs - pair);
-            if (kTwo) *reinterpret_cast<V*>(dst + second) = y[k];
-          }
-          *reinterpret_cast<V*>(dst) = x[k];
-        }
+    // A unit at a time, of as many threads as an SM's registers hold (49,153 tokens
+    // of 32 + 8 heads of 128, neighbours: when that took 165 us, two units of fewer
+    // threads took 184 us, four 186 us, eight 286 us).
+    for (int p = h0; p < total; p += sh.at_once) {
+      // (t is never below zero.  The branch keeps the compiler from moving all that
+      // follows from t's place ahead of the loop, where it does not fit the 32
+      // registers that seven blocks an SM leave: 217 us without it, 164 us with.)
+      const int t = shares.by_heads[n].div(p), h = p - t * heads;
+      if (t < 0) continue;
+      const uint8_t* src = src0 + times(t, z.src_token) + times(h, z.src_head) + e;
+      V x = *reinterpret_cast<const V*>(src), y;
+      if (kTwo && turns) y = *reinterpret_cast<const V*>(src + second);
+      uint8_t* dst;
+      if (PAGED && z.role) {
+        const int64_t at = z.role == 1 ? place[t].k : place[t].v;
+        if (at < 0) continue;
+        dst = (z.role == 1 ? a.cache.k : a.cache.v) + at + times(h, a.cache.head_bytes) + e;
+      } else {
+        dst = z.dst + (t0 + t) * z.dst_token + times(h, z.dst_head) + e;
       }
+      if (turns) {
+        turn_unit<T, VE, IL>(x, y, cs + t * row + pair, a.pairs - pair);
+        if (kTwo) *reinterpret_cast<V*>(dst + second) = y;
+      }
+      *reinterpret_cast<V*>(dst) = x;
     }
   }
 }
