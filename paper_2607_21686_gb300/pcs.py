@@ -439,10 +439,26 @@ def _heads(t: torch.Tensor, what: str, tokens: int) -> pcs_heads:
     return pcs_heads(t.data_ptr(), ts if n > 1 else h * d, hs if h > 1 else d, h, d, dtype, 0)
 
 
-def _like(t: torch.Tensor) -> torch.Tensor:
-    """A new contiguous tensor of t's shape and type."""
+def _on(stream):
+    """New tensors of a call belong to the stream that it writes them on: other
+    streams' memory may still be in use there."""
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+def _like(t: torch.Tensor, stream=None) -> torch.Tensor:
+    """A new contiguous tensor of t's shape and type for a call on `stream`."""
+    if stream is not None:
+        with _on(stream):
+            return _like(t)
     return torch.empty_like(t) if t.is_contiguous() else \
         torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _lse_of(q: torch.Tensor, stream) -> torch.Tensor:
+    if stream is not None:
+        with _on(stream):
+            return _lse_of(q, None)
+    return torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
 
 
 def _int32(t: torch.Tensor, what: str, dim: int) -> torch.Tensor:
@@ -808,12 +824,13 @@ class Context:
         check(st, "pcs_prune_global_part")
 
     # -- paged cache of keys and values ------------------------------------------
+    # Results that a call makes belong to its stream, as torch's own do.
     def rotate(self, xs, rotary: Rotary, out=None, inverse: bool = False, stream=None) -> list:
         """Rotary positions applied to each tensor [tokens, heads, head_dim] of
         xs, or with `inverse` taken back (the gradient).  out: the results'
         tensors (may be xs itself); returns them."""
         if out is None:
-            out = [_like(x) for x in xs]
+            out = [_like(x, stream) for x in xs]
         n, tokens = len(xs), rotary.tokens
         if len(out) != n:
             raise ValueError("%d tensors and %d results" % (n, len(out)))
@@ -841,7 +858,7 @@ class Context:
         qs = ys = None
         if q is not None:
             if q_out is None:
-                q_out = _like(q)
+                q_out = _like(q, stream)
             qs, ys = _heads(q, "q", n), _heads(q_out, "q_out", n)
         elif q_out is not None:
             raise ValueError("q_out without q")
@@ -861,14 +878,14 @@ class Context:
         self._check_tables(cache, batch)
         n = batch.tokens
         if out is None:
-            out = _like(q)
+            out = _like(q, stream)
         qs, ys = _heads(q, "q", n), _heads(out, "out", n)
         if lse is not None:
             if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_cuda \
                     or not lse.is_contiguous():
                 raise ValueError("lse must be a contiguous CUDA float32 [tokens, q heads]")
         elif return_lse:
-            lse = torch.empty((n, qs.heads), dtype=torch.float32, device=q.device)
+            lse = _lse_of(q, stream)
         check(self.lib.pcs_attend(self.h, cache.struct, batch.struct,
                                   pcs_attend_params(scale, window, 0, 0), qs, ys, _ptr(lse),
                                   _stream_ptr(stream)), "pcs_attend")
