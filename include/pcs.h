@@ -684,7 +684,8 @@ typedef struct pcs_rotary {
  * d of head h at page * page_stride + row * row_stride + h * head_stride + d.
  * With a ring only the last `ring` positions are there, and the first `sinks`
  * (sinks = 0: a RING section's window, with ring start len mod ring).  Page -1
- * is empty: its tokens are not written and not seen.
+ * is empty: its tokens are not written and not seen (neither keys nor values,
+ * whichever of their pages is empty).
  */
 typedef struct pcs_kv_cache {
     void *k, *v;             /* device page pools                           */

@@ -143,12 +143,11 @@ __device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t, int s) {
   const int64_t e = s * c.table_stride + page;
   const int32_t kp = __ldg(c.table + e);
   const int32_t vp = c.v_table ? __ldg(c.v_table + e) : kp;
-  Place r = {-1, -1};
-  if (kp >= 0 && kp < c.n_pages) r.k = kp * c.page_bytes + row;
-  else if (kp != -1) atomicOr(a.err, kDevErrIndex);
-  if (vp >= 0 && vp < c.n_pages) r.v = vp * c.page_bytes + row;
-  else if (vp != -1) atomicOr(a.err, kDevErrIndex);
-  return r;
+  if (kp < 0 || kp >= c.n_pages || vp < 0 || vp >= c.n_pages) {  // neither of them is written
+    if (kp < -1 || kp >= c.n_pages || vp < -1 || vp >= c.n_pages) atomicOr(a.err, kDevErrIndex);
+    return {-1, -1};
+  }
+  return {kp * c.page_bytes + row, vp * c.page_bytes + row};
 }
 
 // How a block's threads share out a head: `units` side by side, `at_once` heads.

@@ -56,3 +56,25 @@ def test_split_tokens_of_rings(ctx, dim, rows, sinks, ring, over):
     again, lse2 = attend(ctx, p)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
     check(ctx, p, window=1100)
+
+
+@pytest.mark.parametrize("bad,status", [(-1, None), (10 ** 6, pcs.PCS_E_RANGE), (-7, pcs.PCS_E_RANGE)])
+@pytest.mark.parametrize("of_values", [False, True])
+def test_append_writes_keys_and_values_or_neither(ctx, dev, bad, status, of_values):
+    p = append_case(4, [20, 20], [3, 3], 2, 64, 16, 0, 0, torch.float16)
+    vt = torch.flip(p.table, (1,)).contiguous()
+    (vt if of_values else p.table)[1, 1] = bad
+    dk, dv = p.k.to(dev), p.v.to(dev)
+    cache = pcs.KvCache(dk, dv, p.table.to(dev), v_table=vt.to(dev))
+    batch = pcs.KvBatch(torch.tensor(p.lens, dtype=torch.int32, device=dev), 6)
+    ctx.kv_append(cache, batch, p.nk.to(dev), p.nv.to(dev))
+    if status is None:
+        ctx.sync()
+    else:
+        with pytest.raises(pcs.PcsError) as e:
+            ctx.sync()
+        assert e.value.status == status
+    k, v = p.k.clone(), p.v.clone()
+    k[int(p.table[0, 1]), 1:4] = p.nk[:3]
+    v[int(vt[0, 1]), 1:4] = p.nv[:3]
+    assert torch.equal(dk.cpu(), k) and torch.equal(dv.cpu(), v)
