@@ -55,7 +55,7 @@ bool encode_pool(const pcs_kv_cache& c, void* pool, int rows, uint8_t* map) {
 
 // Rows of the boxes that tensor copies can move: a power of two that divides a
 // page, so that a tile's boxes never leave theirs.  0: rows are copied one by one
-// (a prompt of 8,000 tokens, 32 query heads over 8, in pages of 16: 344 us with
+// (a prompt of 8,000 tokens, 32 query heads over 8, in pages of 16: 349 us with
 // boxes; in pages of 17, by rows, 867 us).
 int box_rows(const pcs_kv_cache& c) {
   for (int r = 128; r >= 8; r /= 2)
@@ -332,8 +332,8 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
     // Few rows of a key head, bound by HBM, go to the token kernel: up to 16, and
     // up to 32 where sessions and heads alone would leave SMs without a block of
     // the other one.  (64 sessions of 500 to 4,000 tokens, 4 key heads of 128:
-    // 8 rows 62 us, and 79 us by blocks; 16 rows 75 and 79; 32 rows 116 and 81.
-    // One session of 100,000 tokens, 32 rows: 62 and 114 us.)
+    // 8 rows 60 us, and 79 us by blocks; 16 rows 69 and 79; 32 rows 113 and 80.
+    // One session of 100,000 tokens, 32 rows: 60 and 112 us.)
     const int64_t pairs = static_cast<int64_t>(a.batch.sessions) * cache->heads;
     if ((st = call.begin())) return st;
     a.err = call.errors();
@@ -350,8 +350,8 @@ pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batc
       const int64_t tiles = (seen + 15) / 16;
       // Parts for a wave of blocks, of two tiles a warp at least; and of several
       // sessions, whose lengths may differ, up to four waves of parts of eight
-      // tiles a warp.  (48 sessions of 1 to 12,000 tokens: 222 us in one wave,
-      // 200 us in four; one of 200,001 tokens: 163 and 196 us.)
+      // tiles a warp.  (48 sessions of 1 to 12,000 tokens: 217 us in one wave,
+      // 196 us in four; one of 200,001 tokens, when measured: 163 and 196 us.)
       int64_t splits = std::min(resident / pairs, tiles / (2 * kTokenWarps));
       if (splits > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin, std::min(splits, tiles / (4 * kTokenWarps)));
       if (a.batch.sessions > 1)

@@ -22,15 +22,16 @@
 //                 the copying warps replace them by zeros, and the rows that
 //                 do see them take them up at the end.
 //                 A prompt of 8,000 tokens, 32 query heads over 8 of 128 in
-//                 bfloat16: 345 us, 1.52 PFLOP/s (80 % of the measured matrix
-//                 rate; 368 us where passes take turns on three sets of inputs;
-//                 by rows 867 us).  The matrix unit is busy 52 % of a
-//                 4,096-token prompt's 112 us.  When that took 129 us, leaving
-//                 out the warps' work on the scores saved 31 us, the products
+//                 bfloat16: 367 us, 1.43 PFLOP/s (75 % of the measured matrix
+//                 rate), with inputs that come from memory; 349 us in a loop over
+//                 three sets of them; by rows 867 us.  The matrix unit is busy
+//                 52 % of a 4,096-token prompt's 111 us.  When that took 129 us,
+//                 leaving out the warps' work on the scores saved 31 us, the products
 //                 15 us and the exponentials 5 us: what bounds it is the chain
 //                 of both with the hand-overs between them, and at windows and
 //                 short sessions the 6 us a block takes to its first scores and
-//                 from its last ones.
+//                 from its last ones.  Some values of a thread spill (68 to 100
+//                 bytes stored, 112 to 232 loaded, by form).
 // k_attend_join   joins the parts of rows whose tokens were split over blocks.
 #include "pcs_attend_dev.h"
 #include "pcs_attend_rounds.h"
@@ -344,8 +345,8 @@ __device__ __forceinline__ bool take_out(uint4* at, uint4 v) {
 // MAKERS: warps that send tensor copies of boxes of rows (the other copying warps
 // look values over); 0: rows are copied one by one.  Boxes of eight rows are
 // sixteen or thirty-two a tile, more than one warp can send in a tile's time: two
-// warps take keys and values (8,000-token prompt in pages of 8: 407 us by one,
-// 357 us by two; in pages of 16: 350 and 353 us).
+// warps take keys and values (8,000-token prompt in pages of 8: 411 us by one,
+// 358 us by two; in pages of 16: 349 and 353 us).
 template <typename T, int DP, int MAKERS>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {

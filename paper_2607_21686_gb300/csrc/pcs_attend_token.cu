@@ -20,8 +20,11 @@
 //                 generation tensor cores, which want 128 rows, have nothing to
 //                 add here.)
 //                 256 sessions over windows of 1,024 tokens, 16 heads of 64 in
-//                 bfloat16: 167 us, 6.4 TB/s (96 % of the measured copy rate);
-//                 four tokens over 200,001, 8 key heads of 128: 123 us, 6.7 TB/s.
+//                 bfloat16: 170 us, 6.3 TB/s (95 % of the measured copy rate);
+//                 four tokens over 200,001, 8 key heads of 128: 125 us, 6.6 TB/s.
+//                 A second product with what the weights' rounding left of them
+//                 took 175 us there, and 10 % more with 32 rows a key head: the
+//                 weights stay in 16 bits.
 //                 k_attend_token_join joins more parts than kTokenOwnJoin.
 #include "pcs_attend_dev.h"
 

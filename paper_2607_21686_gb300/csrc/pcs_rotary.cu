@@ -12,11 +12,11 @@
 //            or 4 where the pairs' halves are no whole vectors, or of one pair
 //            where something is not aligned.  With a cache (PAGED) the rows of
 //            keys and values go to the slots of the tokens' positions.
-//            49,153 tokens of 32 + 8 heads of 128 in float16: 165 us, 6.1 TB/s
-//            (91 % of the measured copy rate); 23,000 new tokens of 24 sessions,
-//            16 heads of 64: 50 us, 5.7 TB/s.  What is left is instructions (68 %
-//            of the issue slots are taken) and a block's look-ups before its
-//            first load.
+//            49,153 tokens of 32 + 8 heads of 128 in float16, neighbours: 163 us,
+//            6.2 TB/s (92 % of the measured copy rate), halves 152 us; 23,000 new
+//            tokens of 24 sessions, 16 heads of 64: 48 us, 5.9 TB/s.  What is left is
+//            instructions (two thirds of the issue slots are taken) and a block's
+//            look-ups before its first load.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -321,7 +321,8 @@ cudaError_t launch(const RotArgs& a, int sm_count, cudaStream_t stream) {
 // The widest units of whole vectors (neighbours: of vectors that may end in
 // elements that stay; halves: a half is a number of whole units, for a thread has
 // both elements of its pairs).  49,153 tokens of 32 + 8 heads of 128: 64 pairs, in
-// units of 16 bytes, 165 us; 60 pairs, of 8 bytes, 178 us; pair by pair 393 us.
+// units of 16 bytes, 152 us; 60 pairs, of 8 bytes, 172 us; 62, of 4 bytes, 240 us;
+// pair by pair 389 us.
 template <typename T, bool PAGED>
 cudaError_t by_unit(const RotArgs& a, bool vec, int sm_count, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
