@@ -554,7 +554,7 @@ pcs_status ws_acquire(pcs_ctx* c, uint64_t bytes, cudaStream_t stream, uint8_t**
       return fail(PCS_E_NOMEM, "cannot allocate %llu bytes of workspace",
                   static_cast<unsigned long long>(want));
     }
-    PCS_CUDA(cudaMemset(W.buf, 0, kWsHeader));
+    PCS_CUDA(cudaMemsetAsync(W.buf, 0, kWsHeader, stream));
     W.bytes = want;
   } else if (W.busy && !W.busy->done()) {
     c->ws_behind = true;
