@@ -442,6 +442,14 @@ namespace {
 
 constexpr uint64_t kStageBytes = 64ull << 20;
 
+// Device words of a context to zero, done on return: kernels of any stream add
+// errors to them, which a memset still behind the default stream's work would
+// take away.
+cudaError_t clear_words(uint32_t* words, int n) {
+  const cudaError_t e = cudaMemset(words, 0, 4 * n);
+  return e == cudaSuccess ? cudaStreamSynchronize(nullptr) : e;
+}
+
 pcs_status set_device(pcs_ctx* c) {
   PCS_CUDA(cudaSetDevice(c->device));
   return PCS_OK;
@@ -1676,7 +1684,7 @@ pcs_status pcs_create(int32_t device, pcs_ctx** out) {
   c->dev_arena = std::make_unique<Arena>(PCS_PLACE_DEVICE, c->events);
   c->host_arena = std::make_unique<Arena>(PCS_PLACE_PINNED_HOST, c->events);
   PCS_CUDA(cudaMalloc(&c->words, 256));
-  PCS_CUDA(cudaMemset(c->words, 0, 256));
+  PCS_CUDA(clear_words(c->words, 64));
   *out = c.release();
   return PCS_OK;
 }
@@ -1799,12 +1807,12 @@ pcs_status pcs_sync(pcs_ctx* c, void* stream) {
   PCS_CUDA(cudaMemcpy(w3, c->words, sizeof w3, cudaMemcpyDeviceToHost));
   const uint32_t w = w3[0];
   if (w3[2] != 0) {
-    PCS_CUDA(cudaMemset(c->words + 2, 0, 4));
-    if (w) PCS_CUDA(cudaMemset(c->words, 0, 4));
+    PCS_CUDA(clear_words(c->words + 2, 1));
+    if (w) PCS_CUDA(clear_words(c->words, 1));
     return fail(PCS_E_CORRUPT, "%u restored sessions failed asynchronous verification", w3[2]);
   }
   if (w != 0) {
-    PCS_CUDA(cudaMemset(c->words, 0, 4));
+    PCS_CUDA(clear_words(c->words, 1));
     if (w & kDevErrTimeout)
       return fail(PCS_E_TIMEOUT, "a bounded wait inside a kernel gave up (error bits 0x%x)", w);
     if (w & kDevErrNoPage)

@@ -28,3 +28,22 @@ def test_calls_on_a_fresh_stream_beside_a_busy_one(ctx, dev):
             torch.cuda.synchronize()
             assert all(torch.equal(out, want) and torch.equal(lse, want_lse) for out, lse in outs)
             own.sync()
+
+
+def test_an_error_beside_a_busy_default_stream_is_kept(ctx, dev):
+    # A context made while the default stream is busy, and an error of another
+    # stream before that one's work is over.
+    p = kv_ref.Population(31, [60, 60], [1, 1], 2, 2, 64)
+    p.table[1, 2] = 10 ** 6
+    cache, batch, q = kv_ref.on_gpu(pcs, p)
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)  # the default stream
+    with pcs.Context(0) as own:
+        own.attend(cache, batch, q, out=out, stream=side)
+        with pytest.raises(pcs.PcsError) as e:
+            own.sync(side)
+        assert e.value.status == pcs.PCS_E_RANGE
+        own.sync(side)  # reported once
+    torch.cuda.synchronize()
