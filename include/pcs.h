@@ -73,6 +73,9 @@ typedef int32_t pcs_status;
 #define PCS_DT_BF16 5
 #define PCS_DT_F32 6
 #define PCS_DT_U64 7
+#define PCS_DT_E4M3 8 /* caches of keys and values: 8-bit floats (4 bits of   */
+                      /* exponent, 3 of mantissa) with a scale a head         */
+#define PCS_DT_I8 9   /* ... or 8-bit whole numbers, -127 to 127              */
 
 /* Section type tags (caller-chosen; these are the conventional ones). */
 #define PCS_SEC_OBS 1       /* uint8 observation (Markovian model)          */
@@ -644,7 +647,9 @@ pcs_status pcs_snapshot_read_file(pcs_ctx *ctx, const char *path, uint32_t place
  * of the window, attend over it.  (The paper's runtime leaves the model to its
  * caller, Sec. 3 "Boundary"; the pages are those of Sec. 7.2's addressable KV
  * and of the copy-on-write pool above.)  Fields said to be 0 that are not, and
- * flags that are not named here -> PCS_E_INVAL.
+ * flags that are not named here -> PCS_E_INVAL.  These calls can be captured into
+ * a graph; attention that needs working memory takes memory of its own then, a few
+ * MB that stay with the context until pcs_destroy, which has to outlive the graph.
  */
 
 /* Heads of tokens: element d of head h of token t is at
@@ -701,8 +706,26 @@ typedef struct pcs_kv_cache {
     int32_t heads, head_dim; /* head_dim: a multiple of 8, 8..128           */
     int32_t sinks;           /* first tokens that stay                      */
     int32_t ring;            /* slots reused in turn; 0: every token stays  */
-    uint32_t dtype;          /* PCS_DT_F16 or PCS_DT_BF16                   */
+    uint32_t dtype;          /* PCS_DT_F16, PCS_DT_BF16, PCS_DT_E4M3, _I8   */
 } pcs_kv_cache;
+
+/*
+ * Caches in 8 bits (dtype PCS_DT_E4M3 or PCS_DT_I8): elements are bytes, strides
+ * and the pools' addresses multiples of 16, head_dim a multiple of 16.  Behind
+ * the codes of a row, at heads * head_stride from its beginning, lies one byte
+ * b a head (so row_stride >= heads * head_stride + heads, head_stride >=
+ * head_dim): element d of the head stands for code_d * 2^(b - 127), b = 255 for
+ * NaN throughout.  A row is one run of bytes, so a RING section or a pool's page
+ * holds codes and scales together.  (Powers of two cost 8-bit floats nothing,
+ * whole numbers one bit at most; what a code stands for is exact in bfloat16, and
+ * a byte a head is 0.8 to 1.6 % of its codes.)
+ * pcs_kv_append writes: e is the least whole number from -126 on with
+ * max |x_d| <= 448 * 2^e (E4M3) or 127 * 2^e (I8), b = e + 127, and code_d is
+ * x_d / 2^e rounded to nearest, ties to even.  x is the key as its 16-bit type
+ * holds it once it is rotated, or the value; a head with an infinity or NaN gets
+ * b = 255 and codes 0.  Queries, keys and values are PCS_DT_F16 or PCS_DT_BF16,
+ * all of a call the same.
+ */
 
 /* The new tokens of a call: rows [q_off[s], q_off[s + 1]) of its tensors are
  * the last tokens of session s, whose length with them is lens[s]. */
@@ -766,6 +789,58 @@ pcs_status pcs_kv_append(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_b
 pcs_status pcs_attend(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_batch *batch,
                       const pcs_attend_params *params, const pcs_heads *q, const pcs_heads *out,
                       float *lse, void *stream);
+
+/*
+ * The same for drafted tokens that form a tree: a session's new tokens are its
+ * nodes, parent[t] (device int32 [tokens], for row t of the call) is the number
+ * among the session's new tokens of the node that t follows, smaller than its
+ * own, or -1 if t follows the context.  Node i lies in the slot of position
+ * first + i, first = lens[s] - its new tokens (as pcs_kv_append put it there),
+ * but its position is first + depth, depth the number of its ancestors: what its
+ * query and key are rotated by, and what the window counts from.  It sees the
+ * tokens of the context as pcs_attend's token at that position does, and of its
+ * ancestors and itself those that the window leaves (or whose position is below
+ * sinks).  At most 64 nodes a session and, with a ring, no more than it has slots
+ * (PCS_E_INVAL).  A parent that is not among -1 .. i - 1 -> PCS_E_RANGE at the
+ * next pcs_sync; that node counts as one that follows the context.
+ */
+#define PCS_TREE_MAX 64
+pcs_status pcs_attend_tree(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_batch *batch,
+                           const pcs_attend_params *params, const int32_t *parent,
+                           const pcs_heads *q, const pcs_heads *out, float *lse, void *stream);
+
+/*
+ * Keep some of the new tokens, for example a tree's accepted path: row
+ * index[s][i] of session s's new tokens, i < count[s], moves to the slot of
+ * position first + i (first as above), keys and values; what the others wrote is
+ * dead once the session's length is first + count[s], which goes to lens_out[s]
+ * (device int32 [sessions], or NULL; may be batch->lens).
+ *   index   device int32 [sessions][index_stride], ascending in a session, of
+ *           whose rows the first `most` elements are looked at
+ *   count   device int32 [sessions], at most `most`
+ * With a ring the tokens that the dead ones overwrote are gone: keep ring >=
+ * window + new tokens, and no more new tokens than the ring has slots
+ * (PCS_E_INVAL).  Indices that do not ascend within the new tokens, a count beyond
+ * `most`, page ids outside the pool, slots beyond the table, a kept token
+ * whose own page is empty while the one it goes to is not -> PCS_E_RANGE at the
+ * next pcs_sync (the first two leave the session and its length as they are).
+ * Pages shared with a fork have to be made the session's own first.
+ */
+pcs_status pcs_kv_keep(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_batch *batch,
+                       const int32_t *index, int64_t index_stride, int32_t most,
+                       const int32_t *count, int32_t *lens_out, void *stream);
+
+/*
+ * Read tokens of the cache: the batch's rows [q_off[s], q_off[s + 1]) are the last
+ * tokens of session s (all of them, where it has lens[s] rows), and get what the
+ * cache's keys and values stand for, 0 for tokens that are not there (overwritten
+ * in the ring, or in no page).  k or v may be NULL.  An 8-bit cache is read
+ * as PCS_DT_F16 (magnitudes beyond 65504 come out as 65504), PCS_DT_BF16 or
+ * PCS_DT_F32, one of 16 bits as it is; any strides of 16-byte multiples
+ * (else PCS_E_ALIGN).
+ */
+pcs_status pcs_kv_read(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_batch *batch,
+                       const pcs_heads *k, const pcs_heads *v, void *stream);
 
 /*
  * Fingerprints without any allocation.  The paper has no counterpart: this is

@@ -103,11 +103,13 @@ bool vector_rows(const pcs_heads& h) {
 pcs_status check_cache(const pcs_kv_cache* c, CacheDev* d) {
   if (!c) return op_fail(PCS_E_INVAL, "cache is null");
   if (!c->k || !c->v || !c->table) return op_fail(PCS_E_INVAL, "cache: null pools or table");
-  if (c->dtype != PCS_DT_F16 && c->dtype != PCS_DT_BF16)
-    return op_fail(PCS_E_INVAL, "cache: element type %u (F16 or BF16)", c->dtype);
+  const bool codes = c->dtype == PCS_DT_E4M3 || c->dtype == PCS_DT_I8;
+  if (c->dtype != PCS_DT_F16 && c->dtype != PCS_DT_BF16 && !codes)
+    return op_fail(PCS_E_INVAL, "cache: element type %u (F16, BF16, E4M3 or I8)", c->dtype);
   if (c->heads < 1 || c->heads > 65535) return op_fail(PCS_E_INVAL, "cache: %d heads", c->heads);
-  if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8 != 0)
-    return op_fail(PCS_E_INVAL, "cache: heads of %d elements (a multiple of 8 up to 128)", c->head_dim);
+  const int32_t part = codes ? 16 : 8;  // elements of 16 bytes
+  if (c->head_dim < part || c->head_dim > 128 || c->head_dim % part != 0)
+    return op_fail(PCS_E_INVAL, "cache: heads of %d elements (a multiple of %d up to 128)", c->head_dim, part);
   if (c->n_pages < 1 || c->page_rows < 1 || c->table_pages < 1)
     return op_fail(PCS_E_INVAL, "cache: n_pages, page_rows and table_pages must be positive");
   const int64_t slots = static_cast<int64_t>(c->page_rows) * c->table_pages;
@@ -120,16 +122,26 @@ pcs_status check_cache(const pcs_kv_cache* c, CacheDev* d) {
                    static_cast<long long>(slots));
   if (c->page_stride < 0 || c->row_stride < 0 || c->head_stride < 0)
     return op_fail(PCS_E_INVAL, "cache: negative stride");
-  if (!aligned(c->k, 16) || !aligned(c->v, 16) || c->page_stride % 8 || c->row_stride % 8 || c->head_stride % 8)
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || c->page_stride % part || c->row_stride % part || c->head_stride % part)
     return op_fail(PCS_E_ALIGN, "cache: pools and strides must be multiples of 16 bytes");
+  if (codes) {
+    if (c->head_stride < c->head_dim || c->head_stride > 0x7FFF)
+      return op_fail(PCS_E_INVAL, "cache: head_stride %lld of %d codes", static_cast<long long>(c->head_stride), c->head_dim);
+    d->scale_at = static_cast<int32_t>(c->heads * c->head_stride);
+    if (c->row_stride < static_cast<int64_t>(d->scale_at) + c->heads)
+      return op_fail(PCS_E_INVAL, "cache: rows of %lld bytes do not hold %d heads and their scales",
+                     static_cast<long long>(c->row_stride), c->heads);
+  }
+  const int64_t size = codes ? 1 : 2;
+  d->codes = c->dtype == PCS_DT_E4M3 ? kCodesE4M3 : c->dtype == PCS_DT_I8 ? kCodesI8 : kElements16;
   d->k = static_cast<uint8_t*>(c->k);
   d->v = static_cast<uint8_t*>(c->v);
   d->table = c->table;
   d->v_table = c->v_table;
   d->table_stride = c->table_stride;
-  d->page_bytes = 2 * c->page_stride;
-  d->row_bytes = 2 * c->row_stride;
-  d->head_bytes = 2 * c->head_stride;
+  d->page_bytes = size * c->page_stride;
+  d->row_bytes = size * c->row_stride;
+  d->head_bytes = size * c->head_stride;
   const uint64_t unit = std::gcd(static_cast<uint64_t>(d->page_bytes), static_cast<uint64_t>(d->row_bytes));
   d->unit = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(unit, 16), 0x7FFFFFF0u));
   if (d->page_bytes % d->unit || d->row_bytes % d->unit) d->unit = 16;
@@ -213,6 +225,165 @@ void add_tensor(RotArgs* a, const pcs_heads& x, const pcs_heads* y, int role) {
 // Whether heads are whole vectors.
 bool vector_parts(const RotArgs& a, uint32_t dtype) { return a.head_dim % (16 / elem_bytes(dtype)) == 0; }
 
+// Working memory of a call.  A stream's own is handed from call to call by events,
+// which a graph that is run again and again cannot follow: a call that is being
+// captured gets memory of its own, that no other graph or call uses, for the
+// context's lifetime.  Its words are put to zero in the graph.
+pcs_status working_memory(OpCall& call, uint64_t bytes, uint8_t** out, uint32_t** words) {
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(call.stream(), &capture);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return op_fail(PCS_E_CUDA, "the stream's capture: %s", cudaGetErrorString(e));
+  }
+  if (capture == cudaStreamCaptureStatusNone) return call.scratch(bytes, out, words);
+  constexpr uint64_t head = 4 * static_cast<uint64_t>(kOpWords);
+  void* p = nullptr;
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  cudaThreadExchangeStreamCaptureMode(&mode);
+  e = cudaMalloc(&p, head + bytes);
+  cudaThreadExchangeStreamCaptureMode(&mode);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return op_fail(PCS_E_NOMEM, "cannot allocate %llu bytes for a captured call", static_cast<unsigned long long>(head + bytes));
+  }
+  call.keep(p);
+  e = cudaMemsetAsync(p, 0, head, call.stream());
+  if (e != cudaSuccess) return op_fail(PCS_E_CUDA, "%s", cudaGetErrorString(e));
+  *words = static_cast<uint32_t*>(p);
+  *out = static_cast<uint8_t*>(p) + head;
+  return PCS_OK;
+}
+
+// A tree's nodes, and tokens of which some are kept, all have to be in the cache.
+pcs_status check_ring(const CacheDev& c, const BatchDev& b) {
+  if (c.ring_rows && b.max_new > c.ring_rows)
+    return op_fail(PCS_E_INVAL, "%d new tokens in a ring of %d slots", b.max_new, c.ring_rows);
+  return PCS_OK;
+}
+
+pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batch* batch,
+                  const pcs_attend_params* params, bool tree, const int32_t* parent, const pcs_heads* q,
+                  const pcs_heads* out, float* lse, void* stream) {
+  return guarded([&]() -> pcs_status {
+    OpCall call(ctx, name, stream);
+    if (!ctx) return op_fail(PCS_E_INVAL, "ctx is null");
+    AttendArgs a = {};
+    pcs_status st = check_cache(cache, &a.cache);
+    if (!st) st = check_batch(batch, &a.batch);
+    if (st) return st;
+    if (!params) return op_fail(PCS_E_INVAL, "params is null");
+    if (params->flags || params->reserved)
+      return op_fail(PCS_E_INVAL, "params: flags (0x%x) and reserved must be 0", params->flags);
+    if (params->window < 0) return op_fail(PCS_E_INVAL, "negative window");
+    if (!(params->scale >= 0.0f) || std::isinf(params->scale))
+      return op_fail(PCS_E_INVAL, "scale must be finite and positive (0: 1 / sqrt(head_dim))");
+    if (a.batch.tokens == 0) return PCS_OK;
+    const bool codes = a.cache.codes != kElements16;
+    if (codes && q && q->dtype != PCS_DT_F16 && q->dtype != PCS_DT_BF16)
+      return op_fail(PCS_E_INVAL, "q: element type %u (F16 or BF16)", q->dtype);
+    const uint32_t dtype = codes && q ? q->dtype : cache->dtype;
+    st = check_heads(q, "q", dtype, cache->head_dim);
+    if (!st) st = check_heads(out, "out", dtype, cache->head_dim);
+    if (st) return st;
+    if (q->heads % cache->heads != 0)
+      return op_fail(PCS_E_INVAL, "%d query heads over %d heads of the cache", q->heads, cache->heads);
+    if (out->heads != q->heads) return op_fail(PCS_E_INVAL, "q and out differ in heads");
+    if (!vector_rows(*q) || !vector_rows(*out))
+      return op_fail(PCS_E_ALIGN, "q, out and their strides must be multiples of 16 bytes");
+    a.q = {static_cast<uint8_t*>(q->data), 2 * q->token_stride, 2 * q->head_stride};
+    a.out = {static_cast<uint8_t*>(out->data), 2 * out->token_stride, 2 * out->head_stride};
+    a.lse = lse;
+    const double scale = params->scale > 0.0f ? params->scale : 1.0 / std::sqrt(double(cache->head_dim));
+    a.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
+    a.window = params->window;
+    a.group = q->heads / cache->heads;
+    a.by_group.set(a.group);
+
+    a.dtype = dtype;
+    if (tree) {
+      if (!parent) return op_fail(PCS_E_INVAL, "parent is null");
+      if (a.batch.max_new > PCS_TREE_MAX)
+        return op_fail(PCS_E_INVAL, "a tree of %d tokens (at most %d)", a.batch.max_new, PCS_TREE_MAX);
+      if ((st = check_ring(a.cache, a.batch))) return st;
+      a.parent = parent;
+    }
+
+    const int64_t rows = static_cast<int64_t>(a.batch.max_new) * a.group;
+    // Few rows of a key head, bound by HBM, go to the token kernel: up to 16, and
+    // up to 32 where sessions and heads alone would leave SMs without a block of
+    // the other one.  (64 sessions of 500 to 4,000 tokens, 4 key heads of 128:
+    // 8 rows 60 us, and 79 us by blocks; 16 rows 69 and 79; 32 rows 113 and 80.
+    // One session of 100,000 tokens, 32 rows: 60 and 112 us.)
+    const int64_t pairs = static_cast<int64_t>(a.batch.sessions) * cache->heads;
+    if ((st = call.begin())) return st;
+    a.err = call.errors();
+    const bool few = rows <= 16 || (rows <= kTokenRowsMax && pairs < call.sm_count());
+    // Tokens that the rows of a block see at most, as far as the host knows: a
+    // hint for the split, which is right for any length.
+    int64_t seen = cache->ring ? static_cast<int64_t>(cache->sinks) + cache->ring : a.cache.slots;
+    if (batch->max_len) seen = std::min<int64_t>(seen, batch->max_len);
+    const int64_t tokens = few || tree ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
+    if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
+    if (few) {
+      const int64_t resident =
+          static_cast<int64_t>(call.sm_count()) * (codes ? attend_token8_blocks_per_sm(cache->head_dim, static_cast<int>(rows))
+                                                         : attend_token_blocks_per_sm(cache->head_dim, static_cast<int>(rows)));
+      const int64_t tiles = (seen + 15) / 16;
+      // Parts for a wave of blocks, of two tiles a warp at least; and of several
+      // sessions, whose lengths may differ, up to four waves of parts of eight
+      // tiles a warp.  (48 sessions of 1 to 12,000 tokens: 217 us in one wave,
+      // 196 us in four; one of 200,001 tokens, when measured: 163 and 196 us.)
+      int64_t splits = std::min(resident / pairs, tiles / (2 * kTokenWarps));
+      if (splits > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin, std::min(splits, tiles / (4 * kTokenWarps)));
+      if (a.batch.sessions > 1)
+        splits = std::max(splits, std::min(4 * resident / pairs, tiles / (8 * kTokenWarps)));
+      splits = std::max<int64_t>(splits, 1);
+      const bool own = splits <= kTokenOwnJoin && pairs <= kOpWords;
+      a.splits = static_cast<int32_t>(splits);
+      if (pairs * splits > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
+      if (splits > 1) {
+        uint8_t* ws = nullptr;
+        uint32_t* words = nullptr;
+        st = working_memory(call, 4 * token_part_floats(static_cast<int>(rows), cache->head_dim) * pairs * splits, &ws, &words);
+        if (st) return st;
+        a.part = reinterpret_cast<float*>(ws);
+        a.ticket = own ? words : nullptr;
+      }
+      call.before(kOpAttendToken);
+      st = call.after(launch_attend_token(a, dtype, static_cast<int>(rows), false, call.stream()));
+      if (!st && splits > 1 && !own) {
+        call.before(kOpAttendJoin);
+        st = call.after(launch_attend_token(a, dtype, static_cast<int>(rows), true, call.stream()));
+      }
+      return st ? st : call.end();
+    }
+    const int64_t blocks = (rows + kBlockRows - 1) / kBlockRows;
+    if (blocks > 0x7FFFFFFFll / pairs) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
+    const int64_t tiles = (seen + kBlockTile - 1) / kBlockTile;
+    int64_t splits = std::max<int64_t>(1, std::min(call.sm_count() / (pairs * blocks), tiles / 4));
+    a.splits = static_cast<int32_t>(splits);
+    if (splits > 1) {
+      uint8_t* ws = nullptr;
+      uint32_t* words = nullptr;
+      st = working_memory(call, 4 * block_part_floats(cache->head_dim) * splits * pairs * blocks, &ws, &words);
+      if (st) return st;
+      a.part = reinterpret_cast<float*>(ws);
+    }
+    TensorMaps maps = {};
+    a.box_rows = codes ? 0 : box_rows(*cache);
+    if (a.box_rows && !(encode_pool(*cache, cache->k, a.box_rows, maps.k) && encode_pool(*cache, cache->v, a.box_rows, maps.v)))
+      a.box_rows = 0;
+    call.before(kOpAttendBlock);
+    if ((st = call.after(launch_attend_block(a, dtype, static_cast<int>(blocks), maps, call.stream())))) return st;
+    if (splits > 1) {
+      call.before(kOpAttendJoin);
+      if ((st = call.after(launch_attend_join(a, dtype, static_cast<int>(blocks), call.stream())))) return st;
+    }
+    return call.end();
+  });
+}
+
 }  // namespace
 
 extern "C" {
@@ -264,7 +435,11 @@ pcs_status pcs_kv_append(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_b
     if (!st) st = check_batch(batch, &a.batch);
     if (st) return st;
     if (a.batch.tokens == 0) return PCS_OK;
-    const uint32_t dtype = cache->dtype;
+    // (A cache in 8 bits takes either 16-bit type.)
+    const bool codes = a.cache.codes != kElements16;
+    if (codes && k && k->dtype != PCS_DT_F16 && k->dtype != PCS_DT_BF16)
+      return op_fail(PCS_E_INVAL, "k: element type %u (F16 or BF16)", k->dtype);
+    const uint32_t dtype = codes && k ? k->dtype : cache->dtype;
     a.head_dim = cache->head_dim;
     a.tokens = a.batch.tokens;
     a.axes = 1;
@@ -289,6 +464,10 @@ pcs_status pcs_kv_append(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_b
     add_tensor(&a, *v, nullptr, 2);
     if ((st = call.begin())) return st;
     a.err = call.errors();
+    if (codes) {
+      call.before(kOpStore);
+      return call.after(launch_store(a, dtype, vec, call.sm_count(), call.stream()));
+    }
     call.before(kOpAppend);
     return call.after(launch_rotate(a, dtype, true, vec, call.sm_count(), call.stream()));
   });
@@ -297,108 +476,70 @@ pcs_status pcs_kv_append(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_b
 pcs_status pcs_attend(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batch* batch,
                       const pcs_attend_params* params, const pcs_heads* q, const pcs_heads* out,
                       float* lse, void* stream) {
+  return attend("pcs_attend", ctx, cache, batch, params, false, nullptr, q, out, lse, stream);
+}
+
+pcs_status pcs_attend_tree(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batch* batch,
+                           const pcs_attend_params* params, const int32_t* parent, const pcs_heads* q,
+                           const pcs_heads* out, float* lse, void* stream) {
+  return attend("pcs_attend_tree", ctx, cache, batch, params, true, parent, q, out, lse, stream);
+}
+
+pcs_status pcs_kv_keep(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batch* batch, const int32_t* index,
+                       int64_t index_stride, int32_t most, const int32_t* count, int32_t* lens_out, void* stream) {
   return guarded([&]() -> pcs_status {
-    OpCall call(ctx, "pcs_attend", stream);
+    OpCall call(ctx, "pcs_kv_keep", stream);
     if (!ctx) return op_fail(PCS_E_INVAL, "ctx is null");
-    AttendArgs a = {};
+    KeepArgs a = {};
     pcs_status st = check_cache(cache, &a.cache);
     if (!st) st = check_batch(batch, &a.batch);
     if (st) return st;
-    if (!params) return op_fail(PCS_E_INVAL, "params is null");
-    if (params->flags || params->reserved)
-      return op_fail(PCS_E_INVAL, "params: flags (0x%x) and reserved must be 0", params->flags);
-    if (params->window < 0) return op_fail(PCS_E_INVAL, "negative window");
-    if (!(params->scale >= 0.0f) || std::isinf(params->scale))
-      return op_fail(PCS_E_INVAL, "scale must be finite and positive (0: 1 / sqrt(head_dim))");
-    if (a.batch.tokens == 0) return PCS_OK;
-    st = check_heads(q, "q", cache->dtype, cache->head_dim);
-    if (!st) st = check_heads(out, "out", cache->dtype, cache->head_dim);
-    if (st) return st;
-    if (q->heads % cache->heads != 0)
-      return op_fail(PCS_E_INVAL, "%d query heads over %d heads of the cache", q->heads, cache->heads);
-    if (out->heads != q->heads) return op_fail(PCS_E_INVAL, "q and out differ in heads");
-    if (!vector_rows(*q) || !vector_rows(*out))
-      return op_fail(PCS_E_ALIGN, "q, out and their strides must be multiples of 16 bytes");
-    a.q = {static_cast<uint8_t*>(q->data), 2 * q->token_stride, 2 * q->head_stride};
-    a.out = {static_cast<uint8_t*>(out->data), 2 * out->token_stride, 2 * out->head_stride};
-    a.lse = lse;
-    const double scale = params->scale > 0.0f ? params->scale : 1.0 / std::sqrt(double(cache->head_dim));
-    a.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
-    a.window = params->window;
-    a.group = q->heads / cache->heads;
-    a.by_group.set(a.group);
-
-    const int64_t rows = static_cast<int64_t>(a.batch.max_new) * a.group;
-    // Few rows of a key head, bound by HBM, go to the token kernel: up to 16, and
-    // up to 32 where sessions and heads alone would leave SMs without a block of
-    // the other one.  (64 sessions of 500 to 4,000 tokens, 4 key heads of 128:
-    // 8 rows 60 us, and 79 us by blocks; 16 rows 69 and 79; 32 rows 113 and 80.
-    // One session of 100,000 tokens, 32 rows: 60 and 112 us.)
-    const int64_t pairs = static_cast<int64_t>(a.batch.sessions) * cache->heads;
+    if (a.batch.sessions == 0) return PCS_OK;
+    if (!index || !count) return op_fail(PCS_E_INVAL, "index or count is null");
+    if (most < 0 || index_stride < most)
+      return op_fail(PCS_E_INVAL, "index: rows of %d elements, %lld apart", most, static_cast<long long>(index_stride));
+    if ((st = check_ring(a.cache, a.batch))) return st;
+    a.index = index;
+    a.index_stride = index_stride;
+    a.count = count;
+    a.lens_out = lens_out;
+    a.most = most;
     if ((st = call.begin())) return st;
     a.err = call.errors();
-    const bool few = rows <= 16 || (rows <= kTokenRowsMax && pairs < call.sm_count());
-    // Tokens that the rows of a block see at most, as far as the host knows: a
-    // hint for the split, which is right for any length.
-    int64_t seen = cache->ring ? static_cast<int64_t>(cache->sinks) + cache->ring : a.cache.slots;
-    if (batch->max_len) seen = std::min<int64_t>(seen, batch->max_len);
-    const int64_t tokens = few ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
-    if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
-    if (few) {
-      const int64_t resident =
-          static_cast<int64_t>(call.sm_count()) * attend_token_blocks_per_sm(cache->head_dim, static_cast<int>(rows));
-      const int64_t tiles = (seen + 15) / 16;
-      // Parts for a wave of blocks, of two tiles a warp at least; and of several
-      // sessions, whose lengths may differ, up to four waves of parts of eight
-      // tiles a warp.  (48 sessions of 1 to 12,000 tokens: 217 us in one wave,
-      // 196 us in four; one of 200,001 tokens, when measured: 163 and 196 us.)
-      int64_t splits = std::min(resident / pairs, tiles / (2 * kTokenWarps));
-      if (splits > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin, std::min(splits, tiles / (4 * kTokenWarps)));
-      if (a.batch.sessions > 1)
-        splits = std::max(splits, std::min(4 * resident / pairs, tiles / (8 * kTokenWarps)));
-      splits = std::max<int64_t>(splits, 1);
-      const bool own = splits <= kTokenOwnJoin && pairs <= kOpWords;
-      a.splits = static_cast<int32_t>(splits);
-      if (pairs * splits > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
-      if (splits > 1) {
-        uint8_t* ws = nullptr;
-        uint32_t* words = nullptr;
-        st = call.scratch(4 * token_part_floats(static_cast<int>(rows), cache->head_dim) * pairs * splits, &ws, &words);
-        if (st) return st;
-        a.part = reinterpret_cast<float*>(ws);
-        a.ticket = own ? words : nullptr;
-      }
-      call.before(kOpAttendToken);
-      st = call.after(launch_attend_token(a, cache->dtype, static_cast<int>(rows), false, call.stream()));
-      if (!st && splits > 1 && !own) {
-        call.before(kOpAttendJoin);
-        st = call.after(launch_attend_token(a, cache->dtype, static_cast<int>(rows), true, call.stream()));
-      }
-      return st ? st : call.end();
+    call.before(kOpKeep);
+    return call.after(launch_keep(a, call.stream()));
+  });
+}
+
+pcs_status pcs_kv_read(pcs_ctx* ctx, const pcs_kv_cache* cache, const pcs_kv_batch* batch, const pcs_heads* k,
+                       const pcs_heads* v, void* stream) {
+  return guarded([&]() -> pcs_status {
+    OpCall call(ctx, "pcs_kv_read", stream);
+    if (!ctx) return op_fail(PCS_E_INVAL, "ctx is null");
+    ReadArgs a = {};
+    pcs_status st = check_cache(cache, &a.cache);
+    if (!st) st = check_batch(batch, &a.batch);
+    if (st) return st;
+    if (a.batch.tokens == 0 || (!k && !v)) return PCS_OK;
+    a.dtype = k ? k->dtype : v->dtype;
+    const bool fits = a.cache.codes == kElements16 ? a.dtype == cache->dtype : elem_bytes(a.dtype) != 0;
+    if (!fits) return op_fail(PCS_E_INVAL, "k, v: element type %u of a cache of type %u", a.dtype, cache->dtype);
+    const pcs_heads* out[2] = {k, v};
+    for (int i = 0; i < 2 && !st; ++i) {
+      const char* what = i ? "v" : "k";
+      if (!out[i]) continue;
+      st = check_heads(out[i], what, a.dtype, cache->head_dim);
+      if (st) break;
+      if (out[i]->heads != cache->heads) return op_fail(PCS_E_INVAL, "%s must have the cache's %d heads", what, cache->heads);
+      if (!vector_rows(*out[i])) return op_fail(PCS_E_ALIGN, "%s and its strides must be multiples of 16 bytes", what);
+      const int e = elem_bytes(a.dtype);
+      a.out[i] = {static_cast<uint8_t*>(out[i]->data), e * out[i]->token_stride, e * out[i]->head_stride};
     }
-    const int64_t blocks = (rows + kBlockRows - 1) / kBlockRows;
-    if (blocks > 0x7FFFFFFFll / pairs) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
-    const int64_t tiles = (seen + kBlockTile - 1) / kBlockTile;
-    int64_t splits = std::max<int64_t>(1, std::min(call.sm_count() / (pairs * blocks), tiles / 4));
-    a.splits = static_cast<int32_t>(splits);
-    if (splits > 1) {
-      uint8_t* ws = nullptr;
-      uint32_t* words = nullptr;
-      st = call.scratch(4 * block_part_floats(cache->head_dim) * splits * pairs * blocks, &ws, &words);
-      if (st) return st;
-      a.part = reinterpret_cast<float*>(ws);
-    }
-    TensorMaps maps = {};
-    a.box_rows = box_rows(*cache);
-    if (a.box_rows && !(encode_pool(*cache, cache->k, a.box_rows, maps.k) && encode_pool(*cache, cache->v, a.box_rows, maps.v)))
-      a.box_rows = 0;
-    call.before(kOpAttendBlock);
-    if ((st = call.after(launch_attend_block(a, cache->dtype, static_cast<int>(blocks), maps, call.stream())))) return st;
-    if (splits > 1) {
-      call.before(kOpAttendJoin);
-      if ((st = call.after(launch_attend_join(a, cache->dtype, static_cast<int>(blocks), call.stream())))) return st;
-    }
-    return call.end();
+    if (st) return st;
+    if ((st = call.begin())) return st;
+    a.err = call.errors();
+    call.before(kOpRead);
+    return call.after(launch_read(a, call.sm_count(), call.stream()));
   });
 }
 

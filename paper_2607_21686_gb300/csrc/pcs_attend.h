@@ -15,7 +15,7 @@ namespace pcs {
 // ---- One call on a context ---------------------------------------------------
 
 // Kernels of the operators, in the order of their names in the timing table.
-enum OpKernel { kOpRotate, kOpAppend, kOpAttendToken, kOpAttendBlock, kOpAttendJoin };
+enum OpKernel { kOpRotate, kOpAppend, kOpAttendToken, kOpAttendBlock, kOpAttendJoin, kOpStore, kOpRead, kOpKeep };
 
 // Words of a call that are zero on entry and have to be on exit.
 constexpr int kOpWords = 1024;
@@ -35,6 +35,8 @@ class OpCall {
   // `bytes` of device memory (256-byte aligned) that are the call's until its
   // end on the stream, and kOpWords words.
   pcs_status scratch(uint64_t bytes, uint8_t** out, uint32_t** words);
+  // Device memory that lives as long as the context.
+  void keep(void* buffer);
   // Around each launch: counts and times it.
   void before(OpKernel k);
   pcs_status after(cudaError_t e);
@@ -71,6 +73,9 @@ struct FastDiv {
 
 // ---- The cache and the sessions of a call -----------------------------------------
 
+// What an element of the cache is.
+enum Codes : int32_t { kElements16, kCodesE4M3, kCodesI8 };
+
 struct CacheDev {
   uint8_t* k;
   uint8_t* v;
@@ -85,6 +90,8 @@ struct CacheDev {
   int32_t heads, head_dim;
   int32_t sinks;
   int32_t ring_rows;        // 0: none
+  int32_t codes;            // Codes
+  int32_t scale_at;         // 8 bits: a row's scale bytes, from its beginning
 
   __host__ __device__ __forceinline__ uint32_t slot_of(uint32_t p) const {
     if (ring_rows == 0 || p < static_cast<uint32_t>(sinks)) return p;
@@ -138,6 +145,31 @@ struct RotArgs {
 // multiples of 16 bytes.
 cudaError_t launch_rotate(const RotArgs& a, uint32_t dtype, bool paged, bool vec, int sm_count,
                           cudaStream_t stream);
+// Append to a cache in 8 bits.
+cudaError_t launch_store(const RotArgs& a, uint32_t dtype, bool vec, int sm_count, cudaStream_t stream);
+
+// ---- Read back, keep -----------------------------------------------------------------
+
+struct ReadArgs {
+  CacheDev cache;
+  BatchDev batch;
+  HeadsDev out[2];         // keys, values; null data: not wanted
+  uint32_t dtype;          // of out
+  uint32_t* err;
+};
+cudaError_t launch_read(const ReadArgs& a, int sm_count, cudaStream_t stream);
+
+struct KeepArgs {
+  CacheDev cache;
+  BatchDev batch;
+  const int32_t* index;    // [sessions][index_stride]
+  int64_t index_stride;
+  const int32_t* count;
+  int32_t* lens_out;
+  int32_t most;
+  uint32_t* err;
+};
+cudaError_t launch_keep(const KeepArgs& a, cudaStream_t stream);
 
 // ---- Attention -------------------------------------------------------------------------
 
@@ -155,6 +187,8 @@ struct AttendArgs {
   uint32_t* ticket;        // token kernel: zero on entry and on exit; null: parts are joined later
   int32_t box_rows;        // block kernel: rows of a tensor copy, 0: rows are copied one by one
   uint32_t* err;
+  const int32_t* parent;   // new tokens form trees; null: each sees those before it
+  uint32_t dtype;          // of q and out
 };
 
 // One row is one query head of one new token; the token kernel takes all rows
@@ -170,8 +204,12 @@ inline uint64_t token_part_floats(int rows, int head_dim) {
 // kTokenOwnJoin of them (a.ticket), else by a second launch (`join`).
 constexpr int kTokenOwnJoin = 16;
 cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream);
+// Forms of it: trees over 16-bit elements, anything over 8-bit codes.
+cudaError_t launch_attend_token_tree(const AttendArgs& a, uint32_t dtype, int rows, cudaStream_t stream);
+cudaError_t launch_attend_token8(const AttendArgs& a, int rows, cudaStream_t stream);
 // Blocks of the token kernel that one SM holds, for `rows` rows a key head.
 int attend_token_blocks_per_sm(int head_dim, int rows);
+int attend_token8_blocks_per_sm(int head_dim, int rows);
 
 // The block kernel: a session and key head's rows in blocks of kBlockRows,
 // `blocks` of them at most.  With splits > 1 a block's part is its rows' sums,
@@ -185,6 +223,10 @@ struct alignas(64) TensorMaps {
 };
 cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
                                 cudaStream_t stream);
+// Forms of it: trees over 16-bit elements, anything over 8-bit codes.
+cudaError_t launch_attend_block_tree(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
+                                     cudaStream_t stream);
+cudaError_t launch_attend_block8(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream);
 
 }  // namespace pcs

@@ -1,0 +1,27 @@
+// pcs_attend_block8.cu -- attention of blocks of new tokens, trees among them, over a
+// paged cache in 8 bits: the kernel of pcs_attend_block.cu, whose copying warps turn
+// codes into elements of the queries' type on their way to the tiles.  That is exact
+// in bfloat16, whose 8 bits hold every code and whose powers of two every scale; a
+// float16 ends at 65504.
+#include "pcs_attend_block_dev.h"
+
+namespace pcs {
+namespace {
+
+template <typename T, int DP>
+cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t stream) {
+  const TensorMaps none = {};
+  return a.parent ? launch_form<T, DP, kCodes, true>(a, blocks, none, stream)
+                  : launch_form<T, DP, kCodes, false>(a, blocks, none, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_block8(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream) {
+  if (dtype == PCS_DT_F16)
+    return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, stream) : launch<__half, 128>(a, blocks, stream);
+  return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, stream)
+                                : launch<__nv_bfloat16, 128>(a, blocks, stream);
+}
+
+}  // namespace pcs

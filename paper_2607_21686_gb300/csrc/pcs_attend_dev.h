@@ -139,4 +139,29 @@ __device__ __forceinline__ const uint8_t* row_at(const AttendArgs& a, const uint
   return base + static_cast<uint64_t>(off) * a.cache.unit;
 }
 
+// A session's nodes into shared memory, by the block's threads (at least
+// PCS_TREE_MAX of them): their parents first, then a thread a node.  (A parent that is
+// not there or not before its child counts as the context and is reported.)
+__device__ __forceinline__ void tree_nodes(const AttendArgs& a, const SessionView& v, int tid, TreeNode* nodes) {
+  __shared__ int32_t parents[PCS_TREE_MAX];
+  const int m = min(v.m, PCS_TREE_MAX);
+  if (tid < m) {
+    const int32_t p = __ldg(a.parent + v.q0 + tid);
+    const bool fine = p >= -1 && p < tid;
+    if (!fine) atomicOr(a.err, kDevErrIndex);
+    parents[tid] = fine ? p : -1;
+  }
+  __syncthreads();
+  if (tid < m) nodes[tid] = tree_node(a, v.first, [&](int k) { return parents[k]; }, tid);
+}
+
+// Whether some of eight elements are infinite or NaN: the lowest bit of an
+// exponent added to one of all ones carries into the sign's place.
+template <typename T>
+__device__ __forceinline__ bool has_specials(const uint4& v) {
+  constexpr uint32_t e = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
+  constexpr uint32_t one = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+  return ((((v.x & e) + one) | ((v.y & e) + one) | ((v.z & e) + one) | ((v.w & e) + one)) & 0x80008000u) != 0;
+}
+
 }  // namespace pcs

@@ -119,4 +119,70 @@ __host__ __device__ __forceinline__ RowsRange rows_range(const AttendArgs& a, co
           static_cast<int32_t>((static_cast<uint32_t>(v.gap1) + 127) >> 7)};
 }
 
+// ---- Trees ---------------------------------------------------------------------------
+// The new tokens of a session are nodes: node i lies where the new token i does, at
+// place(first + i), but its position is first + depth.
+
+// Of one node: those new tokens that it sees (itself, its ancestors), as bits.
+struct TreeNode {
+  uint64_t line;
+  int32_t depth;
+};
+
+// `up`: the parents of a session's nodes, each -1 or smaller than its child.
+template <typename Up>
+__host__ __device__ __forceinline__ TreeNode tree_node(const AttendArgs& a, int32_t first, const Up& up, int i) {
+  TreeNode n = {0, 0};
+  for (int k = up(i); k >= 0; k = up(k)) ++n.depth;
+  int behind = 0;  // positions from the ancestor on
+  for (int k = i; k >= 0; k = up(k), ++behind)
+    if (a.window == 0 || behind < a.window || first + n.depth - behind < a.cache.sinks) n.line |= 1ull << k;
+  return n;
+}
+
+// The last place of the context (the tokens before the new ones); -1 or the last of
+// the first tokens' places where it has none else.
+__host__ __device__ __forceinline__ int32_t context_end(const SessionView& v) {
+  const int32_t p = v.first - 1;
+  return p >= v.lo && !(v.apart && p < v.sinks) ? v.place(p) : smaller(p, v.pad - 1);
+}
+
+// What a node sees of a view's tokens: a range of the context, and some new tokens,
+// node k at place base + k, from `split` on (behind the end of a ring) at base2 + k.
+struct TreeRow {
+  RowRange context;
+  uint64_t line;
+  int32_t base, split, base2;
+  static __host__ __device__ __forceinline__ uint32_t moved(uint64_t x, int32_t by) {
+    return by >= 32 || by <= -64 ? 0u : by >= 0 ? static_cast<uint32_t>(x << by) : static_cast<uint32_t>(x >> -by);
+  }
+  // The tokens [b, b + 32) it sees, as bits.
+  __host__ __device__ __forceinline__ uint32_t bits(int32_t b) const {
+    const uint64_t low = split >= 64 ? ~0ull : (1ull << split) - 1;
+    return context.bits(b) | moved(line & low, base - b) | moved(line & ~low, base2 - b);
+  }
+};
+__host__ __device__ __forceinline__ TreeRow tree_row(const AttendArgs& a, const SessionView& v, const TreeNode& n) {
+  TreeRow r;
+  r.context = row_range(a, v, v.first + n.depth);
+  r.context.hi = context_end(v);
+  r.line = n.line;
+  r.base = v.place(v.first);  // (below 0 for a session shorter than its new tokens: one run from place 0)
+  r.split = 64;
+  r.base2 = 0;
+  if (v.wrap != kNever && v.wrap > v.first && v.wrap - v.first < 64) {
+    r.split = v.wrap - v.first;
+    r.base2 = v.gap1 - r.split;
+  }
+  return r;
+}
+
+// Of all nodes up to number t1, as rows_range has it; depths are not looked at: the
+// deepest one may be anywhere up to t1.
+__host__ __device__ __forceinline__ RowsRange tree_rows_range(const AttendArgs& a, const SessionView& v, int t1) {
+  RowsRange r = rows_range(a, v, v.first, v.first + t1);
+  r.all_to = (context_end(v) + 1) >> 7;
+  return r;
+}
+
 }  // namespace pcs

@@ -22,9 +22,12 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <cstring>
+#include <type_traits>
 
 #include "pcs_attend.h"
 #include "pcs_internal.h"
+#include "pcs_place_dev.h"
 
 namespace pcs {
 namespace {
@@ -87,68 +90,6 @@ template <typename T, int N>
 struct alignas(sizeof(T) * N) Run {
   T e[N];
 };
-
-// Where a token's row of the cache is: byte offsets, or -1.
-struct Place {
-  int64_t k, v;
-};
-
-// The last of the sessions whose first token is at most t, by one warp: 32
-// probes at a time.
-__device__ __forceinline__ int session_of(const BatchDev& b, int64_t t, int lane) {
-  int lo = 0, n = b.sessions;  // it is among [lo, lo + n)
-  while (n > 1) {
-    const int step = (n + 31) / 32;
-    const int i = lo + lane * step;
-    const unsigned m = __ballot_sync(0xffffffffu, lane * step < n && __ldg(b.q_off + i) <= t);
-    const int k = m ? 31 - __clz(m) : 0;
-    lo += k * step;
-    n = min(step, n - k * step);
-  }
-  return lo;
-}
-
-__device__ __forceinline__ Place place_of(const RotArgs& a, int64_t t, int s) {
-  const BatchDev& b = a.batch;
-  int at, m;
-  if (b.q_off) {
-    int32_t o = __ldg(b.q_off + s), end = __ldg(b.q_off + s + 1);
-    while (t >= end && s + 1 < b.sessions) {
-      ++s;
-      o = end;
-      end = __ldg(b.q_off + s + 1);
-    }
-    m = end - o;
-    at = static_cast<int>(t - o);
-    if (at < 0 || at >= m) return {-1, -1};
-  } else {
-    s = static_cast<int>(t / b.each);
-    m = b.each;
-    at = static_cast<int>(t - static_cast<int64_t>(s) * m);
-  }
-  const CacheDev& c = a.cache;
-  const int64_t len = __ldg(b.lens + s), p = len - m + at;
-  if (p < 0) {
-    atomicOr(a.err, kDevErrIndex);
-    return {-1, -1};
-  }
-  if (c.ring_rows && p >= c.sinks && p < len - c.ring_rows) return {-1, -1};
-  const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
-  if (slot >= static_cast<uint32_t>(c.slots)) {
-    atomicOr(a.err, kDevErrIndex);
-    return {-1, -1};
-  }
-  const uint32_t page = c.page_rows.div(slot);
-  const int64_t row = static_cast<int64_t>(slot - page * c.page_rows.d) * c.row_bytes;
-  const int64_t e = s * c.table_stride + page;
-  const int32_t kp = __ldg(c.table + e);
-  const int32_t vp = c.v_table ? __ldg(c.v_table + e) : kp;
-  if (kp < 0 || kp >= c.n_pages || vp < 0 || vp >= c.n_pages) {  // neither of them is written
-    if (kp < -1 || kp >= c.n_pages || vp < -1 || vp >= c.n_pages) atomicOr(a.err, kDevErrIndex);
-    return {-1, -1};
-  }
-  return {kp * c.page_bytes + row, vp * c.page_bytes + row};
-}
 
 // How a block's threads share out a head: `units` side by side, `at_once` heads.
 // (A head has at most 256 elements, so no more units than there are threads.)
@@ -220,7 +161,7 @@ __device__ __forceinline__ BlockWork block_setup(const RotArgs& a, int per_block
   const int tid = threadIdx.x, lane = tid & 31;
   if (PAGED && tid >= kThreads - 32 && a.t[b.n1 - 1].role) {  // the last warp looks the tokens up
     const int s = a.batch.q_off ? session_of(a.batch, b.t0, lane) : 0;
-    if (lane < b.nt) place[lane] = place_of(a, b.t0 + lane, s);
+    if (lane < b.nt) place[lane] = place_of(a.cache, a.batch, a.err, b.t0 + lane, s);
   }
   if (b.n0 < a.plain)
     for (int i = tid; i < b.nt * a.pairs; i += kThreads) {
@@ -288,6 +229,159 @@ __global__ void __launch_bounds__(kThreads, 7)
   }
 }
 
+// ---- Append in 8 bits ---------------------------------------------------------------
+
+// What a head's `lanes` lanes share out: units of two runs of VE elements each.
+struct StoreShape {
+  int32_t units, lanes, groups;   // units of a head; lanes a head; heads a block moves at once
+  int32_t turned;                 // units that are turned
+  FastDiv by_heads[kRotTensors];
+};
+
+// Bits of the larger magnitude of two 16-bit floats (infinity and NaN above all).
+template <typename T>
+__device__ __forceinline__ uint32_t magnitude(T x) {
+  uint16_t b;
+  memcpy(&b, &x, 2);
+  return b & 0x7fffu;
+}
+template <typename T>
+__device__ __forceinline__ float magnitude_value(uint32_t bits) {
+  const uint16_t b = static_cast<uint16_t>(bits);
+  T x;
+  memcpy(&x, &b, 2);
+  return to_float(x);
+}
+
+// Scale of a head whose largest magnitude is `top`, finite: the least e >= -126
+// with top <= 448 * 2^e = 1.75 * 2^(8 + e), or 127 * 2^e = (127 / 64) * 2^(6 + e).
+__device__ __forceinline__ int scale_exponent(float top, int codes) {
+  const uint32_t bits = __float_as_uint(top);
+  const int e = static_cast<int>(bits >> 23) - 127;
+  const uint32_t m = bits & 0x7fffffu;
+  const int s = codes == kCodesE4M3 ? e - 8 + (m > 0x600000u) : e - 6 + (m > 0x7e0000u);
+  return s < -126 ? -126 : s;
+}
+
+// Four codes.  (8-bit floats by the conversion instruction; whole numbers by
+// adding 1.5 * 2^23, whose sum's last byte is the rounded number.)
+__device__ __forceinline__ uint32_t four_codes(float x, float y, float z, float w, int codes) {
+  if (codes == kCodesE4M3) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y), "f"(x));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(w), "f"(z));
+    return lo | static_cast<uint32_t>(hi) << 16;
+  }
+  constexpr float k = 12582912.0f;
+  const uint32_t a = __float_as_uint(x + k), b = __float_as_uint(y + k), c = __float_as_uint(z + k), d = __float_as_uint(w + k);
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+template <typename T, int VE>
+__device__ __forceinline__ void store_codes(uint8_t* at, const Run<T, VE>& x, float by, int codes) {
+  if constexpr (VE >= 4) {
+    uint32_t c[VE / 4];
+#pragma unroll
+    for (int i = 0; i < VE; i += 4)
+      c[i / 4] = four_codes(to_float(x.e[i]) * by, to_float(x.e[i + 1]) * by, to_float(x.e[i + 2]) * by,
+                            to_float(x.e[i + 3]) * by, codes);
+    memcpy(__builtin_assume_aligned(at, VE), c, VE);
+  } else if constexpr (VE == 2) {
+    *reinterpret_cast<uint16_t*>(at) =
+        static_cast<uint16_t>(four_codes(to_float(x.e[0]) * by, to_float(x.e[1]) * by, 0.0f, 0.0f, codes));
+  } else {
+    *at = static_cast<uint8_t>(four_codes(to_float(x.e[0]) * by, 0.0f, 0.0f, 0.0f, codes));
+  }
+}
+
+// A head at a time by `lanes` lanes of a warp: a lane holds U units of two runs,
+// a pair's elements together, so that the head is read once: turned, rounded to its
+// 16-bit type (as pcs_rotate would leave it), its largest magnitude found over the
+// lanes, and written as codes.  Queries are turned on the way.
+template <typename T, int VE, int U, bool IL>
+__global__ void __launch_bounds__(kThreads)
+    k_store(const __grid_constant__ RotArgs a, const __grid_constant__ StoreShape shape, int per_block) {
+  using V = Run<T, VE>;
+  __shared__ __align__(32) float2 cs[kTokens * kPairs + 4];
+  __shared__ Place place[kTokens];
+  const BlockWork b = block_setup<true>(a, per_block, cs, place);
+  const int tid = threadIdx.x, group = tid / shape.lanes, lane = tid - group * shape.lanes;
+  const int half = a.head_dim / 2, row = pairs_row(a);
+  for (int n = b.n0; n < b.n1; ++n) {
+    const RotSlot& z = a.t[n];
+    const int pairs = n < a.plain ? a.pairs : 0;
+    const int heads = z.heads - (n ? a.t[n - 1].heads : 0), total = b.nt * heads;
+    const uint8_t* const src0 = z.src + b.t0 * z.src_token;
+    for (int p0 = 0; p0 < total; p0 += shape.groups) {
+      const int p = p0 + group;
+      const int t = p < total ? shape.by_heads[n].div(p) : 0, h = p < total ? p - t * heads : 0;
+      int64_t at = 0;
+      if (z.role) at = z.role == 1 ? place[t].k : place[t].v;
+      const bool live = p < total && at >= 0;
+      const uint8_t* src = src0 + times(t, z.src_token) + times(h, z.src_head);
+      V x[U], y[U];
+      int first[U], second[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int u = lane + i * shape.lanes;
+        const int turned = IL || pairs == 0 ? 0 : shape.turned;
+        if (VE == 1 && IL) {
+          first[i] = 2 * u, second[i] = 2 * u + 1;
+        } else if (u < turned) {
+          first[i] = VE * u, second[i] = pairs + VE * u;
+        } else {
+          const int begin = turned ? 2 * pairs : 0;
+          first[i] = begin + VE * (u - turned), second[i] = begin + (half - begin / 2) + VE * (u - turned);
+        }
+        x[i] = V{}, y[i] = V{};
+        if (!live || u >= shape.units) continue;
+        x[i] = *reinterpret_cast<const V*>(src + first[i] * sizeof(T));
+        y[i] = *reinterpret_cast<const V*>(src + second[i] * sizeof(T));
+        const float2* c = cs + t * row;
+        if constexpr (!IL) {
+          if (u < turned) turn_unit<T, VE, false>(x[i], y[i], c + first[i], VE);
+        } else if constexpr (VE == 1) {
+          if (u < pairs) turn_unit<T, 1, true>(x[i], y[i], c + u, 1);
+        } else {
+          V none;
+          if (first[i] / 2 < pairs) turn_unit<T, VE, true>(x[i], none, c + first[i] / 2, pairs - first[i] / 2);
+          if (second[i] / 2 < pairs) turn_unit<T, VE, true>(y[i], none, c + second[i] / 2, pairs - second[i] / 2);
+        }
+      }
+      if (z.role == 0) {
+        uint8_t* dst = z.dst + (b.t0 + t) * z.dst_token + times(h, z.dst_head);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (!live || lane + i * shape.lanes >= shape.units) continue;
+          *reinterpret_cast<V*>(dst + first[i] * sizeof(T)) = x[i];
+          *reinterpret_cast<V*>(dst + second[i] * sizeof(T)) = y[i];
+        }
+        continue;
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int k = 0; k < VE; ++k) top = max(top, max(magnitude(x[i].e[k]), magnitude(y[i].e[k])));
+      for (int o = shape.lanes >> 1; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (!live) continue;
+      const bool fine = top < (std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u);
+      const int e = scale_exponent(magnitude_value<T>(top), a.cache.codes);
+      const float by = fine ? __uint_as_float(static_cast<uint32_t>(127 - e) << 23) : 0.0f;
+      uint8_t* const dst = (z.role == 1 ? a.cache.k : a.cache.v) + at;
+      uint8_t* const codes = dst + times(h, a.cache.head_bytes);
+      if (lane == 0) dst[a.cache.scale_at + h] = static_cast<uint8_t>(fine ? e + 127 : 255);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (lane + i * shape.lanes >= shape.units) continue;
+        if (!fine) x[i] = V{}, y[i] = V{};
+        store_codes<T, VE>(codes + first[i], x[i], by, a.cache.codes);
+        store_codes<T, VE>(codes + second[i], y[i], by, a.cache.codes);
+      }
+    }
+  }
+}
+
 // Few tokens: a block for each and each tensor, for latency; many: up to
 // kTokens a block, which shares the setup among them and all tensors while
 // every SM still has two blocks.
@@ -342,7 +436,37 @@ cudaError_t by_form(const RotArgs& a, bool paged, bool vec, int sm_count, cudaSt
   return by_unit<T, false>(a, vec, sm_count, stream);
 }
 
+template <typename T, int VE, bool IL>
+cudaError_t store(const RotArgs& a, int sm_count, cudaStream_t stream) {
+  StoreShape s;
+  s.units = a.head_dim / (2 * VE);
+  s.lanes = 1;
+  while (s.lanes < s.units && s.lanes < 32) s.lanes *= 2;
+  s.groups = kThreads / s.lanes;
+  s.turned = a.pairs / VE;
+  for (int n = 0; n < a.n; ++n) s.by_heads[n].set(a.t[n].heads - (n ? a.t[n - 1].heads : 0));
+  int per_block;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = config(a, sm_count, &per_block, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, k_store<T, VE, VE == 1 ? 2 : 1, IL>, a, s, per_block);
+}
+
+// Units as wide as the pairs' halves allow (head_dim / 2 is a multiple of 8).
+template <typename T>
+cudaError_t store_by_unit(const RotArgs& a, bool vec, int sm_count, cudaStream_t stream) {
+  if (a.interleaved) return vec ? store<T, 8, true>(a, sm_count, stream) : store<T, 1, true>(a, sm_count, stream);
+  if (vec && a.pairs % 8 == 0) return store<T, 8, false>(a, sm_count, stream);
+  if (vec && a.pairs % 4 == 0) return store<T, 4, false>(a, sm_count, stream);
+  if (vec && a.pairs % 2 == 0) return store<T, 2, false>(a, sm_count, stream);
+  return store<T, 1, false>(a, sm_count, stream);
+}
+
 }  // namespace
+
+cudaError_t launch_store(const RotArgs& a, uint32_t dtype, bool vec, int sm_count, cudaStream_t stream) {
+  return dtype == PCS_DT_F16 ? store_by_unit<__half>(a, vec, sm_count, stream)
+                             : store_by_unit<__nv_bfloat16>(a, vec, sm_count, stream);
+}
 
 cudaError_t launch_rotate(const RotArgs& a, uint32_t dtype, bool paged, bool vec, int sm_count,
                           cudaStream_t stream) {

@@ -404,6 +404,7 @@ struct pcs_ctx {
     Ev busy;  // the last call's end
   };
   std::unordered_map<cudaStream_t, Workspace> ws;
+  std::vector<void*> captured;    // workspaces of calls that graphs hold
   Workspace* ws_cur = nullptr;    // of the call in progress (calls hold mu)
   bool ws_behind = false;         // its last call had not finished when this one began
   uint32_t* call_words = nullptr;  // its header words
@@ -461,7 +462,7 @@ enum KernelKind {
   kKFinalizePack, kKFinalizeRestoreV, kKScore, kKTopk, kKBulkHash, kKBulkPack,
   kKBulkRestore, kKBulkRestoreV, kKReduce, kKGSelect, kKGFinish, kKPoolAlloc, kKPoolShare,
   kKPoolCow, kKPoolRelease, kKMismatch, kKClassifyReads, kKUpload, kKRotate, kKAppend, kKAttendToken, kKAttendBlock,
-  kKAttendJoin, kKernelKinds
+  kKAttendJoin, kKStore, kKRead, kKKeep, kKernelKinds
 };
 static_assert(kKernelKinds <= 32, "kernel timing table");
 const char* kKernelNames[kKernelKinds] = {
@@ -470,7 +471,7 @@ const char* kKernelNames[kKernelKinds] = {
     "k_hash", "k_bulk<pack>", "k_bulk<restore>", "k_bulk<restore_verify>",
     "k_reduce_nodes", "k_gselect", "k_gfinish", "k_pool_alloc", "k_pool_share", "k_pool_cow",
     "k_pool_release", "k_mismatch", "k_classify_reads", "k_upload", "k_rotate", "k_rotate<append>",
-    "k_attend_token", "k_attend_block", "k_attend_join"};
+    "k_attend_token", "k_attend_block", "k_attend_join", "k_store", "k_kv_read", "k_kv_keep"};
 
 cudaEvent_t timing_event(pcs_ctx* c) {
   if (!c->timing_events.empty()) {
@@ -1713,6 +1714,8 @@ pcs_status pcs_destroy(pcs_ctx* c) {
       if (kv.second.buf) cudaFree(kv.second.buf);
     }
     c->ws.clear();
+    for (void* p : c->captured) cudaFree(p);
+    c->captured.clear();
     if (c->words) cudaFree(c->words);
     if (c->stage) cudaFreeHost(c->stage);
     for (auto& e : c->plan_slot_busy) e.reset();
@@ -3328,6 +3331,8 @@ pcs_status OpCall::scratch(uint64_t bytes, uint8_t** out, uint32_t** words) {
   scratch_ = true;
   return PCS_OK;
 }
+
+void OpCall::keep(void* buffer) { c_->captured.push_back(buffer); }
 
 void OpCall::before(OpKernel k) { scope_ = new LaunchScope(c_, kKRotate + static_cast<int>(k), stream_); }
 

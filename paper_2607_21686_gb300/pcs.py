@@ -31,6 +31,8 @@ PCS_E_CORRUPT, PCS_E_HANDLE, PCS_E_IO, PCS_E_TIMEOUT, PCS_E_RANGE = -6, -7, -8, 
 
 PCS_DT_RAW, PCS_DT_U8, PCS_DT_I32, PCS_DT_I64 = 0, 1, 2, 3
 PCS_DT_F16, PCS_DT_BF16, PCS_DT_F32, PCS_DT_U64 = 4, 5, 6, 7
+PCS_DT_E4M3, PCS_DT_I8 = 8, 9
+PCS_TREE_MAX = 64
 PCS_SEC_OBS, PCS_SEC_RNG, PCS_SEC_KEPT_IDX, PCS_SEC_KEYS = 1, 2, 3, 4
 PCS_SEC_VALUES, PCS_SEC_META, PCS_SEC_K, PCS_SEC_V = 5, 6, 7, 8
 PCS_KIND_MARKOV, PCS_KIND_BANK, PCS_KIND_KV = 1, 2, 3
@@ -213,6 +215,13 @@ SIGNATURES = {
     "pcs_attend": (_st, [_vp, ctypes.POINTER(pcs_kv_cache), ctypes.POINTER(pcs_kv_batch),
                          ctypes.POINTER(pcs_attend_params), ctypes.POINTER(pcs_heads),
                          ctypes.POINTER(pcs_heads), _vp, _vp]),
+    "pcs_attend_tree": (_st, [_vp, ctypes.POINTER(pcs_kv_cache), ctypes.POINTER(pcs_kv_batch),
+                              ctypes.POINTER(pcs_attend_params), _vp, ctypes.POINTER(pcs_heads),
+                              ctypes.POINTER(pcs_heads), _vp, _vp]),
+    "pcs_kv_keep": (_st, [_vp, ctypes.POINTER(pcs_kv_cache), ctypes.POINTER(pcs_kv_batch), _vp,
+                          ctypes.c_int64, _i32, _vp, _vp, _vp]),
+    "pcs_kv_read": (_st, [_vp, ctypes.POINTER(pcs_kv_cache), ctypes.POINTER(pcs_kv_batch),
+                          ctypes.POINTER(pcs_heads), ctypes.POINTER(pcs_heads), _vp]),
     "pcs_fingerprint_static": (_st, [ctypes.POINTER(pcs_buf), _i32, _vp, _vp]),
 }
 # int32 exchange(void* user, uint64_t* counts, uint64_t* bytes, int32 bins)
@@ -461,6 +470,20 @@ def _lse_of(q: torch.Tensor, stream) -> torch.Tensor:
     return torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
 
 
+def _lse_given(lse: torch.Tensor, q: torch.Tensor) -> None:
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_cuda \
+            or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous CUDA float32 [tokens, q heads]")
+
+
+def _new(cache, tokens: int, dtype: torch.dtype, stream) -> torch.Tensor:
+    """A new tensor [tokens, heads, head_dim] for a call on `stream`."""
+    if stream is not None:
+        with _on(stream):
+            return _new(cache, tokens, dtype, None)
+    return torch.empty(tokens, cache.heads, cache.head_dim, dtype=dtype, device=cache.keep[0].device)
+
+
 def _int32(t: torch.Tensor, what: str, dim: int) -> torch.Tensor:
     if t.dtype != torch.int32 or not t.is_cuda or t.dim() != dim:
         raise ValueError("%s: a CUDA int32 tensor of %d dimensions is wanted" % (what, dim))
@@ -490,38 +513,72 @@ class Rotary:
         self.inverse = pcs_rotary(_ptr(pos), _ptr(freq), len(pairs), p4, flags | PCS_ROT_INVERSE)
 
 
+# What the codes of an 8-bit cache are.
+_CODE_DTYPES = {torch.float8_e4m3fn: PCS_DT_E4M3, torch.int8: PCS_DT_I8}
+
+
+def kv_row_bytes(heads: int, head_dim: int) -> int:
+    """Bytes of a row of an 8-bit cache: codes of all heads, then a scale byte a
+    head, filled up to a multiple of 32 (a sector of memory)."""
+    return -(-heads * (head_dim + 1) // 32) * 32
+
+
 class KvCache:
     """Paged keys and values of many sessions: pools [pages, page_rows, heads,
     head_dim] of float16 or bfloat16 (any strides but the last), table int32
     [sessions, pages of a session], -1 an empty page.  The first `sinks` tokens
     of a session stay; with `ring` the others reuse that many slots in turn.
     v_table: the values' pages, where they are not the keys' (keeps its tensors
-    alive)."""
+    alive).
+
+    In 8 bits: codes torch.float8_e4m3fn or torch.int8, pools uint8 [pages,
+    page_rows, row bytes] whose rows are heads * head_dim codes and a scale byte a
+    head behind them (kv_row_bytes; what they stand for is in include/pcs.h)."""
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, table: torch.Tensor,
-                 sinks: int = 0, ring: int = 0, v_table: torch.Tensor = None):
-        if k_pool.dim() != 4 or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() \
+                 sinks: int = 0, ring: int = 0, v_table: torch.Tensor = None,
+                 codes: torch.dtype = None, heads: int = None, head_dim: int = None):
+        if k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() \
                 or k_pool.dtype != v_pool.dtype or not k_pool.is_cuda or not v_pool.is_cuda:
-            raise ValueError("k_pool and v_pool must be CUDA tensors [pages, page_rows, heads, "
-                             "head_dim] of one shape, type and layout")
-        if k_pool.stride(3) != 1 or k_pool.dtype not in (torch.float16, torch.bfloat16):
-            raise ValueError("pools must hold float16 or bfloat16 with contiguous heads")
+            raise ValueError("k_pool and v_pool must be CUDA tensors of one shape, type and layout")
+        if codes is None:
+            if heads is not None or head_dim is not None:
+                raise ValueError("heads and head_dim are for caches with codes")
+            if k_pool.dim() != 4:
+                raise ValueError("pools must be [pages, page_rows, heads, head_dim]")
+            if k_pool.stride(3) != 1 or k_pool.dtype not in (torch.float16, torch.bfloat16):
+                raise ValueError("pools must hold float16 or bfloat16 with contiguous heads")
+            n, rows, heads, dim = k_pool.shape
+            ps, rs, hs, _ = k_pool.stride()
+            row, dtype = heads * dim, _HEAD_DTYPES[k_pool.dtype]
+        else:
+            if codes not in _CODE_DTYPES:
+                raise ValueError("codes must be torch.float8_e4m3fn or torch.int8")
+            if k_pool.dim() != 3 or k_pool.dtype != torch.uint8 or k_pool.stride(2) != 1:
+                raise ValueError("pools of codes must be uint8 [pages, page_rows, row bytes] with "
+                                 "contiguous rows")
+            if heads is None or head_dim is None or heads < 1 or head_dim < 1:
+                raise ValueError("heads and head_dim are needed with codes")
+            n, rows, row = k_pool.shape
+            if row < heads * (head_dim + 1):
+                raise ValueError("a row of %d bytes does not hold %d heads of %d codes and a scale"
+                                 % (row, heads, head_dim))
+            ps, rs, _ = k_pool.stride()
+            dim, hs, dtype = head_dim, head_dim, _CODE_DTYPES[codes]
         _int32(table, "table", 2)
         if v_table is not None:
             _int32(v_table, "v_table", 2)
             if v_table.shape != table.shape or v_table.stride() != table.stride():
                 raise ValueError("table and v_table must have one shape and layout")
-        n, rows, heads, dim = k_pool.shape
-        ps, rs, hs, _ = k_pool.stride()
         self.sessions = table.shape[0]
-        self.heads, self.head_dim, self.dtype = heads, dim, k_pool.dtype
+        self.heads, self.head_dim = heads, dim
+        self.dtype = k_pool.dtype if codes is None else codes
         self.keep = (k_pool, v_pool, table, v_table)
         self.struct = pcs_kv_cache(
             _ptr(k_pool), _ptr(v_pool), _ptr(table), _ptr(v_table),
             max(table.stride(0), table.shape[1]) if self.sessions <= 1 else table.stride(0),
-            ps if n > 1 else rows * heads * dim, rs if rows > 1 else heads * dim,
-            hs if heads > 1 else dim, n, table.shape[1], rows, heads, dim, sinks, ring,
-            _HEAD_DTYPES[k_pool.dtype])
+            ps if n > 1 else rows * (rs if rows > 1 else row), rs if rows > 1 else row,
+            hs if heads > 1 else dim, n, table.shape[1], rows, heads, dim, sinks, ring, dtype)
 
 
 class KvBatch:
@@ -881,15 +938,74 @@ class Context:
             out = _like(q, stream)
         qs, ys = _heads(q, "q", n), _heads(out, "out", n)
         if lse is not None:
-            if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_cuda \
-                    or not lse.is_contiguous():
-                raise ValueError("lse must be a contiguous CUDA float32 [tokens, q heads]")
+            _lse_given(lse, q)
         elif return_lse:
             lse = _lse_of(q, stream)
         check(self.lib.pcs_attend(self.h, cache.struct, batch.struct,
                                   pcs_attend_params(scale, window, 0, 0), qs, ys, _ptr(lse),
                                   _stream_ptr(stream)), "pcs_attend")
         return out if lse is None else (out, lse)
+
+    def attend_tree(self, cache: KvCache, batch: KvBatch, parent: torch.Tensor, q: torch.Tensor,
+                    out: torch.Tensor = None, lse: torch.Tensor = None, scale: float = 0.0,
+                    window: int = 0, return_lse: bool = False, stream=None):
+        """Attention of drafted tokens that form a tree: each sees the context, its
+        ancestors and itself.  parent int32 [tokens]: the number, among its
+        session's new tokens, of the one that a token follows, -1 for the context.
+        The rest as attend."""
+        self._check_tables(cache, batch)
+        n = batch.tokens
+        if _int32(parent, "parent", 1).numel() != n:
+            raise ValueError("%d parents, the batch has %d tokens" % (parent.numel(), n))
+        if out is None:
+            out = _like(q, stream)
+        qs, ys = _heads(q, "q", n), _heads(out, "out", n)
+        if lse is not None:
+            _lse_given(lse, q)
+        elif return_lse:
+            lse = _lse_of(q, stream)
+        check(self.lib.pcs_attend_tree(self.h, cache.struct, batch.struct,
+                                       pcs_attend_params(scale, window, 0, 0), _ptr(parent), qs, ys,
+                                       _ptr(lse), _stream_ptr(stream)), "pcs_attend_tree")
+        return out if lse is None else (out, lse)
+
+    def kv_keep(self, cache: KvCache, batch: KvBatch, index: torch.Tensor, count: torch.Tensor,
+                lens_out: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """Keep some of each session's new tokens: those numbered index[s, i], i <
+        count[s], ascending, move next to the context.  index int32 [sessions,
+        most], count int32 [sessions]; returns the sessions' lengths (lens_out)."""
+        self._check_tables(cache, batch)
+        n = batch.sessions
+        _int32(index, "index", 2)
+        _int32(count, "count", 1)
+        if index.shape[0] != n or count.numel() != n:
+            raise ValueError("index and count must have a row for each of %d sessions" % n)
+        if lens_out is None:
+            lens_out = _like(count, stream)
+        elif _int32(lens_out, "lens_out", 1).numel() != n:
+            raise ValueError("lens_out must have an element for each of %d sessions" % n)
+        most = index.shape[1]
+        check(self.lib.pcs_kv_keep(self.h, cache.struct, batch.struct, _ptr(index),
+                                   index.stride(0) if n > 1 else most, most, _ptr(count),
+                                   _ptr(lens_out), _stream_ptr(stream)), "pcs_kv_keep")
+        return lens_out
+
+    def kv_read(self, cache: KvCache, batch: KvBatch, dtype: torch.dtype = None,
+                k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
+        """What the cache holds of the batch's tokens (the last ones of each session):
+        keys and values [tokens, heads, head_dim], 0 for tokens that are not there.
+        An 8-bit cache is read as `dtype` (bfloat16), one of 16 bits as it is."""
+        self._check_tables(cache, batch)
+        n = batch.tokens
+        if dtype is None:
+            dtype = cache.dtype if cache.dtype in (torch.float16, torch.bfloat16) else torch.bfloat16
+        if k_out is None:
+            k_out = _new(cache, n, dtype, stream)
+        if v_out is None:
+            v_out = _new(cache, n, dtype, stream)
+        check(self.lib.pcs_kv_read(self.h, cache.struct, batch.struct, _heads(k_out, "k_out", n),
+                                   _heads(v_out, "v_out", n), _stream_ptr(stream)), "pcs_kv_read")
+        return k_out, v_out
 
     # -- snapshots -------------------------------------------------------------
     def record_bytes(self, session: Session) -> int:
