@@ -53,12 +53,45 @@ bool encode_pool(const pcs_kv_cache& c, void* pool, int rows, uint8_t* map) {
   return true;
 }
 
+// A cache in 8 bits: codes copied by boxes of a head of `rows` rows of a page, swizzled
+// by 64 or 128 bytes as its rows are long; scale bytes of 16 heads of as many rows.
+bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, CodeMaps* maps) {
+  const EncodeFn fn = encoder();
+  if (!fn) return false;
+  for (int i = 0; i < 4; ++i) {
+    uint8_t* pool = i & 1 ? d.v : d.k;
+    CUtensorMap m;
+    CUresult r;
+    if (i < 2) {
+      const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.heads),
+                                  static_cast<cuuint64_t>(c.page_rows), static_cast<cuuint64_t>(c.n_pages)};
+      const cuuint64_t strides[3] = {static_cast<cuuint64_t>(c.head_stride), static_cast<cuuint64_t>(c.row_stride),
+                                     static_cast<cuuint64_t>(c.page_stride)};
+      const cuuint32_t wide = c.head_dim <= 64 ? 64 : 128;
+      const cuuint32_t box[4] = {wide, 1, static_cast<cuuint32_t>(rows), 1}, step[4] = {1, 1, 1, 1};
+      r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             wide == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    } else {
+      const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.heads), static_cast<cuuint64_t>(c.page_rows),
+                                  static_cast<cuuint64_t>(c.n_pages)};
+      const cuuint64_t strides[2] = {static_cast<cuuint64_t>(c.row_stride), static_cast<cuuint64_t>(c.page_stride)};
+      const cuuint32_t box[3] = {16, static_cast<cuuint32_t>(rows), 1}, step[3] = {1, 1, 1};
+      r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, pool + d.scale_at, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    }
+    if (r != CUDA_SUCCESS) return false;
+    std::memcpy(maps->map[i], &m, sizeof m);
+  }
+  return true;
+}
+
 // Rows of the boxes that tensor copies can move: a power of two that divides a
 // page, so that a tile's boxes never leave theirs.  0: rows are copied one by one
 // (a prompt of 8,000 tokens, 32 query heads over 8, in pages of 16: 349 us with
 // boxes; in pages of 17, by rows, 867 us).
-int box_rows(const pcs_kv_cache& c) {
-  for (int r = 128; r >= 8; r /= 2)
+int box_rows(const pcs_kv_cache& c, int most) {
+  for (int r = most; r >= 8; r /= 2)
     if (c.page_rows % r == 0) return r;
   return 0;
 }
@@ -350,8 +383,14 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
         a.part = reinterpret_cast<float*>(ws);
         a.ticket = own ? words : nullptr;
       }
+      CodeMaps maps;
+      if (codes) {
+        a.box_rows = box_rows(*cache, kTokenTile8);
+        if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, &maps)) a.box_rows = 0;
+      }
       call.before(kOpAttendToken);
-      st = call.after(launch_attend_token(a, dtype, static_cast<int>(rows), false, call.stream()));
+      st = call.after(codes ? launch_attend_token8(a, static_cast<int>(rows), maps, call.stream())
+                            : launch_attend_token(a, dtype, static_cast<int>(rows), false, call.stream()));
       if (!st && splits > 1 && !own) {
         call.before(kOpAttendJoin);
         st = call.after(launch_attend_token(a, dtype, static_cast<int>(rows), true, call.stream()));
@@ -371,7 +410,7 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       a.part = reinterpret_cast<float*>(ws);
     }
     TensorMaps maps = {};
-    a.box_rows = codes ? 0 : box_rows(*cache);
+    a.box_rows = codes ? 0 : box_rows(*cache, kBlockTile);
     if (a.box_rows && !(encode_pool(*cache, cache->k, a.box_rows, maps.k) && encode_pool(*cache, cache->v, a.box_rows, maps.v)))
       a.box_rows = 0;
     call.before(kOpAttendBlock);

@@ -185,7 +185,7 @@ struct AttendArgs {
   int32_t splits;          // parts of a session's visible tokens
   float* part;             // partial results (splits > 1)
   uint32_t* ticket;        // token kernel: zero on entry and on exit; null: parts are joined later
-  int32_t box_rows;        // block kernel: rows of a tensor copy, 0: rows are copied one by one
+  int32_t box_rows;        // rows of a tensor copy, 0: rows are copied one by one
   uint32_t* err;
   const int32_t* parent;   // new tokens form trees; null: each sees those before it
   uint32_t dtype;          // of q and out
@@ -195,6 +195,7 @@ struct AttendArgs {
 // of a session and key head together.
 constexpr int kTokenRowsMax = 32;
 constexpr int kTokenWarps = 4;
+constexpr int kTokenTile8 = 32;  // tokens of a warp's tile of codes
 // Floats of one partial result: its rows' sums, then their maxima and totals.
 inline uint64_t token_part_floats(int rows, int head_dim) {
   const uint64_t padded = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
@@ -204,9 +205,14 @@ inline uint64_t token_part_floats(int rows, int head_dim) {
 // kTokenOwnJoin of them (a.ticket), else by a second launch (`join`).
 constexpr int kTokenOwnJoin = 16;
 cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream);
+// Tensor maps of a cache in 8 bits (box_rows > 0): codes of keys and of values, scale
+// bytes of keys and of values.
+struct alignas(64) CodeMaps {
+  uint8_t map[4][128];
+};
 // Forms of it: trees over 16-bit elements, anything over 8-bit codes.
 cudaError_t launch_attend_token_tree(const AttendArgs& a, uint32_t dtype, int rows, cudaStream_t stream);
-cudaError_t launch_attend_token8(const AttendArgs& a, int rows, cudaStream_t stream);
+cudaError_t launch_attend_token8(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream);
 // Blocks of the token kernel that one SM holds, for `rows` rows a key head.
 int attend_token_blocks_per_sm(int head_dim, int rows);
 int attend_token8_blocks_per_sm(int head_dim, int rows);

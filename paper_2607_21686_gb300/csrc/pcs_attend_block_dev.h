@@ -33,7 +33,6 @@ template <int MAKERS>
 constexpr int kValidOf = MAKERS == -1 ? 16 : 8;
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kSlack = 8.0f;          // as in the token kernel
-constexpr long long kWaitCycles = 4000000000ll;
 
 // Tiles of keys and of values in shared memory, each a ring of its own: a warp
 // that waits for values alone then sees every phase of their barriers.  (In one
@@ -60,32 +59,6 @@ template <int DP, int MAKERS>
 constexpr uint32_t kStagedBytes = MAKERS == kCodes ? kCopyWarpsOf<MAKERS> * kUnitStages<DP> * kUnitBytes<DP> : 0;
 template <int DP, int MAKERS>
 constexpr uint32_t kSmemBytes = (2 + kBuffers<DP, MAKERS>) * kTileBytes<DP> + kStagedBytes<DP, MAKERS> + 1024;
-
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait for the phase of the given parity; false: it gave up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  if (bar_try(bar, parity)) return true;
-  const long long t0 = clock64();
-  while (!bar_try(bar, parity))
-    if (clock64() - t0 > kWaitCycles) return false;
-  return true;
-}
 
 // A barrier expects `bytes`; a box of rows of a pool for them.
 __device__ __forceinline__ void fill_begins(uint32_t bar, uint32_t bytes, uint32_t one) {
@@ -290,36 +263,6 @@ template <typename T>
 __device__ __forceinline__ uint32_t specials(uint32_t x) {
   const uint32_t e = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
   return ((x & e) == e ? 0xffffu : 0u) | ((x >> 16 & e) == e ? 0xffff0000u : 0u);
-}
-
-// A box of rows: pages of its keys and values as the table has them, the first
-// row in them.  The page ids are on their way from memory until settle().
-struct Box {
-  int32_t k, v, row;
-};
-// The box at place e of a view.
-__device__ __forceinline__ Box box_place(const AttendArgs& a, int s, const SessionView& w, int32_t e) {
-  const CacheDev& c = a.cache;
-  const uint32_t slot = box_slot(a, w, e);
-  if (slot >= static_cast<uint32_t>(c.slots)) {
-    atomicOr(a.err, kDevErrIndex);
-    return {-1, -1, 0};
-  }
-  const uint32_t page = c.page_rows.div(slot);
-  const int64_t at = s * c.table_stride + page;
-  Box x;
-  x.k = __ldg(c.table + at);
-  x.v = __ldg((c.v_table ? c.v_table : c.table) + at);
-  x.row = slot - page * c.page_rows.d;
-  return x;
-}
-// Page n_pages, whose rows come out as zeros, for what is not in the cache.
-__device__ __forceinline__ void settle(const AttendArgs& a, Box& x) {
-  const int32_t n = a.cache.n_pages;
-  if (x.k < 0 || x.k >= n || x.v < 0 || x.v >= n) {
-    if (x.k < -1 || x.k >= n || x.v < -1 || x.v >= n) atomicOr(a.err, kDevErrIndex);
-    x.k = x.v = n;
-  }
 }
 
 // Zeros for them; whether there were any.

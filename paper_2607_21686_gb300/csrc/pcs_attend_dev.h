@@ -164,4 +164,63 @@ __device__ __forceinline__ bool has_specials(const uint4& v) {
   return ((((v.x & e) + one) | ((v.y & e) + one) | ((v.z & e) + one) | ((v.w & e) + one)) & 0x80008000u) != 0;
 }
 
+// ---- Barriers in shared memory, boxes of rows ---------------------------------------------
+
+constexpr long long kWaitCycles = 4000000000ll;
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// Bounded wait for the phase of the given parity; false: it gave up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  if (bar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity))
+    if (clock64() - t0 > kWaitCycles) return false;
+  return true;
+}
+
+// A box of rows: pages of its keys and values as the table has them, the first
+// row in them.  The page ids are on their way from memory until settle().
+struct Box {
+  int32_t k, v, row;
+};
+// The box at place e of a view.
+__device__ __forceinline__ Box box_place(const AttendArgs& a, int s, const SessionView& w, int32_t e) {
+  const CacheDev& c = a.cache;
+  const uint32_t slot = box_slot(a, w, e);
+  if (slot >= static_cast<uint32_t>(c.slots)) {
+    atomicOr(a.err, kDevErrIndex);
+    return {-1, -1, 0};
+  }
+  const uint32_t page = c.page_rows.div(slot);
+  const int64_t at = s * c.table_stride + page;
+  Box x;
+  x.k = __ldg(c.table + at);
+  x.v = __ldg((c.v_table ? c.v_table : c.table) + at);
+  x.row = slot - page * c.page_rows.d;
+  return x;
+}
+// Page n_pages, whose rows come out as zeros, for what is not in the cache.
+__device__ __forceinline__ void settle(const AttendArgs& a, Box& x) {
+  const int32_t n = a.cache.n_pages;
+  if (x.k < 0 || x.k >= n || x.v < 0 || x.v >= n) {
+    if (x.k < -1 || x.k >= n || x.v < -1 || x.v >= n) atomicOr(a.err, kDevErrIndex);
+    x.k = x.v = n;
+  }
+}
+
 }  // namespace pcs

@@ -133,7 +133,6 @@ int attend_token_blocks_per_sm(int head_dim, int rows) {
 }
 
 cudaError_t launch_attend_token(const AttendArgs& a, uint32_t dtype, int rows, bool join, cudaStream_t stream) {
-  if (!join && a.cache.codes != kElements16) return launch_attend_token8(a, rows, stream);
   if (!join && a.parent) return launch_attend_token_tree(a, dtype, rows, stream);
   return dtype == PCS_DT_F16 ? by_size<__half>(a, rows, join, stream) : by_size<__nv_bfloat16>(a, rows, join, stream);
 }

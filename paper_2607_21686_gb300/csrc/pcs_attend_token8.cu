@@ -7,37 +7,47 @@
 //                 shared memory to the matrix instruction (E4M3 by the conversion
 //                 instruction, I8 through 1024 + c; both exactly).  The scales, powers
 //                 of two, stay out of the operands: a key's multiplies its scores, a
-//                 value's is added to the logarithm of its weights.  So a row has two
-//                 running maxima: that of its scores, which the total refers to, and
-//                 that of score + log2(scale), which the weights of the sums refer to
-//                 -- a token with a large weight and small values loses nothing
-//                 beside one with a small weight and large values.  Query rows
-//                 become float16 times a power of two of their own, that no bfloat16
-//                 is too large for it.
+//                 value's its weights.  So what a row's weights refer to is not the
+//                 largest score but the largest score + log2(scale): a token with a
+//                 large weight and small values loses nothing beside one with a small
+//                 weight and large values, and the total, in 32 bits, refers to the
+//                 same.  Query rows become float16 times a power of two of their own,
+//                 that no bfloat16 is too large for it.
 //                 Operands of 16 bits take 4 codes a thread where two elements lay:
 //                 keys as their first operand read 16-byte chunks by ldmatrix (a
 //                 thread gets four neighbouring dims, so the instruction's k runs over
 //                 dims in the order 0 1 4 5 8 9 12 13 2 3 6 7 .., and the query rows are
 //                 read in the same one); values come out transposed by pairs of dims,
 //                 whose bytes are sorted into even and odd dims (rows g and g + 8).
-//                 A warp's tile is 32 tokens: a lane looks up one of them.
+//                 A warp's tile is 32 tokens.  They come by tensor copies of boxes of 8
+//                 to 32 rows of a page (BOX), codes and scale bytes apart, or row by row
+//                 from pages whose size no such box divides.  (What bounds copies by the
+//                 warps' lanes is their number: a scale byte of a row is a request of its
+//                 own beside 64 or 128 bytes of codes.)
 #include "pcs_attend_token_dev.h"
 #include "pcs_codes_dev.h"
 
 namespace pcs {
 namespace {
 
-constexpr int kTile8 = 32;
-// Stages of a warp's ring: 64 to 100 KB in flight on an SM, as with 16 bits.
+constexpr int kTile8 = kTokenTile8;
 template <int DP>
-constexpr int kStages8 = DP == 64 ? 4 : 3;
-// Codes of keys and of values, then a word of scale bytes of each row.
-template <int DP>
-constexpr uint32_t kStage8 = 2 * kTile8 * DP + 2 * kTile8 * 4;
-template <int DP>
-constexpr uint32_t kRing8 = kWarps * kStages8<DP> * kStage8<DP>;
+constexpr int kStages8 = DP == 64 ? 3 : 2;
+// Codes of keys and of values, then scale bytes of each row: 16 heads' (BOX) or 4 heads'.
+template <bool BOX>
+constexpr int kScaleBytes = BOX ? 16 : 4;
+template <int DP, bool BOX>
+constexpr uint32_t kStage8 = 2 * kTile8 * (DP + kScaleBytes<BOX>);
+// (Boxes begin at multiples of 1,024 bytes: room to get there.)
+template <int DP, bool BOX>
+constexpr uint32_t kRing8 = kWarps * kStages8<DP> * kStage8<DP, BOX> + (BOX ? 1024 : 0);
+// The rings, or what the warps' results take, which lie over them at the end.
 template <int DP, int NT>
-constexpr int kResident8 = DP == 64 && NT == 4 ? 2 : static_cast<int>(227 * 1024 / (kRing8<DP> + 4096));
+constexpr uint32_t kJoin8 = kWarps * 8 * NT * (kPadOf<DP> + 2) * 4;
+template <int DP, int NT, bool BOX>
+constexpr uint32_t kSmem8 = kRing8<DP, BOX> > kJoin8<DP, NT> ? kRing8<DP, BOX> : kJoin8<DP, NT>;
+template <int DP, int NT, bool BOX>
+constexpr int kResident8 = NT == 4 ? 2 : NT == 2 ? (DP == 64 ? 3 : 2) : static_cast<int>(227 * 1024 / (kSmem8<DP, NT, BOX> + 3072));
 
 // 4 bytes from global to shared memory, zeros where there is no source.
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
@@ -48,25 +58,40 @@ template <int DP>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
   return DP == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
 }
-// log2 of a scale; NaN for its NaN.
-__device__ __forceinline__ float scale_log2_of(uint32_t b) {
-  return b == 255 ? __uint_as_float(0x7fc00000u) : static_cast<float>(static_cast<int>(b) - 127);
+// Where a row's weights refer to before its first token: nothing is below it.
+constexpr float kNothing = -1e30f;
+// A weight beyond this, or times its value's scale beyond 2^15, raises the reference.
+constexpr float kMostWeight = 1.2676506e30f;  // 2^100
+
+// A box of rows: `x`, `y`, .. where it begins in the tensor.
+__device__ __forceinline__ void box_of_codes(uint32_t to, uint64_t map, int head, int row, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+      "l"(map), "r"(0), "r"(head), "r"(row), "r"(page), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void box_of_scales(uint32_t to, uint64_t map, int byte, int row, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
+      "l"(map), "r"(byte), "r"(row), "r"(page), "r"(bar)
+      : "memory");
 }
 
-template <int CODES, int DP, int NT>
-__global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
-    k_attend_token8(const __grid_constant__ AttendArgs a) {
+template <int CODES, int DP, int NT, bool BOX>
+__global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
+    k_attend_token8(const __grid_constant__ AttendArgs a, const __grid_constant__ CodeMaps maps) {
   constexpr int kStages = kStages8<DP>;
-  constexpr uint32_t kStage = kStage8<DP>;
+  constexpr uint32_t kStage = kStage8<DP, BOX>;
   constexpr int kChunks = DP / 16;           // 16-byte chunks of a row
   constexpr int kRowsAtOnce = 32 / kChunks;  // rows one copy instruction of a warp moves
   constexpr int kRows = 8 * NT;
   constexpr int kPad = kPadOf<DP>;
+  constexpr bool kEarly = NT == 1;           // registers hold a tile's values beside its scores
   constexpr float kUp = 7.0f;                // weights are 2^7 times higher, as kLift says
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t valid[kWarps][kStages];
+  __shared__ __align__(8) uint64_t bars[BOX ? kWarps * kStages : 1];
   __shared__ TreeNode nodes[PCS_TREE_MAX];
-  static_assert(kWarps * (kRows * (kPad + 2)) * 4 <= kRing8<DP>, "the join reuses the ring");
 
   attend_dependency();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -74,16 +99,25 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
   const int head = blockIdx.x % a.cache.heads;
   const int sp = blockIdx.x / a.cache.heads % a.splits;
   const int s = blockIdx.x / a.cache.heads / a.splits;
-  const SessionView view = session_view(a, s);
+  if (BOX && tid < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps.map[tid])) : "memory");
+  SessionView view = session_rows(a, s);
+  narrow(a, view, 0, view.m, BOX ? a.box_rows : 1);
   if (view.m <= 0) return;  // the same in every part
   const int rows = view.m * a.group;
   if (!rows_there(a, view, tid == 0)) return;  // (max_new tokens' rows are at most kRows)
   const int head_dim = a.cache.head_dim;
   const bool tree = a.parent != nullptr;
-  const uint32_t ring = smem_addr(smem) + warp * kStages * kStage;
-  if (head_dim < DP) {  // chunks that no copy writes
+  uint8_t* const ring_ptr = smem + (BOX ? -smem_addr(smem) & 1023u : 0u) + warp * kStages * kStage;
+  const uint32_t ring = smem_addr(ring_ptr), bar0 = smem_addr(bars) + 8 * warp * kStages;
+  if (BOX) {
+    if (lane == 0) {
+      for (int i = 0; i < kStages; ++i) bar_init(bar0 + 8 * i, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+  } else if (head_dim < DP) {  // chunks that no copy writes
     for (uint32_t i = lane * 16; i < kStages * kStage; i += 512)
-      *reinterpret_cast<uint4*>(smem + warp * kStages * kStage + i) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(ring_ptr + i) = make_uint4(0, 0, 0, 0);
     __syncwarp();
   }
   if (tree) {
@@ -97,45 +131,86 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
   const int t_end = min(tiles, (sp + 1) * per);
   int t_next = sp * per + warp;  // the next tile whose places are looked up
 
-  const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes;
-  const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
-  // The aligned word that holds the head's scale byte.  (A row is a multiple of 16 bytes.)
-  const int scale_word = a.cache.scale_at + (head & ~3), scale_byte = head & 3;
+  // What a tile's copies need to know, looked up one tile ahead of them: a lane's row, or
+  // (BOX) a lane's box of rows, of which there are 32 / box_rows a tile.
+  using Ahead = std::conditional_t<BOX, Box, RowPlace>;
+  const int box_shift = BOX ? 31 - __clz(a.box_rows) : 0, boxes = kTile8 >> box_shift;
   auto look = [&](int t) {
-    RowPlace r = {kNoRow, kNoRow};
-    const int e = t * kTile8 + lane;
-    if (t < t_end && e < view.seen) r = row_place(a, s, seen_position(view, e));
-    return r;
-  };
-  const int chunk = lane % kChunks, row0 = lane / kChunks;
-  auto copy = [&](const RowPlace& r, int stage) {
-    const bool mine = r.k != kNoRow;
-    const uint32_t there = __ballot_sync(kFull, mine);
-    if (lane == 0) valid[warp][stage] = there;
-    const uint32_t base = ring + stage * kStage;
-#pragma unroll
-    for (int i = 0; i < kTile8 / kRowsAtOnce; ++i) {
-      const int row = i * kRowsAtOnce + row0;
-      const uint32_t ko = __shfl_sync(kFull, r.k, row), vo = __shfl_sync(kFull, r.v, row);
-      const bool in = ko != kNoRow;
-      if (chunk * 16 < head_dim) {
-        const uint32_t at = base + chunk_at<DP>(row, chunk);
-        copy16(at, row_at(a, kbase, in ? ko : 0) + chunk * 16, in);
-        copy16(at + kTile8 * DP, row_at(a, vbase, in ? vo : 0) + chunk * 16, in);
-      }
+    if constexpr (BOX) {
+      Box x = {-1, -1, 0};
+      const int e = t * kTile8 + lane * a.box_rows;
+      if (t < t_end && lane < boxes && e < view.seen) x = box_place(a, s, view, e);
+      return x;
+    } else {
+      RowPlace r = {kNoRow, kNoRow};
+      const int e = t * kTile8 + lane;
+      if (t < t_end && e < view.seen) r = row_place(a, s, seen_position(view, e));
+      return r;
     }
-    const uint32_t words = base + 2 * kTile8 * DP + lane * 4;
-    copy4(words, row_at(a, a.cache.k, mine ? r.k : 0) + scale_word, mine);
-    copy4(words + kTile8 * 4, row_at(a, a.cache.v, mine ? r.v : 0) + scale_word, mine);
+  };
+  // The bytes of a row that hold the head's scale byte.
+  constexpr int kScales = kScaleBytes<BOX>;
+  const int scale_from = head & -kScales, scale_byte = head & (kScales - 1);
+  auto copy = [&](Ahead& r, int t, int stage) {
+    const uint32_t base = ring + stage * kStage;
+    if constexpr (BOX) {
+      settle(a, r);
+      const int e = t * kTile8 + lane;
+      const bool mine = __shfl_sync(kFull, r.k, lane >> box_shift) < a.cache.n_pages && !(e >= view.gap0 && e < view.gap1);
+      const uint32_t there = __ballot_sync(kFull, mine);
+      const uint32_t bar = bar0 + 8 * stage;
+      if (lane == 0) {
+        valid[warp][stage] = there;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kStage) : "memory");
+      }
+      for (int k = 0; k < boxes; ++k) {
+        const int kp = __shfl_sync(kFull, r.k, k), vp = __shfl_sync(kFull, r.v, k), row = __shfl_sync(kFull, r.row, k);
+        const uint32_t at = k * a.box_rows;
+        if (lane == 0) {
+          box_of_codes(base + at * DP, reinterpret_cast<uint64_t>(maps.map[0]), head, row, kp, bar);
+          box_of_codes(base + (kTile8 + at) * DP, reinterpret_cast<uint64_t>(maps.map[1]), head, row, vp, bar);
+          box_of_scales(base + 2 * kTile8 * DP + at * kScales, reinterpret_cast<uint64_t>(maps.map[2]), scale_from, row, kp, bar);
+          box_of_scales(base + 2 * kTile8 * DP + (kTile8 + at) * kScales, reinterpret_cast<uint64_t>(maps.map[3]), scale_from, row,
+                        vp, bar);
+        }
+      }
+    } else {
+      const int chunk = lane % kChunks, row0 = lane / kChunks;
+      const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes;
+      const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
+      const bool mine = r.k != kNoRow;
+      const uint32_t there = __ballot_sync(kFull, mine);
+      if (lane == 0) valid[warp][stage] = there;
+#pragma unroll
+      for (int i = 0; i < kTile8 / kRowsAtOnce; ++i) {
+        const int row = i * kRowsAtOnce + row0;
+        const uint32_t ko = __shfl_sync(kFull, r.k, row), vo = __shfl_sync(kFull, r.v, row);
+        const bool in = ko != kNoRow;
+        if (chunk * 16 < head_dim) {
+          const uint32_t at = base + chunk_at<DP>(row, chunk);
+          copy16(at, row_at(a, kbase, in ? ko : 0) + chunk * 16, in);
+          copy16(at + kTile8 * DP, row_at(a, vbase, in ? vo : 0) + chunk * 16, in);
+        }
+      }
+      // (A row is a multiple of 16 bytes, so the words that hold scales are in it.)
+      const uint32_t words = base + 2 * kTile8 * DP + lane * 4;
+      copy4(words, row_at(a, a.cache.k, mine ? r.k : 0) + a.cache.scale_at + scale_from, mine);
+      copy4(words + kTile8 * 4, row_at(a, a.cache.v, mine ? r.v : 0) + a.cache.scale_at + scale_from, mine);
+    }
   };
 
-  RowPlace place = look(t_next);
+  Ahead place;
+  {
+    Ahead first[kStages];
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) {
-    if (t_next < t_end) copy(place, i);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    t_next += kWarps;
-    place = look(t_next);
+    for (int i = 0; i < kStages; ++i) first[i] = look(t_next + i * kWarps);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+      if (t_next < t_end) copy(first[i], t_next, i);
+      if (!BOX) asm volatile("cp.async.commit_group;" ::: "memory");
+      t_next += kWarps;
+    }
+    place = first[kStages - 1];
   }
 
   // Query rows as the second operand: of chunk k, dims 4 q4 .. +3 of row g, times
@@ -182,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
         const float2 x = value(qf[n][k][i]);
         qf[n][k][i] = pack2<__half>(x.x * up, x.y * up);
       }
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * a.scale_log2;
+    const float down = fmaxf(__uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * a.scale_log2, 1.2e-38f);
 #pragma unroll
     for (int i = 0; i < 2; ++i) back[n][i] = __shfl_sync(kFull, down, (q4 * 2 + i) * 4);
   }
@@ -205,127 +280,180 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
   };
 
   float o[DP / 16][NT][4];
-  float top[NT][2], mark[NT][2], total[NT][2];  // maxima of scores, of scores with the values' scales
+  float refer[NT][2], total[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    top[n][0] = top[n][1] = mark[n][0] = mark[n][1] = -INFINITY;
+    refer[n][0] = refer[n][1] = kNothing;
     total[n][0] = total[n][1] = 0.0f;
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.0f;
   }
 
   int stage = 0;
+  uint32_t phase = 0;
+  bool ok = true;
   for (int t = sp * per + warp; t < t_end; t += kWarps) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncwarp();
+    if (!BOX) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      __syncwarp();
+    }
     {
       const int into = stage == 0 ? kStages - 1 : stage - 1;
-      if (t_next < t_end) copy(place, into);
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (t_next < t_end) copy(place, t_next, into);
+      if (!BOX) asm volatile("cp.async.commit_group;" ::: "memory");
       t_next += kWarps;
       place = look(t_next);
     }
+    if (BOX) {
+      ok = __all_sync(kFull, bar_wait(bar0 + 8 * stage, phase)) != 0;
+      if (!ok) break;
+    }
     const uint32_t kat = ring + stage * kStage, vat = kat + kTile8 * DP;
-    const uint8_t* scales = smem + (warp * kStages + stage) * kStage + 2 * kTile8 * DP + scale_byte;
+    // This lane's row's scales.
+    const uint8_t* scales = ring_ptr + stage * kStage + 2 * kTile8 * DP + lane * kScales + scale_byte;
+    const float ks = scale_value(scales[0]), vs = scale_value(scales[kTile8 * kScales]);
     const uint32_t there = valid[warp][stage];
     const int e0 = t * kTile8;
-    const bool part = many && !(e0 + kTile8 - 1 <= low.hi && (e0 >= high.lo || e0 + kTile8 <= low.first));
+    // (Boxes begin ahead of what is seen and end behind it.)
+    const bool part = (BOX || many) && !(e0 + kTile8 - 1 <= low.hi && (e0 >= high.lo || e0 + kTile8 <= low.first));
 
-    // c: scores of tokens 16 h + g, + 8; cv: with the logarithm of the values' scales.
-    float c[2][NT][4], cv[2][NT][4];
+    // Two chunks of 16 dims of the tokens 16 h .. +15: pairs of dims by pairs of tokens.
+    auto values = [&](uint32_t (&f)[4], int h, int k) {
+      ldm4t(f, vat + chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)));
+    };
+    // All that the tile gives is on its way out of shared memory before any of it is used.
+    uint32_t kf[2][DP / 32][4], vf[2][DP / 32][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) ldm4(kf[h][k], kat + chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)));
+    if (kEarly) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < DP / 32; ++k) values(vf[h][k], h, k);
+    }
+    // Scores of tokens 16 h + g, + 8, but for the rows' factors.
+    float c[2][NT][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int n = 0; n < NT; ++n) c[h][n][0] = c[h][n][1] = c[h][n][2] = c[h][n][3] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < DP / 32; ++k) {
-        uint32_t f[4];
-        ldm4(f, kat + chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)));
+    for (int k = 0; k < DP / 32; ++k)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
           uint32_t x[4];
-          four_halves<CODES>(f[2 * j], x[0], x[2]);
-          four_halves<CODES>(f[2 * j + 1], x[1], x[3]);
+          four_halves<CODES>(kf[h][k][2 * j], x[0], x[2]);
+          four_halves<CODES>(kf[h][k][2 * j + 1], x[1], x[3]);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma<__half>(c[h][n], x, qf[n][2 * k + j][0], qf[n][2 * k + j][1]);
         }
+    float vscale[2][2];  // of token 16 h + 8 j + g
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float y = __shfl_sync(kFull, ks, h * 16 + j * 8 + g);
+        vscale[h][j] = __shfl_sync(kFull, vs, h * 16 + j * 8 + g);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          c[h][n][2 * j] *= y;
+          c[h][n][2 * j + 1] *= y;
+        }
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {  // token 16 h + 8 i + g
-        const int row = h * 16 + i * 8 + g;
-        const float ks = scale_value(scales[row * 4]), vl = scale_log2_of(scales[(kTile8 + row) * 4]);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            c[h][n][2 * i + j] *= ks * back[n][j];
-            cv[h][n][2 * i + j] = c[h][n][2 * i + j] + vl;
-          }
-      }
-    }
-    if (part || there != kFull) {
+    const bool masked = part || there != kFull;
+    uint32_t seen[NT][2];  // bits of the tokens that a row sees
+    if (masked) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t m = there & (part ? sees(new_token[n][i], e0) : kFull);
+          seen[n][i] = (there & (part ? sees(new_token[n][i], e0) : kFull)) >> g;
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-              if (!(m >> (h * 16 + j * 8 + g) & 1)) c[h][n][2 * j + i] = cv[h][n][2 * j + i] = -INFINITY;
+              if (!(seen[n][i] >> (h * 16 + j * 8) & 1)) c[h][n][2 * j + i] = -INFINITY;
         }
     }
-    bool raise = false;
+    // Weights 2^(score - reference), p; times the values' scales, v.
+    float p[2][NT][4], v[2][NT][4];
+    auto weigh = [&] {
+      float most = 0.0f, largest = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        raise |= fmaxf(fmaxf(c[0][n][i], c[0][n][2 + i]), fmaxf(c[1][n][i], c[1][n][2 + i])) > top[n][i] + kSlack;
-        raise |= fmaxf(fmaxf(cv[0][n][i], cv[0][n][2 + i]), fmaxf(cv[1][n][i], cv[1][n][2 + i])) > mark[n][i] + kSlack;
-      }
-    if (__any_sync(kFull, raise)) {
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int z = 2 * j + i;
+              p[h][n][z] = exp2_fast(fmaf(c[h][n][z], back[n][i], -refer[n][i]));
+              v[h][n][z] = p[h][n][z] * vscale[h][j];
+              largest = fmaxf(largest, p[h][n][z]);
+              most = fmaxf(most, v[h][n][z]);
+            }
+      return most > 32768.0f || largest > kMostWeight;
+    };
+    if (__any_sync(kFull, weigh())) {
+      // The reference becomes the largest score + log2(scale), less 7 as kUp says, and
+      // at least what keeps the largest weight below 2^93.
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float m = fmaxf(fmaxf(c[0][n][i], c[0][n][2 + i]), fmaxf(c[1][n][i], c[1][n][2 + i]));
-          float w = fmaxf(fmaxf(cv[0][n][i], cv[0][n][2 + i]), fmaxf(cv[1][n][i], cv[1][n][2 + i]));
+          float m = -INFINITY, w = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float x = c[h][n][2 * j + i] * back[n][i];
+              const int e = static_cast<int>(__float_as_uint(vscale[h][j]) >> 23) - 127;  // (255: below any other)
+              m = fmaxf(m, x);
+              w = fmaxf(w, x + static_cast<float>(e > 127 ? -127 : e));
+            }
 #pragma unroll
           for (int k = 4; k <= 16; k *= 2) {
             m = fmaxf(m, __shfl_xor_sync(kFull, m, k));
             w = fmaxf(w, __shfl_xor_sync(kFull, w, k));
           }
-          m = fmaxf(m, top[n][i]);
-          w = fmaxf(w, mark[n][i]);
-          total[n][i] *= m == -INFINITY ? 1.0f : exp2_fast(top[n][i] - m);
-          const float f = w == -INFINITY ? 1.0f : exp2_fast(mark[n][i] - w);
-          top[n][i] = m;
-          mark[n][i] = w;
+          const float to = fmaxf(fmaxf(w - kUp, m - 93.0f), refer[n][i]);
+          const float f = exp2_fast(refer[n][i] - to);
+          refer[n][i] = to;
+          total[n][i] *= f;
 #pragma unroll
           for (int d = 0; d < DP / 16; ++d) {
             o[d][n][i] *= f;
             o[d][n][2 + i] *= f;
           }
         }
+      weigh();
+    }
+    if (masked) {  // (a scale that stands for NaN would go through a weight of 0)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              if (!(seen[n][i] >> (h * 16 + j * 8) & 1)) v[h][n][2 * j + i] = 0.0f;
     }
     uint32_t w[2][NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float m0 = top[n][0] == -INFINITY ? 0.0f : top[n][0], m1 = top[n][1] == -INFINITY ? 0.0f : top[n][1];
-      const float w0 = mark[n][0] == -INFINITY ? 0.0f : mark[n][0] - kUp, w1 = mark[n][1] == -INFINITY ? 0.0f : mark[n][1] - kUp;
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        total[n][0] += exp2_fast(c[h][n][0] - m0) + exp2_fast(c[h][n][2] - m0);
-        total[n][1] += exp2_fast(c[h][n][1] - m1) + exp2_fast(c[h][n][3] - m1);
-        w[h][n][0] = transposed(pack2<__half>(exp2_fast(cv[h][n][0] - w0), exp2_fast(cv[h][n][1] - w1)));
-        w[h][n][1] = transposed(pack2<__half>(exp2_fast(cv[h][n][2] - w0), exp2_fast(cv[h][n][3] - w1)));
+        total[n][0] += p[h][n][0] + p[h][n][2];
+        total[n][1] += p[h][n][1] + p[h][n][3];
+        w[h][n][0] = transposed(pack2<__half>(v[h][n][0], v[h][n][1]));
+        w[h][n][1] = transposed(pack2<__half>(v[h][n][2], v[h][n][3]));
       }
-    }
-    // Two chunks of 16 dims of the tokens 16 h .. +15: pairs of dims by pairs of tokens.
-    auto values = [&](uint32_t (&f)[4], int h, int k) {
-      ldm4t(f, vat + chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)));
-    };
     // The first operand of one of them: even dims are its rows g, odd ones its rows g + 8.
     auto operand = [&](uint32_t (&x)[4], uint32_t early, uint32_t late) {
       four_halves<CODES>(__byte_perm(early, 0, 0x3120), x[0], x[1]);
@@ -352,11 +480,11 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < DP / 32; ++k) {
-          uint32_t f[4], x[4];
-          values(f, h, k);
+          uint32_t x[4];
+          if (!kEarly) values(vf[h][k], h, k);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            operand(x, f[2 * j], f[2 * j + 1]);
+            operand(x, vf[h][k][2 * j], vf[h][k][2 * j + 1]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma<__half>(o[2 * k + j][n], x, w[h][n][0], w[h][n][1]);
           }
@@ -392,12 +520,18 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
     }
     __syncwarp();  // the stage may be filled again
     stage = stage + 1 == kStages ? 0 : stage + 1;
+    if (stage == 0) phase ^= 1;
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!BOX) asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!ok) {  // a copy did not come: it and those behind it get as long again, then the block ends
+    for (int t = t_next - kStages * kWarps; t < min(t_next, t_end); t += kWarps) {
+      bar_wait(bar0 + 8 * stage, phase);
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+      if (stage == 0) phase ^= 1;
+    }
+    if (lane == 0) atomicOr(a.err, kDevErrTimeout);
+  }
 
-  // Sums and totals that refer to the scores' maximum, as the join takes them (2^kLift of
-  // the result's type higher).
-  const float lift = half ? kLift<__half> : kLift<__nv_bfloat16>;
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -405,9 +539,9 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
       total[n][i] += __shfl_xor_sync(kFull, total[n][i], 4);
       total[n][i] += __shfl_xor_sync(kFull, total[n][i], 8);
       total[n][i] += __shfl_xor_sync(kFull, total[n][i], 16);
-      total[n][i] *= exp2_fast(lift);
     }
   __syncthreads();
+  const float lift = half ? kLift<__half> : kLift<__nv_bfloat16>;
   float* sums = reinterpret_cast<float*>(smem);           // [warp][row][kPad]
   float* tops = sums + kWarps * kRows * kPad;             // [warp][row]
   float* totals = tops + kWarps * kRows;
@@ -417,12 +551,12 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
     for (int i = 0; i < 2; ++i) {
       const int row = n * 8 + q4 * 2 + i;
       float* r = sums + (warp * kRows + row) * kPad;
-      const float f = mark[n][i] == -INFINITY ? 1.0f : exp2_fast(mark[n][i] - kUp - top[n][i] + lift);
 #pragma unroll
       for (int d = 0; d < DP / 16; ++d)
-        *reinterpret_cast<float2*>(r + d * 16 + 2 * g) = make_float2(o[d][n][i] * f, o[d][n][2 + i] * f);
+        *reinterpret_cast<float2*>(r + d * 16 + 2 * g) = make_float2(o[d][n][i], o[d][n][2 + i]);
       if (g == 0) {
-        tops[warp * kRows + row] = top[n][i];
+        // (The join takes kLift off again, where the result's type has one.)
+        tops[warp * kRows + row] = refer[n][i] == kNothing ? -INFINITY : refer[n][i] + lift;
         totals[warp * kRows + row] = total[n][i];
       }
     }
@@ -433,40 +567,49 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT>))
     join_parts<__nv_bfloat16, DP, NT>(a, view, smem, s, head, sp);
 }
 
-template <int CODES, int DP, int NT>
-cudaError_t launch(const AttendArgs& a, cudaStream_t stream) {
-  auto k = k_attend_token8<CODES, DP, NT>;
+template <int CODES, int DP, int NT, bool BOX>
+cudaError_t launch(const AttendArgs& a, const CodeMaps& maps, cudaStream_t stream) {
+  auto k = k_attend_token8<CODES, DP, NT, BOX>;
   static SmemLimit limit;
-  if (cudaError_t e = limit.set(k, kRing8<DP>)) return e;
+  if (cudaError_t e = limit.set(k, kSmem8<DP, NT, BOX>)) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.batch.sessions) * a.cache.heads * a.splits);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kRing8<DP>;
+  cfg.dynamicSmemBytes = kSmem8<DP, NT, BOX>;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k, a);
+  return cudaLaunchKernelEx(&cfg, k, a, maps);
 }
 
-template <int CODES>
-cudaError_t by_size(const AttendArgs& a, int rows, cudaStream_t stream) {
+template <int CODES, bool BOX>
+cudaError_t by_size(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream) {
   if (a.cache.head_dim <= 64)
-    return rows <= 8 ? launch<CODES, 64, 1>(a, stream) : rows <= 16 ? launch<CODES, 64, 2>(a, stream) : launch<CODES, 64, 4>(a, stream);
-  return rows <= 8 ? launch<CODES, 128, 1>(a, stream) : rows <= 16 ? launch<CODES, 128, 2>(a, stream) : launch<CODES, 128, 4>(a, stream);
+    return rows <= 8    ? launch<CODES, 64, 1, BOX>(a, maps, stream)
+           : rows <= 16 ? launch<CODES, 64, 2, BOX>(a, maps, stream)
+                        : launch<CODES, 64, 4, BOX>(a, maps, stream);
+  return rows <= 8    ? launch<CODES, 128, 1, BOX>(a, maps, stream)
+         : rows <= 16 ? launch<CODES, 128, 2, BOX>(a, maps, stream)
+                      : launch<CODES, 128, 4, BOX>(a, maps, stream);
+}
+template <int CODES>
+cudaError_t by_form(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream) {
+  return a.box_rows ? by_size<CODES, true>(a, rows, maps, stream) : by_size<CODES, false>(a, rows, maps, stream);
 }
 
 }  // namespace
 
 int attend_token8_blocks_per_sm(int head_dim, int rows) {
-  if (head_dim <= 64) return rows <= 16 ? kResident8<64, 2> : kResident8<64, 4>;
-  return kResident8<128, 4>;
+  const int n = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  if (head_dim <= 64) return n == 1 ? kResident8<64, 1, true> : n == 2 ? kResident8<64, 2, true> : kResident8<64, 4, true>;
+  return n == 1 ? kResident8<128, 1, true> : n == 2 ? kResident8<128, 2, true> : kResident8<128, 4, true>;
 }
 
-cudaError_t launch_attend_token8(const AttendArgs& a, int rows, cudaStream_t stream) {
-  return a.cache.codes == kCodesE4M3 ? by_size<kCodesE4M3>(a, rows, stream) : by_size<kCodesI8>(a, rows, stream);
+cudaError_t launch_attend_token8(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream) {
+  return a.cache.codes == kCodesE4M3 ? by_form<kCodesE4M3>(a, rows, maps, stream) : by_form<kCodesI8>(a, rows, maps, stream);
 }
 
 }  // namespace pcs
