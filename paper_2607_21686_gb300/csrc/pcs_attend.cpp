@@ -53,9 +53,10 @@ bool encode_pool(const pcs_kv_cache& c, void* pool, int rows, uint8_t* map) {
   return true;
 }
 
-// A cache in 8 bits: codes copied by boxes of a head of `rows` rows of a page, swizzled
-// by 64 or 128 bytes as its rows are long; scale bytes of 16 heads of as many rows.
-bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, CodeMaps* maps) {
+// A cache in 8 bits: codes copied by boxes of `rows` rows of a page, of `heads` heads one
+// behind the other, swizzled by 64 or 128 bytes as they are long; scale bytes of 16 heads
+// of as many rows.
+bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, int heads, CodeMaps* maps) {
   const EncodeFn fn = encoder();
   if (!fn) return false;
   for (int i = 0; i < 4; ++i) {
@@ -63,12 +64,12 @@ bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, CodeMaps* 
     CUtensorMap m;
     CUresult r;
     if (i < 2) {
-      const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.heads),
-                                  static_cast<cuuint64_t>(c.page_rows), static_cast<cuuint64_t>(c.n_pages)};
-      const cuuint64_t strides[3] = {static_cast<cuuint64_t>(c.head_stride), static_cast<cuuint64_t>(c.row_stride),
+      const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_rows),
+                                  static_cast<cuuint64_t>(c.heads), static_cast<cuuint64_t>(c.n_pages)};
+      const cuuint64_t strides[3] = {static_cast<cuuint64_t>(c.row_stride), static_cast<cuuint64_t>(c.head_stride),
                                      static_cast<cuuint64_t>(c.page_stride)};
       const cuuint32_t wide = c.head_dim <= 64 ? 64 : 128;
-      const cuuint32_t box[4] = {wide, 1, static_cast<cuuint32_t>(rows), 1}, step[4] = {1, 1, 1, 1};
+      const cuuint32_t box[4] = {wide, static_cast<cuuint32_t>(rows), static_cast<cuuint32_t>(heads), 1}, step[4] = {1, 1, 1, 1};
       r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
              wide == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -359,9 +360,17 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
     const int64_t tokens = few || tree ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
     if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
     if (few) {
+      const int n_rows = static_cast<int>(rows);
+      CodeMaps maps;
+      if (codes) {
+        a.box_rows = box_rows(*cache, kTokenTile8);
+        a.box_heads = cache->heads % 4 == 0 ? 4 : cache->heads % 2 == 0 ? 2 : 1;
+        if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, a.box_heads, &maps)) a.box_rows = 0;
+      }
+      const bool boxes = codes && a.box_rows > 0;
       const int64_t resident =
-          static_cast<int64_t>(call.sm_count()) * (codes ? attend_token8_blocks_per_sm(cache->head_dim, static_cast<int>(rows))
-                                                         : attend_token_blocks_per_sm(cache->head_dim, static_cast<int>(rows)));
+          static_cast<int64_t>(call.sm_count()) *
+          (codes ? attend_token8_blocks_per_sm(cache->head_dim, n_rows) : attend_token_blocks_per_sm(cache->head_dim, n_rows));
       const int64_t tiles = (seen + 15) / 16;
       // Parts for a wave of blocks, of two tiles a warp at least; and of several
       // sessions, whose lengths may differ, up to four waves of parts of eight
@@ -371,29 +380,36 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       if (splits > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin, std::min(splits, tiles / (4 * kTokenWarps)));
       if (a.batch.sessions > 1)
         splits = std::max(splits, std::min(4 * resident / pairs, tiles / (8 * kTokenWarps)));
+      // Blocks over codes that take several heads: a warp's result is a part of its head's.
+      int64_t each = 1;
+      if (boxes) {
+        each = kTokenWarps / a.box_heads;
+        const int64_t blocks = pairs / a.box_heads, turns = (tiles + 2 * each - 1) / (2 * each);
+        splits = std::min(resident / blocks, turns / 2);
+        if (splits * each > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin / each, std::min(splits, turns / 4));
+        if (a.batch.sessions > 1) splits = std::max(splits, std::min(4 * resident / blocks, turns / 8));
+      }
       splits = std::max<int64_t>(splits, 1);
-      const bool own = splits <= kTokenOwnJoin && pairs <= kOpWords;
+      const int64_t parts = splits * each;
+      // (Warps that join alone do so for few rows.)
+      const bool own = parts <= kTokenOwnJoin && pairs <= kOpWords && (!boxes || parts * rows <= 128);
       a.splits = static_cast<int32_t>(splits);
-      if (pairs * splits > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
-      if (splits > 1) {
+      if (pairs * parts > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
+      if (parts > 1) {
         uint8_t* ws = nullptr;
         uint32_t* words = nullptr;
-        st = working_memory(call, 4 * token_part_floats(static_cast<int>(rows), cache->head_dim) * pairs * splits, &ws, &words);
+        st = working_memory(call, 4 * token_part_floats(n_rows, cache->head_dim) * pairs * parts, &ws, &words);
         if (st) return st;
         a.part = reinterpret_cast<float*>(ws);
         a.ticket = own ? words : nullptr;
       }
-      CodeMaps maps;
-      if (codes) {
-        a.box_rows = box_rows(*cache, kTokenTile8);
-        if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, &maps)) a.box_rows = 0;
-      }
       call.before(kOpAttendToken);
-      st = call.after(codes ? launch_attend_token8(a, static_cast<int>(rows), maps, call.stream())
-                            : launch_attend_token(a, dtype, static_cast<int>(rows), false, call.stream()));
-      if (!st && splits > 1 && !own) {
+      st = call.after(codes ? launch_attend_token8(a, n_rows, maps, call.stream())
+                            : launch_attend_token(a, dtype, n_rows, false, call.stream()));
+      if (!st && parts > 1 && !own) {
+        a.splits = static_cast<int32_t>(parts);
         call.before(kOpAttendJoin);
-        st = call.after(launch_attend_token(a, dtype, static_cast<int>(rows), true, call.stream()));
+        st = call.after(launch_attend_token(a, dtype, n_rows, true, call.stream()));
       }
       return st ? st : call.end();
     }

@@ -189,6 +189,7 @@ struct AttendArgs {
   uint32_t* err;
   const int32_t* parent;   // new tokens form trees; null: each sees those before it
   uint32_t dtype;          // of q and out
+  int32_t box_heads;       // token kernel over codes: key heads of a block
 };
 
 // One row is one query head of one new token; the token kernel takes all rows

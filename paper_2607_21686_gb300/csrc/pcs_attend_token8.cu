@@ -19,11 +19,15 @@
 //                 dims in the order 0 1 4 5 8 9 12 13 2 3 6 7 .., and the query rows are
 //                 read in the same one); values come out transposed by pairs of dims,
 //                 whose bytes are sorted into even and odd dims (rows g and g + 8).
-//                 A warp's tile is 32 tokens.  They come by tensor copies of boxes of 8
-//                 to 32 rows of a page (BOX), codes and scale bytes apart, or row by row
-//                 from pages whose size no such box divides.  (What bounds copies by the
-//                 warps' lanes is their number: a scale byte of a row is a request of its
-//                 own beside 64 or 128 bytes of codes.)
+//                 A block takes one, two or four key heads of a session and a part of
+//                 its tokens, a warp a head (or a half, a quarter of the tiles of one), in
+//                 tiles of 32 tokens.  Tensor copies bring boxes of 8 to 32 rows of a page,
+//                 of all the block's heads at once, and the scale bytes of 16 heads beside
+//                 them; the warps send them in turn.  (What bounds copies by the warps'
+//                 lanes is their number: a scale byte is a request of its own beside 64 or
+//                 128 bytes of codes.)
+// k_attend_token8_rows  The same from pages whose size no such box divides: each warp
+//                 copies rows of tiles of its own.
 #include "pcs_attend_token_dev.h"
 #include "pcs_codes_dev.h"
 
@@ -31,23 +35,6 @@ namespace pcs {
 namespace {
 
 constexpr int kTile8 = kTokenTile8;
-template <int DP>
-constexpr int kStages8 = DP == 64 ? 3 : 2;
-// Codes of keys and of values, then scale bytes of each row: 16 heads' (BOX) or 4 heads'.
-template <bool BOX>
-constexpr int kScaleBytes = BOX ? 16 : 4;
-template <int DP, bool BOX>
-constexpr uint32_t kStage8 = 2 * kTile8 * (DP + kScaleBytes<BOX>);
-// (Boxes begin at multiples of 1,024 bytes: room to get there.)
-template <int DP, bool BOX>
-constexpr uint32_t kRing8 = kWarps * kStages8<DP> * kStage8<DP, BOX> + (BOX ? 1024 : 0);
-// The rings, or what the warps' results take, which lie over them at the end.
-template <int DP, int NT>
-constexpr uint32_t kJoin8 = kWarps * 8 * NT * (kPadOf<DP> + 2) * 4;
-template <int DP, int NT, bool BOX>
-constexpr uint32_t kSmem8 = kRing8<DP, BOX> > kJoin8<DP, NT> ? kRing8<DP, BOX> : kJoin8<DP, NT>;
-template <int DP, int NT, bool BOX>
-constexpr int kResident8 = NT == 4 ? 2 : NT == 2 ? (DP == 64 ? 3 : 2) : static_cast<int>(227 * 1024 / (kSmem8<DP, NT, BOX> + 3072));
 
 // 4 bytes from global to shared memory, zeros where there is no source.
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
@@ -63,280 +50,110 @@ constexpr float kNothing = -1e30f;
 // A weight beyond this, or times its value's scale beyond 2^15, raises the reference.
 constexpr float kMostWeight = 1.2676506e30f;  // 2^100
 
-// A box of rows: `x`, `y`, .. where it begins in the tensor.
-__device__ __forceinline__ void box_of_codes(uint32_t to, uint64_t map, int head, int row, int page, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
-      "l"(map), "r"(0), "r"(head), "r"(row), "r"(page), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void box_of_scales(uint32_t to, uint64_t map, int byte, int row, int page, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
-      "l"(map), "r"(byte), "r"(row), "r"(page), "r"(bar)
-      : "memory");
-}
-
-template <int CODES, int DP, int NT, bool BOX>
-__global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
-    k_attend_token8(const __grid_constant__ AttendArgs a, const __grid_constant__ CodeMaps maps) {
-  constexpr int kStages = kStages8<DP>;
-  constexpr uint32_t kStage = kStage8<DP, BOX>;
-  constexpr int kChunks = DP / 16;           // 16-byte chunks of a row
-  constexpr int kRowsAtOnce = 32 / kChunks;  // rows one copy instruction of a warp moves
-  constexpr int kRows = 8 * NT;
-  constexpr int kPad = kPadOf<DP>;
-  constexpr bool kEarly = NT == 1;           // registers hold a tile's values beside its scores
-  constexpr float kUp = 7.0f;                // weights are 2^7 times higher, as kLift says
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ uint32_t valid[kWarps][kStages];
-  __shared__ __align__(8) uint64_t bars[BOX ? kWarps * kStages : 1];
-  __shared__ TreeNode nodes[PCS_TREE_MAX];
-
-  attend_dependency();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int g = lane >> 2, q4 = lane & 3;
-  const int head = blockIdx.x % a.cache.heads;
-  const int sp = blockIdx.x / a.cache.heads % a.splits;
-  const int s = blockIdx.x / a.cache.heads / a.splits;
-  if (BOX && tid < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps.map[tid])) : "memory");
-  SessionView view = session_rows(a, s);
-  narrow(a, view, 0, view.m, BOX ? a.box_rows : 1);
-  if (view.m <= 0) return;  // the same in every part
-  const int rows = view.m * a.group;
-  if (!rows_there(a, view, tid == 0)) return;  // (max_new tokens' rows are at most kRows)
-  const int head_dim = a.cache.head_dim;
-  const bool tree = a.parent != nullptr;
-  uint8_t* const ring_ptr = smem + (BOX ? -smem_addr(smem) & 1023u : 0u) + warp * kStages * kStage;
-  const uint32_t ring = smem_addr(ring_ptr), bar0 = smem_addr(bars) + 8 * warp * kStages;
-  if (BOX) {
-    if (lane == 0) {
-      for (int i = 0; i < kStages; ++i) bar_init(bar0 + 8 * i, 1);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncwarp();
-  } else if (head_dim < DP) {  // chunks that no copy writes
-    for (uint32_t i = lane * 16; i < kStages * kStage; i += 512)
-      *reinterpret_cast<uint4*>(ring_ptr + i) = make_uint4(0, 0, 0, 0);
-    __syncwarp();
-  }
-  if (tree) {
-    tree_nodes(a, view, tid, nodes);
-    __syncthreads();
-  }
-
-  // This part's tiles; the warp takes every kWarps-th one.
-  const int tiles = (view.seen + kTile8 - 1) / kTile8;
-  const int per = (tiles + a.splits - 1) / a.splits;
-  const int t_end = min(tiles, (sp + 1) * per);
-  int t_next = sp * per + warp;  // the next tile whose places are looked up
-
-  // What a tile's copies need to know, looked up one tile ahead of them: a lane's row, or
-  // (BOX) a lane's box of rows, of which there are 32 / box_rows a tile.
-  using Ahead = std::conditional_t<BOX, Box, RowPlace>;
-  const int box_shift = BOX ? 31 - __clz(a.box_rows) : 0, boxes = kTile8 >> box_shift;
-  auto look = [&](int t) {
-    if constexpr (BOX) {
-      Box x = {-1, -1, 0};
-      const int e = t * kTile8 + lane * a.box_rows;
-      if (t < t_end && lane < boxes && e < view.seen) x = box_place(a, s, view, e);
-      return x;
-    } else {
-      RowPlace r = {kNoRow, kNoRow};
-      const int e = t * kTile8 + lane;
-      if (t < t_end && e < view.seen) r = row_place(a, s, seen_position(view, e));
-      return r;
-    }
-  };
-  // The bytes of a row that hold the head's scale byte.
-  constexpr int kScales = kScaleBytes<BOX>;
-  const int scale_from = head & -kScales, scale_byte = head & (kScales - 1);
-  auto copy = [&](Ahead& r, int t, int stage) {
-    const uint32_t base = ring + stage * kStage;
-    if constexpr (BOX) {
-      settle(a, r);
-      const int e = t * kTile8 + lane;
-      const bool mine = __shfl_sync(kFull, r.k, lane >> box_shift) < a.cache.n_pages && !(e >= view.gap0 && e < view.gap1);
-      const uint32_t there = __ballot_sync(kFull, mine);
-      const uint32_t bar = bar0 + 8 * stage;
-      if (lane == 0) {
-        valid[warp][stage] = there;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kStage) : "memory");
-      }
-      for (int k = 0; k < boxes; ++k) {
-        const int kp = __shfl_sync(kFull, r.k, k), vp = __shfl_sync(kFull, r.v, k), row = __shfl_sync(kFull, r.row, k);
-        const uint32_t at = k * a.box_rows;
-        if (lane == 0) {
-          box_of_codes(base + at * DP, reinterpret_cast<uint64_t>(maps.map[0]), head, row, kp, bar);
-          box_of_codes(base + (kTile8 + at) * DP, reinterpret_cast<uint64_t>(maps.map[1]), head, row, vp, bar);
-          box_of_scales(base + 2 * kTile8 * DP + at * kScales, reinterpret_cast<uint64_t>(maps.map[2]), scale_from, row, kp, bar);
-          box_of_scales(base + 2 * kTile8 * DP + (kTile8 + at) * kScales, reinterpret_cast<uint64_t>(maps.map[3]), scale_from, row,
-                        vp, bar);
-        }
-      }
-    } else {
-      const int chunk = lane % kChunks, row0 = lane / kChunks;
-      const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes;
-      const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
-      const bool mine = r.k != kNoRow;
-      const uint32_t there = __ballot_sync(kFull, mine);
-      if (lane == 0) valid[warp][stage] = there;
-#pragma unroll
-      for (int i = 0; i < kTile8 / kRowsAtOnce; ++i) {
-        const int row = i * kRowsAtOnce + row0;
-        const uint32_t ko = __shfl_sync(kFull, r.k, row), vo = __shfl_sync(kFull, r.v, row);
-        const bool in = ko != kNoRow;
-        if (chunk * 16 < head_dim) {
-          const uint32_t at = base + chunk_at<DP>(row, chunk);
-          copy16(at, row_at(a, kbase, in ? ko : 0) + chunk * 16, in);
-          copy16(at + kTile8 * DP, row_at(a, vbase, in ? vo : 0) + chunk * 16, in);
-        }
-      }
-      // (A row is a multiple of 16 bytes, so the words that hold scales are in it.)
-      const uint32_t words = base + 2 * kTile8 * DP + lane * 4;
-      copy4(words, row_at(a, a.cache.k, mine ? r.k : 0) + a.cache.scale_at + scale_from, mine);
-      copy4(words + kTile8 * 4, row_at(a, a.cache.v, mine ? r.v : 0) + a.cache.scale_at + scale_from, mine);
-    }
-  };
-
-  Ahead place;
-  {
-    Ahead first[kStages];
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) first[i] = look(t_next + i * kWarps);
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) {
-      if (t_next < t_end) copy(first[i], t_next, i);
-      if (!BOX) asm volatile("cp.async.commit_group;" ::: "memory");
-      t_next += kWarps;
-    }
-    place = first[kStages - 1];
-  }
-
-  // Query rows as the second operand: of chunk k, dims 4 q4 .. +3 of row g, times
-  // 2^-back, the power that puts the row's largest element at 2^14.
+// A warp's query rows over the tiles that it takes.
+template <int CODES, int DP, int NT>
+struct TokenRows {
+  static constexpr int H = NT == 4 ? 1 : 2;     // halves of a tile, 16 tokens, that are in registers at once
+  static constexpr bool kEarly = NT == 1;       // a tile's values beside its scores
+  static constexpr float kUp = 7.0f;            // weights are 2^7 times higher, as kLift says
   uint32_t qf[NT][DP / 16][2];
-  float back[NT][2];  // of the rows this thread has scores of, times the scale
-  const bool half = a.dtype == PCS_DT_F16;
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int r = n * 8 + g;
-    const uint32_t tok = a.by_group.div(r);
-    const uint8_t* q = a.q.data + (view.q0 + tok) * a.q.token_bytes +
-                       (head * a.group + (r - tok * a.group)) * a.q.head_bytes;
-    float top = 0.0f;
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k) {
-      const int d = k * 16 + q4 * 4;
-      uint2 x = make_uint2(0, 0);
-      if (r < rows && d < head_dim) x = *reinterpret_cast<const uint2*>(q + d * 2);
-      qf[n][k][0] = x.x;
-      qf[n][k][1] = x.y;
-    }
-    auto value = [&](uint32_t x) {
-      return half ? __half22float2(*reinterpret_cast<const __half2*>(&x))
-                  : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
-    };
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float2 x = value(qf[n][k][i]);
-        top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
-      }
-    top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
-    // (Rows with an infinity stay as they are, very small ones are not raised above 2^-86.)
-    int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;
-    e = e > 127 ? 14 : max(e, -100);
-    const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float2 x = value(qf[n][k][i]);
-        qf[n][k][i] = pack2<__half>(x.x * up, x.y * up);
-      }
-    const float down = fmaxf(__uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * a.scale_log2, 1.2e-38f);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) back[n][i] = __shfl_sync(kFull, down, (q4 * 2 + i) * 4);
-  }
-  // New tokens of the rows this thread has scores of.
-  const bool many = view.m > 1;
+  float back[NT][2];       // of the rows this thread has scores of, times the scale
   int32_t new_token[NT][2];
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) new_token[n][i] = min(static_cast<int>(a.by_group.div(n * 8 + q4 * 2 + i)), view.m - 1);
-
-  // Ranges of the first and the last new token.  (Nodes of a tree: what all of them
-  // see of the context.)
-  RowRange low = row_range(a, view, view.first);
-  const RowRange high = row_range(a, view, view.first + view.m - 1);
-  if (tree) low.hi = context_end(view);
-  // Which of the tokens from place b on the rows of new token t see, as bits.
-  auto sees = [&](int32_t t, int b) {
-    return tree ? tree_row(a, view, nodes[t]).bits(b) : row_range(a, view, view.first + t).bits(b);
-  };
-
   float o[DP / 16][NT][4];
   float refer[NT][2], total[NT][2];
+  int lane, g, q4, m_new;
+
+  __device__ __forceinline__ void begin(const AttendArgs& a, const SessionView& view, int head, int lane_) {
+    lane = lane_, g = lane >> 2, q4 = lane & 3, m_new = view.m;
+    const int rows = view.m * a.group;
+    // Query rows as the second operand: of chunk k, dims 4 q4 .. +3 of row g, times
+    // 2^-back, the power that puts the row's largest element at 2^14.
+    const bool half = a.dtype == PCS_DT_F16;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    refer[n][0] = refer[n][1] = kNothing;
-    total[n][0] = total[n][1] = 0.0f;
+    for (int n = 0; n < NT; ++n) {
+      const int r = n * 8 + g;
+      const uint32_t tok = a.by_group.div(r);
+      const uint8_t* q = a.q.data + (view.q0 + tok) * a.q.token_bytes +
+                         (head * a.group + (r - tok * a.group)) * a.q.head_bytes;
+      float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.0f;
+      for (int k = 0; k < DP / 16; ++k) {
+        const int d = k * 16 + q4 * 4;
+        uint2 x = make_uint2(0, 0);
+        if (r < rows && d < a.cache.head_dim) x = *reinterpret_cast<const uint2*>(q + d * 2);
+        qf[n][k][0] = x.x;
+        qf[n][k][1] = x.y;
+      }
+      auto value = [&](uint32_t x) {
+        return half ? __half22float2(*reinterpret_cast<const __half2*>(&x))
+                    : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+      };
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 x = value(qf[n][k][i]);
+          top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
+        }
+      top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
+      // (Rows with an infinity stay as they are, very small ones are not raised above 2^-86.)
+      int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;
+      e = e > 127 ? 14 : max(e, -100);
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 x = value(qf[n][k][i]);
+          qf[n][k][i] = pack2<__half>(x.x * up, x.y * up);
+        }
+      const float down = fmaxf(__uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * a.scale_log2, 1.2e-38f);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) back[n][i] = __shfl_sync(kFull, down, (q4 * 2 + i) * 4);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        new_token[n][i] = min(static_cast<int>(a.by_group.div(n * 8 + q4 * 2 + i)), view.m - 1);
+        refer[n][i] = kNothing;
+        total[n][i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.0f;
+    }
   }
 
-  int stage = 0;
-  uint32_t phase = 0;
-  bool ok = true;
-  for (int t = sp * per + warp; t < t_end; t += kWarps) {
-    if (!BOX) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-      __syncwarp();
-    }
-    {
-      const int into = stage == 0 ? kStages - 1 : stage - 1;
-      if (t_next < t_end) copy(place, t_next, into);
-      if (!BOX) asm volatile("cp.async.commit_group;" ::: "memory");
-      t_next += kWarps;
-      place = look(t_next);
-    }
-    if (BOX) {
-      ok = __all_sync(kFull, bar_wait(bar0 + 8 * stage, phase)) != 0;
-      if (!ok) break;
-    }
-    const uint32_t kat = ring + stage * kStage, vat = kat + kTile8 * DP;
-    // This lane's row's scales.
-    const uint8_t* scales = ring_ptr + stage * kStage + 2 * kTile8 * DP + lane * kScales + scale_byte;
-    const float ks = scale_value(scales[0]), vs = scale_value(scales[kTile8 * kScales]);
-    const uint32_t there = valid[warp][stage];
-    const int e0 = t * kTile8;
-    // (Boxes begin ahead of what is seen and end behind it.)
-    const bool part = (BOX || many) && !(e0 + kTile8 - 1 <= low.hi && (e0 >= high.lo || e0 + kTile8 <= low.first));
+  // Tokens [e0, e0 + 32): keys and values in shared memory, at(h, k) the offset of this
+  // lane's chunk of chunks 2 k and 2 k + 1 of half h; the scales of token e0 + lane; which
+  // tokens are in the cache; whether some row does not see all (sees: a new token's bits).
+  template <typename At, typename Sees>
+  __device__ __forceinline__ void tile(uint32_t kat, uint32_t vat, const At& at, float ks, float vs, int e0, uint32_t there, bool part,
+                                       const Sees& sees) {
+#pragma unroll 1
+    for (int h0 = 0; h0 < 2; h0 += H) halves(kat, vat, at, ks, vs, e0, there, part, sees, h0);
+  }
 
-    // Two chunks of 16 dims of the tokens 16 h .. +15: pairs of dims by pairs of tokens.
-    auto values = [&](uint32_t (&f)[4], int h, int k) {
-      ldm4t(f, vat + chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)));
-    };
+  template <typename At, typename Sees>
+  __device__ __forceinline__ void halves(uint32_t kat, uint32_t vat, const At& at, float ks, float vs, int e0, uint32_t there, bool part,
+                                         const Sees& sees, int h0) {
     // All that the tile gives is on its way out of shared memory before any of it is used.
-    uint32_t kf[2][DP / 32][4], vf[2][DP / 32][4];
+    uint32_t kf[H][DP / 32][4], vf[H][DP / 32][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int k = 0; k < DP / 32; ++k) ldm4(kf[h][k], kat + chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)));
+      for (int k = 0; k < DP / 32; ++k) ldm4(kf[h][k], kat + at(h0 + h, k));
     if (kEarly) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int k = 0; k < DP / 32; ++k) values(vf[h][k], h, k);
+        for (int k = 0; k < DP / 32; ++k) ldm4t(vf[h][k], vat + at(h0 + h, k));
     }
     // Scores of tokens 16 h + g, + 8, but for the rows' factors.
-    float c[2][NT][4];
+    float c[H][NT][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int n = 0; n < NT; ++n) c[h][n][0] = c[h][n][1] = c[h][n][2] = c[h][n][3] = 0.0f;
 #pragma unroll
@@ -344,20 +161,20 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
           uint32_t x[4];
           four_halves<CODES>(kf[h][k][2 * j], x[0], x[2]);
           four_halves<CODES>(kf[h][k][2 * j + 1], x[1], x[3]);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma<__half>(c[h][n], x, qf[n][2 * k + j][0], qf[n][2 * k + j][1]);
         }
-    float vscale[2][2];  // of token 16 h + 8 j + g
+    float vscale[H][2];  // of token 16 h + 8 j + g
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float y = __shfl_sync(kFull, ks, h * 16 + j * 8 + g);
-        vscale[h][j] = __shfl_sync(kFull, vs, h * 16 + j * 8 + g);
+        const float y = __shfl_sync(kFull, ks, (h0 + h) * 16 + j * 8 + g);
+        vscale[h][j] = __shfl_sync(kFull, vs, (h0 + h) * 16 + j * 8 + g);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           c[h][n][2 * j] *= y;
@@ -371,22 +188,22 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          seen[n][i] = (there & (part ? sees(new_token[n][i], e0) : kFull)) >> g;
+          seen[n][i] = (there & (part ? sees(new_token[n][i], e0) : kFull)) >> (16 * h0 + g);
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
               if (!(seen[n][i] >> (h * 16 + j * 8) & 1)) c[h][n][2 * j + i] = -INFINITY;
         }
     }
     // Weights 2^(score - reference), p; times the values' scales, v.
-    float p[2][NT][4], v[2][NT][4];
+    float p[H][NT][4], v[H][NT][4];
     auto weigh = [&] {
       float most = 0.0f, largest = 0.0f;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < H; ++h)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -408,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
         for (int i = 0; i < 2; ++i) {
           float m = -INFINITY, w = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const float x = c[h][n][2 * j + i] * back[n][i];
@@ -439,16 +256,16 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
               if (!(seen[n][i] >> (h * 16 + j * 8) & 1)) v[h][n][2 * j + i] = 0.0f;
     }
-    uint32_t w[2][NT][2];
+    uint32_t w[H][NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < H; ++h) {
         total[n][0] += p[h][n][0] + p[h][n][2];
         total[n][1] += p[h][n][1] + p[h][n][3];
         w[h][n][0] = transposed(pack2<__half>(v[h][n][0], v[h][n][1]));
@@ -465,11 +282,11 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
     if (CODES == kCodesE4M3 && part) {
       uint32_t nan = 0;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int k = 0; k < DP / 32; ++k) {
           uint32_t f[4];
-          values(f, h, k);
+          ldm4t(f, vat + at(h0 + h, k));
 #pragma unroll
           for (int i = 0; i < 4; ++i) nan |= (f[i] & 0x7f7f7f7fu) + 0x01010101u;
         }
@@ -477,11 +294,11 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
     }
     if (!apart) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int k = 0; k < DP / 32; ++k) {
           uint32_t x[4];
-          if (!kEarly) values(vf[h][k], h, k);
+          if (!kEarly) ldm4t(vf[h][k], vat + at(h0 + h, k));
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             operand(x, vf[h][k][2 * j], vf[h][k][2 * j + 1]);
@@ -490,10 +307,10 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
           }
         }
     } else {
-      for (int i = 0; i < view.m; ++i) {
-        const uint32_t m = sees(i, e0) >> (2 * q4);
+      for (int i = 0; i < m_new; ++i) {
+        const uint32_t m = sees(i, e0) >> (16 * h0 + 2 * q4);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
           uint32_t in[2];  // of tokens 16 h + 2 q4, +1 and 8 more
 #pragma unroll
           for (int z = 0; z < 2; ++z)
@@ -501,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
 #pragma unroll
           for (int k = 0; k < DP / 32; ++k) {
             uint32_t f[4], x[4];
-            values(f, h, k);
+            ldm4t(f, vat + at(h0 + h, k));
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               operand(x, f[2 * j] & in[0], f[2 * j + 1] & in[1]);
@@ -518,29 +335,429 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
         }
       }
     }
-    __syncwarp();  // the stage may be filled again
+  }
+
+  // The rows' totals over the warp.
+  __device__ __forceinline__ void end() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        total[n][i] += __shfl_xor_sync(kFull, total[n][i], 4);
+        total[n][i] += __shfl_xor_sync(kFull, total[n][i], 8);
+        total[n][i] += __shfl_xor_sync(kFull, total[n][i], 16);
+      }
+  }
+};
+
+// ---- Boxes of rows ---------------------------------------------------------------------
+
+// A block's turn is its warps' tiles: those of its heads, or several of one's.  Codes of
+// keys and of values of a turn, each box with its heads one behind the other; then scale
+// bytes of 16 heads, of keys and of values.
+template <int DP>
+constexpr int kStages8 = DP == 64 ? 3 : 2;
+template <int DP, int HEADS>
+constexpr uint32_t kStage8 = 2 * kWarps * kTile8 * DP + 2 * (kWarps / HEADS) * kTile8 * 16;
+// (Boxes begin at multiples of 1,024 bytes: room to get there.)
+template <int DP, int HEADS>
+constexpr uint32_t kSmem8 = kStages8<DP> * kStage8<DP, HEADS> + 1024;
+// Blocks that one SM holds, by its registers and by its shared memory.
+template <int DP, int NT>
+constexpr int kByRegisters8 = NT == 4 ? 2 : NT == 2 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 3;
+template <int DP, int NT, int HEADS>
+constexpr int kResident8 = kByRegisters8<DP, NT> * (kSmem8<DP, HEADS> + 3072) <= 227 * 1024
+                               ? kByRegisters8<DP, NT>
+                               : static_cast<int>(227 * 1024 / (kSmem8<DP, HEADS> + 3072));
+
+__device__ __forceinline__ void box_of_codes(uint32_t to, uint64_t map, int row, int head, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+      "l"(map), "r"(0), "r"(row), "r"(head), "r"(page), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void box_of_scales(uint32_t to, uint64_t map, int byte, int row, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
+      "l"(map), "r"(byte), "r"(row), "r"(page), "r"(bar)
+      : "memory");
+}
+
+template <int CODES, int DP, int NT, int HEADS>
+__global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, HEADS>))
+    k_attend_token8(const __grid_constant__ AttendArgs a, const __grid_constant__ CodeMaps maps) {
+  constexpr int kStages = kStages8<DP>;
+  constexpr uint32_t kStage = kStage8<DP, HEADS>;
+  constexpr int kTiles = kWarps / HEADS;        // tiles of a turn
+  constexpr uint32_t kCodeBytes = kWarps * kTile8 * DP, kScaleBytes = kTiles * kTile8 * 16;
+  constexpr int kRows = 8 * NT;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint32_t valid[kStages][kTiles];
+  __shared__ __align__(8) uint64_t bars[2 * kStages];  // filled, free
+  __shared__ TreeNode nodes[PCS_TREE_MAX];
+
+  attend_dependency();
+  const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
+  const int groups = a.cache.heads / HEADS;
+  const int head0 = blockIdx.x % groups * HEADS;
+  const int sp = blockIdx.x / groups % a.splits;
+  const int s = blockIdx.x / groups / a.splits;
+  const int head = head0 + warp % HEADS, turn = warp / HEADS;  // this warp's head, and its tile of a turn
+  if (tid < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps.map[tid])) : "memory");
+  SessionView view = session_rows(a, s);
+  narrow(a, view, 0, view.m, a.box_rows);
+  if (view.m <= 0) return;  // the same in every part
+  const int rows = view.m * a.group;
+  if (!rows_there(a, view, tid == 0)) return;  // (max_new tokens' rows are at most kRows)
+  const bool tree = a.parent != nullptr;
+  const uint32_t ring = (smem_addr(smem) + 1023) & ~1023u, bar0 = smem_addr(bars);
+  uint8_t* const ring_ptr = smem + (ring - smem_addr(smem));
+  auto full = [&](int stage) { return bar0 + 8 * stage; };
+  auto empty = [&](int stage) { return bar0 + 8 * (kStages + stage); };
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      bar_init(full(i), 1);
+      bar_init(empty(i), kWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tree) tree_nodes(a, view, tid, nodes);
+  __syncthreads();
+
+  // This part's turns.
+  const int all = (view.seen + kTile8 * kTiles - 1) / (kTile8 * kTiles);
+  const int per = (all + a.splits - 1) / a.splits;
+  const int begin = min(all, sp * per), turns = min(all, begin + per) - begin;
+
+  // A lane's box of the rows of turn i, of which there are `boxes`.
+  const int shift = 31 - __clz(a.box_rows), boxes = kTiles * kTile8 >> shift;
+  auto look = [&](int i) {
+    Box x = {-1, -1, 0};
+    const int e = ((begin + i) * kTiles * kTile8) + (lane << shift);
+    if (i < turns && lane < boxes && e < view.seen) x = box_place(a, s, view, e);
+    return x;
+  };
+  auto send = [&](Box x, int i, int stage) {
+    settle(a, x);
+    const uint32_t at = ring + stage * kStage, bar = full(stage);
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k) {
+      const int r = k * kTile8 + lane, e = (begin + i) * kTiles * kTile8 + r;
+      const bool in = __shfl_sync(kFull, x.k, r >> shift) < a.cache.n_pages && !(e >= view.gap0 && e < view.gap1);
+      const uint32_t there = __ballot_sync(kFull, in);
+      if (lane == 0) valid[stage][k] = there;
+    }
+    if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kStage) : "memory");
+    for (int k = 0; k < boxes; ++k) {
+      const int kp = __shfl_sync(kFull, x.k, k), vp = __shfl_sync(kFull, x.v, k), row = __shfl_sync(kFull, x.row, k);
+      const uint32_t codes = at + (k << shift) * HEADS * DP, scales = at + 2 * kCodeBytes + (k << shift) * 16;
+      if (lane == 0) {
+        box_of_codes(codes, reinterpret_cast<uint64_t>(maps.map[0]), row, head0, kp, bar);
+        box_of_codes(codes + kCodeBytes, reinterpret_cast<uint64_t>(maps.map[1]), row, head0, vp, bar);
+        box_of_scales(scales, reinterpret_cast<uint64_t>(maps.map[2]), head0 & ~15, row, kp, bar);
+        box_of_scales(scales + kScaleBytes, reinterpret_cast<uint64_t>(maps.map[3]), head0 & ~15, row, vp, bar);
+      }
+    }
+  };
+  // The first turns are sent by a warp each; then warp i % kWarps sends turn i + kStages - 1
+  // when it comes to turn i, whose stage was used up in the turn before.
+  static_assert(kStages - 1 <= kWarps, "a warp a stage");
+  if (warp < kStages - 1 && warp < turns) send(look(warp), warp, warp);
+  Box ahead = look(warp + kStages - 1);
+
+  TokenRows<CODES, DP, NT> work;
+  work.begin(a, view, head, lane);
+  // Ranges of the first and the last new token.  (Nodes of a tree: what all of them
+  // see of the context.)
+  RowRange low = row_range(a, view, view.first);
+  const RowRange high = row_range(a, view, view.first + view.m - 1);
+  if (tree) low.hi = context_end(view);
+  // Which of the tokens from place b on the rows of new token t see, as bits.
+  auto sees = [&](int32_t t, int b) {
+    return tree ? tree_row(a, view, nodes[t]).bits(b) : row_range(a, view, view.first + t).bits(b);
+  };
+  // Where this lane's rows of its warp's tile lie in a turn's codes: row 16 h + (lane & 15)
+  // of it in box r >> shift, at the warp's head.
+  uint32_t row_at_h[2], chunk[DP / 32];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = h * 16 + (lane & 15), b = (turn * kTile8 + r) >> shift;
+    row_at_h[h] = ((((b * HEADS + warp % HEADS) << shift) + (r & (a.box_rows - 1)))) * DP;
+  }
+#pragma unroll
+  for (int k = 0; k < DP / 32; ++k)  // (the swizzle goes by a row's number modulo 8, as boxes have at least 8)
+    chunk[k] = chunk_at<DP>(lane & 7, 2 * k + (lane >> 4)) - (lane & 7) * DP;
+  auto at = [&](int h, int k) { return row_at_h[h] + chunk[k]; };
+
+  bool ok = true;
+  int stage = 0;
+  uint32_t phase = 0;
+  for (int i = 0; i < turns; ++i) {
+    if (i + kStages - 1 < turns && i % kWarps == warp) {
+      const int into = stage == 0 ? kStages - 1 : stage - 1;  // the stage of turn i - 1
+      if (i > 0) ok = __all_sync(kFull, bar_wait(empty(into), phase ^ (stage == 0 ? 1 : 0))) != 0;
+      if (!ok) break;
+      send(ahead, i + kStages - 1, into);
+      ahead = look(i + kWarps + kStages - 1);
+    }
+    ok = __all_sync(kFull, bar_wait(full(stage), phase)) != 0;
+    if (!ok) break;
+    const int e0 = ((begin + i) * kTiles + turn) * kTile8;
+    if (e0 < view.seen) {
+      const uint32_t codes = ring + stage * kStage;
+      const uint8_t* scales = ring_ptr + stage * kStage + 2 * kCodeBytes + (turn * kTile8 + lane) * 16 + (head & 15);
+      // (Boxes begin ahead of what is seen and end behind it.)
+      const bool part = !(e0 + kTile8 - 1 <= low.hi && (e0 >= high.lo || e0 + kTile8 <= low.first));
+      work.tile(codes, codes + kCodeBytes, at, scale_value(scales[0]), scale_value(scales[kScaleBytes]), e0, valid[stage][turn], part,
+                sees);
+    }
+    __syncwarp();
+    if (lane == 0) bar_arrive(empty(stage));
     stage = stage + 1 == kStages ? 0 : stage + 1;
     if (stage == 0) phase ^= 1;
   }
-  if (!BOX) asm volatile("cp.async.wait_all;" ::: "memory");
-  if (!ok) {  // a copy did not come: it and those behind it get as long again, then the block ends
-    for (int t = t_next - kStages * kWarps; t < min(t_next, t_end); t += kWarps) {
-      bar_wait(bar0 + 8 * stage, phase);
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-      if (stage == 0) phase ^= 1;
-    }
+  if (!ok) {
+    // A copy did not come.  Those that this warp knows of get as long again, then the
+    // block ends: every warp that gives up does so, so none is on its way then.
+    for (int k = 0; k < kStages; ++k) bar_wait(full(k), phase ^ (k < stage ? 1 : 0));
     if (lane == 0) atomicOr(a.err, kDevErrTimeout);
   }
+  work.end();
 
+  // A warp's result is its part's: one of splits * kTiles of its head.
+  const int parts = a.splits * kTiles, part = sp * kTiles + turn;
+  const int64_t pair = static_cast<int64_t>(s) * a.cache.heads + head;
+  const int64_t part_floats = static_cast<int64_t>(kRows) * (DP + 2);
+  const bool half = a.dtype == PCS_DT_F16;
+  const int g = lane >> 2, q4 = lane & 3;
+  // Row `row`'s dims d, d + 1 and, from one thread, its log sum of exponentials.
+  auto write = [&](int row, int d, float x, float y, float inv) {
+    const uint32_t tok = a.by_group.div(row);
+    if (d < a.cache.head_dim)
+      *reinterpret_cast<uint32_t*>(a.out.data + (view.q0 + tok) * a.out.token_bytes +
+                                   (head * a.group + (row - static_cast<int>(tok) * a.group)) * a.out.head_bytes + d * 2) =
+          half ? pack2<__half>(x * inv, y * inv) : pack2<__nv_bfloat16>(x * inv, y * inv);
+  };
+  auto write_lse = [&](int row, float top, float total) {
+    const uint32_t tok = a.by_group.div(row);
+    if (a.lse)
+      a.lse[(view.q0 + tok) * (static_cast<int64_t>(a.cache.heads) * a.group) + head * a.group + (row - static_cast<int>(tok) * a.group)] =
+          total == 0.0f ? -INFINITY : fmaf(top, 0.693147180559945309f, logf(total));
+  };
+  if (parts == 1) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = n * 8 + q4 * 2 + i;
+        if (row >= rows) continue;
+        const float total = work.total[n][i], inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) write(row, d * 16 + 2 * g, work.o[d][n][i], work.o[d][n][2 + i], inv);
+        if (g == 0) write_lse(row, work.refer[n][i], total);
+      }
+    return;
+  }
+  float* mine = a.part + (pair * parts + part) * part_floats;
+  // (A join in a launch of its own takes kLift off the maxima, where the result's type has one.)
+  const float lift = a.ticket ? 0.0f : half ? kLift<__half> : kLift<__nv_bfloat16>;
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      total[n][i] += __shfl_xor_sync(kFull, total[n][i], 4);
-      total[n][i] += __shfl_xor_sync(kFull, total[n][i], 8);
-      total[n][i] += __shfl_xor_sync(kFull, total[n][i], 16);
+      const int row = n * 8 + q4 * 2 + i;
+      if (row >= rows) continue;
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d)
+        *reinterpret_cast<float2*>(mine + row * DP + d * 16 + 2 * g) = make_float2(work.o[d][n][i], work.o[d][n][2 + i]);
+      if (g == 0) {
+        mine[kRows * DP + row] = work.refer[n][i] == kNothing ? -INFINITY : work.refer[n][i] + lift;
+        mine[kRows * DP + kRows + row] = work.total[n][i];
+      }
     }
+  if (a.ticket == nullptr) return;
+
+  // The part that ends last joins all, in the parts' order: a part a lane for a row's
+  // factors, then two dims a lane.
+  __threadfence();
+  __syncwarp();
+  uint32_t before = 0;
+  if (lane == 0) before = atomicInc(a.ticket + pair, parts - 1);
+  if (__shfl_sync(kFull, before, 0) != static_cast<uint32_t>(parts - 1)) return;
+  __threadfence();
+  const float* first = a.part + pair * parts * part_floats;
+  for (int row = 0; row < rows; ++row) {
+    float top = -INFINITY, total = 0.0f;
+    if (lane < parts) {
+      top = __ldcg(first + lane * part_floats + kRows * DP + row);
+      total = __ldcg(first + lane * part_floats + kRows * DP + kRows + row);
+    }
+    float m = top;
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) m = fmaxf(m, __shfl_xor_sync(kFull, m, k));
+    const float factor = exp2_fast(top - (m == -INFINITY ? 0.0f : m));
+    total *= factor;
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) total += __shfl_xor_sync(kFull, total, k);
+    float2 x[DP / 64];
+#pragma unroll
+    for (int d = 0; d < DP / 64; ++d) x[d] = make_float2(0.0f, 0.0f);
+#pragma unroll 4
+    for (int w = 0; w < parts; ++w) {
+      const float f = __shfl_sync(kFull, factor, w);
+#pragma unroll
+      for (int d = 0; d < DP / 64; ++d) {
+        const float2 y = __ldcg(reinterpret_cast<const float2*>(first + w * part_floats + row * DP + 64 * d + 2 * lane));
+        x[d].x = fmaf(y.x, f, x[d].x);
+        x[d].y = fmaf(y.y, f, x[d].y);
+      }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int d = 0; d < DP / 64; ++d) write(row, 64 * d + 2 * lane, x[d].x, x[d].y, inv);
+    if (lane == 0) write_lse(row, m, total);
+  }
+}
+
+// ---- Rows one by one ---------------------------------------------------------------------
+
+template <int DP>
+constexpr int kRowStages = DP == 64 ? 3 : 2;
+// Codes of keys and of values, then a word of scale bytes of each row.
+template <int DP>
+constexpr uint32_t kRowStage = 2 * kTile8 * (DP + 4);
+// The rings, or what the warps' results take, which lie over them at the end.
+template <int DP>
+constexpr uint32_t kRowRing = kWarps * kRowStages<DP> * kRowStage<DP>;
+template <int DP, int NT>
+constexpr uint32_t kRowJoin = kWarps * 8 * NT * (kPadOf<DP> + 2) * 4;
+template <int DP, int NT>
+constexpr uint32_t kRowSmem = kRowRing<DP> > kRowJoin<DP, NT> ? kRowRing<DP> : kRowJoin<DP, NT>;
+
+template <int CODES, int DP, int NT>
+__global__ void __launch_bounds__(kThreads, (kByRegisters8<DP, NT>))
+    k_attend_token8_rows(const __grid_constant__ AttendArgs a) {
+  constexpr int kStages = kRowStages<DP>;
+  constexpr uint32_t kStage = kRowStage<DP>;
+  constexpr int kChunks = DP / 16;           // 16-byte chunks of a row
+  constexpr int kRowsAtOnce = 32 / kChunks;  // rows one copy instruction of a warp moves
+  constexpr int kRows = 8 * NT;
+  constexpr int kPad = kPadOf<DP>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint32_t valid[kWarps][kStages];
+  __shared__ TreeNode nodes[PCS_TREE_MAX];
+
+  attend_dependency();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = lane >> 2, q4 = lane & 3;
+  const int head = blockIdx.x % a.cache.heads;
+  const int sp = blockIdx.x / a.cache.heads % a.splits;
+  const int s = blockIdx.x / a.cache.heads / a.splits;
+  const SessionView view = session_view(a, s);
+  if (view.m <= 0) return;  // the same in every part
+  if (!rows_there(a, view, tid == 0)) return;  // (max_new tokens' rows are at most kRows)
+  const int head_dim = a.cache.head_dim;
+  const bool tree = a.parent != nullptr;
+  uint8_t* const ring_ptr = smem + warp * kStages * kStage;
+  const uint32_t ring = smem_addr(ring_ptr);
+  if (head_dim < DP) {  // chunks that no copy writes
+    for (uint32_t i = lane * 16; i < kStages * kStage; i += 512)
+      *reinterpret_cast<uint4*>(ring_ptr + i) = make_uint4(0, 0, 0, 0);
+    __syncwarp();
+  }
+  if (tree) {
+    tree_nodes(a, view, tid, nodes);
+    __syncthreads();
+  }
+
+  // This part's tiles; the warp takes every kWarps-th one.
+  const int tiles = (view.seen + kTile8 - 1) / kTile8;
+  const int per = (tiles + a.splits - 1) / a.splits;
+  const int t_end = min(tiles, (sp + 1) * per);
+  int t_next = sp * per + warp;  // the next tile whose places are looked up
+
+  const uint8_t* kbase = a.cache.k + head * a.cache.head_bytes;
+  const uint8_t* vbase = a.cache.v + head * a.cache.head_bytes;
+  // The aligned word that holds the head's scale byte.  (A row is a multiple of 16 bytes.)
+  const int scale_word = a.cache.scale_at + (head & ~3), scale_byte = head & 3;
+  auto look = [&](int t) {
+    RowPlace r = {kNoRow, kNoRow};
+    const int e = t * kTile8 + lane;
+    if (t < t_end && e < view.seen) r = row_place(a, s, seen_position(view, e));
+    return r;
+  };
+  const int chunk = lane % kChunks, row0 = lane / kChunks;
+  auto copy = [&](const RowPlace& r, int stage) {
+    const bool mine = r.k != kNoRow;
+    const uint32_t there = __ballot_sync(kFull, mine);
+    if (lane == 0) valid[warp][stage] = there;
+    const uint32_t base = ring + stage * kStage;
+#pragma unroll
+    for (int i = 0; i < kTile8 / kRowsAtOnce; ++i) {
+      const int row = i * kRowsAtOnce + row0;
+      const uint32_t ko = __shfl_sync(kFull, r.k, row), vo = __shfl_sync(kFull, r.v, row);
+      const bool in = ko != kNoRow;
+      if (chunk * 16 < head_dim) {
+        const uint32_t at = base + chunk_at<DP>(row, chunk);
+        copy16(at, row_at(a, kbase, in ? ko : 0) + chunk * 16, in);
+        copy16(at + kTile8 * DP, row_at(a, vbase, in ? vo : 0) + chunk * 16, in);
+      }
+    }
+    const uint32_t words = base + 2 * kTile8 * DP + lane * 4;
+    copy4(words, row_at(a, a.cache.k, mine ? r.k : 0) + scale_word, mine);
+    copy4(words + kTile8 * 4, row_at(a, a.cache.v, mine ? r.v : 0) + scale_word, mine);
+  };
+
+  RowPlace place;
+  {
+    RowPlace ahead[kStages];
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) ahead[i] = look(t_next + i * kWarps);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+      if (t_next < t_end) copy(ahead[i], i);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      t_next += kWarps;
+    }
+    place = ahead[kStages - 1];
+  }
+  TokenRows<CODES, DP, NT> work;
+  work.begin(a, view, head, lane);
+  const bool many = view.m > 1;
+  // Ranges of the first and the last new token.  (Nodes of a tree: what all of them
+  // see of the context.)
+  RowRange low = row_range(a, view, view.first);
+  const RowRange high = row_range(a, view, view.first + view.m - 1);
+  if (tree) low.hi = context_end(view);
+  // Which of the tokens from place b on the rows of new token t see, as bits.
+  auto sees = [&](int32_t t, int b) {
+    return tree ? tree_row(a, view, nodes[t]).bits(b) : row_range(a, view, view.first + t).bits(b);
+  };
+  auto at = [&](int h, int k) { return chunk_at<DP>(h * 16 + (lane & 15), 2 * k + (lane >> 4)); };
+  int stage = 0;
+  for (int t = sp * per + warp; t < t_end; t += kWarps) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();
+    {
+      const int into = stage == 0 ? kStages - 1 : stage - 1;
+      if (t_next < t_end) copy(place, into);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      t_next += kWarps;
+      place = look(t_next);
+    }
+    const uint32_t kat = ring + stage * kStage;
+    const uint8_t* scales = ring_ptr + stage * kStage + 2 * kTile8 * DP + lane * 4 + scale_byte;
+    const int e0 = t * kTile8;
+    const bool part = many && !(e0 + kTile8 - 1 <= low.hi && (e0 >= high.lo || e0 + kTile8 <= low.first));
+    work.tile(kat, kat + kTile8 * DP, at, scale_value(scales[0]), scale_value(scales[kTile8 * 4]), e0, valid[warp][stage], part, sees);
+    __syncwarp();  // the stage may be filled again
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  work.end();
+
   __syncthreads();
+  const bool half = a.dtype == PCS_DT_F16;
   const float lift = half ? kLift<__half> : kLift<__nv_bfloat16>;
   float* sums = reinterpret_cast<float*>(smem);           // [warp][row][kPad]
   float* tops = sums + kWarps * kRows * kPad;             // [warp][row]
@@ -553,11 +770,11 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
       float* r = sums + (warp * kRows + row) * kPad;
 #pragma unroll
       for (int d = 0; d < DP / 16; ++d)
-        *reinterpret_cast<float2*>(r + d * 16 + 2 * g) = make_float2(o[d][n][i], o[d][n][2 + i]);
+        *reinterpret_cast<float2*>(r + d * 16 + 2 * g) = make_float2(work.o[d][n][i], work.o[d][n][2 + i]);
       if (g == 0) {
         // (The join takes kLift off again, where the result's type has one.)
-        tops[warp * kRows + row] = refer[n][i] == kNothing ? -INFINITY : refer[n][i] + lift;
-        totals[warp * kRows + row] = total[n][i];
+        tops[warp * kRows + row] = work.refer[n][i] == kNothing ? -INFINITY : work.refer[n][i] + lift;
+        totals[warp * kRows + row] = work.total[n][i];
       }
     }
   __syncthreads();
@@ -567,49 +784,66 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, BOX>))
     join_parts<__nv_bfloat16, DP, NT>(a, view, smem, s, head, sp);
 }
 
-template <int CODES, int DP, int NT, bool BOX>
-cudaError_t launch(const AttendArgs& a, const CodeMaps& maps, cudaStream_t stream) {
-  auto k = k_attend_token8<CODES, DP, NT, BOX>;
-  static SmemLimit limit;
-  if (cudaError_t e = limit.set(k, kSmem8<DP, NT, BOX>)) return e;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+cudaLaunchConfig_t config(int64_t blocks, uint32_t smem, cudaLaunchAttribute* attr, cudaStream_t stream) {
+  attr->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr->val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.batch.sessions) * a.cache.heads * a.splits);
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem8<DP, NT, BOX>;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  return cfg;
+}
+
+template <int CODES, int DP, int NT, int HEADS>
+cudaError_t launch_boxes(const AttendArgs& a, const CodeMaps& maps, cudaStream_t stream) {
+  auto k = k_attend_token8<CODES, DP, NT, HEADS>;
+  static SmemLimit limit;
+  if (cudaError_t e = limit.set(k, kSmem8<DP, HEADS>)) return e;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg =
+      config(static_cast<int64_t>(a.batch.sessions) * (a.cache.heads / HEADS) * a.splits, kSmem8<DP, HEADS>, &attr, stream);
   return cudaLaunchKernelEx(&cfg, k, a, maps);
 }
 
-template <int CODES, bool BOX>
+template <int CODES, int DP, int NT>
+cudaError_t launch(const AttendArgs& a, const CodeMaps& maps, cudaStream_t stream) {
+  if (a.box_rows)
+    return a.box_heads == 4   ? launch_boxes<CODES, DP, NT, 4>(a, maps, stream)
+           : a.box_heads == 2 ? launch_boxes<CODES, DP, NT, 2>(a, maps, stream)
+                              : launch_boxes<CODES, DP, NT, 1>(a, maps, stream);
+  auto k = k_attend_token8_rows<CODES, DP, NT>;
+  static SmemLimit limit;
+  if (cudaError_t e = limit.set(k, kRowSmem<DP, NT>)) return e;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg =
+      config(static_cast<int64_t>(a.batch.sessions) * a.cache.heads * a.splits, kRowSmem<DP, NT>, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, k, a);
+}
+
+template <int CODES>
 cudaError_t by_size(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream) {
   if (a.cache.head_dim <= 64)
-    return rows <= 8    ? launch<CODES, 64, 1, BOX>(a, maps, stream)
-           : rows <= 16 ? launch<CODES, 64, 2, BOX>(a, maps, stream)
-                        : launch<CODES, 64, 4, BOX>(a, maps, stream);
-  return rows <= 8    ? launch<CODES, 128, 1, BOX>(a, maps, stream)
-         : rows <= 16 ? launch<CODES, 128, 2, BOX>(a, maps, stream)
-                      : launch<CODES, 128, 4, BOX>(a, maps, stream);
-}
-template <int CODES>
-cudaError_t by_form(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream) {
-  return a.box_rows ? by_size<CODES, true>(a, rows, maps, stream) : by_size<CODES, false>(a, rows, maps, stream);
+    return rows <= 8    ? launch<CODES, 64, 1>(a, maps, stream)
+           : rows <= 16 ? launch<CODES, 64, 2>(a, maps, stream)
+                        : launch<CODES, 64, 4>(a, maps, stream);
+  return rows <= 8    ? launch<CODES, 128, 1>(a, maps, stream)
+         : rows <= 16 ? launch<CODES, 128, 2>(a, maps, stream)
+                      : launch<CODES, 128, 4>(a, maps, stream);
 }
 
 }  // namespace
 
 int attend_token8_blocks_per_sm(int head_dim, int rows) {
   const int n = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-  if (head_dim <= 64) return n == 1 ? kResident8<64, 1, true> : n == 2 ? kResident8<64, 2, true> : kResident8<64, 4, true>;
-  return n == 1 ? kResident8<128, 1, true> : n == 2 ? kResident8<128, 2, true> : kResident8<128, 4, true>;
+  if (head_dim <= 64) return n == 1 ? kResident8<64, 1, 4> : n == 2 ? kResident8<64, 2, 4> : kResident8<64, 4, 4>;
+  return n == 1 ? kResident8<128, 1, 4> : n == 2 ? kResident8<128, 2, 4> : kResident8<128, 4, 4>;
 }
 
 cudaError_t launch_attend_token8(const AttendArgs& a, int rows, const CodeMaps& maps, cudaStream_t stream) {
-  return a.cache.codes == kCodesE4M3 ? by_form<kCodesE4M3>(a, rows, maps, stream) : by_form<kCodesI8>(a, rows, maps, stream);
+  return a.cache.codes == kCodesE4M3 ? by_size<kCodesE4M3>(a, rows, maps, stream) : by_size<kCodesI8>(a, rows, maps, stream);
 }
 
 }  // namespace pcs
