@@ -387,7 +387,7 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
         const int64_t blocks = pairs / a.box_heads, turns = (tiles + 2 * each - 1) / (2 * each);
         splits = std::min(resident / blocks, turns / 2);
         if (splits * each > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin / each, std::min(splits, turns / 4));
-        if (a.batch.sessions > 1) splits = std::max(splits, std::min(4 * resident / blocks, turns / 8));
+        if (a.batch.sessions > 1) splits = std::max(splits, std::min(4 * resident / blocks, turns / 32));
       }
       splits = std::max<int64_t>(splits, 1);
       const int64_t parts = splits * each;
