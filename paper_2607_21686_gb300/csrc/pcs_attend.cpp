@@ -54,9 +54,9 @@ bool encode_pool(const pcs_kv_cache& c, void* pool, int rows, uint8_t* map) {
 }
 
 // A cache in 8 bits: codes copied by boxes of `rows` rows of a page, of `heads` heads one
-// behind the other, swizzled by 64 or 128 bytes as they are long; scale bytes of 16 heads
-// of as many rows.
-bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, int heads, CodeMaps* maps) {
+// behind the other, as they are or swizzled by 64 or 128 bytes as they are long; scale bytes
+// of 16 heads of as many rows.
+bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, int heads, bool swizzled, CodeMaps* maps) {
   const EncodeFn fn = encoder();
   if (!fn) return false;
   for (int i = 0; i < 4; ++i) {
@@ -71,7 +71,10 @@ bool encode_codes(const pcs_kv_cache& c, const CacheDev& d, int rows, int heads,
       const cuuint32_t wide = c.head_dim <= 64 ? 64 : 128;
       const cuuint32_t box[4] = {wide, static_cast<cuuint32_t>(rows), static_cast<cuuint32_t>(heads), 1}, step[4] = {1, 1, 1, 1};
       r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             wide == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+             !swizzled    ? CU_TENSOR_MAP_SWIZZLE_NONE
+             : wide == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                          : CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_NONE,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     } else {
       const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.heads), static_cast<cuuint64_t>(c.page_rows),
@@ -365,7 +368,7 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       if (codes) {
         a.box_rows = box_rows(*cache, kTokenTile8);
         a.box_heads = cache->heads % 4 == 0 ? 4 : cache->heads % 2 == 0 ? 2 : 1;
-        if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, a.box_heads, &maps)) a.box_rows = 0;
+        if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, a.box_heads, true, &maps)) a.box_rows = 0;
       }
       const bool boxes = codes && a.box_rows > 0;
       const int64_t resident =
@@ -425,12 +428,21 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       if (st) return st;
       a.part = reinterpret_cast<float*>(ws);
     }
-    TensorMaps maps = {};
-    a.box_rows = codes ? 0 : box_rows(*cache, kBlockTile);
-    if (a.box_rows && !(encode_pool(*cache, cache->k, a.box_rows, maps.k) && encode_pool(*cache, cache->v, a.box_rows, maps.v)))
-      a.box_rows = 0;
-    call.before(kOpAttendBlock);
-    if ((st = call.after(launch_attend_block(a, dtype, static_cast<int>(blocks), maps, call.stream())))) return st;
+    a.box_rows = box_rows(*cache, kBlockTile);
+    if (codes) {
+      CodeMaps maps;
+      if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, 1, false, &maps)) a.box_rows = 0;
+      call.before(kOpAttendBlock);
+      st = call.after(launch_attend_block8(a, dtype, static_cast<int>(blocks), maps, call.stream()));
+    } else {
+      TensorMaps maps = {};
+      if (a.box_rows &&
+          !(encode_pool(*cache, cache->k, a.box_rows, maps.k) && encode_pool(*cache, cache->v, a.box_rows, maps.v)))
+        a.box_rows = 0;
+      call.before(kOpAttendBlock);
+      st = call.after(launch_attend_block(a, dtype, static_cast<int>(blocks), maps, call.stream()));
+    }
+    if (st) return st;
     if (splits > 1) {
       call.before(kOpAttendJoin);
       if ((st = call.after(launch_attend_join(a, dtype, static_cast<int>(blocks), call.stream())))) return st;

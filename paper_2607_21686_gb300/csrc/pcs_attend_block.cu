@@ -105,7 +105,6 @@ cudaError_t launch_join(const AttendArgs& a, int blocks, cudaStream_t stream) {
 
 cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
                                 cudaStream_t stream) {
-  if (a.cache.codes != kElements16) return launch_attend_block8(a, dtype, blocks, stream);
   if (a.parent) return launch_attend_block_tree(a, dtype, blocks, maps, stream);
   if (dtype == PCS_DT_F16)
     return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, maps, stream) : launch<__half, 128>(a, blocks, maps, stream);

@@ -9,19 +9,18 @@ namespace pcs {
 namespace {
 
 template <typename T, int DP>
-cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t stream) {
-  const TensorMaps none = {};
-  return a.parent ? launch_form<T, DP, kCodes, true>(a, blocks, none, stream)
-                  : launch_form<T, DP, kCodes, false>(a, blocks, none, stream);
+cudaError_t launch(const AttendArgs& a, int blocks, const CodeMaps& maps, cudaStream_t stream) {
+  return a.parent ? launch_form<T, DP, kCodes, true>(a, blocks, maps, stream)
+                  : launch_form<T, DP, kCodes, false>(a, blocks, maps, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_block8(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream) {
+cudaError_t launch_attend_block8(const AttendArgs& a, uint32_t dtype, int blocks, const CodeMaps& maps, cudaStream_t stream) {
   if (dtype == PCS_DT_F16)
-    return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, stream) : launch<__half, 128>(a, blocks, stream);
-  return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, stream)
-                                : launch<__nv_bfloat16, 128>(a, blocks, stream);
+    return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, maps, stream) : launch<__half, 128>(a, blocks, maps, stream);
+  return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, maps, stream)
+                                : launch<__nv_bfloat16, 128>(a, blocks, maps, stream);
 }
 
 }  // namespace pcs

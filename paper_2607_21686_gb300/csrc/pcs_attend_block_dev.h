@@ -11,8 +11,8 @@ namespace pcs {
 namespace {
 
 constexpr int kTile = 128;              // rows of a row tile, tokens of a tile
-// Warps 0-3 and 4-7: a row tile each, a thread a row; 8: matrix products; 9-11, or
-// with codes (MAKERS kCodes) 9-15: copies.
+// Warps 0-3 and 4-7: a row tile each, a thread a row; 8: matrix products; 9-11: copies.
+// With codes (MAKERS kCodes) 9: copies, 10-15: turn them into elements.
 constexpr int kCodes = -1;
 constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8;
@@ -27,8 +27,8 @@ template <int MAKERS>
 constexpr int kSoftRegsOf = MAKERS == kCodes ? 200 : 224;
 constexpr int kOtherRegs = 56;
 constexpr int kLag = 2;                 // copies in flight behind the newest
-// Tiles whose masks are kept.  (Codes are looked up four tiles before they are converted,
-// and those up to four before their scores are read.)
+// Tiles whose masks are kept.  (Codes are copied up to three tiles before they are
+// converted, and those up to four before their scores are read.)
 template <int MAKERS>
 constexpr int kValidOf = MAKERS == -1 ? 16 : 8;
 constexpr unsigned kFull = 0xffffffffu;
@@ -47,16 +47,15 @@ template <int DP, int MAKERS>
 constexpr int kBuffers = kKeyTiles<DP> + kValueTiles<DP, MAKERS>;
 template <int DP>
 constexpr uint32_t kTileBytes = kTile * DP * 2;
-// Codes wait for their conversion in rings of their own, one a copying warp: units of
-// 16 rows, each with a word of scale bytes a row.  They are what is in flight, 42 KB an
-// SM; the tiles they become need no more than one of values with heads of 128.
-constexpr int kUnitRows = 16, kUnits = kTile / kUnitRows;
+// Codes wait for their conversion in a ring of their own, a tile's keys or values a stage
+// and 16 scale bytes a row: that is what is in flight, 40 to 55 KB an SM.  The tiles they
+// become need no more than one of values with heads of 128.
 template <int DP>
-constexpr int kUnitStages = DP == 64 ? 8 : 4;
+constexpr int kCodeStages = DP == 64 ? 5 : 3;
 template <int DP>
-constexpr uint32_t kUnitBytes = kUnitRows * (DP + 4);
+constexpr uint32_t kCodeStage = kTile * (DP + 16);
 template <int DP, int MAKERS>
-constexpr uint32_t kStagedBytes = MAKERS == kCodes ? kCopyWarpsOf<MAKERS> * kUnitStages<DP> * kUnitBytes<DP> : 0;
+constexpr uint32_t kStagedBytes = MAKERS == kCodes ? kCodeStages<DP> * kCodeStage<DP> : 0;
 template <int DP, int MAKERS>
 constexpr uint32_t kSmemBytes = (2 + kBuffers<DP, MAKERS>) * kTileBytes<DP> + kStagedBytes<DP, MAKERS> + 1024;
 
@@ -75,6 +74,15 @@ __device__ __forceinline__ void copy_box(uint32_t to, uint64_t map, int d, int h
       "@q cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
       "[%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(to),
       "l"(map), "r"(d), "r"(head), "r"(row), "r"(page), "r"(bar), "r"(one)
+      : "memory");
+}
+
+__device__ __forceinline__ void copy_scales(uint32_t to, uint64_t map, int byte, int row, int page, uint32_t bar, uint32_t one) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(to),
+      "l"(map), "r"(byte), "r"(row), "r"(page), "r"(bar), "r"(one)
       : "memory");
 }
 
@@ -275,31 +283,6 @@ __device__ __forceinline__ bool take_out(uint4* at, uint4 v) {
   return true;
 }
 
-// Sixteen codes, times their scale, to 16-bit elements.
-__device__ __forceinline__ float limited(float x) {  // to float16's largest number; NaN stays
-  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(65504.0f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-65504.0f));
-  return x;
-}
-template <typename T, int CODES>
-__device__ __forceinline__ uint2 four_elements(uint32_t x, float scale) {
-  float y[4];
-  four_values<CODES>(x, y);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] *= scale;
-    if (std::is_same<T, __half>::value) y[i] = limited(y[i]);
-  }
-  return make_uint2(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]));
-}
-template <typename T, int CODES>
-__device__ __forceinline__ void sixteen_elements(const uint4& x, float scale, uint4& lo, uint4& hi) {
-  const uint2 a = four_elements<T, CODES>(x.x, scale), b = four_elements<T, CODES>(x.y, scale);
-  lo = make_uint4(a.x, a.y, b.x, b.y);
-  const uint2 c = four_elements<T, CODES>(x.z, scale), d = four_elements<T, CODES>(x.w, scale);
-  hi = make_uint4(c.x, c.y, d.x, d.y);
-}
-
 // MAKERS: warps that send tensor copies of boxes of rows (the other copying warps
 // look values over); 0: rows are copied one by one; kCodes: rows of codes are, and
 // become 16-bit elements on their way to the tiles.  TREE: the new tokens are nodes of
@@ -307,9 +290,11 @@ __device__ __forceinline__ void sixteen_elements(const uint4& x, float scale, ui
 // sixteen or thirty-two a tile, more than one warp can send in a tile's time: two
 // warps take keys and values (8,000-token prompt in pages of 8: 411 us by one,
 // 358 us by two; in pages of 16: 349 and 353 us).
+template <int MAKERS>
+using MapsOf = std::conditional_t<MAKERS == kCodes, CodeMaps, TensorMaps>;
 template <typename T, int DP, int MAKERS, bool TREE>
 __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
-    k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ TensorMaps maps, int blocks) {
+    k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ MapsOf<MAKERS> maps, int blocks) {
   constexpr bool BOX = MAKERS > 0;
   constexpr int kRing = kBuffers<DP, MAKERS>, kKeys = kKeyTiles<DP>, kValues = kValueTiles<DP, MAKERS>;
   constexpr int kCopyWarps = kCopyWarpsOf<MAKERS>;
@@ -322,6 +307,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
   __shared__ __align__(8) uint64_t bars[Bars::kCount];
+  __shared__ __align__(8) uint64_t code_bars[MAKERS == kCodes ? 2 * kCodeStages<DP> : 1];  // filled, free
   __shared__ uint32_t tmem_at;
   constexpr int kValid = kValidOf<MAKERS>;
   __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
@@ -331,8 +317,13 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
 
   attend_dependency();
   const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
-  if (BOX && warp == kCopyWarp && lane < 2)
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? maps.v : maps.k)) : "memory");
+  if constexpr (BOX) {
+    if (warp == kCopyWarp && lane < 2)
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? maps.v : maps.k)) : "memory");
+  } else if constexpr (MAKERS == kCodes) {
+    if (warp == kCopyWarp && lane < 4 && a.box_rows > 0)
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps.map[lane])) : "memory");
+  }
   int b = blockIdx.x;
   const int head = b % a.cache.heads;
   b /= a.cache.heads;
@@ -357,8 +348,13 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   auto s_read = [&](int t) { return bar0 + 8 * Bars::s_read(t); };  // kAhead: scores are in registers
   auto v_fine = [&](int j) { return bar0 + 8 * Bars::v_fine(j); };  // BOX: the values of tile j are looked over
   if (tid == 0) {
-    Bars::each(kTile, 32 * kSoftWarps / 2 * nq, BOX ? 1 : MAKERS == kCodes ? 32 * kUnits : 32 * kCopyWarps, 32 * (kCopyWarps - MAKERS),
+    Bars::each(kTile, 32 * kSoftWarps / 2 * nq, BOX ? 1 : MAKERS == kCodes ? 32 * (kCopyWarps - 1) : 32 * kCopyWarps, 32 * (kCopyWarps - MAKERS),
                [&](int i, int count) { bar_init(bar0 + 8 * i, count); });
+    if (MAKERS == kCodes)
+      for (int i = 0; i < kCodeStages<DP>; ++i) {
+        bar_init(smem_addr(code_bars) + 8 * i, a.box_rows > 0 ? 1 : 33);
+        bar_init(smem_addr(code_bars) + 8 * (kCodeStages<DP> + i), kCopyWarps - 1);
+      }
     special = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -463,101 +459,139 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
         }
       }
     } else if constexpr (MAKERS == kCodes) {
-      // Unit x: rows [16 u, 16 u + 16) of fill x / 8, u = x % 8; this warp takes units c,
-      // c + 7, .. through its ring: codes and a word of scale bytes a row copied as they
-      // are, then turned into elements in the tile.
-      constexpr int kStages = kUnitStages<DP>, kCodeChunks = DP / 16, kCodeRows = 32 / kCodeChunks;
-      const int units = 2 * w.tiles * kUnits;
-      const int code_chunk = lane % kCodeChunks, code_row = lane / kCodeChunks;
-      const bool live = code_chunk * 16 < a.cache.head_dim;
-      uint8_t* const staged = ring_ptr + kRing * kBytes + c * kStages * kUnitBytes<DP>;
-      const uint32_t staged_at = smem_addr(staged);
-      if (!live)
-        for (int i = 0; i < kStages; ++i)
-#pragma unroll
-          for (int r = 0; r < kUnitRows; r += kCodeRows)
-            *reinterpret_cast<uint4*>(staged + i * kUnitBytes<DP> + (r + code_row) * DP + code_chunk * 16) = make_uint4(0, 0, 0, 0);
-      auto look = [&](int x) {  // lanes 16 .. 31 as lanes 0 .. 15
-        const int i = x / kUnits, e = (w.tile0 + i / 2) * kTile + x % kUnits * kUnitRows + (lane & 15);
-        RowPlace p = {kNoRow, kNoRow};
-        if (x < units && e < w.view.seen) p = row_place(a, s, seen_position(w.view, e));
-        if (x < units && (i & 1) == 0) {  // a bit per token that is in the cache
-          const uint32_t there = __ballot_sync(kFull, p.k != kNoRow);
-          if (lane == 0)
-            reinterpret_cast<uint16_t*>(valid[(i / 2) % kValid])[x % kUnits] = static_cast<uint16_t>(there);
-        }
-        return i & 1 ? p.v : p.k;
-      };
-      const int scale_word = a.cache.scale_at + (head & ~3), scale_byte = head & 3;
-      auto copy = [&](uint32_t place, int x, int stage) {
-        const uint8_t* pool = x / kUnits & 1 ? a.cache.v : a.cache.k;
-        const uint32_t at = staged_at + stage * kUnitBytes<DP>;
-#pragma unroll
-        for (int r = 0; r < kUnitRows; r += kCodeRows) {
-          const uint32_t o = __shfl_sync(kFull, place, r + code_row);
-          const bool in = o != kNoRow;
-          if (live)
-            copy16(at + (r + code_row) * DP + code_chunk * 16,
-                   row_at(a, pool, in ? o : 0) + head * a.cache.head_bytes + code_chunk * 16, in);
-        }
-        if (lane < kUnitRows) {
-          const bool in = place != kNoRow;
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + kUnitRows * DP + lane * 4),
-                       "l"(row_at(a, pool, in ? place : 0) + scale_word), "r"(in ? 4 : 0)
-                       : "memory");
-        }
-      };
-      int ahead = c;  // the next unit that is copied
-      uint32_t place = look(ahead);
-#pragma unroll
-      for (int i = 0; i < kStages - 1; ++i) {
-        if (ahead < units) copy(place, ahead, i);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        ahead += kCopyWarps;
-        place = look(ahead);
-      }
+      // Fill i, as everywhere: keys of tile i / 2, or its values.  The first warp copies
+      // its codes and scale bytes to stage i of their ring, the others turn them into
+      // elements in the tile.
+      constexpr int kStages = kCodeStages<DP>, kCodeChunks = DP / 16, kCodeRows = 32 / kCodeChunks;
+      constexpr uint32_t kStage = kCodeStage<DP>, kScalesAt = kTile * DP;
+      uint8_t* const staged = ring_ptr + kRing * kBytes;
+      const uint32_t staged_at = smem_addr(staged), code_bar = smem_addr(code_bars);
+      auto full = [&](int stage) { return code_bar + 8 * stage; };
+      auto empty = [&](int stage) { return code_bar + 8 * (kStages + stage); };
+      const int fills = 2 * w.tiles, code_chunk = lane % kCodeChunks, code_row = lane / kCodeChunks;
       int stage = 0;
-      for (int x = c; x < units; x += kCopyWarps) {
-        const int i = x / kUnits, u = x % kUnits, buf = buf_of(i), use = use_of(i);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-        __syncwarp();
-        if (ahead < units) copy(place, ahead, stage == 0 ? kStages - 1 : stage - 1);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        ahead += kCopyWarps;
-        place = look(ahead);
-        if (use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
-        ok = __all_sync(kFull, ok);
-        if (!ok) break;
-        const uint8_t* from = staged + stage * kUnitBytes<DP>;
-        uint8_t* tile = ring_ptr + buf * kBytes;
-        const bool clear = (i & 1) && !range.whole_and_filled(w.tile0 + i / 2);
-        bool any = false;
-#pragma unroll
-        for (int r = 0; r < kUnitRows; r += kCodeRows) {
-          const int row = r + code_row, at = u * kUnitRows + row;
-          const uint4 y = *reinterpret_cast<const uint4*>(from + row * DP + code_chunk * 16);
-          const float scale = scale_value(from[kUnitRows * DP + row * 4 + scale_byte]);
-          uint4 lo, hi;
-          if (a.cache.codes == kCodesE4M3)
-            sixteen_elements<T, kCodesE4M3>(y, scale, lo, hi);
-          else
-            sixteen_elements<T, kCodesI8>(y, scale, lo, hi);
-          uint4* lo_at = reinterpret_cast<uint4*>(tile + spot(at, 2 * code_chunk));
-          uint4* hi_at = reinterpret_cast<uint4*>(tile + spot(at, 2 * code_chunk + 1));
-          *lo_at = lo;
-          *hi_at = hi;
-          if (clear) {
-            any |= take_out<T>(lo_at, lo);
-            any |= take_out<T>(hi_at, hi);
-          }
-        }
-        if (any) special = 1;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(kv_full(buf));
-        __syncwarp();  // the stage may be filled again
+      uint32_t phase = 0;
+      auto next_stage = [&] {
         stage = stage + 1 == kStages ? 0 : stage + 1;
+        if (stage == 0) phase ^= 1;
+      };
+      if (c == 0) {
+        int sent = 0;
+        // A place for the next fill; false: the wait ran out.
+        auto room = [&] {
+          if (sent >= kStages) ok = __all_sync(kFull, bar_wait(empty(stage), phase ^ 1)) != 0;
+          return ok;
+        };
+        if (a.box_rows > 0) {
+          const int rows = a.box_rows, boxes = kTile / rows;
+          auto look = [&](int t) {
+            Box x = {-1, -1, 0};
+            const int e = t * kTile + lane * rows;
+            if (lane < boxes && e < w.view.seen) x = box_place(a, s, w.view, e);
+            return x;
+          };
+          const uint32_t one = elected();
+          Box box, next = look(w.tile0);
+          for (int i = 0; i < fills && room(); ++i, ++sent, next_stage()) {
+            if ((i & 1) == 0) {
+              box = next;
+              if (i / 2 + 1 < w.tiles) next = look(w.tile0 + i / 2 + 1);
+              settle(a, box);
+              // A bit per token of the tile: its box is in the cache.
+              const uint32_t there = __ballot_sync(kFull, lane < boxes && box.k < a.cache.n_pages);
+              if (lane < 4) {
+                uint32_t m = 0;
+                for (int k = 0; k < 32; k += 8)
+                  if (there >> ((lane * 32 + k) / rows) & 1) m |= 0xffu << k;
+                const int32_t e = (w.tile0 + i / 2) * kTile + lane * 32;
+                m &= ~(RowRange::upto(w.view.gap1 - e) & ~RowRange::upto(w.view.gap0 - e));
+                valid[(i / 2) % kValid][lane] = m;
+              }
+              __syncwarp();
+            }
+            const uint32_t at = staged_at + stage * kStage, bar = full(stage);
+            const uint64_t codes = reinterpret_cast<uint64_t>(maps.map[i & 1]), scales = reinterpret_cast<uint64_t>(maps.map[2 + (i & 1)]);
+            fill_begins(bar, kStage, one);
+            for (int k = 0; k < boxes; ++k) {
+              const int row = __shfl_sync(kFull, box.row, k), page = __shfl_sync(kFull, i & 1 ? box.v : box.k, k);
+              copy_box(at + k * rows * DP, codes, 0, row, head, page, bar, one);
+              copy_scales(at + kScalesAt + k * rows * 16, scales, head & ~15, row, page, bar, one);
+            }
+          }
+        } else {
+          // Rows one by one; a lane's copies arrive at the barrier when they have come.
+          for (int i = 0; i < fills && room(); ++i, ++sent, next_stage()) {
+            const uint8_t* pool = i & 1 ? a.cache.v : a.cache.k;
+            const uint32_t at = staged_at + stage * kStage;
+            for (int r0 = 0; r0 < kTile; r0 += 32) {
+              RowPlace p = {kNoRow, kNoRow};
+              const int e = (w.tile0 + i / 2) * kTile + r0 + lane;
+              if (e < w.view.seen) p = row_place(a, s, seen_position(w.view, e));
+              const uint32_t there = __ballot_sync(kFull, p.k != kNoRow), place = i & 1 ? p.v : p.k;
+              if (lane == 0 && (i & 1) == 0) valid[(i / 2) % kValid][r0 / 32] = there;
+#pragma unroll 4
+              for (int r = 0; r < 32; r += kCodeRows) {
+                const uint32_t o = __shfl_sync(kFull, place, r + code_row);
+                const bool in = o != kNoRow;
+                if (code_chunk * 16 < a.cache.head_dim)
+                  copy16(at + (r0 + r + code_row) * DP + code_chunk * 16,
+                         row_at(a, pool, in ? o : 0) + head * a.cache.head_bytes + code_chunk * 16, in);
+              }
+              // The word that holds the scale byte, where it lies among 16 heads' bytes.
+              const bool in = place != kNoRow;
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + kScalesAt + (r0 + lane) * 16 + (head & 12)),
+                           "l"(row_at(a, pool, in ? place : 0) + a.cache.scale_at + (head & ~3)), "r"(in ? 4 : 0)
+                           : "memory");
+            }
+            __syncwarp();
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full(stage)) : "memory");
+            if (lane == 0) bar_arrive(full(stage));  // (and what was written of valid[])
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+        }
+        // No copy is on its way into a block that has ended, whoever gave up.
+        for (int i = max(0, sent - kStages); i < sent; ++i) {
+          const bool landed = bar_wait(full(i % kStages), i / kStages & 1);
+          ok = ok && landed;
+        }
+      } else {
+        for (int i = 0; i < fills; ++i, next_stage()) {
+          const int buf = buf_of(i), use = use_of(i);
+          ok = bar_wait(full(stage), phase);
+          if (ok && use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
+          ok = __all_sync(kFull, ok);
+          if (!ok) break;
+          const uint8_t* from = staged + stage * kStage;
+          uint8_t* tile = ring_ptr + buf * kBytes;
+          const bool clear = (i & 1) && !range.whole_and_filled(w.tile0 + i / 2);
+          bool any = false;
+#pragma unroll 2
+          for (int r = (c - 1) * kCodeRows; r < kTile; r += (kCopyWarps - 1) * kCodeRows) {
+            const int row = r + code_row;
+            uint4 y = *reinterpret_cast<const uint4*>(from + row * DP + code_chunk * 16);
+            if (code_chunk * 16 >= a.cache.head_dim) y = make_uint4(0, 0, 0, 0);  // (rows one by one: nobody wrote there)
+            const uint32_t scale = from[kScalesAt + row * 16 + (head & 15)];
+            uint4 lo, hi;
+            if (a.cache.codes == kCodesE4M3)
+              sixteen_elements<T, kCodesE4M3>(y, scale, lo, hi);
+            else
+              sixteen_elements<T, kCodesI8>(y, scale, lo, hi);
+            uint4* lo_at = reinterpret_cast<uint4*>(tile + spot(row, 2 * code_chunk));
+            uint4* hi_at = reinterpret_cast<uint4*>(tile + spot(row, 2 * code_chunk + 1));
+            *lo_at = lo;
+            *hi_at = hi;
+            if (clear) {
+              any |= take_out<T>(lo_at, lo);
+              any |= take_out<T>(hi_at, hi);
+            }
+          }
+          if (any) special = 1;
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          bar_arrive(kv_full(buf));
+          __syncwarp();
+          if (lane == 0) bar_arrive(empty(stage));  // the stage may be filled again
+        }
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
       constexpr int kGroups = kTile / kAtOnce;  // warp c moves every kCopyWarps-th
       if (!mine)                                // chunks that no copy writes
@@ -963,7 +997,7 @@ cudaLaunchConfig_t config(int64_t grid, int threads, uint32_t smem, cudaLaunchAt
 }
 
 template <typename T, int DP, int MAKERS, bool TREE>
-cudaError_t launch_form(const AttendArgs& a, int blocks, const TensorMaps& maps, cudaStream_t stream) {
+cudaError_t launch_form(const AttendArgs& a, int blocks, const MapsOf<MAKERS>& maps, cudaStream_t stream) {
   auto k = k_attend_block<T, DP, MAKERS, TREE>;
   constexpr uint32_t smem = kSmemBytes<DP, MAKERS>;
   static SmemLimit limit;

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "pcs_attend.h"
 
@@ -52,17 +53,74 @@ __device__ __forceinline__ void four_values(uint32_t x, float* y) {
   y[0] = a.x, y[1] = a.y, y[2] = b.x, y[3] = b.y;
 }
 
-// Rounded to T; float16 ends at its largest number (a head whose largest element is
-// near it may stand for 65536, the next code).  NaN stays.
+// To float16's largest number (a head whose largest element is near it may stand for
+// 65536, the next code); NaN stays.
+__device__ __forceinline__ float limited(float x) {
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(65504.0f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-65504.0f));
+  return x;
+}
 template <typename T>
-__device__ __forceinline__ T rounded(float x);
+__device__ __forceinline__ uint32_t pair_of(float lo, float hi);
 template <>
-__device__ __forceinline__ float rounded<float>(float x) { return x; }
+__device__ __forceinline__ uint32_t pair_of<__half>(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(limited(lo), limited(hi));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 template <>
-__device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <>
-__device__ __forceinline__ __half rounded<__half>(float x) {
-  return __float2half_rn(x > 65504.0f ? 65504.0f : x < -65504.0f ? -65504.0f : x);
+__device__ __forceinline__ uint32_t pair_of<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Four codes times their scale to four elements of 16 bits.
+template <typename T, int CODES>
+__device__ __forceinline__ uint2 four_elements(uint32_t x, float scale) {
+  float y[4];
+  if constexpr (CODES == kCodesI8) {
+    x ^= 0x80808080u;  // 0x4b0000 and a byte u are 2^23 + u
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7650 + i)) - 8388736.0f) * scale;
+  } else {
+    four_values<CODES>(x, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] *= scale;
+  }
+  return make_uint2(pair_of<T>(y[0], y[1]), pair_of<T>(y[2], y[3]));
+}
+// Sixteen, with the scale's byte.  To float16 by its own arithmetic, two at a time, where the
+// scale is a normal number of it and nothing comes near its end.
+template <typename T, int CODES>
+__device__ __forceinline__ void sixteen_elements(const uint4& x, uint32_t b, uint4& lo, uint4& hi) {
+  if constexpr (std::is_same<T, __half>::value) {
+    if (b >= 127 - 14 && b <= 127 + 5) {
+      const uint16_t bits = static_cast<uint16_t>((b - 127 + 15) << 10);
+      const __half2 s = __halves2half2(__ushort_as_half(bits), __ushort_as_half(bits));
+      const __half2 less = __hmul2(s, __halves2half2(__ushort_as_half(0xe480), __ushort_as_half(0xe480)));  // -1152
+      auto four = [&](uint32_t w, uint32_t& p, uint32_t& q) {
+        if constexpr (CODES == kCodesE4M3) {
+          const uint32_t u = pair_e4m3(static_cast<uint16_t>(w)), v = pair_e4m3(static_cast<uint16_t>(w >> 16));
+          const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&u), s), z = __hmul2(*reinterpret_cast<const __half2*>(&v), s);
+          p = *reinterpret_cast<const uint32_t*>(&y), q = *reinterpret_cast<const uint32_t*>(&z);
+        } else {
+          w ^= 0x80808080u;
+          const uint32_t u = __byte_perm(w, 0x64646464u, 0x4140), v = __byte_perm(w, 0x64646464u, 0x4342);
+          const __half2 y = __hfma2(*reinterpret_cast<const __half2*>(&u), s, less), z = __hfma2(*reinterpret_cast<const __half2*>(&v), s, less);
+          p = *reinterpret_cast<const uint32_t*>(&y), q = *reinterpret_cast<const uint32_t*>(&z);
+        }
+      };
+      four(x.x, lo.x, lo.y);
+      four(x.y, lo.z, lo.w);
+      four(x.z, hi.x, hi.y);
+      four(x.w, hi.z, hi.w);
+      return;
+    }
+  }
+  const float scale = scale_value(b);
+  const uint2 a = four_elements<T, CODES>(x.x, scale), d = four_elements<T, CODES>(x.y, scale);
+  const uint2 e = four_elements<T, CODES>(x.z, scale), f = four_elements<T, CODES>(x.w, scale);
+  lo = make_uint4(a.x, a.y, d.x, d.y);
+  hi = make_uint4(e.x, e.y, f.x, f.y);
 }
 
 }  // namespace pcs

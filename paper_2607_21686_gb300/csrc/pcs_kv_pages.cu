@@ -4,8 +4,9 @@
 // k_kv_read  y = code * 2^(b - 127), a head's tokens gathered from their pages;
 //            16-bit elements as they are.  Each code is read once and each value
 //            written once: the bound is HBM, two thirds of it the writes.  A block
-//            takes a few tokens, whose rows its first warp looks up; a thread moves
-//            units of eight elements, several of them in flight.
+//            takes a few tokens, whose rows its first warp looks up; a thread takes
+//            16 bytes of a row in several of them, so that what it computes of heads and
+//            offsets serves all its tokens.
 // k_kv_keep  rows to lower slots of the same session.  Kept row i comes from an index
 //            of at least i, so what is read after row i is written lies further on: a
 //            thread that takes a column of 16 bytes through all rows in their order
@@ -14,8 +15,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
-#include <type_traits>
 
 #include "pcs_attend.h"
 #include "pcs_codes_dev.h"
@@ -26,7 +27,7 @@ namespace pcs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kReadTokens = 8;   // tokens of a block at most
+constexpr int kReadTokens = 128;  // tokens of a block at most
 constexpr int kFlight = 4;       // units of a thread in flight
 
 __device__ __forceinline__ void grid_dependency() {
@@ -34,83 +35,100 @@ __device__ __forceinline__ void grid_dependency() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// A thread takes a unit of 16 bytes of a row -- of one head of the keys or of the values --
+// in every `lanes`-th token of its block.
 struct ReadShape {
-  FastDiv by_units, by_heads, by_tokens;
-  int32_t per_block, tensors;
+  FastDiv by_units, by_row, by_threads;  // units of a head, of a row, threads a token lane
+  int32_t per_block, units, lanes;       // tokens of a block, units of both rows, tokens at once
 };
 
-// Eight values of type T.
-template <typename T>
-struct alignas(16) Eight {
-  T e[8];
-};
+// 32 bytes at once, where their place is a multiple of that, else 16 and 16.
+template <bool WIDE>
+__device__ __forceinline__ void store32(uint8_t* to, const uint4& x, const uint4& y) {
+  if constexpr (WIDE) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w),
+                 "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w)
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = x;
+    reinterpret_cast<uint4*>(to)[1] = y;
+  }
+}
 
-template <int CODES, typename T>
-__global__ void __launch_bounds__(kThreads) k_kv_read(const __grid_constant__ ReadArgs a, const __grid_constant__ ReadShape shape) {
+template <int CODES, typename T, bool WIDE>
+__device__ __forceinline__ void write_unit(uint8_t* to, const uint4& x, uint32_t b) {
+  if constexpr (CODES == kElements16) {
+    *reinterpret_cast<uint4*>(to) = x;
+  } else if constexpr (sizeof(T) == 4) {
+    const float s = scale_value(b);
+    float y[16];
+    four_values<CODES>(x.x, y);
+    four_values<CODES>(x.y, y + 4);
+    four_values<CODES>(x.z, y + 8);
+    four_values<CODES>(x.w, y + 12);
+    uint4 z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      z[i] = make_uint4(__float_as_uint(y[4 * i] * s), __float_as_uint(y[4 * i + 1] * s), __float_as_uint(y[4 * i + 2] * s),
+                        __float_as_uint(y[4 * i + 3] * s));
+    store32<WIDE>(to, z[0], z[1]);
+    store32<WIDE>(to + 32, z[2], z[3]);
+  } else {
+    uint4 lo, hi;
+    sixteen_elements<T, CODES>(x, b, lo, hi);
+    store32<WIDE>(to, lo, hi);
+  }
+}
+
+template <int CODES, typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 6) k_kv_read(const __grid_constant__ ReadArgs a, const __grid_constant__ ReadShape shape) {
   __shared__ Place place[kReadTokens];
   grid_dependency();
   const CacheDev& c = a.cache;
   const int tid = threadIdx.x;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * shape.per_block;
   const int nt = static_cast<int>(a.batch.tokens - t0 < shape.per_block ? a.batch.tokens - t0 : shape.per_block);
-  if (tid < 32) {
-    const int s = a.batch.q_off ? session_of(a.batch, t0, tid) : 0;
+  if ((tid & ~31) < nt) {  // a warp looks up 32 tokens
+    const int s = a.batch.q_off ? session_of(a.batch, t0 + (tid & ~31), tid & 31) : 0;
     if (tid < nt) place[tid] = place_of(c, a.batch, a.err, t0 + tid, s);
   }
   __syncthreads();
-  const int total = shape.per_block * shape.tensors * c.heads * static_cast<int>(shape.by_units.d);
-  for (int i0 = tid; i0 < total; i0 += kFlight * kThreads) {
-    using Codes = std::conditional_t<CODES == kElements16, uint4, uint2>;
-    Codes x[kFlight];
-    uint32_t b[kFlight];
-    uint8_t* to[kFlight];
+  constexpr int kElements = CODES == kElements16 ? 8 : 16;  // of a unit
+  const int lane = shape.by_threads.div(tid);
+  for (int v = tid - lane * static_cast<int>(shape.by_threads.d); v < shape.units && lane < shape.lanes; v += kThreads) {
+    // Unit u of head h of the keys (w 0) or the values.
+    int w = shape.by_row.div(v);
+    const uint32_t r = v - w * shape.by_row.d, h = shape.by_units.div(r), u = r - h * shape.by_units.d;
+    if (a.out[0].data == nullptr) w = 1;
+    const HeadsDev& out = a.out[w];
+    const uint8_t* const from = (w ? c.v : c.k) + static_cast<int64_t>(h) * c.head_bytes + u * 16;
+    const uint8_t* const scale = (w ? c.v : c.k) + c.scale_at + h;
+    uint8_t* to = out.data + (t0 + lane) * out.token_bytes + static_cast<int64_t>(h) * out.head_bytes + u * (kElements * sizeof(T));
+    const int64_t step = shape.lanes * out.token_bytes;
+    for (int i = lane; i < nt; i += kFlight * shape.lanes) {
+      uint4 x[kFlight];
+      uint32_t b[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      const int i = i0 + k * kThreads;
-      x[k] = Codes{};
-      b[k] = 127;
-      to[k] = nullptr;
-      if (i >= total) continue;
-      // Unit u of head h of token t of tensor w.
-      uint32_t q = shape.by_units.div(i);
-      const uint32_t u = i - q * shape.by_units.d;
-      uint32_t r = shape.by_heads.div(q);
-      const uint32_t h = q - r * shape.by_heads.d;
-      const uint32_t w = shape.by_tokens.div(r), t = r - w * shape.by_tokens.d;
-      if (static_cast<int>(t) >= nt) continue;
-      const int which = a.out[0].data == nullptr ? 1 : static_cast<int>(w);
-      to[k] = a.out[which].data + (t0 + t) * a.out[which].token_bytes + h * a.out[which].head_bytes + u * 8 * sizeof(T);
-      const int64_t at = which ? place[t].v : place[t].k;
-      if (at < 0) continue;
-      const uint8_t* row = (which ? c.v : c.k) + at;
-      x[k] = __ldg(reinterpret_cast<const Codes*>(row + h * c.head_bytes + u * sizeof(Codes)));
-      if (CODES != kElements16) b[k] = __ldg(row + c.scale_at + h);
-    }
+      for (int k = 0; k < kFlight; ++k) {
+        const int t = i + k * shape.lanes;
+        x[k] = make_uint4(0, 0, 0, 0);
+        b[k] = 127;
+        if (t >= nt) continue;
+        const int64_t at = w ? place[t].v : place[t].k;
+        if (at < 0) continue;
+        x[k] = __ldg(reinterpret_cast<const uint4*>(from + at));
+        if (CODES != kElements16) b[k] = __ldg(scale + at);
+      }
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      if (to[k] == nullptr) continue;
-      if constexpr (CODES == kElements16) {
-        *reinterpret_cast<uint4*>(to[k]) = x[k];
-      } else {
-        const float s = scale_value(b[k]);
-        float y[8];
-        four_values<CODES>(x[k].x, y);
-        four_values<CODES>(x[k].y, y + 4);
-        Eight<T> z;
-#pragma unroll
-        for (int d = 0; d < 8; ++d) z.e[d] = rounded<T>(y[d] * s);
-        if constexpr (sizeof(T) == 4) {
-          reinterpret_cast<float4*>(to[k])[0] = make_float4(z.e[0], z.e[1], z.e[2], z.e[3]);
-          reinterpret_cast<float4*>(to[k])[1] = make_float4(z.e[4], z.e[5], z.e[6], z.e[7]);
-        } else {
-          *reinterpret_cast<uint4*>(to[k]) = *reinterpret_cast<const uint4*>(&z);
-        }
+      for (int k = 0; k < kFlight; ++k) {
+        if (i + k * shape.lanes < nt) write_unit<CODES, T, WIDE>(to, x[k], b[k]);
+        to += step;
       }
     }
   }
 }
 
-template <int CODES, typename T>
+template <int CODES, typename T, bool WIDE>
 cudaError_t read(const ReadArgs& a, const ReadShape& shape, cudaStream_t stream) {
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -121,15 +139,15 @@ cudaError_t read(const ReadArgs& a, const ReadShape& shape, cudaStream_t stream)
   cfg.stream = stream;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_kv_read<CODES, T>, a, shape);
+  return cudaLaunchKernelEx(&cfg, k_kv_read<CODES, T, WIDE>, a, shape);
 }
 
-template <int CODES>
+template <int CODES, bool WIDE>
 cudaError_t read_as(const ReadArgs& a, const ReadShape& shape, cudaStream_t stream) {
   switch (a.dtype) {
-    case PCS_DT_F16: return read<CODES, __half>(a, shape, stream);
-    case PCS_DT_BF16: return read<CODES, __nv_bfloat16>(a, shape, stream);
-    default: return read<CODES, float>(a, shape, stream);
+    case PCS_DT_F16: return read<CODES, __half, WIDE>(a, shape, stream);
+    case PCS_DT_BF16: return read<CODES, __nv_bfloat16, WIDE>(a, shape, stream);
+    default: return read<CODES, float, WIDE>(a, shape, stream);
   }
 }
 
@@ -226,20 +244,23 @@ __global__ void __launch_bounds__(kThreads) k_kv_keep(const __grid_constant__ Ke
 
 cudaError_t launch_read(const ReadArgs& a, int sm_count, cudaStream_t stream) {
   ReadShape shape;
-  shape.by_units.set(a.cache.head_dim / 8);
-  shape.by_heads.set(a.cache.heads);
-  shape.tensors = (a.out[0].data != nullptr) + (a.out[1].data != nullptr);
-  // Few tokens: a block for each; many: as many as keep four units a thread in flight.
-  const int64_t share = a.batch.tokens / (2 * sm_count);
-  const int64_t units = static_cast<int64_t>(shape.tensors) * a.cache.heads * (a.cache.head_dim / 8);
-  int64_t most = (kFlight * kThreads + units - 1) / units;
-  if (most > kReadTokens) most = kReadTokens;
-  shape.per_block = static_cast<int32_t>(share < 1 ? 1 : share > most ? most : share);
-  shape.by_tokens.set(shape.per_block);
+  const int head = a.cache.head_dim / (a.cache.codes == kElements16 ? 8 : 16), row = a.cache.heads * head;
+  shape.by_units.set(head);
+  shape.by_row.set(row);
+  shape.units = row * ((a.out[0].data != nullptr) + (a.out[1].data != nullptr));
+  shape.lanes = shape.units >= kThreads ? 1 : kThreads / shape.units;
+  shape.by_threads.set(kThreads / shape.lanes);
+  // Few tokens: as many blocks as there are; many: blocks that look up as many tokens as
+  // their threads take in a few rounds.
+  const int64_t share = a.batch.tokens / (4 * sm_count), most = std::min<int64_t>(kReadTokens, 2 * kFlight * shape.lanes);
+  shape.per_block = static_cast<int32_t>(std::max<int64_t>(1, std::min(share, most)));
+  bool wide = true;
+  for (const HeadsDev& o : a.out)
+    wide = wide && reinterpret_cast<uintptr_t>(o.data) % 32 == 0 && o.token_bytes % 32 == 0 && o.head_bytes % 32 == 0;
   switch (a.cache.codes) {
-    case kCodesE4M3: return read_as<kCodesE4M3>(a, shape, stream);
-    case kCodesI8: return read_as<kCodesI8>(a, shape, stream);
-    default: return read<kElements16, __half>(a, shape, stream);
+    case kCodesE4M3: return wide ? read_as<kCodesE4M3, true>(a, shape, stream) : read_as<kCodesE4M3, false>(a, shape, stream);
+    case kCodesI8: return wide ? read_as<kCodesI8, true>(a, shape, stream) : read_as<kCodesI8, false>(a, shape, stream);
+    default: return read<kElements16, __half, false>(a, shape, stream);
   }
 }
 
