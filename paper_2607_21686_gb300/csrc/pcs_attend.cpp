@@ -292,6 +292,10 @@ pcs_status working_memory(OpCall& call, uint64_t bytes, uint8_t** out, uint32_t*
   return PCS_OK;
 }
 
+uint64_t round_up_256(uint64_t x) { return (x + 255) / 256 * 256; }
+// Working memory for codes that are turned into elements ahead of attention over them.
+constexpr uint64_t kWidenMost = 1ull << 30;
+
 // A tree's nodes, and tokens of which some are kept, all have to be in the cache.
 pcs_status check_ring(const CacheDev& c, const BatchDev& b) {
   if (c.ring_rows && b.max_new > c.ring_rows)
@@ -360,6 +364,7 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
     // hint for the split, which is right for any length.
     int64_t seen = cache->ring ? static_cast<int64_t>(cache->sinks) + cache->ring : a.cache.slots;
     if (batch->max_len) seen = std::min<int64_t>(seen, batch->max_len);
+    const int64_t all_seen = a.window ? std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + a.batch.max_new) : seen;
     const int64_t tokens = few || tree ? a.batch.max_new : std::min<int64_t>(a.batch.max_new, kBlockRows / a.group + 2);
     if (a.window) seen = std::min<int64_t>(seen, static_cast<int64_t>(cache->sinks) + a.window + tokens);
     if (few) {
@@ -384,13 +389,18 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       if (a.batch.sessions > 1)
         splits = std::max(splits, std::min(4 * resident / pairs, tiles / (8 * kTokenWarps)));
       // Blocks over codes that take several heads: a warp's result is a part of its head's.
+      // Of several sessions whose lengths may differ by much, the longest come first and
+      // there are parts for two waves and a quarter.  (48 sessions of 1 to 12,000 tokens, 8
+      // heads of 128: 131 us in one wave as they come, 110 to 116 us so; 256 over windows of
+      // 1,024, 16 heads of 64, as they come: 105 us whole, 140 us in two parts.)
       int64_t each = 1;
       if (boxes) {
         each = kTokenWarps / a.box_heads;
         const int64_t blocks = pairs / a.box_heads, turns = (tiles + 2 * each - 1) / (2 * each);
         splits = std::min(resident / blocks, turns / 2);
         if (splits * each > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin / each, std::min(splits, turns / 4));
-        if (a.batch.sessions > 1) splits = std::max(splits, std::min(4 * resident / blocks, turns / 32));
+        a.ranked = a.batch.sessions > 1 && a.batch.sessions <= kRankMost && tiles >= 128;
+        if (a.ranked) splits = std::max(splits, std::min((9 * resident / 4 + blocks / 2) / blocks, turns / 16));
       }
       splits = std::max<int64_t>(splits, 1);
       const int64_t parts = splits * each;
@@ -421,15 +431,42 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
     const int64_t tiles = (seen + kBlockTile - 1) / kBlockTile;
     int64_t splits = std::max<int64_t>(1, std::min(call.sm_count() / (pairs * blocks), tiles / 4));
     a.splits = static_cast<int32_t>(splits);
-    if (splits > 1) {
-      uint8_t* ws = nullptr;
+    // (Parts are numbered by their blocks: a launch that joins them takes sessions as they come.)
+    a.ranked = splits == 1 && a.batch.sessions > 1 && a.batch.sessions <= kRankMost;
+    const uint64_t parts = splits > 1 ? round_up_256(4 * block_part_floats(cache->head_dim) * splits * pairs * blocks) : 0;
+    // Codes that several blocks of rows go over are turned into elements once, ahead of
+    // them, where that takes no more than kWidenMost.
+    pcs_kv_cache wide;
+    const uint64_t pages = static_cast<uint64_t>(a.batch.sessions) * cache->table_pages;
+    const uint64_t pool = codes ? pages * cache->page_rows * (2ull * cache->heads * cache->head_dim) : 0;
+    const bool widen = codes && blocks > 1 && 2 * pool <= kWidenMost;
+    const uint64_t table = widen ? round_up_256(4 * pages) : 0;
+    uint8_t* ws = nullptr;
+    if (parts || widen) {
       uint32_t* words = nullptr;
-      st = working_memory(call, 4 * block_part_floats(cache->head_dim) * splits * pairs * blocks, &ws, &words);
+      st = working_memory(call, parts + (widen ? table + 2 * pool : 0), &ws, &words);
       if (st) return st;
       a.part = reinterpret_cast<float*>(ws);
     }
+    if (widen) {
+      const WidenTo to = {ws + parts + table, ws + parts + table + pool, reinterpret_cast<int32_t*>(ws + parts),
+                          2ll * cache->heads * cache->head_dim};
+      a.box_rows = box_rows(*cache, kBlockTile);
+      call.before(kOpWiden);
+      if ((st = call.after(launch_widen(a, to, all_seen, call.stream())))) return st;
+      wide = *cache;
+      wide.k = to.k, wide.v = to.v, wide.table = to.table, wide.v_table = nullptr;
+      wide.table_stride = cache->table_pages;
+      wide.head_stride = cache->head_dim;
+      wide.row_stride = static_cast<int64_t>(cache->heads) * cache->head_dim;
+      wide.page_stride = wide.row_stride * cache->page_rows;
+      wide.n_pages = static_cast<int32_t>(pages);
+      wide.dtype = dtype;
+      cache = &wide;
+      if ((st = check_cache(cache, &a.cache))) return st;
+    }
     a.box_rows = box_rows(*cache, kBlockTile);
-    if (codes) {
+    if (codes && !widen) {
       CodeMaps maps;
       if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, 1, false, &maps)) a.box_rows = 0;
       call.before(kOpAttendBlock);

@@ -15,7 +15,7 @@ namespace pcs {
 // ---- One call on a context ---------------------------------------------------
 
 // Kernels of the operators, in the order of their names in the timing table.
-enum OpKernel { kOpRotate, kOpAppend, kOpAttendToken, kOpAttendBlock, kOpAttendJoin, kOpStore, kOpRead, kOpKeep };
+enum OpKernel { kOpRotate, kOpAppend, kOpAttendToken, kOpAttendBlock, kOpAttendJoin, kOpStore, kOpRead, kOpKeep, kOpWiden };
 
 // Words of a call that are zero on entry and have to be on exit.
 constexpr int kOpWords = 1024;
@@ -173,6 +173,8 @@ cudaError_t launch_keep(const KeepArgs& a, cudaStream_t stream);
 
 // ---- Attention -------------------------------------------------------------------------
 
+constexpr int kRankMost = 512;  // sessions that blocks rank by length
+
 struct AttendArgs {
   CacheDev cache;
   BatchDev batch;
@@ -190,7 +192,19 @@ struct AttendArgs {
   const int32_t* parent;   // new tokens form trees; null: each sees those before it
   uint32_t dtype;          // of q and out
   int32_t box_heads;       // token kernel over codes: key heads of a block
+  int32_t ranked;          // kernels over codes and for trees: blocks take the longest sessions first
 };
+
+// What the new tokens of a call see of a cache in 8 bits, as elements of their queries'
+// type in pages of the same slots: session s's page p is page s * pages + p, its table says
+// which of them are there.
+struct WidenTo {
+  uint8_t *k, *v;
+  int32_t* table;
+  int64_t row_bytes;
+};
+// seen: a hint, tokens that a session's new ones see.
+cudaError_t launch_widen(const AttendArgs& a, const WidenTo& to, int64_t seen, cudaStream_t stream);
 
 // One row is one query head of one new token; the token kernel takes all rows
 // of a session and key head together.

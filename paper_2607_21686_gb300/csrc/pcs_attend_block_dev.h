@@ -329,7 +329,9 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   b /= a.cache.heads;
   const int sp = b % a.splits;
   b /= a.splits;
-  const int s = b % a.batch.sessions;
+  int s = b % a.batch.sessions;
+  if constexpr (MAKERS == kCodes || TREE)
+    if (a.ranked) s = ranked_session(a.batch, s, tid, kThreadsOf<MAKERS>, reinterpret_cast<uint32_t*>(raw));
   const int blk = blocks - 1 - b / a.batch.sessions;  // the longest first
   const Work w = block_work<TREE>(a, s, blk, sp);
   if (w.row0 >= w.rows || !rows_there(a, w.all, tid == 0)) return;
@@ -555,34 +557,54 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
           ok = ok && landed;
         }
       } else {
+        // A warp's rows are kStep apart, a multiple of eight: their chunks' places in a tile
+        // differ by whole rows.
+        constexpr int kStep = (kCopyWarps - 1) * kCodeRows, kTurns = (kTile + kStep - 1) / kStep, kTogether = 3;
+        static_assert(kStep % 8 == 0, "the swizzle goes by a row's number modulo 8");
+        const int row0 = (c - 1) * kCodeRows;
+        const bool live = code_chunk * 16 < a.cache.head_dim;  // (rows one by one: nobody wrote elsewhere)
+        const uint32_t lo_off = spot(row0 + code_row, 2 * code_chunk), hi_off = spot(row0 + code_row, 2 * code_chunk + 1);
         for (int i = 0; i < fills; ++i, next_stage()) {
           const int buf = buf_of(i), use = use_of(i);
           ok = bar_wait(full(stage), phase);
           if (ok && use > 0) ok = bar_wait(kv_empty(buf), (use - 1) & 1);
           ok = __all_sync(kFull, ok);
           if (!ok) break;
-          const uint8_t* from = staged + stage * kStage;
+          const uint8_t* from = staged + stage * kStage + (row0 + code_row) * DP + code_chunk * 16;
+          const uint8_t* scales = staged + stage * kStage + kScalesAt + (row0 + code_row) * 16 + (head & 15);
           uint8_t* tile = ring_ptr + buf * kBytes;
           const bool clear = (i & 1) && !range.whole_and_filled(w.tile0 + i / 2);
           bool any = false;
-#pragma unroll 2
-          for (int r = (c - 1) * kCodeRows; r < kTile; r += (kCopyWarps - 1) * kCodeRows) {
-            const int row = r + code_row;
-            uint4 y = *reinterpret_cast<const uint4*>(from + row * DP + code_chunk * 16);
-            if (code_chunk * 16 >= a.cache.head_dim) y = make_uint4(0, 0, 0, 0);  // (rows one by one: nobody wrote there)
-            const uint32_t scale = from[kScalesAt + row * 16 + (head & 15)];
-            uint4 lo, hi;
-            if (a.cache.codes == kCodesE4M3)
-              sixteen_elements<T, kCodesE4M3>(y, scale, lo, hi);
-            else
-              sixteen_elements<T, kCodesI8>(y, scale, lo, hi);
-            uint4* lo_at = reinterpret_cast<uint4*>(tile + spot(row, 2 * code_chunk));
-            uint4* hi_at = reinterpret_cast<uint4*>(tile + spot(row, 2 * code_chunk + 1));
-            *lo_at = lo;
-            *hi_at = hi;
-            if (clear) {
-              any |= take_out<T>(lo_at, lo);
-              any |= take_out<T>(hi_at, hi);
+#pragma unroll
+          for (int r0 = 0; r0 < kTurns; r0 += kTogether) {
+            uint4 y[kTogether];
+            uint32_t scale[kTogether];
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+              const int r = (r0 + k) * kStep;
+              y[k] = make_uint4(0, 0, 0, 0);
+              scale[k] = 127;
+              if (r0 + k >= kTurns || row0 + r >= kTile || !live) continue;  // (row0: the same in a warp)
+              y[k] = *reinterpret_cast<const uint4*>(from + r * DP);
+              scale[k] = scales[r * 16];
+            }
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+              const int r = (r0 + k) * kStep;
+              if (r0 + k >= kTurns || row0 + r >= kTile) continue;
+              uint4 lo, hi;
+              if (a.cache.codes == kCodesE4M3)
+                sixteen_elements<T, kCodesE4M3>(y[k], scale[k], lo, hi);
+              else
+                sixteen_elements<T, kCodesI8>(y[k], scale[k], lo, hi);
+              uint4* lo_at = reinterpret_cast<uint4*>(tile + lo_off + r * 128);
+              uint4* hi_at = reinterpret_cast<uint4*>(tile + hi_off + r * 128);
+              *lo_at = lo;
+              *hi_at = hi;
+              if (clear) {
+                any |= take_out<T>(lo_at, lo);
+                any |= take_out<T>(hi_at, hi);
+              }
             }
           }
           if (any) special = 1;

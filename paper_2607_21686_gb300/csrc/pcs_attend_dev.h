@@ -108,16 +108,15 @@ __device__ __forceinline__ SessionView session_view(const AttendArgs& a, int s) 
   return v;
 }
 
-// Where position p of session s is in the cache (of head 0): offsets of its
-// key and value in units, kNoRow if it is in no page.
+// Where a slot of session s is in the cache (of head 0): offsets of its key and
+// value in units, kNoRow if it is in no page; where position p is.
 constexpr uint32_t kNoRow = 0xffffffffu;
 struct RowPlace {
   uint32_t k, v;
 };
-__device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_t p) {
+__device__ __forceinline__ RowPlace slot_place(const AttendArgs& a, int s, uint32_t slot) {
   const CacheDev& c = a.cache;
   RowPlace r = {kNoRow, kNoRow};
-  const uint32_t slot = c.slot_of(static_cast<uint32_t>(p));
   if (slot >= static_cast<uint32_t>(c.slots)) {
     atomicOr(a.err, kDevErrIndex);
     return r;
@@ -135,8 +134,36 @@ __device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_
   r.v = vp * c.page_units + row;
   return r;
 }
+__device__ __forceinline__ RowPlace row_place(const AttendArgs& a, int s, int32_t p) {
+  return slot_place(a, s, a.cache.slot_of(static_cast<uint32_t>(p)));
+}
 __device__ __forceinline__ const uint8_t* row_at(const AttendArgs& a, const uint8_t* base, uint32_t off) {
   return base + static_cast<uint64_t>(off) * a.cache.unit;
+}
+
+// The session that is the r-th longest (of equal ones, and of those beyond four million
+// tokens, the first comes first), for blocks that take sessions in that order: the last
+// blocks of a launch are then short ones.  `scratch` holds kRankMost numbers, free again
+// when this returns to all threads.
+__device__ __forceinline__ int ranked_session(const BatchDev& b, int r, int tid, int threads, uint32_t* scratch) {
+  __shared__ int found;
+  const int n = (b.sessions + 3) & ~3;
+  for (int i = tid; i < n; i += threads) {
+    const int32_t len = i < b.sessions ? __ldg(b.lens + i) : 0;
+    scratch[i] = i < b.sessions ? static_cast<uint32_t>(min(max(len, 0), 0x3ffffe) + 1) << 9 | (kRankMost - 1 - i) : 0u;
+  }
+  __syncthreads();
+  for (int i = tid; i < b.sessions; i += threads) {
+    const uint32_t mine = scratch[i];
+    int ahead = 0;
+    for (int k = 0; k < n; k += 4) {
+      const uint4 x = *reinterpret_cast<const uint4*>(scratch + k);
+      ahead += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+    }
+    if (ahead == r) found = i;
+  }
+  __syncthreads();
+  return found;
 }
 
 // A session's nodes into shared memory, by the block's threads (at least

@@ -7,6 +7,9 @@
 //            takes a few tokens, whose rows its first warp looks up; a thread takes
 //            16 bytes of a row in several of them, so that what it computes of heads and
 //            offsets serves all its tokens.
+// k_widen    the same into pages of 16-bit elements, slot by slot, of what the new tokens
+//            of a call see: the cache that attention of many rows a key head goes over,
+//            where every tile of codes would be converted once for each block of rows.
 // k_kv_keep  rows to lower slots of the same session.  Kept row i comes from an index
 //            of at least i, so what is read after row i is written lies further on: a
 //            thread that takes a column of 16 bytes through all rows in their order
@@ -19,6 +22,7 @@
 #include <cstdint>
 
 #include "pcs_attend.h"
+#include "pcs_attend_dev.h"
 #include "pcs_codes_dev.h"
 #include "pcs_internal.h"
 #include "pcs_place_dev.h"
@@ -81,7 +85,7 @@ __device__ __forceinline__ void write_unit(uint8_t* to, const uint4& x, uint32_t
 }
 
 template <int CODES, typename T, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 6) k_kv_read(const __grid_constant__ ReadArgs a, const __grid_constant__ ReadShape shape) {
+__global__ void __launch_bounds__(kThreads, 5) k_kv_read(const __grid_constant__ ReadArgs a, const __grid_constant__ ReadShape shape) {
   __shared__ Place place[kReadTokens];
   grid_dependency();
   const CacheDev& c = a.cache;
@@ -149,6 +153,87 @@ cudaError_t read_as(const ReadArgs& a, const ReadShape& shape, cudaStream_t stre
     case PCS_DT_BF16: return read<CODES, __nv_bfloat16, WIDE>(a, shape, stream);
     default: return read<CODES, float, WIDE>(a, shape, stream);
   }
+}
+
+// ---- Codes to pages of elements -----------------------------------------------------------
+
+constexpr int kWidenRows = 32;   // tokens of a block at a time
+
+template <int CODES, typename T>
+__global__ void __launch_bounds__(kThreads) k_widen(const __grid_constant__ AttendArgs a, const __grid_constant__ ReadShape shape,
+                                                    const __grid_constant__ WidenTo to, int chunks) {
+  __shared__ RowPlace place[kWidenRows];
+  __shared__ int64_t row[kWidenRows];
+  grid_dependency();
+  const CacheDev& c = a.cache;
+  const int tid = threadIdx.x, s = blockIdx.x / chunks, chunk = blockIdx.x - s * chunks;
+  // Whole boxes of rows, as the kernel behind copies them: rows that nobody sees must not
+  // hold what was in this memory before.
+  SessionView view = session_rows(a, s);
+  const int align = a.box_rows > 0 ? a.box_rows : 1;
+  narrow(a, view, 0, view.m, align);
+  if (view.m <= 0 || !rows_there(a, view, false)) return;  // nobody looks at the session
+  const int places = (view.seen + align - 1) & -align;
+  const int pages = c.slots / static_cast<int>(c.page_rows.d);
+  if (chunk == 0)
+    for (int p = tid; p < pages; p += kThreads) {
+      const int32_t k = __ldg(c.table + s * c.table_stride + p), v = c.v_table ? __ldg(c.v_table + s * c.table_stride + p) : k;
+      to.table[static_cast<int64_t>(s) * pages + p] = k < 0 || k >= c.n_pages || v < 0 || v >= c.n_pages ? -1 : s * pages + p;
+    }
+  const int lane = shape.by_threads.div(tid), v0 = tid - lane * static_cast<int>(shape.by_threads.d);
+  for (int e0 = chunk * kWidenRows; e0 < places; e0 += chunks * kWidenRows) {
+    __syncthreads();
+    const int e = e0 + tid;
+    if (tid < kWidenRows && e < places) {
+      const uint32_t slot = align > 1 ? box_slot(a, view, e & -align) + (e & (align - 1)) : c.slot_of(static_cast<uint32_t>(seen_position(view, e)));
+      place[tid] = slot_place(a, s, slot);
+      row[tid] = static_cast<int64_t>(s) * c.slots + slot;
+    }
+    __syncthreads();
+    const int nt = min(kWidenRows, places - e0);
+    for (int v = v0; v < shape.units && lane < shape.lanes; v += kThreads) {
+      const int w = shape.by_row.div(v);
+      const uint32_t r = v - w * shape.by_row.d, h = shape.by_units.div(r), u = r - h * shape.by_units.d;
+      const uint8_t* const pool = w ? c.v : c.k;
+      const uint32_t from = h * static_cast<uint32_t>(c.head_bytes) + u * 16;
+      uint8_t* const out = (w ? to.v : to.k) + r * 32;
+      for (int i = lane; i < nt; i += kFlight * shape.lanes) {
+        uint4 x[kFlight];
+        uint32_t b[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+          const int t = i + k * shape.lanes;
+          x[k] = make_uint4(0, 0, 0, 0);
+          b[k] = 127;
+          if (t >= nt) continue;
+          const uint32_t at = w ? place[t].v : place[t].k;
+          if (at == kNoRow) continue;
+          const uint8_t* z = row_at(a, pool, at);
+          x[k] = __ldg(reinterpret_cast<const uint4*>(z + from));
+          b[k] = __ldg(z + c.scale_at + h);
+        }
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+          const int t = i + k * shape.lanes;
+          if (t < nt && place[t].k != kNoRow) write_unit<CODES, T, true>(out + row[t] * to.row_bytes, x[k], b[k]);
+        }
+      }
+    }
+  }
+}
+
+template <int CODES, typename T>
+cudaError_t widen(const AttendArgs& a, const ReadShape& shape, const WidenTo& to, int chunks, cudaStream_t stream) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(a.batch.sessions) * chunks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_widen<CODES, T>, a, shape, to, chunks);
 }
 
 // ---- Keep ------------------------------------------------------------------------------
@@ -242,14 +327,33 @@ __global__ void __launch_bounds__(kThreads) k_kv_keep(const __grid_constant__ Ke
 
 }  // namespace
 
-cudaError_t launch_read(const ReadArgs& a, int sm_count, cudaStream_t stream) {
+namespace {
+// Shares out the units of a row of `tensors` pools.
+ReadShape shape_of(const CacheDev& c, int tensors) {
   ReadShape shape;
-  const int head = a.cache.head_dim / (a.cache.codes == kElements16 ? 8 : 16), row = a.cache.heads * head;
+  const int head = c.head_dim / (c.codes == kElements16 ? 8 : 16), row = c.heads * head;
   shape.by_units.set(head);
   shape.by_row.set(row);
-  shape.units = row * ((a.out[0].data != nullptr) + (a.out[1].data != nullptr));
+  shape.units = row * tensors;
   shape.lanes = shape.units >= kThreads ? 1 : kThreads / shape.units;
   shape.by_threads.set(kThreads / shape.lanes);
+  shape.per_block = 0;
+  return shape;
+}
+}  // namespace
+
+cudaError_t launch_widen(const AttendArgs& a, const WidenTo& to, int64_t seen, cudaStream_t stream) {
+  const ReadShape shape = shape_of(a.cache, 2);
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((seen + kWidenRows - 1) / kWidenRows, 0x7fffffff / a.batch.sessions));
+  const int n = static_cast<int>(chunks);
+  const bool half = a.dtype == PCS_DT_F16;
+  if (a.cache.codes == kCodesE4M3)
+    return half ? widen<kCodesE4M3, __half>(a, shape, to, n, stream) : widen<kCodesE4M3, __nv_bfloat16>(a, shape, to, n, stream);
+  return half ? widen<kCodesI8, __half>(a, shape, to, n, stream) : widen<kCodesI8, __nv_bfloat16>(a, shape, to, n, stream);
+}
+
+cudaError_t launch_read(const ReadArgs& a, int sm_count, cudaStream_t stream) {
+  ReadShape shape = shape_of(a.cache, (a.out[0].data != nullptr) + (a.out[1].data != nullptr));
   // Few tokens: as many blocks as there are; many: blocks that look up as many tokens as
   // their threads take in a few rounds.
   const int64_t share = a.batch.tokens / (4 * sm_count), most = std::min<int64_t>(kReadTokens, 2 * kFlight * shape.lanes);

@@ -462,7 +462,7 @@ enum KernelKind {
   kKFinalizePack, kKFinalizeRestoreV, kKScore, kKTopk, kKBulkHash, kKBulkPack,
   kKBulkRestore, kKBulkRestoreV, kKReduce, kKGSelect, kKGFinish, kKPoolAlloc, kKPoolShare,
   kKPoolCow, kKPoolRelease, kKMismatch, kKClassifyReads, kKUpload, kKRotate, kKAppend, kKAttendToken, kKAttendBlock,
-  kKAttendJoin, kKStore, kKRead, kKKeep, kKernelKinds
+  kKAttendJoin, kKStore, kKRead, kKKeep, kKWiden, kKernelKinds
 };
 static_assert(kKernelKinds <= 32, "kernel timing table");
 const char* kKernelNames[kKernelKinds] = {
@@ -471,7 +471,7 @@ const char* kKernelNames[kKernelKinds] = {
     "k_hash", "k_bulk<pack>", "k_bulk<restore>", "k_bulk<restore_verify>",
     "k_reduce_nodes", "k_gselect", "k_gfinish", "k_pool_alloc", "k_pool_share", "k_pool_cow",
     "k_pool_release", "k_mismatch", "k_classify_reads", "k_upload", "k_rotate", "k_rotate<append>",
-    "k_attend_token", "k_attend_block", "k_attend_join", "k_store", "k_kv_read", "k_kv_keep"};
+    "k_attend_token", "k_attend_block", "k_attend_join", "k_store", "k_kv_read", "k_kv_keep", "k_widen"};
 
 cudaEvent_t timing_event(pcs_ctx* c) {
   if (!c->timing_events.empty()) {
