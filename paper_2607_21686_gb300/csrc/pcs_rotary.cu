@@ -238,12 +238,20 @@ struct StoreShape {
   FastDiv by_heads[kRotTensors];
 };
 
-// Bits of the larger magnitude of two 16-bit floats (infinity and NaN above all).
-template <typename T>
-__device__ __forceinline__ uint32_t magnitude(T x) {
-  uint16_t b;
-  memcpy(&b, &x, 2);
-  return b & 0x7fffu;
+// The largest magnitude of some 16-bit floats, as bits (infinity and NaN above all): of
+// those in the lower and in the upper halves of words.
+template <typename T, int VE>
+__device__ __forceinline__ void raise(uint32_t& top, const Run<T, VE>& x) {
+  if constexpr (VE == 1) {
+    uint16_t b;
+    memcpy(&b, &x, 2);
+    top = __vmaxu2(top, b & 0x7fffu);
+  } else {
+    uint32_t w[VE / 2];
+    memcpy(w, &x, sizeof w);
+#pragma unroll
+    for (int i = 0; i < VE / 2; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+  }
 }
 template <typename T>
 __device__ __forceinline__ float magnitude_value(uint32_t bits) {
@@ -263,17 +271,19 @@ __device__ __forceinline__ int scale_exponent(float top, int codes) {
   return s < -126 ? -126 : s;
 }
 
-// Four codes.  (8-bit floats by the conversion instruction; whole numbers by
-// adding 1.5 * 2^23, whose sum's last byte is the rounded number.)
-__device__ __forceinline__ uint32_t four_codes(float x, float y, float z, float w, int codes) {
+// Four codes, of numbers times `by`, a power of two.  (8-bit floats by the conversion
+// instruction; whole numbers by adding 1.5 * 2^23, whose sum's last byte is the rounded
+// number: the product is exact, so the sum is rounded once.)
+__device__ __forceinline__ uint32_t four_codes(float x, float y, float z, float w, float by, int codes) {
   if (codes == kCodesE4M3) {
     uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y), "f"(x));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(w), "f"(z));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y * by), "f"(x * by));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(w * by), "f"(z * by));
     return lo | static_cast<uint32_t>(hi) << 16;
   }
   constexpr float k = 12582912.0f;
-  const uint32_t a = __float_as_uint(x + k), b = __float_as_uint(y + k), c = __float_as_uint(z + k), d = __float_as_uint(w + k);
+  const uint32_t a = __float_as_uint(fmaf(x, by, k)), b = __float_as_uint(fmaf(y, by, k));
+  const uint32_t c = __float_as_uint(fmaf(z, by, k)), d = __float_as_uint(fmaf(w, by, k));
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 
@@ -283,14 +293,13 @@ __device__ __forceinline__ void store_codes(uint8_t* at, const Run<T, VE>& x, fl
     uint32_t c[VE / 4];
 #pragma unroll
     for (int i = 0; i < VE; i += 4)
-      c[i / 4] = four_codes(to_float(x.e[i]) * by, to_float(x.e[i + 1]) * by, to_float(x.e[i + 2]) * by,
-                            to_float(x.e[i + 3]) * by, codes);
+      c[i / 4] = four_codes(to_float(x.e[i]), to_float(x.e[i + 1]), to_float(x.e[i + 2]), to_float(x.e[i + 3]), by, codes);
     memcpy(__builtin_assume_aligned(at, VE), c, VE);
   } else if constexpr (VE == 2) {
     *reinterpret_cast<uint16_t*>(at) =
-        static_cast<uint16_t>(four_codes(to_float(x.e[0]) * by, to_float(x.e[1]) * by, 0.0f, 0.0f, codes));
+        static_cast<uint16_t>(four_codes(to_float(x.e[0]), to_float(x.e[1]), 0.0f, 0.0f, by, codes));
   } else {
-    *at = static_cast<uint8_t>(four_codes(to_float(x.e[0]) * by, 0.0f, 0.0f, 0.0f, codes));
+    *at = static_cast<uint8_t>(four_codes(to_float(x.e[0]), 0.0f, 0.0f, 0.0f, by, codes));
   }
 }
 
@@ -360,11 +369,13 @@ __global__ void __launch_bounds__(kThreads)
       }
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int k = 0; k < VE; ++k) top = max(top, max(magnitude(x[i].e[k]), magnitude(y[i].e[k])));
-      for (int o = shape.lanes >> 1; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int i = 0; i < U; ++i) {
+        raise(top, x[i]);
+        raise(top, y[i]);
+      }
+      for (int o = shape.lanes >> 1; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
       if (!live) continue;
+      top = max(top & 0xffffu, top >> 16);
       const bool fine = top < (std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u);
       const int e = scale_exponent(magnitude_value<T>(top), a.cache.codes);
       const float by = fine ? __uint_as_float(static_cast<uint32_t>(127 - e) << 23) : 0.0f;
