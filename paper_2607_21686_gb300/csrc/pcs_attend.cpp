@@ -470,7 +470,8 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       CodeMaps maps;
       if (a.box_rows && !encode_codes(*cache, a.cache, a.box_rows, 1, false, &maps)) a.box_rows = 0;
       call.before(kOpAttendBlock);
-      st = call.after(launch_attend_block8(a, dtype, static_cast<int>(blocks), maps, call.stream()));
+      const auto launch = a.cache.codes == kCodesE4M3 ? launch_attend_block_e4m3 : launch_attend_block_i8;
+      st = call.after(launch(a, dtype, static_cast<int>(blocks), maps, call.stream()));
     } else {
       TensorMaps maps = {};
       if (a.box_rows &&

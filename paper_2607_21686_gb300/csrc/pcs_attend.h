@@ -247,8 +247,9 @@ cudaError_t launch_attend_block(const AttendArgs& a, uint32_t dtype, int blocks,
 // Forms of it: trees over 16-bit elements, anything over 8-bit codes.
 cudaError_t launch_attend_block_tree(const AttendArgs& a, uint32_t dtype, int blocks, const TensorMaps& maps,
                                      cudaStream_t stream);
-cudaError_t launch_attend_block8(const AttendArgs& a, uint32_t dtype, int blocks, const CodeMaps& maps,
-                                 cudaStream_t stream);
+cudaError_t launch_attend_block_e4m3(const AttendArgs& a, uint32_t dtype, int blocks, const CodeMaps& maps,
+                                     cudaStream_t stream);
+cudaError_t launch_attend_block_i8(const AttendArgs& a, uint32_t dtype, int blocks, const CodeMaps& maps, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttendArgs& a, uint32_t dtype, int blocks, cudaStream_t stream);
 
 }  // namespace pcs

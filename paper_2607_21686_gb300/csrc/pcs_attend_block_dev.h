@@ -12,25 +12,26 @@ namespace {
 
 constexpr int kTile = 128;              // rows of a row tile, tokens of a tile
 // Warps 0-3 and 4-7: a row tile each, a thread a row; 8: matrix products; 9-11: copies.
-// With codes (MAKERS kCodes) 9: copies, 10-15: turn them into elements.
-constexpr int kCodes = -1;
+// With codes (MAKERS below 0: E4M3, I8) 9: copies, 10-15: turn them into elements.
+template <int MAKERS>
+constexpr int kCodesOf = MAKERS == -1 ? kCodesE4M3 : kCodesI8;
 constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8;
 constexpr int kCopyWarp = 9;
 template <int MAKERS>
-constexpr int kCopyWarpsOf = MAKERS == kCodes ? 7 : 3;
+constexpr int kCopyWarpsOf = MAKERS < 0 ? 7 : 3;
 template <int MAKERS>
 constexpr int kThreadsOf = 32 * (kCopyWarp + kCopyWarpsOf<MAKERS>);
 // Registers of a thread: the launch's shared out anew, 256 x 224 + 128 x 56 = 384 x
 // 168, with codes 256 x 200 + 256 x 56 = 512 x 128.
 template <int MAKERS>
-constexpr int kSoftRegsOf = MAKERS == kCodes ? 200 : 224;
+constexpr int kSoftRegsOf = MAKERS < 0 ? 200 : 224;
 constexpr int kOtherRegs = 56;
 constexpr int kLag = 2;                 // copies in flight behind the newest
 // Tiles whose masks are kept.  (Codes are copied up to three tiles before they are
 // converted, and those up to four before their scores are read.)
 template <int MAKERS>
-constexpr int kValidOf = MAKERS == -1 ? 16 : 8;
+constexpr int kValidOf = MAKERS < 0 ? 16 : 8;
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kSlack = 8.0f;          // as in the token kernel
 
@@ -42,7 +43,7 @@ constexpr float kSlack = 8.0f;          // as in the token kernel
 template <int DP>
 constexpr int kKeyTiles = DP == 64 ? 4 : 2;
 template <int DP, int MAKERS>
-constexpr int kValueTiles = DP == 64 ? 4 : MAKERS > 0 ? 3 : MAKERS == kCodes ? 1 : 2;
+constexpr int kValueTiles = DP == 64 ? 4 : MAKERS > 0 ? 3 : MAKERS < 0 ? 1 : 2;
 template <int DP, int MAKERS>
 constexpr int kBuffers = kKeyTiles<DP> + kValueTiles<DP, MAKERS>;
 template <int DP>
@@ -55,7 +56,7 @@ constexpr int kCodeStages = DP == 64 ? 5 : 3;
 template <int DP>
 constexpr uint32_t kCodeStage = kTile * (DP + 16);
 template <int DP, int MAKERS>
-constexpr uint32_t kStagedBytes = MAKERS == kCodes ? kCodeStages<DP> * kCodeStage<DP> : 0;
+constexpr uint32_t kStagedBytes = MAKERS < 0 ? kCodeStages<DP> * kCodeStage<DP> : 0;
 template <int DP, int MAKERS>
 constexpr uint32_t kSmemBytes = (2 + kBuffers<DP, MAKERS>) * kTileBytes<DP> + kStagedBytes<DP, MAKERS> + 1024;
 
@@ -284,14 +285,14 @@ __device__ __forceinline__ bool take_out(uint4* at, uint4 v) {
 }
 
 // MAKERS: warps that send tensor copies of boxes of rows (the other copying warps
-// look values over); 0: rows are copied one by one; kCodes: rows of codes are, and
+// look values over); 0: rows are copied one by one; below 0: rows of codes are, and
 // become 16-bit elements on their way to the tiles.  TREE: the new tokens are nodes of
 // a tree.  Boxes of eight rows are
 // sixteen or thirty-two a tile, more than one warp can send in a tile's time: two
 // warps take keys and values (8,000-token prompt in pages of 8: 411 us by one,
 // 358 us by two; in pages of 16: 349 and 353 us).
 template <int MAKERS>
-using MapsOf = std::conditional_t<MAKERS == kCodes, CodeMaps, TensorMaps>;
+using MapsOf = std::conditional_t<MAKERS < 0, CodeMaps, TensorMaps>;
 template <typename T, int DP, int MAKERS, bool TREE>
 __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
     k_attend_block(const __grid_constant__ AttendArgs a, const __grid_constant__ MapsOf<MAKERS> maps, int blocks) {
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(16) uint8_t raw[];
   __shared__ __align__(8) uint64_t bars[Bars::kCount];
-  __shared__ __align__(8) uint64_t code_bars[MAKERS == kCodes ? 2 * kCodeStages<DP> : 1];  // filled, free
+  __shared__ __align__(8) uint64_t code_bars[MAKERS < 0 ? 2 * kCodeStages<DP> : 1];  // filled, free
   __shared__ uint32_t tmem_at;
   constexpr int kValid = kValidOf<MAKERS>;
   __shared__ __align__(16) uint32_t valid[kValid][4];  // a bit per token that is in the cache
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   if constexpr (BOX) {
     if (warp == kCopyWarp && lane < 2)
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? maps.v : maps.k)) : "memory");
-  } else if constexpr (MAKERS == kCodes) {
+  } else if constexpr (MAKERS < 0) {
     if (warp == kCopyWarp && lane < 4 && a.box_rows > 0)
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps.map[lane])) : "memory");
   }
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   const int sp = b % a.splits;
   b /= a.splits;
   int s = b % a.batch.sessions;
-  if constexpr (MAKERS == kCodes || TREE)
+  if constexpr (MAKERS < 0 || TREE)
     if (a.ranked) s = ranked_session(a.batch, s, tid, kThreadsOf<MAKERS>, reinterpret_cast<uint32_t*>(raw));
   const int blk = blocks - 1 - b / a.batch.sessions;  // the longest first
   const Work w = block_work<TREE>(a, s, blk, sp);
@@ -350,9 +351,9 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   auto s_read = [&](int t) { return bar0 + 8 * Bars::s_read(t); };  // kAhead: scores are in registers
   auto v_fine = [&](int j) { return bar0 + 8 * Bars::v_fine(j); };  // BOX: the values of tile j are looked over
   if (tid == 0) {
-    Bars::each(kTile, 32 * kSoftWarps / 2 * nq, BOX ? 1 : MAKERS == kCodes ? 32 * (kCopyWarps - 1) : 32 * kCopyWarps, 32 * (kCopyWarps - MAKERS),
+    Bars::each(kTile, 32 * kSoftWarps / 2 * nq, BOX ? 1 : MAKERS < 0 ? 32 * (kCopyWarps - 1) : 32 * kCopyWarps, 32 * (kCopyWarps - MAKERS),
                [&](int i, int count) { bar_init(bar0 + 8 * i, count); });
-    if (MAKERS == kCodes)
+    if (MAKERS < 0)
       for (int i = 0; i < kCodeStages<DP>; ++i) {
         bar_init(smem_addr(code_bars) + 8 * i, a.box_rows > 0 ? 1 : 33);
         bar_init(smem_addr(code_bars) + 8 * (kCodeStages<DP> + i), kCopyWarps - 1);
@@ -460,7 +461,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
           bar_arrive(v_fine(i / 2));
         }
       }
-    } else if constexpr (MAKERS == kCodes) {
+    } else if constexpr (MAKERS < 0) {
       // Fill i, as everywhere: keys of tile i / 2, or its values.  The first warp copies
       // its codes and scale bytes to stage i of their ring, the others turn them into
       // elements in the tile.
@@ -579,6 +580,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
           for (int r0 = 0; r0 < kTurns; r0 += kTogether) {
             uint4 y[kTogether];
             uint32_t scale[kTogether];
+            bool plain = true;
 #pragma unroll
             for (int k = 0; k < kTogether; ++k) {
               const int r = (r0 + k) * kStep;
@@ -587,23 +589,36 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
               if (r0 + k >= kTurns || row0 + r >= kTile || !live) continue;  // (row0: the same in a warp)
               y[k] = *reinterpret_cast<const uint4*>(from + r * DP);
               scale[k] = scales[r * 16];
+              plain = plain && plain_scale<T>(scale[k]);
             }
+            // What is rare goes its own way, for all of a warp: a branch for each unit kept
+            // their instructions apart (trees of 60 nodes, 32 sessions: 252 us).
+            if (!clear && __all_sync(kFull, plain)) {
 #pragma unroll
-            for (int k = 0; k < kTogether; ++k) {
-              const int r = (r0 + k) * kStep;
-              if (r0 + k >= kTurns || row0 + r >= kTile) continue;
-              uint4 lo, hi;
-              if (a.cache.codes == kCodesE4M3)
-                sixteen_elements<T, kCodesE4M3>(y[k], scale[k], lo, hi);
-              else
-                sixteen_elements<T, kCodesI8>(y[k], scale[k], lo, hi);
-              uint4* lo_at = reinterpret_cast<uint4*>(tile + lo_off + r * 128);
-              uint4* hi_at = reinterpret_cast<uint4*>(tile + hi_off + r * 128);
-              *lo_at = lo;
-              *hi_at = hi;
-              if (clear) {
-                any |= take_out<T>(lo_at, lo);
-                any |= take_out<T>(hi_at, hi);
+              for (int k = 0; k < kTogether; ++k) {
+                const int r = (r0 + k) * kStep;
+                if (r0 + k >= kTurns || row0 + r >= kTile) continue;
+                uint4 lo, hi;
+                sixteen_plain<T, kCodesOf<MAKERS>>(y[k], scale[k], lo, hi);
+                *reinterpret_cast<uint4*>(tile + lo_off + r * 128) = lo;
+                *reinterpret_cast<uint4*>(tile + hi_off + r * 128) = hi;
+              }
+            } else {
+#pragma unroll 1
+              for (int k = 0; k < kTogether; ++k) {
+                const int r = (r0 + k) * kStep;
+                if (r0 + k >= kTurns || row0 + r >= kTile) continue;
+                uint4 x = make_uint4(0, 0, 0, 0), lo, hi;
+                if (live) x = *reinterpret_cast<const uint4*>(from + r * DP);
+                sixteen_elements<T, kCodesOf<MAKERS>>(x, live ? scales[r * 16] : 127, lo, hi);
+                uint4* lo_at = reinterpret_cast<uint4*>(tile + lo_off + r * 128);
+                uint4* hi_at = reinterpret_cast<uint4*>(tile + hi_off + r * 128);
+                *lo_at = lo;
+                *hi_at = hi;
+                if (clear) {
+                  any |= take_out<T>(lo_at, lo);
+                  any |= take_out<T>(hi_at, hi);
+                }
               }
             }
           }
@@ -935,16 +950,14 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
               const RowPlace pl = row_place(a, s, seen_position(w.view, e));
               if (pl.k == kNoRow) continue;
               const uint8_t* v = row_at(a, a.cache.v, pl.v);
-              const float scale = MAKERS == kCodes ? scale_value(v[a.cache.scale_at + head]) : 1.0f;
-              v += head * a.cache.head_bytes + d0 * (MAKERS == kCodes ? 1 : 2);
+              const float scale = MAKERS < 0 ? scale_value(v[a.cache.scale_at + head]) : 1.0f;
+              v += head * a.cache.head_bytes + d0 * (MAKERS < 0 ? 1 : 2);
 #pragma unroll
               for (int k = 0; k < 32; k += 2) {
                 if (d0 + k >= a.cache.head_dim) continue;
                 uint32_t y;
-                if constexpr (MAKERS == kCodes) {
-                  const uint32_t codes = *reinterpret_cast<const uint16_t*>(v + k);
-                  y = a.cache.codes == kCodesE4M3 ? four_elements<T, kCodesE4M3>(codes, scale).x
-                                                  : four_elements<T, kCodesI8>(codes, scale).x;
+                if constexpr (MAKERS < 0) {
+                  y = four_elements<T, kCodesOf<MAKERS>>(*reinterpret_cast<const uint16_t*>(v + k), scale).x;
                 } else {
                   y = *reinterpret_cast<const uint32_t*>(v + 2 * k);
                 }

@@ -1,5 +1,5 @@
-// pcs_attend_block8.cu -- attention of blocks of new tokens, trees among them, over a
-// paged cache in 8 bits: the kernel of pcs_attend_block.cu, whose copying warps turn
+// pcs_attend_block_e4m3.cu -- attention of blocks of new tokens, trees among them, over a
+// paged cache of 8-bit floats: the kernel of pcs_attend_block.cu, whose copying warps turn
 // codes into elements of the queries' type on their way to the tiles.  That is exact
 // in bfloat16, whose 8 bits hold every code and whose powers of two every scale; a
 // float16 ends at 65504.
@@ -8,15 +8,17 @@
 namespace pcs {
 namespace {
 
+constexpr int kMakers = -1;
+
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs& a, int blocks, const CodeMaps& maps, cudaStream_t stream) {
-  return a.parent ? launch_form<T, DP, kCodes, true>(a, blocks, maps, stream)
-                  : launch_form<T, DP, kCodes, false>(a, blocks, maps, stream);
+  return a.parent ? launch_form<T, DP, kMakers, true>(a, blocks, maps, stream)
+                  : launch_form<T, DP, kMakers, false>(a, blocks, maps, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_block8(const AttendArgs& a, uint32_t dtype, int blocks, const CodeMaps& maps, cudaStream_t stream) {
+cudaError_t launch_attend_block_e4m3(const AttendArgs& a, uint32_t dtype, int blocks, const CodeMaps& maps, cudaStream_t stream) {
   if (dtype == PCS_DT_F16)
     return a.cache.head_dim <= 64 ? launch<__half, 64>(a, blocks, maps, stream) : launch<__half, 128>(a, blocks, maps, stream);
   return a.cache.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, blocks, maps, stream)

@@ -110,20 +110,36 @@ __device__ __forceinline__ void four_scaled(uint32_t x, uint32_t scale, uint32_t
     hi = fma_f16(__byte_perm(x, 0x64646464u, 0x4342), scale, less);
   }
 }
-// Sixteen codes times their scale, by its byte.  (To bfloat16 by way of floats: two at a time
+// Whether a scale is such a one, with nothing near float16's ends; to bfloat16 any is plain.
+template <typename T>
+__device__ __forceinline__ bool plain_scale(uint32_t b) {
+  return !std::is_same<T, __half>::value || (b >= 127 - 14 && b <= 127 + 5);
+}
+// Sixteen codes times a plain scale, by its byte.  (To bfloat16 by way of floats: two at a time
 // in its own arithmetic, codes put in place by their bits, took longer, 346 -> 384 us for
 // trees of 60 nodes over contexts of 32 sessions.)
 template <typename T, int CODES>
-__device__ __forceinline__ void sixteen_elements(const uint4& x, uint32_t b, uint4& lo, uint4& hi) {
+__device__ __forceinline__ void sixteen_plain(const uint4& x, uint32_t b, uint4& lo, uint4& hi) {
   if constexpr (std::is_same<T, __half>::value) {
-    if (b >= 127 - 14 && b <= 127 + 5) {  // far from float16's ends
-      const uint32_t scale = (b - 112) * 0x04000400u, less = CODES == kCodesI8 ? mul_f16(scale, 0xe480e480u) : 0;
-      four_scaled<CODES>(x.x, scale, less, lo.x, lo.y);
-      four_scaled<CODES>(x.y, scale, less, lo.z, lo.w);
-      four_scaled<CODES>(x.z, scale, less, hi.x, hi.y);
-      four_scaled<CODES>(x.w, scale, less, hi.z, hi.w);
-      return;
-    }
+    const uint32_t scale = (b - 112) * 0x04000400u, less = CODES == kCodesI8 ? mul_f16(scale, 0xe480e480u) : 0;  // -1152
+    four_scaled<CODES>(x.x, scale, less, lo.x, lo.y);
+    four_scaled<CODES>(x.y, scale, less, lo.z, lo.w);
+    four_scaled<CODES>(x.z, scale, less, hi.x, hi.y);
+    four_scaled<CODES>(x.w, scale, less, hi.z, hi.w);
+  } else {
+    const float s = scale_value(b);
+    const uint2 a = four_elements<T, CODES>(x.x, s), d = four_elements<T, CODES>(x.y, s);
+    const uint2 e = four_elements<T, CODES>(x.z, s), f = four_elements<T, CODES>(x.w, s);
+    lo = make_uint4(a.x, a.y, d.x, d.y);
+    hi = make_uint4(e.x, e.y, f.x, f.y);
+  }
+}
+// Any scale.
+template <typename T, int CODES>
+__device__ __forceinline__ void sixteen_elements(const uint4& x, uint32_t b, uint4& lo, uint4& hi) {
+  if (plain_scale<T>(b)) {
+    sixteen_plain<T, CODES>(x, b, lo, hi);
+    return;
   }
   const float s = scale_value(b);
   const uint2 a = four_elements<T, CODES>(x.x, s), d = four_elements<T, CODES>(x.y, s);
