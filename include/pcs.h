@@ -648,8 +648,10 @@ pcs_status pcs_snapshot_read_file(pcs_ctx *ctx, const char *path, uint32_t place
  * caller, Sec. 3 "Boundary"; the pages are those of Sec. 7.2's addressable KV
  * and of the copy-on-write pool above.)  Fields said to be 0 that are not, and
  * flags that are not named here -> PCS_E_INVAL.  These calls can be captured into
- * a graph; attention that needs working memory takes memory of its own then, a few
- * MB that stay with the context until pcs_destroy, which has to outlive the graph.
+ * a graph; attention that needs working memory (parts of results, an 8-bit cache's
+ * values where many rows go over them, at most 1 GiB and the parts) takes memory of
+ * its own then, which stays with the context until pcs_destroy: that has to come
+ * after the graph's last run.
  */
 
 /* Heads of tokens: element d of head h of token t is at
@@ -780,7 +782,9 @@ pcs_status pcs_kv_append(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_b
  * that sees nothing gives 0.  lse: device float[tokens][q heads] or NULL,
  * log sum exp(scale * q.k_j) (-inf if it sees nothing), by which results over
  * several caches can be joined.  Sums are in 32 bits, weights are rounded to
- * the cache's type before they multiply values.  What is in slots that no new
+ * the cache's type before they multiply values (a cache in 8 bits: to float16, or
+ * to the queries' type, in which its values then are, float16 up to 65504; q and
+ * out are PCS_DT_F16 or PCS_DT_BF16).  What is in slots that no new
  * token sees (infinities, NaN) does not matter.  out may be q.  q and out:
  * 16-byte multiples (else PCS_E_ALIGN).  Page ids outside the pool, slots beyond the table, more
  * new tokens than max_new or than lens says -> PCS_E_RANGE at the next

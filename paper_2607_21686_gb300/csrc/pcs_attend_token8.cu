@@ -46,7 +46,7 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
   return DP == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
 }
 // Where a row's weights refer to before its first token: nothing is below it.
-constexpr float kNothing = -1e30f;
+constexpr float kNothing = -3e38f;
 // A weight beyond this, or times its value's scale beyond 2^15, raises the reference.
 constexpr float kMostWeight = 1.2676506e30f;  // 2^100
 
