@@ -26,8 +26,12 @@
 //                 them; the warps send them in turn.  (What bounds copies by the warps'
 //                 lanes is their number: a scale byte is a request of its own beside 64 or
 //                 128 bytes of codes.)
+//                 256 sessions over windows of 1,024 tokens, 16 heads of 64, E4M3: 104 us,
+//                 5.3 TB/s (78 % of the measured copy rate; 1.7 waves of equal blocks); 48
+//                 sessions of 1 to 12,000 tokens, 32 over 8 heads of 128, I8: 116 us.  The
+//                 copies alone, a warp a head, took 94 us of the first.
 // k_attend_token8_rows  The same from pages whose size no such box divides: each warp
-//                 copies rows of tiles of its own.
+//                 copies rows of tiles of its own (the 48 sessions in pages of 25: 182 us).
 #include "pcs_attend_token_dev.h"
 #include "pcs_codes_dev.h"
 

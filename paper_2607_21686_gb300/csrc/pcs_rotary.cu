@@ -17,6 +17,10 @@
 //            tokens of 24 sessions, 16 heads of 64: 48 us, 5.9 TB/s.  What is left is
 //            instructions (two thirds of the issue slots are taken) and a block's
 //            look-ups before its first load.
+// k_store    the append to a cache in 8 bits, which needs a head's largest magnitude
+//            before it can write its first code: a few lanes hold a head, so it is read
+//            once.  22,700 new tokens of 24 sessions, 16 heads of 64 in float16, I8: 50 us,
+//            of 35 us for its bytes; four fifths of the issue slots are taken.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
