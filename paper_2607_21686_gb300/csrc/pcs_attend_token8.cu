@@ -370,9 +370,9 @@ constexpr uint32_t kSmem8 = kStages8<DP> * kStage8<DP, HEADS> + 1024;
 template <int DP, int NT>
 constexpr int kByRegisters8 = NT == 4 ? 2 : NT == 2 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 3;
 template <int DP, int NT, int HEADS>
-constexpr int kResident8 = kByRegisters8<DP, NT> * (kSmem8<DP, HEADS> + 3072) <= 227 * 1024
+constexpr int kResident8 = kByRegisters8<DP, NT> * (kSmem8<DP, HEADS> + 3 * 1024) <= 227 * 1024
                                ? kByRegisters8<DP, NT>
-                               : static_cast<int>(227 * 1024 / (kSmem8<DP, HEADS> + 3072));
+                               : static_cast<int>(227 * 1024 / (kSmem8<DP, HEADS> + 3 * 1024));
 
 __device__ __forceinline__ void box_of_codes(uint32_t to, uint64_t map, int row, int head, int page, uint32_t bar) {
   asm volatile(

@@ -22,7 +22,7 @@ uint32_t draw() {
 }
 int32_t upto(int32_t n) { return static_cast<int32_t>(draw() % (static_cast<uint32_t>(n) + 1)); }
 
-struct Checker {
+struct Session {
   AttendArgs a = {};
   int align = 1, group = 1;
   int64_t len = 0;
@@ -126,7 +126,7 @@ int main(int argc, char** argv) {
   state = std::strtoull(argv[1], nullptr, 10) * 7919 + 1;
   const int n = std::atoi(argv[2]), kind = std::atoi(argv[3]);
   for (int g = 0; g < n; ++g) {
-    Checker c;
+    Session c;
     c.align = 1 << (draw() % 4 ? 3 + draw() % 5 : 0);
     const int32_t groups[] = {1, 2, 4, 5, 8, 40};
     c.group = groups[draw() % 6];

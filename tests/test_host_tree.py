@@ -13,7 +13,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
-def checker(tmp_path_factory):
+def program(tmp_path_factory):
     gxx = shutil.which("g++")
     cuda = os.path.join(build._cuda_home(), "include")
     if not gxx or not os.path.exists(os.path.join(cuda, "cuda_runtime.h")):
@@ -26,6 +26,6 @@ def checker(tmp_path_factory):
 
 @pytest.mark.parametrize("kind", [0, 1])
 @pytest.mark.parametrize("seed", [1, 2, 3])
-def test_what_nodes_see(checker, seed, kind):
-    out = subprocess.run([checker, str(seed), "1500", str(kind)], capture_output=True, text=True, timeout=300)
+def test_what_nodes_see(program, seed, kind):
+    out = subprocess.run([program, str(seed), "1500", str(kind)], capture_output=True, text=True, timeout=300)
     assert out.returncode == 0 and out.stdout.strip() == "ok", out.stdout + out.stderr
