@@ -389,23 +389,26 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
       if (a.batch.sessions > 1)
         splits = std::max(splits, std::min(4 * resident / pairs, tiles / (8 * kTokenWarps)));
       // Blocks over codes that take several heads: a warp's result is a part of its head's.
-      // Of several sessions whose lengths may differ by much, the longest come first and
-      // there are parts for two waves and a quarter.  (48 sessions of 1 to 12,000 tokens, 8
-      // heads of 128: 131 us in one wave as they come, 110 to 116 us so; 256 over windows of
-      // 1,024, 16 heads of 64, as they come: 105 us whole, 140 us in two parts.)
+      // Of several sessions whose lengths may differ by much (no window or ring makes them
+      // alike), the longest come first and there are parts for two waves and a quarter.  (48
+      // sessions of 1 to 12,000 tokens, 8 heads of 128: 131 us in one wave as they come, 106 us
+      // so; 128 over windows of 2,048, 16 heads of 64: 97 us whole, 114 us in three parts.)
       int64_t each = 1;
       if (boxes) {
         each = kTokenWarps / a.box_heads;
         const int64_t blocks = pairs / a.box_heads, turns = (tiles + 2 * each - 1) / (2 * each);
         splits = std::min(resident / blocks, turns / 2);
         if (splits * each > kTokenOwnJoin) splits = std::max<int64_t>(kTokenOwnJoin / each, std::min(splits, turns / 4));
-        a.ranked = a.batch.sessions > 1 && a.batch.sessions <= kRankMost && tiles >= 128;
+        const int64_t longest = batch->max_len ? batch->max_len : cache->ring ? INT32_MAX : a.cache.slots;
+        a.ranked = a.batch.sessions > 1 && a.batch.sessions <= kRankMost && tiles >= 128 && seen >= longest;
         if (a.ranked) splits = std::max(splits, std::min((9 * resident / 4 + blocks / 2) / blocks, turns / 16));
       }
       splits = std::max<int64_t>(splits, 1);
       const int64_t parts = splits * each;
-      // (Warps that join alone do so for few rows.)
-      const bool own = parts <= kTokenOwnJoin && pairs <= kOpWords && (!boxes || parts * rows <= 128);
+      // (Warps over codes join alone what is little: each of their parts waits for its writes.
+      // 64 sessions in two parts of a row: 33 us, 39 us by a second launch; the 48 of above in
+      // eleven of four rows 115 and 106 us.)
+      const bool own = parts <= kTokenOwnJoin && pairs <= kOpWords && (!boxes || parts * rows <= 16);
       a.splits = static_cast<int32_t>(splits);
       if (pairs * parts > 0x7FFFFFFFll) return op_fail(PCS_E_INVAL, "too many sessions and heads in one call");
       if (parts > 1) {

@@ -28,7 +28,7 @@
 //                 128 bytes of codes.)
 //                 256 sessions over windows of 1,024 tokens, 16 heads of 64, E4M3: 104 us,
 //                 5.3 TB/s (78 % of the measured copy rate; 1.7 waves of equal blocks); 48
-//                 sessions of 1 to 12,000 tokens, 32 over 8 heads of 128, I8: 116 us.  The
+//                 sessions of 1 to 12,000 tokens, 32 over 8 heads of 128, I8: 107 us.  The
 //                 copies alone, a warp a head, took 94 us of the first.
 // k_attend_token8_rows  The same from pages whose size no such box divides: each warp
 //                 copies rows of tiles of its own (the 48 sessions in pages of 25: 182 us).
@@ -359,16 +359,19 @@ struct TokenRows {
 // A block's turn is its warps' tiles: those of its heads, or several of one's.  Codes of
 // keys and of values of a turn, each box with its heads one behind the other; then scale
 // bytes of 16 heads, of keys and of values.
-template <int DP>
-constexpr int kStages8 = DP == 64 ? 3 : 2;
+// Three turns, two of them on their way: 139 KB an SM with heads of 64 and four blocks, 135 KB
+// with heads of 128 and two.  (48 sessions of 1 to 12,000 tokens, 8 heads of 128: 107 us, 108
+// us with two turns of three blocks; heads of 64, 256 sessions: 104 us, three blocks of four
+// turns 128 us, five of two 118 us.)
+constexpr int kStages8 = 3;
 template <int DP, int HEADS>
 constexpr uint32_t kStage8 = 2 * kWarps * kTile8 * DP + 2 * (kWarps / HEADS) * kTile8 * 16;
 // (Boxes begin at multiples of 1,024 bytes: room to get there.)
 template <int DP, int HEADS>
-constexpr uint32_t kSmem8 = kStages8<DP> * kStage8<DP, HEADS> + 1024;
+constexpr uint32_t kSmem8 = kStages8 * kStage8<DP, HEADS> + 1024;
 // Blocks that one SM holds, by its registers and by its shared memory.
 template <int DP, int NT>
-constexpr int kByRegisters8 = NT == 4 ? 2 : NT == 2 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 3;
+constexpr int kByRegisters8 = NT == 4 ? 2 : NT == 2 ? (DP == 64 ? 3 : 2) : DP == 64 ? 4 : 2;
 template <int DP, int NT, int HEADS>
 constexpr int kResident8 = kByRegisters8<DP, NT> * (kSmem8<DP, HEADS> + 3 * 1024) <= 227 * 1024
                                ? kByRegisters8<DP, NT>
@@ -390,7 +393,7 @@ __device__ __forceinline__ void box_of_scales(uint32_t to, uint64_t map, int byt
 template <int CODES, int DP, int NT, int HEADS>
 __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, HEADS>))
     k_attend_token8(const __grid_constant__ AttendArgs a, const __grid_constant__ CodeMaps maps) {
-  constexpr int kStages = kStages8<DP>;
+  constexpr int kStages = kStages8;
   constexpr uint32_t kStage = kStage8<DP, HEADS>;
   constexpr int kTiles = kWarps / HEADS;        // tiles of a turn
   constexpr uint32_t kCodeBytes = kWarps * kTile8 * DP, kScaleBytes = kTiles * kTile8 * 16;
