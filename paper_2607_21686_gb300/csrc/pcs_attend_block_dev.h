@@ -23,10 +23,11 @@ constexpr int kCopyWarpsOf = MAKERS < 0 ? 7 : 3;
 template <int MAKERS>
 constexpr int kThreadsOf = 32 * (kCopyWarp + kCopyWarpsOf<MAKERS>);
 // Registers of a thread: the launch's shared out anew, 256 x 224 + 128 x 56 = 384 x
-// 168, with codes 256 x 200 + 256 x 56 = 512 x 128.
+// 168, with codes 256 x 192 + 256 x 64 = 512 x 128.
 template <int MAKERS>
-constexpr int kSoftRegsOf = MAKERS < 0 ? 200 : 224;
-constexpr int kOtherRegs = 56;
+constexpr int kSoftRegsOf = MAKERS < 0 ? 192 : 224;
+template <int MAKERS>
+constexpr int kOtherRegsOf = MAKERS < 0 ? 64 : 56;
 constexpr int kLag = 2;                 // copies in flight behind the newest
 // Tiles whose masks are kept.  (Codes are copied up to three tiles before they are
 // converted, and those up to four before their scores are read.)
@@ -380,7 +381,7 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
   auto spot = [](int row, int c) { return (c >> 3) * kPanel + row * 128 + (((c & 7) ^ (row & 7)) << 4); };
 
   if (warp >= kSoftWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegsOf<MAKERS>));
     if (warp >= kCopyWarp && w.tiles > 0) {
     // ---- Copying warps.  Fill i: keys of tile i / 2, or its values ----
     const int c = warp - kCopyWarp;
@@ -559,8 +560,9 @@ __global__ void __launch_bounds__(kThreadsOf<MAKERS>, 1)
         }
       } else {
         // A warp's rows are kStep apart, a multiple of eight: their chunks' places in a tile
-        // differ by whole rows.
-        constexpr int kStep = (kCopyWarps - 1) * kCodeRows, kTurns = (kTile + kStep - 1) / kStep, kTogether = 3;
+        // differ by whole rows.  (All of a warp's units in registers at once: 210 us for trees
+        // of 60 nodes over 32 sessions, 214 us by threes.)
+        constexpr int kStep = (kCopyWarps - 1) * kCodeRows, kTurns = (kTile + kStep - 1) / kStep, kTogether = 6;
         static_assert(kStep % 8 == 0, "the swizzle goes by a row's number modulo 8");
         const int row0 = (c - 1) * kCodeRows;
         const bool live = code_chunk * 16 < a.cache.head_dim;  // (rows one by one: nobody wrote elsewhere)

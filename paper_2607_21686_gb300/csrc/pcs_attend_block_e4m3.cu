@@ -3,7 +3,7 @@
 // codes into elements of the queries' type on their way to the tiles.  That is exact
 // in bfloat16, whose 8 bits hold every code and whose powers of two every scale; a
 // float16 ends at 65504.  Trees of 60 nodes over contexts of 500 to 9,000 tokens of 32
-// sessions, 32 query heads over 8 of 128: 214 us (over 16-bit pages 155 us).  The bound is
+// sessions, 32 query heads over 8 of 128: 210 us (over 16-bit pages 155 us).  The bound is
 // the conversion, some 10 codes a cycle of an SM; more warps for it would take registers
 // from the softmax threads.
 #include "pcs_attend_block_dev.h"
