@@ -26,9 +26,9 @@
 //                 them; the warps send them in turn.  (What bounds copies by the warps'
 //                 lanes is their number: a scale byte is a request of its own beside 64 or
 //                 128 bytes of codes.)
-//                 256 sessions over windows of 1,024 tokens, 16 heads of 64, E4M3: 104 us,
-//                 5.3 TB/s (78 % of the measured copy rate; 1.7 waves of equal blocks); 48
-//                 sessions of 1 to 12,000 tokens, 32 over 8 heads of 128, I8: 107 us.  The
+//                 256 sessions over windows of 1,024 tokens, 16 heads of 64, E4M3: 102 us,
+//                 5.4 TB/s (79 % of the measured copy rate; 1.7 waves of equal blocks); 48
+//                 sessions of 1 to 12,000 tokens, 32 over 8 heads of 128, I8: 104 us.  The
 //                 copies alone, a warp a head, took 94 us of the first.
 // k_attend_token8_rows  The same from pages whose size no such box divides: each warp
 //                 copies rows of tiles of its own (the 48 sessions in pages of 25: 182 us).
@@ -360,7 +360,7 @@ struct TokenRows {
 // keys and of values of a turn, each box with its heads one behind the other; then scale
 // bytes of 16 heads, of keys and of values.
 // Three turns, two of them on their way: 139 KB an SM with heads of 64 and four blocks, 135 KB
-// with heads of 128 and two.  (48 sessions of 1 to 12,000 tokens, 8 heads of 128: 107 us, 108
+// with heads of 128 and two.  (48 sessions of 1 to 12,000 tokens, 8 heads of 128: 106 us, 108
 // us with two turns of three blocks; heads of 64, 256 sessions: 104 us, three blocks of four
 // turns 128 us, five of two 118 us.)
 constexpr int kStages8 = 3;
