@@ -280,10 +280,11 @@ struct TokenRows {
       four_halves<CODES>(__byte_perm(early, 0, 0x3120), x[0], x[1]);
       four_halves<CODES>(__byte_perm(late, 0, 0x3120), x[2], x[3]);
     };
-    // (Only the NaN of 8-bit floats would go through a weight of 0: tokens that some rows
-    // see and others do not are told apart where there is one.)
+    // (Only the NaN of 8-bit floats would go through a weight of 0: where there is one among
+    // tokens that some rows do not see, or rows that a box brought along that are nobody's,
+    // as those behind the end of a ring, each new token takes the codes of what it sees.)
     bool apart = false;
-    if (CODES == kCodesE4M3 && part) {
+    if (CODES == kCodesE4M3 && masked) {
       uint32_t nan = 0;
 #pragma unroll
       for (int h = 0; h < H; ++h)
@@ -312,7 +313,7 @@ struct TokenRows {
         }
     } else {
       for (int i = 0; i < m_new; ++i) {
-        const uint32_t m = sees(i, e0) >> (16 * h0 + 2 * q4);
+        const uint32_t m = (there & (part ? sees(i, e0) : kFull)) >> (16 * h0 + 2 * q4);
 #pragma unroll
         for (int h = 0; h < H; ++h) {
           uint32_t in[2];  // of tokens 16 h + 2 q4, +1 and 8 more
@@ -328,11 +329,15 @@ struct TokenRows {
               operand(x, f[2 * j] & in[0], f[2 * j + 1] & in[1]);
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                // (On top of the sums, in the order of the products above: what is taken
+                // out changes no rounding of what stays.)
+                float y[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) y[z] = o[2 * k + j][n][z];
                 mma<__half>(y, x, w[h][n][0], w[h][n][1]);
 #pragma unroll
                 for (int z = 0; z < 4; ++z)
-                  if (new_token[n][z & 1] == i) o[2 * k + j][n][z] += y[z];
+                  if (new_token[n][z & 1] == i) o[2 * k + j][n][z] = y[z];
               }
             }
           }
