@@ -429,11 +429,15 @@ __global__ void __launch_bounds__(kThreads, (kResident<DP, NT>))
           f[0] &= in[0], f[1] &= in[0], f[2] &= in[1], f[3] &= in[1];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            // (A tree's products come on top of the sums, as above, where its rows are not
+            // told apart: what is taken out changes no rounding of what stays.)
+            float x[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) x[h] = TREE ? o[d][n][h] : 0.0f;
             mma<T>(x, f, w[n][0], w[n][1]);
 #pragma unroll
             for (int h = 0; h < 4; ++h)
-              if (mine[n][h & 1]) o[d][n][h] += x[h];
+              if (mine[n][h & 1]) o[d][n][h] = TREE ? x[h] : o[d][n][h] + x[h];
           }
         }
       }
