@@ -414,7 +414,12 @@ __global__ void __launch_bounds__(kThreads, (kResident8<DP, NT, HEADS>))
   const int head0 = blockIdx.x % groups * HEADS;
   const int sp = blockIdx.x / groups % a.splits;
   int s = blockIdx.x / groups / a.splits;
-  if (a.ranked) s = ranked_session(a.batch, s, tid, kThreads, reinterpret_cast<uint32_t*>(smem));
+  if (a.ranked) {
+    s = ranked_session(a.batch, s, tid, kThreads, reinterpret_cast<uint32_t*>(smem));
+    // The ring lies over its numbers: what this thread wrote and read comes before the tensor
+    // copies behind the barrier below.
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
   const int head = head0 + warp % HEADS, turn = warp / HEADS;  // this warp's head, and its tile of a turn
   if (tid < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps.map[tid])) : "memory");
   SessionView view = session_rows(a, s);
