@@ -648,10 +648,13 @@ pcs_status pcs_snapshot_read_file(pcs_ctx *ctx, const char *path, uint32_t place
  * caller, Sec. 3 "Boundary"; the pages are those of Sec. 7.2's addressable KV
  * and of the copy-on-write pool above.)  Fields said to be 0 that are not, and
  * flags that are not named here -> PCS_E_INVAL.  These calls can be captured into
- * a graph; attention that needs working memory (parts of results, an 8-bit cache's
- * values where many rows go over them, at most 1 GiB and the parts) takes memory of
- * its own then, which stays with the context until pcs_destroy: that has to come
- * after the graph's last run.
+ * a graph; attention that needs working memory (parts of results; an 8-bit cache's
+ * elements where many rows go over them, at most 1 GiB) takes memory of its own
+ * then, which stays with the context until pcs_destroy: that has to come after the
+ * graph's last run.  Else a stream's calls share its working memory, which stays as
+ * large as the largest of them and a quarter more wanted it.  Where there is none
+ * for a cache's elements, attention does without, at up to twice the time; for parts
+ * of results it has to be there (PCS_E_NOMEM).
  */
 
 /* Heads of tokens: element d of head h of token t is at

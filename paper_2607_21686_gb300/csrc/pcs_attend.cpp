@@ -438,18 +438,22 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
     a.ranked = splits == 1 && a.batch.sessions > 1 && a.batch.sessions <= kRankMost;
     const uint64_t parts = splits > 1 ? round_up_256(4 * block_part_floats(cache->head_dim) * splits * pairs * blocks) : 0;
     // Codes that several blocks of rows go over are turned into elements once, ahead of
-    // them, where that takes no more than kWidenMost.
+    // them, where that takes no more than kWidenMost and there is memory for it.
     pcs_kv_cache wide;
     const uint64_t pages = static_cast<uint64_t>(a.batch.sessions) * cache->table_pages;
     const uint64_t pool = codes ? pages * cache->page_rows * (2ull * cache->heads * cache->head_dim) : 0;
-    const bool widen = codes && blocks > 1 && 2 * pool <= kWidenMost;
+    bool widen = codes && blocks > 1 && 2 * pool <= kWidenMost;
     const uint64_t table = widen ? round_up_256(4 * pages) : 0;
     uint8_t* ws = nullptr;
     if (parts || widen) {
       uint32_t* words = nullptr;
       st = working_memory(call, parts + (widen ? table + 2 * pool : 0), &ws, &words);
+      if (st == PCS_E_NOMEM && widen) {  // the kernel over codes needs none of it
+        widen = false;
+        st = parts ? working_memory(call, parts, &ws, &words) : PCS_OK;
+      }
       if (st) return st;
-      a.part = reinterpret_cast<float*>(ws);
+      a.part = parts ? reinterpret_cast<float*>(ws) : nullptr;
     }
     if (widen) {
       const WidenTo to = {ws + parts + table, ws + parts + table + pool, reinterpret_cast<int32_t*>(ws + parts),
