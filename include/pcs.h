@@ -737,7 +737,10 @@ typedef struct pcs_kv_cache {
 typedef struct pcs_kv_batch {
     const int32_t *lens;     /* device [sessions]                           */
     const int32_t *q_off;    /* device [sessions + 1], ascending from 0 to  */
-                             /* tokens; NULL: tokens / sessions each        */
+                             /* at most tokens (rows behind the last        */
+                             /* session's are nobody's: no result and no    */
+                             /* page is written for them, but queries are   */
+                             /* rotated); NULL: tokens / sessions each      */
     int64_t tokens;
     int32_t sessions;
     int32_t max_new;         /* with q_off: no session has more new tokens  */

@@ -104,7 +104,9 @@ __global__ void __launch_bounds__(kThreads, kReadBlocks<CODES>) k_kv_read(const 
   const CacheDev& c = a.cache;
   const int tid = threadIdx.x;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * shape.per_block;
-  const int nt = static_cast<int>(a.batch.tokens - t0 < shape.per_block ? a.batch.tokens - t0 : shape.per_block);
+  // (Rows behind the last session's are nobody's: they stay as they are.)
+  const int64_t end = a.batch.q_off ? min(a.batch.tokens, static_cast<int64_t>(__ldg(a.batch.q_off + a.batch.sessions))) : a.batch.tokens;
+  const int nt = static_cast<int>(min(end - t0, static_cast<int64_t>(shape.per_block)));
   if ((tid & ~31) < nt) {  // a warp looks up 32 tokens
     const int s = a.batch.q_off ? session_of(a.batch, t0 + (tid & ~31), tid & 31) : 0;
     if (tid < nt) place[tid] = place_of(c, a.batch, a.err, t0 + tid, s);
