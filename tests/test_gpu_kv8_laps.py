@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 KINDS = [ref.E4M3, ref.I8]
 
 
-@pytest.mark.parametrize("dim,hq,codes", [(64, 1, ref.E4M3), (64, 4, ref.I8), (128, 4, ref.E4M3)])
+@pytest.mark.parametrize("dim,hq,codes", [(64, 1, ref.I8), (128, 4, ref.E4M3)])
 @pytest.mark.parametrize("sinks,ring,rows", [(4, 64, 16), (16, 203, 8), (64, 128, 128), (100, 64, 16), (130, 150, 32),
                                              (5, 90, 17)])
 def test_prompts_that_lap_their_ring(ctx, dim, hq, codes, sinks, ring, rows):
@@ -25,7 +25,7 @@ def test_prompts_that_lap_their_ring(ctx, dim, hq, codes, sinks, ring, rows):
 
 @pytest.mark.parametrize("codes", KINDS)
 @pytest.mark.parametrize("sinks,ring", [(0, 101), (5, 64), (16, 203), (130, 190), (7, 129)])
-@pytest.mark.parametrize("rows", [8, 16, 24, 64])
+@pytest.mark.parametrize("rows", [8, 24, 64])
 @pytest.mark.parametrize("new", [1, 9])
 def test_rings_that_wrap_anywhere(ctx, codes, sinks, ring, rows, new):
     lens = [ring + sinks + d for d in (-1, 0, 1, 7, 40, 100, ring // 2)]

@@ -41,7 +41,7 @@ def check(ctx, p, window=0):
 @pytest.mark.parametrize("hq,hk,dim", [(4, 1, 64), (8, 2, 128), (4, 1, 80)])
 def test_blocks_over_codes(ctx, codes, dtype, hq, hk, dim):
     for rows in (16, 25):
-        check(ctx, ref.Population8(dim + rows, [300, 150, 90, 1], [300, 66, 70, 1], hq, hk, dim, codes, dtype=dtype, page_rows=rows))
+        check(ctx, ref.Population8(dim + rows, [200, 150, 90, 1], [140, 66, 70, 1], hq, hk, dim, codes, dtype=dtype, page_rows=rows))
 
 
 @pytest.mark.parametrize("sinks,ring,window", [(4, 0, 50), (0, 200, 0), (5, 201, 90), (16, 230, 40)])
@@ -57,8 +57,8 @@ def test_trees_over_codes(ctx, codes):
 
 @pytest.mark.parametrize("codes", [ref.E4M3, ref.I8])
 def test_parts_over_codes(ctx, codes):
-    # One session of three blocks in parts, with and without a hint of its length.
-    p = ref.Population8(2, [2500], [300], 4, 2, 64, codes)
+    # One session of two blocks in parts, with and without a hint of its length.
+    p = ref.Population8(2, [1300], [140], 4, 2, 64, codes)
     for hint in (True, False):
         out, lse = attend(ctx, p, 0, True, hint)
         kv_ref.check_attend(p, out, lse)
