@@ -722,7 +722,8 @@ typedef struct pcs_kv_cache {
  * head_dim): element d of the head stands for code_d * 2^(b - 127), b = 255 for
  * NaN throughout.  A row is one run of bytes, so a RING section or a pool's page
  * holds codes and scales together.  (Powers of two cost 8-bit floats nothing,
- * whole numbers one bit at most; what a code stands for is exact in bfloat16, and
+ * whole numbers one bit at most; what a code stands for is exact in bfloat16, but
+ * for numbers below its normal ones (2^-126) and 448 * 2^127, which it has not; and
  * a byte a head is 0.8 to 1.6 % of its codes.)
  * pcs_kv_append writes: e is the least whole number from -126 on with
  * max |x_d| <= 448 * 2^e (E4M3) or 127 * 2^e (I8), b = e + 127, and code_d is
@@ -788,9 +789,11 @@ pcs_status pcs_kv_append(pcs_ctx *ctx, const pcs_kv_cache *cache, const pcs_kv_b
  * that sees nothing gives 0.  lse: device float[tokens][q heads] or NULL,
  * log sum exp(scale * q.k_j) (-inf if it sees nothing), by which results over
  * several caches can be joined.  Sums are in 32 bits, weights are rounded to
- * the cache's type before they multiply values (a cache in 8 bits: to float16, or
- * to the queries' type, in which its values then are, float16 up to 65504; q and
- * out are PCS_DT_F16 or PCS_DT_BF16).  What is in slots that no new
+ * the cache's type before they multiply values.  Over a cache in 8 bits q and out
+ * are PCS_DT_F16 or PCS_DT_BF16; few query rows a key head (up to 16, or 32 where
+ * sessions and heads are few) have weights in float16 and values as the codes give
+ * them, more have both in the queries' type, values in float16 then up to 65504 and
+ * from 2^-24 on.  What is in slots that no new
  * token sees (infinities, NaN) does not matter.  out may be q.  q and out:
  * 16-byte multiples (else PCS_E_ALIGN).  Page ids outside the pool, slots beyond the table, more
  * new tokens than max_new or than lens says -> PCS_E_RANGE at the next

@@ -438,7 +438,11 @@ pcs_status attend(const char* name, pcs_ctx* ctx, const pcs_kv_cache* cache, con
     a.ranked = splits == 1 && a.batch.sessions > 1 && a.batch.sessions <= kRankMost;
     const uint64_t parts = splits > 1 ? round_up_256(4 * block_part_floats(cache->head_dim) * splits * pairs * blocks) : 0;
     // Codes that several blocks of rows go over are turned into elements once, ahead of
-    // them, where that takes no more than kWidenMost and there is memory for it.
+    // them, where that takes no more than kWidenMost and there is memory for it.  (Trees of 60
+    // nodes over 16 sessions of 500 to 9,000 tokens, 8 heads of 128, two, three and four blocks
+    // of rows: 188 to 192, 265 and 301 us, over the codes 178 to 186, 312 and 364 us; 8,000
+    // tokens, the last 128, 192 and 512: 53, 52 and 76 us, over the codes 52, 57 and 107 us; two
+    // blocks of a frame of heads of 64: 32 and 28 us.)
     pcs_kv_cache wide;
     const uint64_t pages = static_cast<uint64_t>(a.batch.sessions) * cache->table_pages;
     const uint64_t pool = codes ? pages * cache->page_rows * (2ull * cache->heads * cache->head_dim) : 0;

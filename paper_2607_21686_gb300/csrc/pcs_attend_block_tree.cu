@@ -1,8 +1,9 @@
 // pcs_attend_block_tree.cu -- attention of trees of drafted tokens with many query rows
 // a key head, over a cache of 16-bit elements: the kernel of pcs_attend_block.cu, whose
 // rows see what the tree says of the new tokens.  60 nodes of each of 32 sessions over 500
-// to 9,000 tokens, 32 query heads over 8 of 128, bfloat16: 155 us (177 us with sessions as
-// they come: the longest first); the bound is a block's loads, 44 GB/s an SM.
+// to 9,000 tokens, 32 query heads over 8 of 128, bfloat16: 136 us, of 96 us for its bytes
+// (longest sessions first; as they came they took a seventh more); the bound is a block's
+// loads, 44 GB/s an SM.
 #include "pcs_attend_block_dev.h"
 
 namespace pcs {

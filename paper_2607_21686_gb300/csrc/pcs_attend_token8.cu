@@ -31,7 +31,7 @@
 //                 sessions of 1 to 12,000 tokens, 32 over 8 heads of 128, I8: 104 us.  The
 //                 copies alone, a warp a head, took 94 us of the first.
 // k_attend_token8_rows  The same from pages whose size no such box divides: each warp
-//                 copies rows of tiles of its own (the 48 sessions in pages of 25: 182 us).
+//                 copies rows of tiles of its own (the 48 sessions in pages of 25: 139 us).
 #include "pcs_attend_token_dev.h"
 #include "pcs_codes_dev.h"
 
